@@ -263,7 +263,7 @@ def _plain(st):
         dx = (g - g.mean(1, keepdim=True) - xhat * (g * xhat).mean(1, keepdim=True)) * st["rstd"][:, None]
         row, at = torch.arange(T, device=dy.device), st["start"]
         of = ((row >= at[:-1, None]) & (row < at[1:, None])).float()
-        return {"dx": dx.to(dy.dtype), "dgamma": of @ (dy * xhat), "dbeta": of @ dy}
+        return {"dx": dx.to(st["dy"].dtype), "dgamma": of @ (dy * xhat), "dbeta": of @ dy}
     if op == "checkpoint":
         codes, scales = _pack(_leaky(st["x"].float(), c["slope"]))
         return {"y": _values([codes.view(torch.uint8), scales.view(torch.uint8)], T, C).to(st["x"].dtype)}
