@@ -288,6 +288,96 @@ lgc_status lgc_topk_noalloc(const float *v, int64_t n, int64_t k, int32_t *idx_o
  * the record.  (No counterpart in the paper either.) */
 lgc_status lgc_topk_noalloc_check(void *stream);
 
+/* ---- layer operators ------------------------------------------------------------------------
+ * The operators of a transformer's layers whose gradients the calls above compress.  The K nodes'
+ * tokens are K runs of rows of one activation matrix (node k has rows node_start[k] ..
+ * node_start[k + 1] - 1; a run may be empty), and the gradients of the weights come out per node, at
+ * `node_stride` elements from each other: the rows of the [K][N] `grads` of lgc_accumulate.
+ *
+ * (The paper has no counterpart: it takes the gradients as given.)  These calls need no context;
+ * everything is enqueued on `stream` (a cudaStream_t) and nothing synchronises.  Matrices are row
+ * major, rows `ld` elements apart.  num_rows may be 0 (nothing to do, except that gradients per node
+ * become 0).  No buffer that a call writes may overlap one that it reads, except where said.
+ *
+ * 8-bit matrices.  Codes are e4m3 (sign, four exponent bits, three of mantissa); entries that share a
+ * scale byte s stand for code * 2^(s - 127).  A block of entries with one scale is 128 neighbours of a row
+ * (block_rows = 1: activations, gradients) or 128 x 128 entries (block_rows = 128: weights), counted
+ * from the matrix's corner; the last blocks of a row or column may be narrower.  s is the smallest
+ * value, at least 7 and at most 246, that brings the block's largest magnitude to 448 or less, and
+ * codes are rounded to nearest, ties to even, larger magnitudes to 448.  Every value that a code
+ * stands for is a bf16 number.  A block with an entry that is not finite has s = 255 and codes 0x7f
+ * or 0xff (the entries' signs stay): all its entries stand for NaN.  Codes 0x7f and 0xff occur in no
+ * other block. */
+typedef enum { LGC_TYPE_FP32 = 0, LGC_TYPE_BF16 = 1, LGC_TYPE_PACKED = 2 } lgc_type;
+
+typedef struct {
+    uint8_t *codes;     /* device, rows `ld` bytes apart: 16-byte aligned, ld a multiple of 16 */
+    int64_t ld;
+    uint8_t *scales;    /* device, [ceil(rows / block_rows)] rows of ceil(cols / 128) bytes, `ld_scales` apart: */
+    int64_t ld_scales;  /* 4-byte aligned, ld_scales a multiple of 4 */
+} lgc_packed;
+
+/* Rounds a matrix to 8 bits, a checkpoint for the backward pass or an operand of lgc_product.
+ *   x      : fp32 or bf16 (type)          block_rows : 1 or 128
+ *   slope  : of the leaky ReLU that x goes through first (x > 0 ? x : slope * x); 1 = none
+ *   gate   : NULL, or the 8-bit result of that leaky ReLU in the forward pass (block_rows = 1): x is
+ *            then a gradient and is multiplied by the derivative instead, `slope` where the gate's code has its
+ *            sign bit set, 1 elsewhere (the sign survives the rounding, so this is exact; +0 counts as positive)
+ *   y      : NULL, or bf16 [num_rows] rows `ldy` apart: what was rounded, in bf16 */
+lgc_status lgc_pack(const void *x, int32_t type, int64_t num_rows, int64_t num_cols, int64_t ldx, int32_t block_rows,
+                    float slope, const lgc_packed *gate, const lgc_packed *out, void *y, int64_t ldy, void *stream);
+
+/* The values of an 8-bit matrix in fp32 or bf16 (exact in both). */
+lgc_status lgc_unpack(const lgc_packed *src, int64_t num_rows, int64_t num_cols, int32_t block_rows, void *y, int32_t type,
+                      int64_t ldy, void *stream);
+
+/* Layer norm of every row:  mean = sum(x) / C,  rstd = 1 / sqrt(sum((x - mean)^2) / C + eps),
+ *     y = (x - mean) * rstd * gamma + beta.
+ * x, y: fp32 or bf16 (one type).  y and packed: either may be NULL; packed gets the unrounded y in 8 bits
+ * (block_rows = 1).  mean, rstd: fp32 [num_rows], what the backward pass needs.  1 <= num_cols <= 16384. */
+lgc_status lgc_layer_norm(const void *x, int32_t type, int64_t num_rows, int64_t num_cols, int64_t ldx, const float *gamma,
+                          const float *beta, float eps, void *y, int64_t ldy, const lgc_packed *packed, float *mean,
+                          float *rstd, void *stream);
+
+/* Its backward pass.  With xh = (x - mean) * rstd and g = dy * gamma:
+ *     dx = rstd * (g - sum(g) / C - xh * sum(g * xh) / C),
+ *     dgamma_k = sum over node k's rows of dy * xh,   dbeta_k = sum over node k's rows of dy.
+ * dy, dx: fp32 or bf16 (dy_type); dx may be dy.  x: fp32, bf16, or (x_type = LGC_TYPE_PACKED, x_packed) the 8-bit
+ * checkpoint of the input; mean and rstd are those of lgc_layer_norm.  node_start: device int64
+ * [num_nodes + 1], or NULL for one node with every row; dgamma, dbeta: node k's C floats start
+ * k * node_stride after node 0's.  The sums over rows are taken in a fixed order in fp32.
+ * scratch: lgc_layer_norm_backward_scratch bytes, 16-byte aligned. */
+lgc_status lgc_layer_norm_backward_scratch(int64_t num_rows, int64_t num_cols, int32_t num_nodes, size_t *bytes);
+lgc_status lgc_layer_norm_backward(const void *dy, int32_t dy_type, int64_t ld_dy, const void *x, int32_t x_type, int64_t ldx,
+                                   const lgc_packed *x_packed, int64_t num_rows, int64_t num_cols, const float *gamma,
+                                   const float *mean, const float *rstd, const int64_t *node_start, int32_t num_nodes,
+                                   void *dx, int64_t ld_dx, float *dgamma, float *dbeta, int64_t node_stride, void *scratch,
+                                   size_t scratch_bytes, void *stream);
+
+/* Product of 8-bit matrices on the tensor cores, fp32 sums:
+ *     across = 0:  Y[t][n] = act(sum_i A[t][i] B[n][i])     (a linear layer: A activations, B weights)
+ *     across = 1:  Y[t][n] = act(sum_i A[t][i] B[i][n])     (the gradient at its input: the same weights, A the
+ *                                                            gradient at its output)
+ * for t < num_rows, n < num_cols, i < inner.  A has block_rows = 1, B block_rows = 128.
+ * act is the leaky ReLU with `slope` (1 = none).  y: NULL, or fp32 / bf16 (type); packed: NULL, or Y in 8 bits
+ * (block_rows = 1), rounded from the fp32 sums.  At least one of the two. */
+lgc_status lgc_product(const lgc_packed *a, const lgc_packed *b, int32_t across, int64_t num_rows, int64_t num_cols,
+                       int64_t inner, float slope, void *y, int32_t type, int64_t ldy, const lgc_packed *packed, void *stream);
+
+/* Gradient of a linear layer's weights, per node, from the 8-bit checkpoint of the layer's input:
+ *     dW_k[n][i] = sum over node k's rows t of dY[t][n] X[t][i],    fp32, n < num_cols, i < inner,
+ * written back to back (num_cols * inner floats, node k's k * node_stride floats after node 0's).
+ * dy: bf16, 16-byte aligned, ld_dy a multiple of 8.  x: block_rows = 1.  The products are exact in the tensor
+ * cores' bf16 form (a code times its scale is a bf16 number), the sums fp32.  Rows outside a node's run have no
+ * influence on its gradient, whatever they hold. */
+lgc_status lgc_weight_gradient(const void *dy, int64_t ld_dy, const lgc_packed *x, int64_t num_rows, int64_t num_cols,
+                               int64_t inner, const int64_t *node_start, int32_t num_nodes, float *dw, int64_t node_stride,
+                               void *stream);
+
+/* What the kernels of lgc_product and lgc_weight_gradient recorded on the current device (a wait inside a kernel
+ * that ran out): waits for `stream`, returns LGC_OK or LGC_ERR_DEVICE_CHECK and clears the record. */
+lgc_status lgc_layers_check(void *stream);
+
 /* ---- inspection --------------------------------------------------------------------------- */
 
 /* N, mu, encoder lengths L1 (after the first convolution) and L2 (code length per channel), and

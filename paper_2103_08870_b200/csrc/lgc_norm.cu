@@ -1,0 +1,388 @@
+// Layer norm over the rows of a matrix, and its backward pass with the weight's and bias's gradients per node.
+//
+// Forward: a row stays in registers between its three uses (sum, sum of squared deviations, result), so x is read once
+// and y (and / or its 8-bit form) written once: DRAM bounds it.  The variance is the mean of the squared deviations from
+// the mean that was found, not a difference of squares.
+// Backward: dx needs two sums per row, the weight's gradient a sum over rows per column.  A CTA walks down a chunk of
+// consecutive rows of one node; a thread keeps its columns' gradients in registers on the way, so dy and x are read once;
+// the chunks' partial sums (fp32) are added up per node, in chunk order, by a second small kernel.
+#include "lgc_layers.cuh"
+
+namespace lgc {
+
+namespace {
+
+// Sums over the TPR threads that share a row (a warp, or the whole CTA); every thread gets the result.
+template <int TPR, int COUNT>
+__device__ __forceinline__ void row_sums(float (&v)[COUNT], float *shared)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) v[i] = __fadd_rn(v[i], __shfl_xor_sync(0xffffffffu, v[i], o));
+    if (TPR > 32) {
+        constexpr int kWarps = TPR / 32;
+        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+        if (lane == 0)
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) shared[i * kWarps + warp] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) {
+            float t = lane < kWarps ? shared[i * kWarps + lane] : 0.0f;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) t = __fadd_rn(t, __shfl_xor_sync(0xffffffffu, t, o));
+            v[i] = t;
+        }
+    }
+}
+
+// TPR threads per row, NV vectors of eight entries each.  Lanes hold neighbouring vectors, so that 16 lanes hold a block
+// of the 8-bit form.
+template <typename T, bool VEC, int TPR, int NV>
+__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR)
+layer_norm_kernel(const T *__restrict__ x, int64_t ldx, int64_t rows, int64_t cols, const float *__restrict__ gamma,
+                  const float *__restrict__ beta, float eps, T *__restrict__ y, int64_t ldy, bool y_vec, uint8_t *__restrict__ codes,
+                  int64_t ld_codes, uint8_t *__restrict__ scales, int64_t ld_scales, float *__restrict__ mean_out,
+                  float *__restrict__ rstd_out, bool gb_vec)
+{
+    __shared__ float shared[2][TPR / 32];
+    constexpr int kRows = TPR < 128 ? 128 / TPR : 1;
+    const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
+    const int t = threadIdx.x % TPR;
+    if (row >= rows) return;                                    // a whole warp (TPR = 32): no barrier follows
+    const T *xr = x + row * ldx;
+    float v[NV][8];
+    float sum[1] = {0.0f};
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        load8<T, VEC>(xr, (int64_t)(i * TPR + t) * 8, cols, v[i]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[0] = __fadd_rn(sum[0], v[i][j]);
+    }
+    row_sums<TPR>(sum, shared[0]);
+    const float mean = __fdiv_rn(sum[0], (float)cols);
+    float sq[1] = {0.0f};
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            v[i][j] = __fsub_rn(v[i][j], mean);
+            if ((int64_t)(i * TPR + t) * 8 + j < cols) sq[0] = __fmaf_rn(v[i][j], v[i][j], sq[0]);
+        }
+    row_sums<TPR>(sq, shared[1]);
+    const float rstd = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(__fdiv_rn(sq[0], (float)cols), eps)));
+    if (t == 0) {
+        mean_out[row] = mean;
+        rstd_out[row] = rstd;
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int64_t c = (int64_t)(i * TPR + t) * 8;
+        if ((int64_t)(i * TPR + (t & ~31)) * 8 >= cols) break;   // the whole warp is past the row's end
+        float g[8], b[8];
+        if (gb_vec) {
+            load8<float, true>(gamma, c, cols, g);
+            load8<float, true>(beta, c, cols, b);
+        } else {
+            load8<float, false>(gamma, c, cols, g);
+            load8<float, false>(beta, c, cols, b);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] = c + j < cols ? __fmaf_rn(__fmul_rn(v[i][j], rstd), g[j], b[j]) : 0.0f;
+        if (y) {
+            if (y_vec) store8<T, true>(y + row * ldy, c, cols, v[i]);
+            else store8<T, false>(y + row * ldy, c, cols, v[i]);
+        }
+        if (codes) {
+            const uint32_t s = block_scale(most_of_block(v[i]));
+            store_codes8(codes + row * ld_codes, c, cols, codes4(v[i][0], v[i][1], v[i][2], v[i][3], s),
+                         codes4(v[i][4], v[i][5], v[i][6], v[i][7], s));
+            if ((t & 15) == 0 && c < cols) scales[row * ld_scales + c / kBlock] = (uint8_t)s;
+        }
+    }
+}
+
+// ---- backward ---------------------------------------------------------------------------------------------------------
+// Chunk `want` of the nodes' rows, each node's rows cut into chunks of `chunk_rows`: its rows and its node.  Called by a
+// whole warp; 32 nodes at a time.
+struct Chunk {
+    int64_t begin, end;
+    int node;
+};
+__device__ __forceinline__ Chunk find_chunk(const int64_t *start, int nodes, int64_t rows, int64_t chunk_rows, int64_t want)
+{
+    const int lane = threadIdx.x & 31;
+    for (int k0 = 0; k0 < nodes; k0 += 32) {
+        const int k = k0 + lane;
+        int64_t lo = 0, hi = 0;
+        if (k < nodes) {
+            lo = node_first_row(start, k, rows);
+            hi = node_first_row(start, k + 1, rows);
+            if (hi < lo) hi = lo;
+        }
+        const int64_t mine = (hi - lo + chunk_rows - 1) / chunk_rows;
+        int64_t upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t t = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += t;
+        }
+        const unsigned hit = __ballot_sync(0xffffffffu, want < upto);
+        if (hit) {
+            const int src = __ffs(hit) - 1;
+            const int64_t before = __shfl_sync(0xffffffffu, upto - mine, src);
+            const int64_t l = __shfl_sync(0xffffffffu, lo, src), h = __shfl_sync(0xffffffffu, hi, src);
+            const int64_t b = l + (want - before) * chunk_rows;
+            return {b, b + chunk_rows < h ? b + chunk_rows : h, k0 + src};
+        }
+        want -= __shfl_sync(0xffffffffu, upto, 31);
+    }
+    return {0, 0, -1};
+}
+
+// x may be the 8-bit checkpoint (XT = uint8_t).
+template <typename XT, bool VEC>
+__device__ __forceinline__ void load_x8(const XT *x, int64_t ldx, const uint8_t *scales, int64_t ld_scales, int64_t row, int64_t c,
+                                        int64_t cols, float (&v)[8])
+{
+    if constexpr (sizeof(XT) == 1) {
+        const uint2 q = load_codes8(x + row * ldx, c, cols);
+        const float f = c < cols ? block_factor(__ldg(scales + row * ld_scales + c / kBlock)) : 0.0f;
+        float a[4], b[4];
+        codes_to_float4(q.x, a);
+        codes_to_float4(q.y, b);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            v[j] = __fmul_rn(a[j], f);
+            v[4 + j] = __fmul_rn(b[j], f);
+        }
+    } else {
+        load8<XT, VEC>(x + row * ldx, c, cols, v);
+    }
+}
+
+// partial: [chunks][2][cols], the weight's then the bias's gradient over the chunk's rows.
+template <typename T, typename XT, bool VEC, int TPR, int NV>
+__global__ void __launch_bounds__(TPR)
+layer_norm_backward_kernel(const T *__restrict__ dy, int64_t ld_dy, const XT *__restrict__ x, int64_t ldx,
+                           const uint8_t *__restrict__ x_scales, int64_t ld_scales, int64_t rows, int64_t cols,
+                           const float *__restrict__ gamma, const float *__restrict__ mean, const float *__restrict__ rstd,
+                           const int64_t *__restrict__ node_start, int nodes, int64_t chunk_rows, T *__restrict__ dx, int64_t ld_dx,
+                           float *__restrict__ partial)
+{
+    __shared__ float shared[2][2 * (TPR / 32)];
+    const int t = threadIdx.x;
+    const Chunk ch = find_chunk(node_start, nodes, rows, chunk_rows, blockIdx.x);
+    if (ch.node < 0) return;
+    float g[NV][8], dg[NV][8], db[NV][8];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        load8<float, false>(gamma, (int64_t)(i * TPR + t) * 8, cols, g[i]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dg[i][j] = db[i][j] = 0.0f;
+    }
+    const float count = (float)cols;
+    for (int64_t row = ch.begin; row < ch.end; ++row) {
+        float d[NV][8], h[NV][8];
+        float sums[2] = {0.0f, 0.0f};
+        const float mu = __ldg(mean + row), rs = __ldg(rstd + row);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int64_t c = (int64_t)(i * TPR + t) * 8;
+            load8<T, VEC>(dy + row * ld_dy, c, cols, d[i]);
+            load_x8<XT, VEC>(x, ldx, x_scales, ld_scales, row, c, cols, h[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                // entries beyond the row's end: d = g = 0, and their xh enters no sum
+                h[i][j] = __fmul_rn(__fsub_rn(h[i][j], mu), rs);
+                dg[i][j] = __fmaf_rn(d[i][j], h[i][j], dg[i][j]);
+                db[i][j] = __fadd_rn(db[i][j], d[i][j]);
+                d[i][j] = __fmul_rn(d[i][j], g[i][j]);
+                sums[0] = __fadd_rn(sums[0], d[i][j]);
+                sums[1] = __fmaf_rn(d[i][j], h[i][j], sums[1]);
+            }
+        row_sums<TPR>(sums, shared[row & 1]);                    // two sets: a fast warp may be a row ahead of a slow one
+        const float m1 = __fdiv_rn(sums[0], count), m2 = __fdiv_rn(sums[1], count);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) d[i][j] = __fmul_rn(rs, __fsub_rn(__fsub_rn(d[i][j], m1), __fmul_rn(h[i][j], m2)));
+            store8<T, VEC>(dx + row * ld_dx, (int64_t)(i * TPR + t) * 8, cols, d[i]);
+        }
+    }
+    float *out = partial + (int64_t)blockIdx.x * 2 * cols;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        store8<float, false>(out, (int64_t)(i * TPR + t) * 8, cols, dg[i]);
+        store8<float, false>(out + cols, (int64_t)(i * TPR + t) * 8, cols, db[i]);
+    }
+}
+
+// The chunks' sums of one node, 32 columns per CTA: 16 slices of the chunks side by side, each in chunk order, then the
+// slices in order.
+__global__ void __launch_bounds__(512)
+layer_norm_gradient_kernel(const float *__restrict__ partial, int64_t rows, int64_t cols, const int64_t *__restrict__ node_start,
+                           int64_t chunk_rows, int64_t max_chunks, float *__restrict__ dgamma, float *__restrict__ dbeta,
+                           int64_t node_stride)
+{
+    __shared__ float part[2][16][33];
+    const int node = blockIdx.y, lane = threadIdx.x & 31, slice = threadIdx.x >> 5;
+    // this node's chunks: those of the nodes in front come first
+    int64_t first = 0;
+    for (int k0 = 0; k0 < node; k0 += 32) {
+        const int k = k0 + lane;
+        int64_t mine = 0;
+        if (k < node) {
+            const int64_t lo = node_first_row(node_start, k, rows), hi = node_first_row(node_start, k + 1, rows);
+            mine = hi > lo ? (hi - lo + chunk_rows - 1) / chunk_rows : 0;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+        first += mine;
+    }
+    const int64_t lo = node_first_row(node_start, node, rows), hi = node_first_row(node_start, node + 1, rows);
+    int64_t count = hi > lo ? (hi - lo + chunk_rows - 1) / chunk_rows : 0;
+    if (first + count > max_chunks) count = first < max_chunks ? max_chunks - first : 0;   // (only if node_start does not ascend)
+    const int64_t each = (count + 15) / 16;
+    const int64_t c = (int64_t)blockIdx.x * 32 + lane;
+    float g = 0.0f, b = 0.0f;
+    if (c < cols) {
+        const int64_t end = (slice + 1) * each < count ? (slice + 1) * each : count;
+#pragma unroll 4
+        for (int64_t i = slice * each; i < end; ++i) {
+            const float *p = partial + (first + i) * 2 * cols + c;
+            g = __fadd_rn(g, __ldg(p));
+            b = __fadd_rn(b, __ldg(p + cols));
+        }
+    }
+    part[0][slice][lane] = g;
+    part[1][slice][lane] = b;
+    __syncthreads();
+    if (slice < 2 && c < cols) {
+        float t = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) t = __fadd_rn(t, part[slice][i][lane]);
+        (slice == 0 ? dgamma : dbeta)[(int64_t)node * node_stride + c] = t;
+    }
+}
+
+// Rows per chunk: about four chunks per SM, at least eight rows, so that a chunk's 2 * cols partial sums stay small
+// beside its rows.
+int64_t chunk_rows_for(int64_t rows)
+{
+    const int64_t r = (rows + 4 * 148 - 1) / (4 * 148);
+    return r < 8 ? 8 : r;
+}
+int64_t max_chunks_for(int64_t rows, int32_t nodes)
+{
+    const int64_t r = chunk_rows_for(rows);
+    return (rows + r - 1) / r + nodes;
+}
+
+template <typename T, bool VEC>
+cudaError_t norm_type(const Matrix &x, int64_t rows, int64_t cols, const float *gamma, const float *beta, float eps, T *y, int64_t ldy,
+                      const lgc_packed *p, float *mean, float *rstd, cudaStream_t s)
+{
+    const bool y_vec = matrix_rows_aligned(y, ldy, sizeof(T)), gb_vec = matrix_rows_aligned(gamma, 4, 4) && matrix_rows_aligned(beta, 4, 4);
+    auto launch = [&](auto kern, int64_t ctas, int threads) {
+        kern<<<(unsigned)ctas, threads, 0, s>>>(static_cast<const T *>(x.p), x.ld, rows, cols, gamma, beta, eps, y, ldy, y_vec,
+                                                p ? p->codes : nullptr, p ? p->ld : 0, p ? p->scales : nullptr, p ? p->ld_scales : 0, mean,
+                                                rstd, gb_vec);
+    };
+    if (cols <= 1024) launch(layer_norm_kernel<T, VEC, 32, 4>, (rows + 3) / 4, 128);
+    else if (cols <= 4096) launch(layer_norm_kernel<T, VEC, 128, 4>, rows, 128);
+    else if (cols <= 8192) launch(layer_norm_kernel<T, VEC, 256, 4>, rows, 256);
+    else launch(layer_norm_kernel<T, VEC, 512, 4>, rows, 512);
+    ++g_kernel_launches;
+    return cudaGetLastError();
+}
+
+struct BackwardArgs {
+    const Matrix &dy, &x;
+    const lgc_packed *xp;
+    int64_t rows, cols;
+    const float *gamma, *mean, *rstd;
+    const int64_t *node_start;
+    int32_t nodes;
+    void *dx;
+    int64_t ld_dx;
+    float *partial;
+    cudaStream_t s;
+};
+
+template <typename T, typename XT, bool VEC>
+void backward_kernel(const BackwardArgs &a)
+{
+    const int64_t chunk = chunk_rows_for(a.rows), ctas = max_chunks_for(a.rows, a.nodes);
+    auto launch = [&](auto kern, int threads) {
+        kern<<<(unsigned)ctas, threads, 0, a.s>>>(static_cast<const T *>(a.dy.p), a.dy.ld,
+                                                  static_cast<const XT *>(a.xp ? a.xp->codes : a.x.p), a.xp ? a.xp->ld : a.x.ld,
+                                                  a.xp ? a.xp->scales : nullptr, a.xp ? a.xp->ld_scales : 0, a.rows, a.cols, a.gamma, a.mean,
+                                                  a.rstd, a.node_start, a.nodes, chunk, static_cast<T *>(a.dx), a.ld_dx, a.partial);
+    };
+    if (a.cols <= 512) launch(layer_norm_backward_kernel<T, XT, VEC, 32, 2>, 32);
+    else if (a.cols <= 2048) launch(layer_norm_backward_kernel<T, XT, VEC, 128, 2>, 128);
+    else if (a.cols <= 4096) launch(layer_norm_backward_kernel<T, XT, VEC, 256, 2>, 256);
+    else if (a.cols <= 8192) launch(layer_norm_backward_kernel<T, XT, VEC, 512, 2>, 512);
+    else launch(layer_norm_backward_kernel<T, XT, VEC, 1024, 2>, 1024);
+}
+template <typename T, typename XT>
+void backward_aligned(const BackwardArgs &a)
+{
+    const bool vec = matrix_rows_aligned(a.dy.p, a.dy.ld, sizeof(T)) && matrix_rows_aligned(a.dx, a.ld_dx, sizeof(T)) &&
+                     (sizeof(XT) == 1 || matrix_rows_aligned(a.x.p, a.x.ld, sizeof(XT)));
+    if (vec) backward_kernel<T, XT, true>(a);
+    else backward_kernel<T, XT, false>(a);
+}
+template <typename T>
+void backward_type(const BackwardArgs &a)
+{
+    if (a.xp) backward_aligned<T, uint8_t>(a);
+    else if (a.x.type == LGC_TYPE_FP32) backward_aligned<T, float>(a);
+    else backward_aligned<T, __nv_bfloat16>(a);
+}
+
+}  // namespace
+
+cudaError_t launch_layer_norm(const Matrix &x, int64_t rows, int64_t cols, const float *gamma, const float *beta, float eps, void *y,
+                              int64_t ldy, const lgc_packed *packed, float *mean, float *rstd, cudaStream_t s)
+{
+    if (x.type == LGC_TYPE_FP32) {
+        float *yf = static_cast<float *>(y);
+        return matrix_rows_aligned(x.p, x.ld, 4) ? norm_type<float, true>(x, rows, cols, gamma, beta, eps, yf, ldy, packed, mean, rstd, s)
+                                                 : norm_type<float, false>(x, rows, cols, gamma, beta, eps, yf, ldy, packed, mean, rstd, s);
+    }
+    __nv_bfloat16 *yb = static_cast<__nv_bfloat16 *>(y);
+    return matrix_rows_aligned(x.p, x.ld, 2) ? norm_type<__nv_bfloat16, true>(x, rows, cols, gamma, beta, eps, yb, ldy, packed, mean, rstd, s)
+                                             : norm_type<__nv_bfloat16, false>(x, rows, cols, gamma, beta, eps, yb, ldy, packed, mean, rstd, s);
+}
+
+size_t layer_norm_backward_scratch(int64_t rows, int64_t cols, int32_t num_nodes)
+{
+    return (size_t)max_chunks_for(rows, num_nodes) * 2 * (size_t)cols * sizeof(float);
+}
+
+cudaError_t launch_layer_norm_backward(const Matrix &dy, const Matrix &x, const lgc_packed *x_packed, int64_t rows, int64_t cols,
+                                       const float *gamma, const float *mean, const float *rstd, const int64_t *node_start,
+                                       int32_t num_nodes, void *dx, int64_t ld_dx, float *dgamma, float *dbeta, int64_t node_stride,
+                                       void *scratch, cudaStream_t s)
+{
+    const BackwardArgs a{dy, x, x_packed, rows, cols, gamma, mean, rstd, node_start, num_nodes, dx, ld_dx, static_cast<float *>(scratch), s};
+    if (rows > 0) {
+        if (dy.type == LGC_TYPE_FP32) backward_type<float>(a);
+        else backward_type<__nv_bfloat16>(a);
+        ++g_kernel_launches;
+        const cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
+    }
+    layer_norm_gradient_kernel<<<dim3((unsigned)((cols + 31) / 32), (unsigned)num_nodes), 512, 0, s>>>(
+        a.partial, rows, cols, node_start, chunk_rows_for(rows), max_chunks_for(rows, num_nodes), dgamma, dbeta, node_stride);
+    ++g_kernel_launches;
+    return cudaGetLastError();
+}
+
+}  // namespace lgc

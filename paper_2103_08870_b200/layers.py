@@ -1,0 +1,217 @@
+"""Layer operators in front of the gradient compression: layer norm, 8-bit checkpoints, block-scaled 8-bit products and
+per-node weight gradients (binding of the section "layer operators" of include/lgc.h: argument checks and marshalling
+only).
+
+The K nodes' tokens are K runs of rows of one activation matrix; node k has rows ``node_start[k] .. node_start[k+1]-1``.
+Gradients of weights come out per node, in views of the ``[K][N]`` gradients that :meth:`lgc.LGC.accumulate` reads::
+
+    h8 = layers.packed_empty(rows, C)
+    layers.layer_norm(x, gamma, beta, 1e-5, mean, rstd, packed=h8)           # h = norm(x), in 8 bits
+    layers.product(h8, w8, y=z)                                              # z = h W^T
+    ...
+    layers.pack(dz, dz8)
+    layers.product(dz8, w8, y=dh, across=True)                               # dh = dz W, the same weight bytes
+    layers.weight_gradient(dz, h8, grads[:, at:at + n], node_start=starts)   # dW of every node into its row
+    layers.layer_norm_backward(dh, x, gamma, mean, rstd, dx, grads[:, g0:g1], grads[:, b0:b1], node_start=starts)
+
+Outputs are the caller's tensors; a call enqueues on ``stream`` (default: the current stream) and returns.
+"""
+from __future__ import annotations
+
+import ctypes as C
+from typing import Optional, Union
+
+import torch
+
+from . import lgc
+from .lgc import LGC_OK, LGCError
+
+BLOCK = 128
+TYPE_FP32, TYPE_BF16, TYPE_PACKED = 0, 1, 2
+_TYPES = {torch.float32: TYPE_FP32, torch.bfloat16: TYPE_BF16}
+
+
+class Packed:
+    """An 8-bit matrix: e4m3 `codes` (uint8 [rows][ld], unit column stride, 16-byte aligned rows) and the blocks' scale
+    bytes (uint8 [ceil(rows / block_rows)][..]); `cols` of the codes' columns belong to it."""
+
+    __slots__ = ("codes", "scales", "rows", "cols", "block_rows", "_c")
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, cols: Optional[int] = None, block_rows: int = 1):
+        if not (codes.is_cuda and scales.is_cuda and codes.dtype == torch.uint8 and scales.dtype == torch.uint8
+                and codes.dim() == 2 and scales.dim() == 2):
+            raise ValueError("codes and scales: need 2-D uint8 CUDA tensors")
+        rows = codes.shape[0]
+        cols = codes.shape[1] if cols is None else cols
+        if block_rows not in (1, BLOCK):
+            raise ValueError("block_rows: 1 or 128")
+        if not (0 < cols <= codes.shape[1] and codes.stride(1) == 1 and scales.stride(1) == 1
+                and scales.shape[0] == -(-rows // block_rows) and scales.shape[1] * BLOCK >= cols):
+            raise ValueError("codes need unit column stride and `cols` columns, scales a row per row of blocks and a byte per block")
+        self.codes, self.scales, self.rows, self.cols, self.block_rows = codes, scales, rows, cols, block_rows
+        # (the row stride of a tensor with one row may be anything)
+        ld = codes.stride(0) if rows > 1 else max(codes.stride(0), -(-codes.shape[1] // 16) * 16)
+        lds = scales.stride(0) if scales.shape[0] > 1 else max(scales.stride(0), -(-scales.shape[1] // 4) * 4)
+        self._c = lgc.lgc_packed(codes.data_ptr(), ld, scales.data_ptr(), lds)
+
+
+def packed_empty(rows: int, cols: int, block_rows: int = 1, device: Optional[torch.device] = None) -> Packed:
+    """Room for an 8-bit matrix, its rows padded to what the calls need."""
+    dev = device if device is not None else torch.device("cuda")
+    return Packed(torch.empty(rows, -(-cols // 16) * 16, dtype=torch.uint8, device=dev),
+                  torch.empty(-(-rows // block_rows), -(-cols // (4 * BLOCK)) * 4, dtype=torch.uint8, device=dev), cols, block_rows)
+
+
+def _stream(stream: Optional[torch.cuda.Stream], device: torch.device) -> int:
+    return (stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream
+
+
+def _matrix(t: torch.Tensor, name: str, rows: Optional[int] = None, cols: Optional[int] = None) -> int:
+    """Row stride of a matrix argument, after the checks that need the tensor (the library checks the numbers)."""
+    if not t.is_cuda or t.dtype not in _TYPES or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name}: need a 2-D fp32 or bf16 CUDA tensor with unit column stride")
+    if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
+        raise ValueError(f"{name}: need {rows} x {cols} elements, got {t.shape[0]} x {t.shape[1]}")
+    # a single row may have any stride: report one that the library accepts
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), -(-t.shape[1] // 8) * 8)
+
+
+def _vector(t: torch.Tensor, n: int, name: str) -> int:
+    if not (t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and t.numel() == n):
+        raise ValueError(f"{name}: need a contiguous fp32 CUDA tensor of {n} elements")
+    return t.data_ptr()
+
+
+def _packed(p: Packed, name: str, rows: int, cols: int, block_rows: int = 1):
+    if p.rows != rows or p.cols != cols or p.block_rows != block_rows:
+        raise ValueError(f"{name}: need a {rows} x {cols} 8-bit matrix with block_rows {block_rows}, got {p.rows} x {p.cols}, {p.block_rows}")
+    return C.byref(p._c)
+
+
+def _nodes(node_start: Optional[torch.Tensor], out: torch.Tensor, n: int, name: str):
+    """(pointer to node_start, number of nodes, node stride) for per-node results in `out` [K][n]."""
+    if not (out.is_cuda and out.dtype == torch.float32 and out.dim() == 2 and out.shape[1] == n and (n == 1 or out.stride(1) == 1)):
+        raise ValueError(f"{name}: need a [nodes][{n}] fp32 CUDA view with unit column stride")
+    K = out.shape[0]
+    if node_start is None:
+        if K != 1:
+            raise ValueError("node_start: needed with more than one node")
+        return None, 1, n
+    if not (node_start.is_cuda and node_start.dtype == torch.int64 and node_start.is_contiguous() and node_start.numel() == K + 1):
+        raise ValueError(f"node_start: need a contiguous int64 CUDA tensor of {K + 1} elements")
+    return node_start.data_ptr(), K, (out.stride(0) if K > 1 else n)
+
+
+def _done(status: int, where: str) -> None:
+    if status != LGC_OK:
+        raise LGCError(status, where, lgc.lib().lgc_last_error(None).decode())
+
+
+def pack(x: torch.Tensor, out: Packed, slope: float = 1.0, gate: Optional[Packed] = None, y: Optional[torch.Tensor] = None,
+         stream: Optional[torch.cuda.Stream] = None) -> None:
+    """`x` (fp32 or bf16), through a leaky ReLU of `slope` (1: none), to 8 bits.  With `gate` (the 8-bit result of that
+    leaky ReLU) `x` is a gradient and gets its derivative instead.  `y` (bf16): also what was rounded."""
+    ldx = _matrix(x, "x")
+    rows, cols = x.shape
+    ldy = 0
+    if y is not None:
+        ldy = _matrix(y, "y", rows, cols)
+        if y.dtype != torch.bfloat16:
+            raise ValueError("y: need a bf16 tensor")
+    _done(lgc.lib().lgc_pack(x.data_ptr(), _TYPES[x.dtype], rows, cols, ldx, out.block_rows, slope,
+                             None if gate is None else _packed(gate, "gate", rows, cols), _packed(out, "out", rows, cols, out.block_rows),
+                             None if y is None else y.data_ptr(), ldy, _stream(stream, x.device)), "lgc_pack")
+
+
+def unpack(src: Packed, y: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """The values of an 8-bit matrix in `y` (fp32 or bf16; exact in both)."""
+    ldy = _matrix(y, "y", src.rows, src.cols)
+    _done(lgc.lib().lgc_unpack(C.byref(src._c), src.rows, src.cols, src.block_rows, y.data_ptr(), _TYPES[y.dtype], ldy,
+                               _stream(stream, y.device)), "lgc_unpack")
+
+
+def layer_norm(x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor, eps: float, mean: torch.Tensor, rstd: torch.Tensor,
+               y: Optional[torch.Tensor] = None, packed: Optional[Packed] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Layer norm of the rows of `x` into `y` (x's type) and / or, in 8 bits, `packed`; `mean` and `rstd` for the backward pass."""
+    ldx = _matrix(x, "x")
+    rows, cols = x.shape
+    ldy = 0
+    if y is not None:
+        ldy = _matrix(y, "y", rows, cols)
+        if y.dtype != x.dtype:
+            raise ValueError("y: need x's type")
+    _done(lgc.lib().lgc_layer_norm(x.data_ptr(), _TYPES[x.dtype], rows, cols, ldx, _vector(gamma, cols, "gamma"), _vector(beta, cols, "beta"),
+                                   eps, None if y is None else y.data_ptr(), ldy,
+                                   None if packed is None else _packed(packed, "packed", rows, cols),
+                                   _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"), _stream(stream, x.device)), "lgc_layer_norm")
+
+
+def layer_norm_backward_scratch(rows: int, cols: int, num_nodes: int = 1) -> int:
+    """Bytes of scratch that layer_norm_backward needs."""
+    n = C.c_size_t()
+    _done(lgc.lib().lgc_layer_norm_backward_scratch(rows, cols, num_nodes, C.byref(n)), "lgc_layer_norm_backward_scratch")
+    return n.value
+
+
+def layer_norm_backward(dy: torch.Tensor, x: Union[torch.Tensor, Packed], gamma: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
+                        dx: torch.Tensor, dgamma: torch.Tensor, dbeta: torch.Tensor, node_start: Optional[torch.Tensor] = None,
+                        scratch: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Backward pass of layer_norm.  `x`: the input, or its 8-bit checkpoint.  `dgamma`, `dbeta`: [nodes][cols] views with
+    one row stride (columns of the nodes' gradients).  `scratch`: a uint8 tensor of layer_norm_backward_scratch bytes;
+    without one it comes from PyTorch's allocator."""
+    ld_dy = _matrix(dy, "dy")
+    rows, cols = dy.shape
+    ld_dx = _matrix(dx, "dx", rows, cols)
+    if dx.dtype != dy.dtype:
+        raise ValueError("dx: need dy's type")
+    start, K, stride = _nodes(node_start, dgamma, cols, "dgamma")
+    if _nodes(node_start, dbeta, cols, "dbeta")[1:] != (K, stride):
+        raise ValueError("dgamma and dbeta: need the same nodes and row stride")
+    kept = isinstance(x, Packed)
+    need = layer_norm_backward_scratch(rows, cols, K)
+    st = stream if stream is not None else torch.cuda.current_stream(dy.device)
+    if scratch is None:
+        scratch = torch.empty(need, dtype=torch.uint8, device=dy.device)
+        if stream is not None:
+            scratch.record_stream(stream)
+    elif not (scratch.is_cuda and scratch.dtype == torch.uint8 and scratch.is_contiguous()):
+        raise ValueError("scratch: need a contiguous uint8 CUDA tensor")
+    _done(lgc.lib().lgc_layer_norm_backward(
+        dy.data_ptr(), _TYPES[dy.dtype], ld_dy, None if kept else x.data_ptr(), TYPE_PACKED if kept else _TYPES.get(x.dtype, -1),
+        0 if kept else _matrix(x, "x", rows, cols), _packed(x, "x", rows, cols) if kept else None, rows, cols, _vector(gamma, cols, "gamma"),
+        _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"), start, K, dx.data_ptr(), ld_dx, dgamma.data_ptr(), dbeta.data_ptr(), stride,
+        scratch.data_ptr(), scratch.numel(), st.cuda_stream), "lgc_layer_norm_backward")
+
+
+def product(a: Packed, b: Packed, y: Optional[torch.Tensor] = None, packed: Optional[Packed] = None, across: bool = False,
+            slope: float = 1.0, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """act(a b^T), or with `across` act(a b), of 8-bit matrices (`b`: weights, block_rows 128) into `y` (fp32 or bf16) and / or,
+    in 8 bits, `packed`.  act: the leaky ReLU of `slope` (1: none)."""
+    rows, inner = a.rows, a.cols
+    cols = b.cols if across else b.rows
+    ap = _packed(a, "a", rows, inner)
+    bp = _packed(b, "b", inner if across else cols, cols if across else inner, BLOCK)
+    ldy = 0 if y is None else _matrix(y, "y", rows, cols)
+    _done(lgc.lib().lgc_product(ap, bp, 1 if across else 0, rows, cols, inner, slope, None if y is None else y.data_ptr(),
+                                TYPE_BF16 if y is None else _TYPES[y.dtype], ldy, None if packed is None else _packed(packed, "packed", rows, cols),
+                                _stream(stream, a.codes.device)), "lgc_product")
+
+
+def weight_gradient(dy: torch.Tensor, x: Packed, dw: torch.Tensor, node_start: Optional[torch.Tensor] = None,
+                    stream: Optional[torch.cuda.Stream] = None) -> None:
+    """dw[k] = the sum over node k's rows of dy^T x ([dy's columns][x's columns], flat), from the bf16 gradient `dy` (rows
+    16-byte aligned) and the 8-bit checkpoint `x`.  `dw`: a [nodes][n] fp32 view (columns of the nodes' gradients)."""
+    ld_dy = _matrix(dy, "dy")
+    if dy.dtype != torch.bfloat16:
+        raise ValueError("dy: need a bf16 tensor")
+    rows, cols = dy.shape
+    xp = _packed(x, "x", rows, x.cols)
+    start, K, stride = _nodes(node_start, dw, cols * x.cols, "dw")
+    _done(lgc.lib().lgc_weight_gradient(dy.data_ptr(), ld_dy, xp, rows, cols, x.cols, start, K, dw.data_ptr(), stride,
+                                        _stream(stream, dy.device)), "lgc_weight_gradient")
+
+
+def check(stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Waits for the stream and raises if a kernel of product or weight_gradient recorded a failure."""
+    s = stream if stream is not None else torch.cuda.current_stream()
+    _done(lgc.lib().lgc_layers_check(s.cuda_stream), "lgc_layers_check")

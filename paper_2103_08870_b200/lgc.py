@@ -28,6 +28,8 @@ EXPORTS = (
     "lgc_get_layout", "lgc_keep_counts", "lgc_get_slots", "lgc_get_buffers", "lgc_set_ae_params", "lgc_get_ae_params",
     "lgc_check", "lgc_status_string", "lgc_last_error", "lgc_topk_noalloc", "lgc_topk_noalloc_check", "lgc_kernel_launches",
     "lgc_selection_stats",
+    "lgc_pack", "lgc_unpack", "lgc_layer_norm", "lgc_layer_norm_backward_scratch", "lgc_layer_norm_backward", "lgc_product",
+    "lgc_weight_gradient", "lgc_layers_check",
 )
 NOALLOC_MAX_N = 16777216
 
@@ -40,6 +42,10 @@ class lgc_config(C.Structure):
         ("adam_lr", C.c_float), ("adam_beta1", C.c_float), ("adam_beta2", C.c_float), ("adam_eps", C.c_float),
         ("stream", C.c_void_p), ("grad_row_stride", C.c_int64), ("layer_mode", C.POINTER(C.c_uint8)),
     ]
+
+
+class lgc_packed(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("ld", C.c_int64), ("scales", C.c_void_p), ("ld_scales", C.c_int64)]
 
 
 _lib = None
@@ -86,6 +92,15 @@ def lib() -> C.CDLL:
         l.lgc_selection_stats.argtypes = [vp] + [C.POINTER(C.c_int64)] * 5
         l.lgc_kernel_launches.argtypes = []
         l.lgc_kernel_launches.restype = C.c_uint64
+        i32, i64, f32, pk = C.c_int32, C.c_int64, C.c_float, C.POINTER(lgc_packed)
+        l.lgc_pack.argtypes = [vp, i32, i64, i64, i64, i32, f32, pk, pk, vp, i64, vp]
+        l.lgc_unpack.argtypes = [pk, i64, i64, i32, vp, i32, i64, vp]
+        l.lgc_layer_norm.argtypes = [vp, i32, i64, i64, i64, vp, vp, f32, vp, i64, pk, vp, vp, vp]
+        l.lgc_layer_norm_backward_scratch.argtypes = [i64, i64, i32, C.POINTER(sz)]
+        l.lgc_layer_norm_backward.argtypes = [vp, i32, i64, vp, i32, i64, pk, i64, i64, vp, vp, vp, vp, i32, vp, i64, vp, vp, i64, vp, sz, vp]
+        l.lgc_product.argtypes = [pk, pk, i32, i64, i64, i64, f32, vp, i32, i64, pk, vp]
+        l.lgc_weight_gradient.argtypes = [vp, i64, pk, i64, i64, i64, vp, i32, vp, i64, vp]
+        l.lgc_layers_check.argtypes = [vp]
         for name in EXPORTS:            # every declared entry point must be exported
             getattr(l, name)
         _lib = l
