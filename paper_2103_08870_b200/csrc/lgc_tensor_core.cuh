@@ -6,7 +6,7 @@
 
 namespace lgc {
 
-constexpr int kTcSpinLimit = 4000000;   // mbarrier polls before a wait gives up
+constexpr long long kWaitCycles = 2000000000ll;   // a wait on an mbarrier gives up after about a second
 
 __device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
@@ -26,7 +26,8 @@ __device__ __forceinline__ void bar_arrive(uint32_t bar)
 // Polls the barrier; gives up when the limit is reached or another role has given up (then *failed is set).
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *failed)
 {
-    for (int i = 0; i < kTcSpinLimit; ++i) {
+    long long begin = 0;
+    for (;;) {
         uint32_t done;
         asm volatile(
             "{\n\t.reg .pred p;\n\t"
@@ -36,7 +37,10 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
             : "r"(bar), "r"(parity)
             : "memory");
         if (done) return true;
-        if ((i & 255) == 255 && *failed) return false;
+        const long long now = clock64();
+        if (begin == 0) begin = now;
+        if (*failed) return false;
+        if (now - begin > kWaitCycles) break;
     }
     *failed = 1;
     return false;
@@ -48,6 +52,50 @@ __device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity, vol
     if ((threadIdx.x & 31) == 0) have = bar_wait(bar, parity, failed) ? 1 : 0;
     return __shfl_sync(0xffffffffu, have, 0) != 0;
 }
+
+// ---- pairs of CTAs (clusters of two) ---------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t cluster_rank()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// The address, in CTA `rank` of the cluster, of what lies at `addr` in this one.
+__device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, uint32_t rank)
+{
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+// What the arrival publishes is this CTA's own shared memory and tensor memory, for the tensor cores: CTA scope is enough
+// (after async_proxy_fence or tc_fence_before).  Cluster scope would make every arrival drain the thread's writes and every
+// wait drop the L1 cache: 0.4 us per stage of the weight gradient.
+__device__ __forceinline__ void bar_arrive_cluster(uint32_t cluster_bar)
+{
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+// tcgen05 for the pair: tensor memory is allocated in both CTAs, one thread of CTA 0 issues, and completion arrives at the
+// same barrier of both.
+__device__ __forceinline__ void tc_alloc_pair(uint32_t *where, uint32_t cols)
+{
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(where)), "r"(cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tc_free_pair(uint32_t tmem, uint32_t cols)
+{
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols) : "memory");
+}
+__device__ __forceinline__ void tc_commit_pair(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3)
+                 : "memory");
+}
+
 // Shared memory that threads have written becomes visible to the tensor cores and the TMA.
 __device__ __forceinline__ void async_proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 

@@ -2,12 +2,15 @@
 //
 // The sum runs along the rows (tokens) of both operands, and the checkpoint's scale changes from row to row, so the
 // 8-bit tensor-core form, whose scales cover 32 steps of the sum, cannot take X without rounding it a second time.
-// Instead a code times its scale, exactly a bf16 number, is formed in shared memory by four warps between the TMA and the
+// Instead a code times its scale, exactly a bf16 number, is formed in shared memory by sixteen warps between the TMA and the
 // MMA; dY is bf16 and goes in as it is.  Both operands lie along their rows (MN-major): 128 bytes of columns per row.
 //
+// Two CTAs make a tile of 256 x 256 together (cta_group::2): each loads, and converts, half of both operands, which halves
+// what a tile of this size costs in loads and conversions per product.
+//
 // Rows of other nodes that a tile's last block of rows reaches are set to zero in both operands.
-// Sums: the tensor cores add in fp32 in tensor memory over at most kFlushRows rows; then the accumulator is drained into
-// registers and added to the total there, so that a long sum does not lose to the accumulator's rounding.
+// Sums: the tensor cores add in fp32 in tensor memory over at most 64 * 64 rows; longer sums are added up in memory from
+// there, so that they do not lose to the accumulator's rounding (it errs by about 2^-24 of the sum per 16 rows).
 #include "lgc_layers.cuh"
 #include "lgc_tensor_core.cuh"
 
@@ -15,16 +18,18 @@ namespace lgc {
 
 namespace {
 
-constexpr int kM = 128, kN = 128;                 // a CTA's tile: columns of dY x columns of X
+constexpr int kM = 256, kN = 256;                 // a pair's tile: columns of dY x columns of X; each CTA loads half of both
 constexpr int kRows = 64;                         // rows per stage
-constexpr int kABytes = kM * kRows * 2, kCodeBytes = kN * kRows, kBBytes = kN * kRows * 2;
+constexpr int kHalf = 128;
+constexpr int kABytes = kHalf * kRows * 2, kBBytes = kHalf * kRows * 2, kCodeBytes = kHalf * kRows;
+constexpr int kStageBytes = kABytes + kBBytes + kCodeBytes;
 constexpr int kPiece = 64 * kRows * 2;            // 64 columns (128 bytes) of a stage's rows in bf16
-constexpr int kStages = 4, kReady = 3;            // dY and codes as loaded; X as bf16
-constexpr int kFlushRows = 1024;
+constexpr int kStages = 5;
+constexpr int kFlushSteps = 64;                   // stages that the tensor cores add up before their sums go to memory
 constexpr int kPitch = 33;                        // floats per row of the result's staging blocks
 constexpr int kOutBytes = 4 * 32 * kPitch * 4;
-constexpr int kSmemBytes = kStages * (kABytes + kCodeBytes) + kReady * kBBytes + kOutBytes + 1024;
-constexpr int kThreads = 320;                     // warp 0: TMA and tensor memory, 1: MMA, 2..5: X to bf16, 6..9: results
+constexpr int kSmemBytes = kStages * (kStageBytes + kRows * 4) + kOutBytes + 1024;
+constexpr int kThreads = 768;                     // warp 0: TMA, 1: MMA, 2: scales, 3: tensor memory, 4..7: results, 8..23: X to bf16
 constexpr int kTmemCols = 2 * kN;
 
 __device__ __forceinline__ void mma_bf16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate)
@@ -32,7 +37,7 @@ __device__ __forceinline__ void mma_bf16(uint32_t d, uint64_t a, uint64_t b, uin
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
         "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
         ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate ? 1u : 0u)
         : "memory");
 }
@@ -80,190 +85,225 @@ __device__ __forceinline__ Tile tile_of(const WeightArgs &p, int64_t t)
     return w;
 }
 
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 weight_gradient_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ WeightArgs p)
 {
     extern __shared__ uint8_t dyn_smem[];
-    __shared__ __align__(8) uint64_t full_bar[kStages], empty_bar[kStages], ready_bar[kReady], used_bar[kReady], tfull_bar[2], tempty_bar[2];
+    // full: loads of a stage (both CTAs have their own); ready (CTA 0's): X of both halves is bf16; empty: the MMAs are through
+    __shared__ __align__(8) uint64_t full_bar[kStages], ready_bar[kStages], empty_bar[kStages], tfull_bar[2], tempty_bar[2];
     __shared__ uint32_t tmem_base;
     __shared__ volatile int failed;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t base = (smem_addr(dyn_smem) + 1023u) & ~1023u;
-    const uint32_t b_tiles = base + kStages * kABytes, codes = b_tiles + kReady * kBBytes;
-    constexpr int kFlushSteps = kFlushRows / kRows;
+    const uint32_t scale_words = base + kStages * kStageBytes;
     const int64_t total = (int64_t)p.tiles_m * p.tiles_n * p.nodes;
+    const uint32_t rank = cluster_rank();
+    const int64_t first = blockIdx.x >> 1, step = gridDim.x >> 1;
 
     if (threadIdx.x == 0) {
         failed = 0;
         for (int s = 0; s < kStages; ++s) {
-            bar_init(smem_addr(&full_bar[s]), 1);
+            bar_init(smem_addr(&full_bar[s]), 1 + 32);
+            bar_init(smem_addr(&ready_bar[s]), 2 * 8);
             bar_init(smem_addr(&empty_bar[s]), 1);
-        }
-        for (int s = 0; s < kReady; ++s) {
-            bar_init(smem_addr(&ready_bar[s]), 4);
-            bar_init(smem_addr(&used_bar[s]), 1);
         }
         for (int s = 0; s < 2; ++s) {
             bar_init(smem_addr(&tfull_bar[s]), 1);
-            bar_init(smem_addr(&tempty_bar[s]), 4);
+            bar_init(smem_addr(&tempty_bar[s]), 2 * 4);
         }
         bar_init_fence();
     }
-    if (warp == 0) tc_alloc(&tmem_base, kTmemCols);
+    if (warp == 3) tc_alloc_pair(&tmem_base, kTmemCols);
     tc_fence_before();
     __syncthreads();
+    cluster_sync();
     tc_fence_after();
     const uint32_t tmem = tmem_base;
 
     if (threadIdx.x == 0) {
         int it = 0;
-        for (int64_t t = blockIdx.x; t < total && !failed; t += gridDim.x) {
+        for (int64_t t = first; t < total && !failed; t += step) {
             const Tile w = tile_of(p, t);
+            const int mc = w.m * kM + (int)rank * kHalf, nc = w.n * kN + (int)rank * kHalf;
             for (int i = 0; i < w.steps; ++i, ++it) {
                 const int s = it % kStages;
                 if (it >= kStages && !bar_wait(smem_addr(&empty_bar[s]), ((it / kStages) & 1) ^ 1, &failed)) break;
-                const uint32_t bar = smem_addr(&full_bar[s]);
+                const uint32_t bar = smem_addr(&full_bar[s]), st = base + s * kStageBytes;
                 const int row = (int)(w.begin + (int64_t)i * kRows);
                 bar_expect(bar, kABytes + kCodeBytes);
 #pragma unroll
-                for (int j = 0; j < kM / 64; ++j) tma_load(base + s * kABytes + j * kPiece, &map_dy, bar, w.m * kM + 64 * j, row);
-#pragma unroll
-                for (int j = 0; j < kN / 64; ++j)
-                    tma_load(codes + s * kCodeBytes + j * 64 * kRows, &map_x, bar, w.n * kN + 64 * j, row);
+                for (int j = 0; j < 2; ++j) {
+                    tma_load(st + j * kPiece, &map_dy, bar, mc + 64 * j, row);
+                    tma_load(st + kABytes + kBBytes + j * 64 * kRows, &map_x, bar, nc + 64 * j, row);
+                }
             }
         }
-    } else if (threadIdx.x == 32) {
+    } else if (threadIdx.x == 32 && rank == 0) {
         // fp32 sums, bf16 x bf16, both operands MN-major
         constexpr uint32_t idesc = 1u << 4 | 1u << 7 | 1u << 10 | 1u << 15 | 1u << 16 | (uint32_t)(kN >> 3) << 17 | (uint32_t)(kM >> 4) << 24;
         int it = 0, acc = 0;
-        for (int64_t t = blockIdx.x; t < total && !failed; t += gridDim.x) {
+        for (int64_t t = first; t < total && !failed; t += step) {
             const Tile w = tile_of(p, t);
             bool ok = true;
             for (int i = 0; i < w.steps; ++i, ++it) {
-                const int s = it % kStages, b = it % kReady, buf = acc & 1;
-                const bool first = i % kFlushSteps == 0;
-                if (first && acc >= 2 && !bar_wait(smem_addr(&tempty_bar[buf]), ((acc >> 1) & 1) ^ 1, &failed)) { ok = false; break; }
-                // the warps that make B have waited for the loads; this thread reads dY and waits for itself
-                if (!bar_wait(smem_addr(&full_bar[s]), (it / kStages) & 1, &failed) ||
-                    !bar_wait(smem_addr(&ready_bar[b]), (it / kReady) & 1, &failed)) { ok = false; break; }
+                const int s = it % kStages, buf = acc & 1;
+                const bool begin = i % kFlushSteps == 0;
+                if (begin && acc >= 2 && !bar_wait(smem_addr(&tempty_bar[buf]), ((acc >> 1) & 1) ^ 1, &failed)) { ok = false; break; }
+                // the warps that make B wait for the loads of their CTA, dY among them
+                if (!bar_wait(smem_addr(&ready_bar[s]), (it / kStages) & 1, &failed)) { ok = false; break; }
                 tc_fence_after();
+                const uint32_t st = base + s * kStageBytes;
 #pragma unroll
                 for (int ks = 0; ks < kRows / 16; ++ks)           // 16 rows of 128 bytes per step
-                    mma_bf16(tmem + buf * kN, tc_desc(base + s * kABytes + ks * 2048, kPiece), tc_desc(b_tiles + b * kBBytes + ks * 2048, kPiece),
-                             idesc, !first || ks > 0);
-                tc_commit(smem_addr(&empty_bar[s]));
-                tc_commit(smem_addr(&used_bar[b]));
+                    mma_bf16(tmem + buf * kN, tc_desc(st + ks * 2048, kPiece), tc_desc(st + kABytes + ks * 2048, kPiece), idesc, !begin || ks > 0);
+                tc_commit_pair(smem_addr(&empty_bar[s]));
                 if (i % kFlushSteps == kFlushSteps - 1 || i == w.steps - 1) {
-                    tc_commit(smem_addr(&tfull_bar[buf]));
+                    tc_commit_pair(smem_addr(&tfull_bar[buf]));
                     ++acc;
                 }
             }
             if (!ok) break;
         }
-    } else if (warp >= 2 && warp < 6) {
-        const int id = threadIdx.x - 64;
+    } else if (warp == 2) {
+        // scale words of the stage's rows (four blocks each; this CTA's columns are one of them)
         int it = 0;
         bool ok = true;
-        for (int64_t t = blockIdx.x; t < total && ok; t += gridDim.x) {
+        for (int64_t t = first; t < total && ok; t += step) {
             const Tile w = tile_of(p, t);
+            const int64_t block = (int64_t)w.n * 2 + rank;
             for (int i = 0; i < w.steps; ++i, ++it) {
-                const int s = it % kStages, b = it % kReady;
-                const int64_t row0 = w.begin + (int64_t)i * kRows;
-                const int live = (int)min((int64_t)kRows, w.end - row0);          // rows of this node in the stage
-                if (!bar_wait_warp(smem_addr(&full_bar[s]), (it / kStages) & 1, &failed) ||
-                    (it >= kReady && !bar_wait_warp(smem_addr(&used_bar[b]), ((it / kReady) & 1) ^ 1, &failed))) { ok = false; break; }
-                // unit: 16 neighbouring codes of a row; four lanes per row of 64 columns
+                const int s = it % kStages;
+                if (it >= kStages && !bar_wait_warp(smem_addr(&empty_bar[s]), ((it / kStages) & 1) ^ 1, &failed)) { ok = false; break; }
 #pragma unroll
-                for (int u = id; u < kN * kRows / 16; u += 128) {
-                    const int quarter = u & 3, r = (u >> 2) & (kRows - 1), piece = u >> 8;
-                    uint32_t q[4], scale = 0;
+                for (int j = 0; j < kRows / 32; ++j) {
+                    const int64_t row = w.begin + (int64_t)i * kRows + 32 * j + lane;
+                    if (row < w.end && block * kBlock < p.inner)
+                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(scale_words + (s * kRows + 32 * j + lane) * 4),
+                                     "l"(p.scales + row * p.ld_scales + (block & ~(int64_t)3))
+                                     : "memory");
+                }
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_addr(&full_bar[s])) : "memory");
+            }
+        }
+    } else if (warp >= 8) {
+        // Two groups of eight warps take the stages in turn.  A thread converts 16 neighbouring codes of one row in both
+        // 64-column pieces; four lanes per row, so that eight lanes read and write 128 bytes without bank conflicts.
+        const int group = (warp - 8) >> 3, id = threadIdx.x & 255, quarter = id & 3, r = id >> 2;
+        const uint32_t from = kABytes + kBBytes + r * 64 + quarter * 16, to = kABytes + r * 128;
+        const uint32_t c0 = ((quarter * 2) ^ (r & 7)) << 4, c1 = ((quarter * 2 + 1) ^ (r & 7)) << 4;    // 16-byte chunks, swizzled by the row
+        int it = 0;
+        bool ok = true;
+        for (int64_t t = first; t < total && ok; t += step) {
+            const Tile w = tile_of(p, t);
+            const int64_t block = (int64_t)w.n * 2 + rank;
+            const bool any = block * kBlock < p.inner;
+            const int shift = (int)(block & 3) * 8;
+            for (int i = 0; i < w.steps; ++i, ++it) {
+                if ((it & 1) != group) continue;
+                const int s = it % kStages;
+                const uint32_t st = base + s * kStageBytes;
+                const bool live = r < w.end - (w.begin + (int64_t)i * kRows);        // the row is this node's
+                if (!bar_wait_warp(smem_addr(&full_bar[s]), (it / kStages) & 1, &failed)) { ok = false; break; }
+                uint32_t q[2][4], word;
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
                     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                                 : "=r"(q[0]), "=r"(q[1]), "=r"(q[2]), "=r"(q[3])
-                                 : "r"(codes + s * kCodeBytes + piece * 64 * kRows + r * 64 + quarter * 16));
-                    const int64_t block = ((int64_t)w.n * kN + piece * 64) / kBlock;
-                    uint32_t f1 = 0, f2 = 0x3f803f80u;
-                    if (r < live && block * kBlock < p.inner) {
-                        scale = __ldg(p.scales + (row0 + r) * p.ld_scales + block);
-                        // scale * 2^120 in two factors where one is beyond bf16's exponents
-                        const uint32_t e1 = scale == 255u ? 255u : min(scale, 134u) + 120u, e2 = scale == 255u ? 127u : max(scale, 134u) - 7u;
-                        f1 = scale == 255u ? 0x7fff7fffu : (e1 << 7) * 0x10001u;
-                        f2 = (e2 << 7) * 0x10001u;
-                    }
-                    uint32_t x[8];
+                                 : "=r"(q[j][0]), "=r"(q[j][1]), "=r"(q[j][2]), "=r"(q[j][3])
+                                 : "r"(st + from + j * 64 * kRows));
+                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(word) : "r"(scale_words + (s * kRows + r) * 4));
+                const uint32_t scale = (word >> shift) & 255u;
+                // scale * 2^120, in two factors where that is beyond bf16's exponents
+                uint32_t f1 = ((min(scale, 134u) + 120u) << 7) * 0x10001u, f2 = 0;
+                if (scale > 134u) {
+                    if (scale == 255u) f1 = 0x7fff7fffu;
+                    else f2 = ((scale - 7u) << 7) * 0x10001u;
+                }
+                if (!live || !any) f1 = f2 = 0;
+                uint32_t x[2][8];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        x[2 * j] = codes_to_bf16(q[j], 0x1404, f1);
-                        x[2 * j + 1] = codes_to_bf16(q[j], 0x3424, f1);
-                    }
-                    if (scale > 134u)
+                for (int j = 0; j < 2; ++j)
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(x[j]) : "r"(f2));
-                    const uint32_t at = b_tiles + b * kBBytes + piece * kPiece + r * 128;
-                    const int c0 = quarter * 2;                                    // 16-byte chunks, swizzled by the row
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + (((c0) ^ (r & 7)) << 4)), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + (((c0 + 1) ^ (r & 7)) << 4)), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]) : "memory");
-                    if (r >= live) {
-                        // a row of another node: dY's part becomes zero as well (its chunks of 16 bytes, whatever their order)
-                        const uint32_t a = base + s * kABytes + piece * kPiece + r * 128 + quarter * 32;
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(a), "r"(0) : "memory");
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(a + 16), "r"(0) : "memory");
+                    for (int k = 0; k < 4; ++k) {
+                        x[j][2 * k] = codes_to_bf16(q[j][k], 0x1404, f1);
+                        x[j][2 * k + 1] = codes_to_bf16(q[j][k], 0x3424, f1);
                     }
+                if (f2 != 0)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(x[j >> 3][j & 7]) : "r"(f2));
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const uint32_t at = st + to + j * kPiece;
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + c0), "r"(x[j][0]), "r"(x[j][1]), "r"(x[j][2]), "r"(x[j][3]) : "memory");
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + c1), "r"(x[j][4]), "r"(x[j][5]), "r"(x[j][6]), "r"(x[j][7]) : "memory");
+                }
+                if (!live) {
+                    // a row of another node: dY's part becomes zero as well (its chunks of 16 bytes, whatever their order)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(st + (j >> 1) * kPiece + r * 128 + quarter * 32 + (j & 1) * 16), "r"(0)
+                                     : "memory");
                 }
                 async_proxy_fence();
                 __syncwarp();
-                if (lane == 0) bar_arrive(smem_addr(&ready_bar[b]));
+                if (lane == 0) bar_arrive_cluster(cluster_addr(smem_addr(&ready_bar[s]), 0));
             }
         }
-    } else if (warp >= 6) {
+    } else if (warp >= 4) {
         const int q = warp & 3;
-        float *stage = reinterpret_cast<float *>(dyn_smem + (base - smem_addr(dyn_smem)) + kStages * (kABytes + kCodeBytes) + kReady * kBBytes) +
-                       q * 32 * kPitch;
+        float *stage = reinterpret_cast<float *>(dyn_smem + (scale_words - smem_addr(dyn_smem)) + kStages * kRows * 4) + q * 32 * kPitch;
         int acc = 0;
         bool ok = true;
-        for (int64_t t = blockIdx.x; t < total && ok; t += gridDim.x) {
+        for (int64_t t = first; t < total && ok; t += step) {
             const Tile w = tile_of(p, t);
-            float v[kN];
-#pragma unroll
-            for (int c = 0; c < kN; ++c) v[c] = 0.0f;
-            for (int i = 0; i < w.steps; i += kFlushSteps, ++acc) {
-                const int buf = acc & 1;
-                if (!bar_wait_warp(smem_addr(&tfull_bar[buf]), (acc >> 1) & 1, &failed)) { ok = false; break; }
-                tc_fence_after();
-                const uint32_t at = tmem + buf * kN + ((uint32_t)(q * 32) << 16);
-#pragma unroll
-                for (int c = 0; c < kN; c += 32) {
-                    uint32_t r[32];
-                    tc_read32(at + c, r);
-                    tc_read_wait(r);
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) v[c + j] = __fadd_rn(v[c + j], __uint_as_float(r[j]));
-                }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) bar_arrive(smem_addr(&tempty_bar[buf]));
-            }
-            if (!ok) break;
-            // 32 x 32 entries at a time through shared memory: a warp writes 32 neighbours of a row, wherever the row starts
             float *out = p.dw + w.node * p.node_stride;
-            const int64_t row0 = (int64_t)w.m * kM + q * 32;
+            const int64_t row0 = (int64_t)w.m * kM + rank * kHalf + q * 32;
+            // (a node without rows: its gradient is zero)
+            for (int i = 0; i == 0 || i < w.steps; i += kFlushSteps) {
+                const int buf = acc & 1;
+                if (w.steps > 0) {
+                    if (!bar_wait_warp(smem_addr(&tfull_bar[buf]), (acc >> 1) & 1, &failed)) { ok = false; break; }
+                    tc_fence_after();
+                    ++acc;
+                }
+                const uint32_t at = tmem + buf * kN + ((uint32_t)(q * 32) << 16);
+#pragma unroll 1
+                for (int c = 0; c < kN; c += 32) {
+                    uint32_t v[32];
+                    if (w.steps > 0) {
+                        tc_read32(at + c, v);
+                        tc_read_wait(v);
+                    } else {
 #pragma unroll
-            for (int c = 0; c < kN; c += 32) {
-                __syncwarp();
+                        for (int j = 0; j < 32; ++j) v[j] = 0;
+                    }
+                    // 32 x 32 entries through shared memory: a warp writes 32 neighbours of a row, wherever the row starts
+                    __syncwarp();
 #pragma unroll
-                for (int j = 0; j < 32; ++j) stage[lane * kPitch + j] = v[c + j];
-                __syncwarp();
-                const int64_t col = (int64_t)w.n * kN + c + lane;
-                if (col < p.inner)
+                    for (int j = 0; j < 32; ++j) stage[lane * kPitch + j] = __uint_as_float(v[j]);
+                    __syncwarp();
+                    const int64_t col = (int64_t)w.n * kN + c + lane;
+                    if (col < p.inner)
 #pragma unroll 8
-                    for (int j = 0; j < 32; ++j)
-                        if (row0 + j < p.cols) out[(row0 + j) * p.inner + col] = stage[j * kPitch + lane];
+                        for (int j = 0; j < 32; ++j)
+                            if (row0 + j < p.cols) {
+                                float *o = out + (row0 + j) * p.inner + col;
+                                const float x = stage[j * kPitch + lane];
+                                *o = i == 0 ? x : __fadd_rn(*o, x);
+                            }
+                }
+                if (w.steps > 0) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive_cluster(cluster_addr(smem_addr(&tempty_bar[buf]), 0));
+                }
             }
         }
     }
     tc_fence_before();
     __syncthreads();
+    cluster_sync();                       // the other CTA's MMAs read this one's shared memory
     if (threadIdx.x == 0 && failed) atomicExch(p.errword, 2);
-    if (warp == 0) tc_free(tmem, kTmemCols);
+    if (warp == 3) tc_free_pair(tmem, kTmemCols);
 }
 
 }  // namespace
@@ -283,7 +323,8 @@ cudaError_t launch_weight_gradient(const void *dy, int64_t ld_dy, const lgc_pack
     e = configured.run([&] { return cudaFuncSetAttribute(weight_gradient_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes); });
     if (e != cudaSuccess) return e;
     const int64_t total = (int64_t)p.tiles_m * p.tiles_n * num_nodes;
-    weight_gradient_kernel<<<(unsigned)(total < sm_count() ? total : sm_count()), kThreads, kSmemBytes, s>>>(map_dy, map_x, p);
+    const int64_t pairs = sm_count() / 2;
+    weight_gradient_kernel<<<(unsigned)(2 * (total < pairs ? total : pairs)), kThreads, kSmemBytes, s>>>(map_dy, map_x, p);
     ++g_kernel_launches;
     return cudaGetLastError();
 }
