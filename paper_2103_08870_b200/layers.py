@@ -38,21 +38,22 @@ class Packed:
     __slots__ = ("codes", "scales", "rows", "cols", "block_rows", "_c")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, cols: Optional[int] = None, block_rows: int = 1):
-        if not (codes.is_cuda and scales.is_cuda and codes.dtype == torch.uint8 and scales.dtype == torch.uint8
-                and codes.dim() == 2 and scales.dim() == 2):
+        if not (codes.is_cuda and scales.is_cuda and codes.dtype is torch.uint8 and scales.dtype is torch.uint8):
             raise ValueError("codes and scales: need 2-D uint8 CUDA tensors")
-        rows = codes.shape[0]
-        cols = codes.shape[1] if cols is None else cols
-        if block_rows not in (1, BLOCK):
+        shape, tall, ld, lds = codes.shape, scales.shape, codes.stride(), scales.stride()
+        if len(shape) != 2 or len(tall) != 2:
+            raise ValueError("codes and scales: need 2-D uint8 CUDA tensors")
+        rows, width = shape
+        if cols is None:
+            cols = width
+        if block_rows != 1 and block_rows != BLOCK:
             raise ValueError("block_rows: 1 or 128")
-        if not (0 < cols <= codes.shape[1] and codes.stride(1) == 1 and scales.stride(1) == 1
-                and scales.shape[0] == -(-rows // block_rows) and scales.shape[1] * BLOCK >= cols):
+        if not (0 < cols <= width and ld[1] == 1 and lds[1] == 1 and tall[0] == -(-rows // block_rows) and tall[1] * BLOCK >= cols):
             raise ValueError("codes need unit column stride and `cols` columns, scales a row per row of blocks and a byte per block")
         self.codes, self.scales, self.rows, self.cols, self.block_rows = codes, scales, rows, cols, block_rows
         # (the row stride of a tensor with one row may be anything)
-        ld = codes.stride(0) if rows > 1 else max(codes.stride(0), -(-codes.shape[1] // 16) * 16)
-        lds = scales.stride(0) if scales.shape[0] > 1 else max(scales.stride(0), -(-scales.shape[1] // 4) * 4)
-        self._c = lgc.lgc_packed(codes.data_ptr(), ld, scales.data_ptr(), lds)
+        self._c = lgc.lgc_packed(codes.data_ptr(), ld[0] if rows > 1 else -(-width // 16) * 16,
+                                 scales.data_ptr(), lds[0] if tall[0] > 1 else -(-tall[1] // 4) * 4)
 
 
 def packed_empty(rows: int, cols: int, block_rows: int = 1, device: Optional[torch.device] = None) -> Packed:
@@ -62,22 +63,29 @@ def packed_empty(rows: int, cols: int, block_rows: int = 1, device: Optional[tor
                   torch.empty(-(-rows // block_rows), -(-cols // (4 * BLOCK)) * 4, dtype=torch.uint8, device=dev), cols, block_rows)
 
 
-def _stream(stream: Optional[torch.cuda.Stream], device: torch.device) -> int:
-    return (stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream
+def _stream(stream: Optional[torch.cuda.Stream], t: torch.Tensor) -> int:
+    # (torch.cuda.current_stream builds a Stream object: 2 us, as much as the launch)
+    return torch._C._cuda_getCurrentRawStream(t.get_device()) if stream is None else stream.cuda_stream
 
 
-def _matrix(t: torch.Tensor, name: str, rows: Optional[int] = None, cols: Optional[int] = None) -> int:
-    """Row stride of a matrix argument, after the checks that need the tensor (the library checks the numbers)."""
-    if not t.is_cuda or t.dtype not in _TYPES or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+def _matrix(t: torch.Tensor, name: str, want: Optional[tuple] = None):
+    """(rows, columns, row stride, type) of a matrix argument, after the checks that need the tensor (the library checks the
+    numbers)."""
+    shape, kind = t.shape, _TYPES.get(t.dtype)
+    if kind is None or len(shape) != 2 or not t.is_cuda:
         raise ValueError(f"{name}: need a 2-D fp32 or bf16 CUDA tensor with unit column stride")
-    if (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
-        raise ValueError(f"{name}: need {rows} x {cols} elements, got {t.shape[0]} x {t.shape[1]}")
+    ld, unit = t.stride()
+    rows, cols = shape
+    if unit != 1 and cols > 1:
+        raise ValueError(f"{name}: need a 2-D fp32 or bf16 CUDA tensor with unit column stride")
+    if want is not None and (rows, cols) != want:
+        raise ValueError(f"{name}: need {want[0]} x {want[1]} elements, got {rows} x {cols}")
     # a single row may have any stride: report one that the library accepts
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), -(-t.shape[1] // 8) * 8)
+    return rows, cols, (ld if rows > 1 else -(-cols // 8) * 8), kind
 
 
 def _vector(t: torch.Tensor, n: int, name: str) -> int:
-    if not (t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and t.numel() == n):
+    if not (t.dtype is torch.float32 and t.is_cuda and t.numel() == n and t.is_contiguous()):
         raise ValueError(f"{name}: need a contiguous fp32 CUDA tensor of {n} elements")
     return t.data_ptr()
 
@@ -111,39 +119,37 @@ def pack(x: torch.Tensor, out: Packed, slope: float = 1.0, gate: Optional[Packed
          stream: Optional[torch.cuda.Stream] = None) -> None:
     """`x` (fp32 or bf16), through a leaky ReLU of `slope` (1: none), to 8 bits.  With `gate` (the 8-bit result of that
     leaky ReLU) `x` is a gradient and gets its derivative instead.  `y` (bf16): also what was rounded."""
-    ldx = _matrix(x, "x")
-    rows, cols = x.shape
-    ldy = 0
+    rows, cols, ldx, kind = _matrix(x, "x")
+    yp = ldy = None
     if y is not None:
-        ldy = _matrix(y, "y", rows, cols)
-        if y.dtype != torch.bfloat16:
+        _, _, ldy, ykind = _matrix(y, "y", (rows, cols))
+        if ykind != TYPE_BF16:
             raise ValueError("y: need a bf16 tensor")
-    _done(lgc.lib().lgc_pack(x.data_ptr(), _TYPES[x.dtype], rows, cols, ldx, out.block_rows, slope,
+        yp = y.data_ptr()
+    _done(lgc.lib().lgc_pack(x.data_ptr(), kind, rows, cols, ldx, out.block_rows, slope,
                              None if gate is None else _packed(gate, "gate", rows, cols), _packed(out, "out", rows, cols, out.block_rows),
-                             None if y is None else y.data_ptr(), ldy, _stream(stream, x.device)), "lgc_pack")
+                             yp, ldy or 0, _stream(stream, x)), "lgc_pack")
 
 
 def unpack(src: Packed, y: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
     """The values of an 8-bit matrix in `y` (fp32 or bf16; exact in both)."""
-    ldy = _matrix(y, "y", src.rows, src.cols)
-    _done(lgc.lib().lgc_unpack(C.byref(src._c), src.rows, src.cols, src.block_rows, y.data_ptr(), _TYPES[y.dtype], ldy,
-                               _stream(stream, y.device)), "lgc_unpack")
+    rows, cols, ldy, kind = _matrix(y, "y", (src.rows, src.cols))
+    _done(lgc.lib().lgc_unpack(C.byref(src._c), rows, cols, src.block_rows, y.data_ptr(), kind, ldy, _stream(stream, y)), "lgc_unpack")
 
 
 def layer_norm(x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor, eps: float, mean: torch.Tensor, rstd: torch.Tensor,
                y: Optional[torch.Tensor] = None, packed: Optional[Packed] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
     """Layer norm of the rows of `x` into `y` (x's type) and / or, in 8 bits, `packed`; `mean` and `rstd` for the backward pass."""
-    ldx = _matrix(x, "x")
-    rows, cols = x.shape
-    ldy = 0
+    rows, cols, ldx, kind = _matrix(x, "x")
+    yp = ldy = None
     if y is not None:
-        ldy = _matrix(y, "y", rows, cols)
-        if y.dtype != x.dtype:
+        _, _, ldy, ykind = _matrix(y, "y", (rows, cols))
+        if ykind != kind:
             raise ValueError("y: need x's type")
-    _done(lgc.lib().lgc_layer_norm(x.data_ptr(), _TYPES[x.dtype], rows, cols, ldx, _vector(gamma, cols, "gamma"), _vector(beta, cols, "beta"),
-                                   eps, None if y is None else y.data_ptr(), ldy,
-                                   None if packed is None else _packed(packed, "packed", rows, cols),
-                                   _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"), _stream(stream, x.device)), "lgc_layer_norm")
+        yp = y.data_ptr()
+    _done(lgc.lib().lgc_layer_norm(x.data_ptr(), kind, rows, cols, ldx, _vector(gamma, cols, "gamma"), _vector(beta, cols, "beta"), eps, yp,
+                                   ldy or 0, None if packed is None else _packed(packed, "packed", rows, cols),
+                                   _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"), _stream(stream, x)), "lgc_layer_norm")
 
 
 def layer_norm_backward_scratch(rows: int, cols: int, num_nodes: int = 1) -> int:
@@ -153,34 +159,42 @@ def layer_norm_backward_scratch(rows: int, cols: int, num_nodes: int = 1) -> int
     return n.value
 
 
+def _scratch(need: int, scratch: Optional[torch.Tensor], stream: Optional[torch.cuda.Stream], like: torch.Tensor):
+    """(tensor, bytes) of a call's scratch: the caller's, or from PyTorch's allocator."""
+    if scratch is None:
+        scratch = torch.empty(need, dtype=torch.uint8, device=like.device)
+        if stream is not None:
+            scratch.record_stream(stream)
+        return scratch, need
+    if not (scratch.is_cuda and scratch.dtype is torch.uint8 and scratch.is_contiguous()):
+        raise ValueError("scratch: need a contiguous uint8 CUDA tensor")
+    return scratch, scratch.numel()
+
+
 def layer_norm_backward(dy: torch.Tensor, x: Union[torch.Tensor, Packed], gamma: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
                         dx: torch.Tensor, dgamma: torch.Tensor, dbeta: torch.Tensor, node_start: Optional[torch.Tensor] = None,
                         scratch: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
     """Backward pass of layer_norm.  `x`: the input, or its 8-bit checkpoint.  `dgamma`, `dbeta`: [nodes][cols] views with
     one row stride (columns of the nodes' gradients).  `scratch`: a uint8 tensor of layer_norm_backward_scratch bytes;
     without one it comes from PyTorch's allocator."""
-    ld_dy = _matrix(dy, "dy")
-    rows, cols = dy.shape
-    ld_dx = _matrix(dx, "dx", rows, cols)
-    if dx.dtype != dy.dtype:
+    rows, cols, ld_dy, kind = _matrix(dy, "dy")
+    _, _, ld_dx, dx_kind = _matrix(dx, "dx", (rows, cols))
+    if dx_kind != kind:
         raise ValueError("dx: need dy's type")
-    start, K, stride = _nodes(node_start, dgamma, cols, "dgamma")
-    if _nodes(node_start, dbeta, cols, "dbeta")[1:] != (K, stride):
+    nodes = _nodes(node_start, dgamma, cols, "dgamma")
+    if _nodes(node_start, dbeta, cols, "dbeta") != nodes:
         raise ValueError("dgamma and dbeta: need the same nodes and row stride")
-    kept = isinstance(x, Packed)
-    need = layer_norm_backward_scratch(rows, cols, K)
-    st = stream if stream is not None else torch.cuda.current_stream(dy.device)
-    if scratch is None:
-        scratch = torch.empty(need, dtype=torch.uint8, device=dy.device)
-        if stream is not None:
-            scratch.record_stream(stream)
-    elif not (scratch.is_cuda and scratch.dtype == torch.uint8 and scratch.is_contiguous()):
-        raise ValueError("scratch: need a contiguous uint8 CUDA tensor")
+    start, K, stride = nodes
+    if isinstance(x, Packed):
+        xp, ldx, xkind, x8 = None, 0, TYPE_PACKED, _packed(x, "x", rows, cols)
+    else:
+        _, _, ldx, xkind = _matrix(x, "x", (rows, cols))
+        xp, x8 = x.data_ptr(), None
+    scratch, size = _scratch(layer_norm_backward_scratch(rows, cols, K), scratch, stream, dy)
     _done(lgc.lib().lgc_layer_norm_backward(
-        dy.data_ptr(), _TYPES[dy.dtype], ld_dy, None if kept else x.data_ptr(), TYPE_PACKED if kept else _TYPES.get(x.dtype, -1),
-        0 if kept else _matrix(x, "x", rows, cols), _packed(x, "x", rows, cols) if kept else None, rows, cols, _vector(gamma, cols, "gamma"),
-        _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"), start, K, dx.data_ptr(), ld_dx, dgamma.data_ptr(), dbeta.data_ptr(), stride,
-        scratch.data_ptr(), scratch.numel(), st.cuda_stream), "lgc_layer_norm_backward")
+        dy.data_ptr(), kind, ld_dy, xp, xkind, ldx, x8, rows, cols, _vector(gamma, cols, "gamma"), _vector(mean, rows, "mean"),
+        _vector(rstd, rows, "rstd"), start, K, dx.data_ptr(), ld_dx, dgamma.data_ptr(), dbeta.data_ptr(), stride, scratch.data_ptr(), size,
+        _stream(stream, dy)), "lgc_layer_norm_backward")
 
 
 def product(a: Packed, b: Packed, y: Optional[torch.Tensor] = None, packed: Optional[Packed] = None, across: bool = False,
@@ -191,24 +205,26 @@ def product(a: Packed, b: Packed, y: Optional[torch.Tensor] = None, packed: Opti
     cols = b.cols if across else b.rows
     ap = _packed(a, "a", rows, inner)
     bp = _packed(b, "b", inner if across else cols, cols if across else inner, BLOCK)
-    ldy = 0 if y is None else _matrix(y, "y", rows, cols)
-    _done(lgc.lib().lgc_product(ap, bp, 1 if across else 0, rows, cols, inner, slope, None if y is None else y.data_ptr(),
-                                TYPE_BF16 if y is None else _TYPES[y.dtype], ldy, None if packed is None else _packed(packed, "packed", rows, cols),
-                                _stream(stream, a.codes.device)), "lgc_product")
+    yp, ldy, kind = None, 0, TYPE_BF16
+    if y is not None:
+        _, _, ldy, kind = _matrix(y, "y", (rows, cols))
+        yp = y.data_ptr()
+    _done(lgc.lib().lgc_product(ap, bp, 1 if across else 0, rows, cols, inner, slope, yp, kind, ldy,
+                                None if packed is None else _packed(packed, "packed", rows, cols), _stream(stream, a.codes)), "lgc_product")
 
 
 def weight_gradient(dy: torch.Tensor, x: Packed, dw: torch.Tensor, node_start: Optional[torch.Tensor] = None,
                     stream: Optional[torch.cuda.Stream] = None) -> None:
     """dw[k] = the sum over node k's rows of dy^T x ([dy's columns][x's columns], flat), from the bf16 gradient `dy` (rows
     16-byte aligned) and the 8-bit checkpoint `x`.  `dw`: a [nodes][n] fp32 view (columns of the nodes' gradients)."""
-    ld_dy = _matrix(dy, "dy")
-    if dy.dtype != torch.bfloat16:
+    rows, cols, ld_dy, kind = _matrix(dy, "dy")
+    if kind != TYPE_BF16:
         raise ValueError("dy: need a bf16 tensor")
-    rows, cols = dy.shape
-    xp = _packed(x, "x", rows, x.cols)
-    start, K, stride = _nodes(node_start, dw, cols * x.cols, "dw")
-    _done(lgc.lib().lgc_weight_gradient(dy.data_ptr(), ld_dy, xp, rows, cols, x.cols, start, K, dw.data_ptr(), stride,
-                                        _stream(stream, dy.device)), "lgc_weight_gradient")
+    inner = x.cols
+    xp = _packed(x, "x", rows, inner)
+    start, K, stride = _nodes(node_start, dw, cols * inner, "dw")
+    _done(lgc.lib().lgc_weight_gradient(dy.data_ptr(), ld_dy, xp, rows, cols, inner, start, K, dw.data_ptr(), stride, _stream(stream, dy)),
+          "lgc_weight_gradient")
 
 
 def check(stream: Optional[torch.cuda.Stream] = None) -> None:
