@@ -12,6 +12,12 @@ bool matrix_rows_aligned(const void *p, int64_t ld, int elem_bytes)
     return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && (ld * elem_bytes) % 16 == 0;
 }
 
+int matrix_alignment(const void *p, int64_t ld, int elem_bytes)
+{
+    const uint64_t bits = reinterpret_cast<uintptr_t>(p) | (uint64_t)(ld * elem_bytes);
+    return bits % 32 == 0 ? 32 : bits % 16 == 0 ? 16 : 0;
+}
+
 namespace {
 
 static __device__ int32_t g_layers_record;      // a handle in host code: see record_address

@@ -27,16 +27,27 @@ __device__ __forceinline__ float block_inverse(uint32_t s) { return __uint_as_fl
 __device__ __forceinline__ float block_factor(uint32_t s) { return s == 255u ? __uint_as_float(0x7fffffffu) : __uint_as_float(s << 23); }
 
 // Four entries of a block to codes, first entry in the lowest byte.
+__device__ __forceinline__ uint32_t codes4_bad(float a, float b, float c, float d)       // a block with s = 255: the signs stay
+{
+    return 0x7f7f7f7fu | (__float_as_uint(a) >> 31) << 7 | (__float_as_uint(b) >> 31) << 15 | (__float_as_uint(c) >> 31) << 23 |
+           (__float_as_uint(d) >> 31) << 31;
+}
+__device__ __forceinline__ uint32_t codes4_scaled(float a, float b, float c, float d)    // entries times 2^(127 - s)
+{
+    uint32_t r;
+    asm("{\n\t.reg .b16 l, h;\n\t"
+        "cvt.rn.satfinite.e4m3x2.f32 l, %2, %1;\n\t"
+        "cvt.rn.satfinite.e4m3x2.f32 h, %4, %3;\n\t"
+        "mov.b32 %0, {l, h};\n\t}"
+        : "=r"(r)
+        : "f"(a), "f"(b), "f"(c), "f"(d));
+    return r;
+}
 __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, uint32_t s)
 {
-    if (s == 255u)
-        return 0x7f7f7f7fu | (__float_as_uint(a) >> 31) << 7 | (__float_as_uint(b) >> 31) << 15 | (__float_as_uint(c) >> 31) << 23 |
-               (__float_as_uint(d) >> 31) << 31;
+    if (s == 255u) return codes4_bad(a, b, c, d);
     const float r = block_inverse(s);                                 // exact products: r is a power of two
-    uint16_t lo, hi;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(__fmul_rn(b, r)), "f"(__fmul_rn(a, r)));
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(__fmul_rn(d, r)), "f"(__fmul_rn(c, r)));
-    return (uint32_t)lo | (uint32_t)hi << 16;
+    return codes4_scaled(__fmul_rn(a, r), __fmul_rn(b, r), __fmul_rn(c, r), __fmul_rn(d, r));
 }
 // Four codes to floats (without the scale).
 __device__ __forceinline__ void codes_to_float4(uint32_t q, float (&v)[4])
@@ -134,6 +145,147 @@ __device__ __forceinline__ uint32_t most_of_block(const float (&v)[8])
     return m;
 }
 
+// ---- sixteen neighbouring entries of a row, as pairs ---------------------------------------------------------------------
+// The streaming kernels are close to the issue rate, so they work on pairs of fp32 numbers in one instruction (add, mul,
+// fma .f32x2), take the magnitude's maximum of two entries at a time, and give a lane 16 neighbours: eight lanes hold a
+// block, three shuffles find its maximum, and a lane's codes are one 16-byte store.
+typedef unsigned long long f2;          // (lower entry, upper entry)
+__device__ __forceinline__ f2 f2_of(float lo, float hi)
+{
+    f2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float f2_lo(f2 a) { return __uint_as_float((uint32_t)a); }
+__device__ __forceinline__ float f2_hi(f2 a) { return __uint_as_float((uint32_t)(a >> 32)); }
+__device__ __forceinline__ f2 f2_add(f2 a, f2 b) { f2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f2 f2_mul(f2 a, f2 b) { f2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f2 f2_fma(f2 a, f2 b, f2 c) { f2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+// The largest magnitude, NaN if there is one.
+__device__ __forceinline__ float most2(f2 a, float m)
+{
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(f2_lo(a)), "f"(f2_hi(a)), "f"(m));
+    return r;
+}
+
+template <typename T>
+struct Raw16 {                           // sixteen entries as they lie in memory
+    uint32_t w[4 * sizeof(T)];
+};
+__device__ __forceinline__ f2 raw_pair(const Raw16<__nv_bfloat16> &q, int i)
+{
+    return f2_of(__uint_as_float(q.w[i] << 16), __uint_as_float(q.w[i] & 0xffff0000u));
+}
+__device__ __forceinline__ f2 raw_pair(const Raw16<float> &q, int i) { return f2_of(__uint_as_float(q.w[2 * i]), __uint_as_float(q.w[2 * i + 1])); }
+
+// AL: the rows' alignment in bytes (32, 16; 0 = any), c a multiple of 16.  Entries from `cols` on read as zero.
+template <int AL, typename T>
+__device__ __forceinline__ void load16(const T *row, int c, int cols, Raw16<T> &q)
+{
+    constexpr int kWords = 4 * sizeof(T);
+    if (AL > 0 && c + 16 <= cols) {
+        const uint32_t *p = reinterpret_cast<const uint32_t *>(row + c);
+        if (AL == 32) {
+#pragma unroll
+            for (int i = 0; i < kWords; i += 8)
+                asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                             : "=r"(q.w[i]), "=r"(q.w[i + 1]), "=r"(q.w[i + 2]), "=r"(q.w[i + 3]), "=r"(q.w[i + 4]), "=r"(q.w[i + 5]),
+                               "=r"(q.w[i + 6]), "=r"(q.w[i + 7])
+                             : "l"(p + i));
+        } else {
+#pragma unroll
+            for (int i = 0; i < kWords; i += 4) {
+                const uint4 a = __ldg(reinterpret_cast<const uint4 *>(p + i));
+                q.w[i] = a.x, q.w[i + 1] = a.y, q.w[i + 2] = a.z, q.w[i + 3] = a.w;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const uint32_t x = c + i < cols ? (sizeof(T) == 2 ? (uint32_t)reinterpret_cast<const uint16_t *>(row)[c + i]
+                                                              : reinterpret_cast<const uint32_t *>(row)[c + i])
+                                            : 0u;
+            if (sizeof(T) == 4) q.w[i % kWords] = x;
+            else if (i & 1) q.w[i / 2] |= x << 16;
+            else q.w[i / 2] = x;
+        }
+    }
+}
+template <int AL, typename T>
+__device__ __forceinline__ void store16(T *row, int c, int cols, const f2 (&v)[8])
+{
+    if (AL > 0 && c + 16 <= cols) {
+        uint32_t w[4 * sizeof(T)];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (sizeof(T) == 2) w[i] = bf16_pair(f2_lo(v[i]), f2_hi(v[i]));
+            else w[(2 * i) % (4 * sizeof(T))] = (uint32_t)v[i], w[(2 * i + 1) % (4 * sizeof(T))] = (uint32_t)(v[i] >> 32);
+        uint32_t *p = reinterpret_cast<uint32_t *>(row + c);
+        if (AL == 32) {
+#pragma unroll
+            for (int i = 0; i < (int)(4 * sizeof(T)); i += 8)
+                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p + i), "r"(w[i]), "r"(w[i + 1]), "r"(w[i + 2]),
+                             "r"(w[i + 3]), "r"(w[i + 4]), "r"(w[i + 5]), "r"(w[i + 6]), "r"(w[i + 7])
+                             : "memory");
+        } else {
+#pragma unroll
+            for (int i = 0; i < (int)(4 * sizeof(T)); i += 4) *reinterpret_cast<uint4 *>(p + i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (c + i < cols) row[c + i] = (T)((i & 1) ? f2_hi(v[i / 2]) : f2_lo(v[i / 2]));
+    }
+}
+__device__ __forceinline__ void store_codes16(uint8_t *row, int c, int cols, const uint32_t (&q)[4])
+{
+    if (c + 16 <= cols) {
+        *reinterpret_cast<uint4 *>(row + c) = make_uint4(q[0], q[1], q[2], q[3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (c + i < cols) row[c + i] = (uint8_t)(q[i / 4] >> (8 * (i % 4)));
+    }
+}
+__device__ __forceinline__ void load_codes16(const uint8_t *row, int c, int cols, uint32_t (&q)[4])
+{
+    if (c + 16 <= cols) {
+        const uint4 a = __ldg(reinterpret_cast<const uint4 *>(row + c));
+        q[0] = a.x, q[1] = a.y, q[2] = a.z, q[3] = a.w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            if (i % 4 == 0) q[i / 4] = 0;
+            if (c + i < cols) q[i / 4] |= (uint32_t)row[c + i] << (8 * (i % 4));
+        }
+    }
+}
+// The scale byte of a block whose 128 entries lie in eight consecutive lanes, and this lane's sixteen codes.
+__device__ __forceinline__ uint32_t codes16(const f2 (&v)[8], uint32_t (&q)[4])
+{
+    float m = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = most2(v[i], m);
+    uint32_t most = __float_as_uint(m);
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+    const uint32_t s = block_scale(most);
+    if (s != 255u) {
+        const float r = block_inverse(s);
+        const f2 rr = f2_of(r, r);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const f2 a = f2_mul(v[2 * i], rr), b = f2_mul(v[2 * i + 1], rr);
+            q[i] = codes4_scaled(f2_lo(a), f2_hi(a), f2_lo(b), f2_hi(b));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[i] = codes4_bad(f2_lo(v[2 * i]), f2_hi(v[2 * i]), f2_lo(v[2 * i + 1]), f2_hi(v[2 * i + 1]));
+    }
+    return s;
+}
+
 // Row at which node k starts: inside [0, rows] whatever the array holds.  start == nullptr: one node with every row.
 __device__ __forceinline__ int64_t node_first_row(const int64_t *start, int k, int64_t rows)
 {
@@ -149,6 +301,7 @@ struct Matrix {                // rows x cols of `type`, rows `ld` elements apar
     int64_t ld;
 };
 bool matrix_rows_aligned(const void *p, int64_t ld, int elem_bytes);   // every row starts on a 16-byte boundary
+int matrix_alignment(const void *p, int64_t ld, int elem_bytes);       // of every row: 32, 16 or 0 (less) bytes
 
 cudaError_t launch_layer_norm(const Matrix &x, int64_t rows, int64_t cols, const float *gamma, const float *beta, float eps, void *y,
                               int64_t ldy, const lgc_packed *packed, float *mean, float *rstd, cudaStream_t s);

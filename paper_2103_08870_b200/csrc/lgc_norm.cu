@@ -12,6 +12,11 @@ namespace lgc {
 
 namespace {
 
+__device__ __forceinline__ float sum8(const float (&p)[8])
+{
+    return __fadd_rn(__fadd_rn(__fadd_rn(p[0], p[1]), __fadd_rn(p[2], p[3])), __fadd_rn(__fadd_rn(p[4], p[5]), __fadd_rn(p[6], p[7])));
+}
+
 // Sums over the TPR threads that share a row (a warp, or the whole CTA); every thread gets the result.
 template <int TPR, int COUNT>
 __device__ __forceinline__ void row_sums(float (&v)[COUNT], float *shared)
@@ -37,11 +42,11 @@ __device__ __forceinline__ void row_sums(float (&v)[COUNT], float *shared)
     }
 }
 
-// TPR threads per row, NV vectors of eight entries each.  Lanes hold neighbouring vectors, so that 16 lanes hold a block
-// of the 8-bit form.
+// Few rows, wide rows, rows that start anywhere: TPR threads share a row, NV vectors of eight entries each.  Lanes hold
+// neighbouring vectors, so that 16 lanes hold a block of the 8-bit form.
 template <typename T, bool VEC, int TPR, int NV>
 __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR)
-layer_norm_kernel(const T *__restrict__ x, int64_t ldx, int64_t rows, int64_t cols, const float *__restrict__ gamma,
+layer_norm_kernel(const T *__restrict__ x, int64_t ldx, int64_t rows, int cols, const float *__restrict__ gamma,
                   const float *__restrict__ beta, float eps, T *__restrict__ y, int64_t ldy, bool y_vec, uint8_t *__restrict__ codes,
                   int64_t ld_codes, uint8_t *__restrict__ scales, int64_t ld_scales, float *__restrict__ mean_out,
                   float *__restrict__ rstd_out, bool gb_vec)
@@ -53,23 +58,33 @@ layer_norm_kernel(const T *__restrict__ x, int64_t ldx, int64_t rows, int64_t co
     if (row >= rows) return;                                    // a whole warp (TPR = 32): no barrier follows
     const T *xr = x + row * ldx;
     float v[NV][8];
-    float sum[1] = {0.0f};
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        load8<T, VEC>(xr, (int64_t)(i * TPR + t) * 8, cols, v[i]);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sum[0] = __fadd_rn(sum[0], v[i][j]);
-    }
-    row_sums<TPR>(sum, shared[0]);
-    const float mean = __fdiv_rn(sum[0], (float)cols);
-    float sq[1] = {0.0f};
+    for (int i = 0; i < NV; ++i) load8<T, VEC>(xr, (i * TPR + t) * 8, cols, v[i]);
+    float part[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            v[i][j] = __fsub_rn(v[i][j], mean);
-            if ((int64_t)(i * TPR + t) * 8 + j < cols) sq[0] = __fmaf_rn(v[i][j], v[i][j], sq[0]);
+        for (int j = 0; j < 8; ++j) part[j] = __fadd_rn(part[j], v[i][j]);
+    float sum[1] = {sum8(part)};
+    row_sums<TPR>(sum, shared[0]);
+    const float mean = __fdiv_rn(sum[0], (float)cols);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) part[j] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * TPR + t) * 8;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] = __fsub_rn(v[i][j], mean);
+        if (c + 8 <= cols) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) part[j] = __fmaf_rn(v[i][j], v[i][j], part[j]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (c + j < cols) part[j] = __fmaf_rn(v[i][j], v[i][j], part[j]);
         }
+    }
+    float sq[1] = {sum8(part)};
     row_sums<TPR>(sq, shared[1]);
     const float rstd = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(__fdiv_rn(sq[0], (float)cols), eps)));
     if (t == 0) {
@@ -78,8 +93,8 @@ layer_norm_kernel(const T *__restrict__ x, int64_t ldx, int64_t rows, int64_t co
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int64_t c = (int64_t)(i * TPR + t) * 8;
-        if ((int64_t)(i * TPR + (t & ~31)) * 8 >= cols) break;   // the whole warp is past the row's end
+        const int c = (i * TPR + t) * 8;
+        if ((i * TPR + (t & ~31)) * 8 >= cols) break;            // the whole warp is past the row's end
         float g[8], b[8];
         if (gb_vec) {
             load8<float, true>(gamma, c, cols, g);
@@ -89,7 +104,11 @@ layer_norm_kernel(const T *__restrict__ x, int64_t ldx, int64_t rows, int64_t co
             load8<float, false>(beta, c, cols, b);
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[i][j] = c + j < cols ? __fmaf_rn(__fmul_rn(v[i][j], rstd), g[j], b[j]) : 0.0f;
+        for (int j = 0; j < 8; ++j) v[i][j] = __fmaf_rn(__fmul_rn(v[i][j], rstd), g[j], b[j]);
+        if (c + 8 > cols)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (c + j >= cols) v[i][j] = 0.0f;
         if (y) {
             if (y_vec) store8<T, true>(y + row * ldy, c, cols, v[i]);
             else store8<T, false>(y + row * ldy, c, cols, v[i]);
@@ -99,6 +118,135 @@ layer_norm_kernel(const T *__restrict__ x, int64_t ldx, int64_t rows, int64_t co
             store_codes8(codes + row * ld_codes, c, cols, codes4(v[i][0], v[i][1], v[i][2], v[i][3], s),
                          codes4(v[i][4], v[i][5], v[i][6], v[i][7], s));
             if ((t & 15) == 0 && c < cols) scales[row * ld_scales + c / kBlock] = (uint8_t)s;
+        }
+    }
+}
+
+// Takes away the compiler's knowledge of the entries: it would keep them as fp32 numbers from one use to the next, which
+// costs twice the registers and half the warps.
+template <typename T, int UNITS>
+__device__ __forceinline__ void keep_raw(Raw16<T> (&raw)[UNITS])
+{
+    if (sizeof(T) == 2)
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u)
+#pragma unroll
+            for (int i = 0; i < (int)(4 * sizeof(T)); ++i) asm volatile("" : "+r"(raw[u].w[i]));
+}
+
+// Many rows: WPR warps per row, walking from row to row.  The row stays as it was loaded (bf16: half the registers of fp32
+// numbers), UNITS times 16 neighbouring entries per lane; gamma and beta lie in shared memory in the order in which lanes
+// read them, one 16-byte piece per lane without bank conflicts.
+constexpr int kRowThreads = 256;
+
+// A sum over the WPR warps of a row; the groups of a CTA have a named barrier each.
+template <int WPR>
+__device__ __forceinline__ float group_sum(const f2 (&p)[4], float *shared)
+{
+    const f2 t = f2_add(f2_add(p[0], p[1]), f2_add(p[2], p[3]));
+    float v = __fadd_rn(f2_lo(t), f2_hi(t));
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = __fadd_rn(v, __shfl_xor_sync(0xffffffffu, v, o));
+    if (WPR > 1) {
+        const int warp = threadIdx.x >> 5, group = warp / WPR;
+        if ((threadIdx.x & 31) == 0) shared[warp] = v;
+        asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(32 * WPR) : "memory");
+        v = shared[group * WPR];
+#pragma unroll
+        for (int i = 1; i < WPR; ++i) v = __fadd_rn(v, shared[group * WPR + i]);
+    }
+    return v;
+}
+
+template <typename T, int UNITS>
+constexpr int row_ctas()                 // CTAs per SM that the registers of a lane's raw entries and about 40 more allow
+{
+    constexpr int raw = 4 * UNITS * (int)sizeof(T);
+    return raw <= 16 ? 4 : raw <= 32 ? 3 : raw <= 64 ? 2 : 1;
+}
+template <typename T, int AL, int YAL, int UNITS, int WPR>
+__global__ void __launch_bounds__(kRowThreads, row_ctas<T, UNITS>())
+layer_norm_rows_kernel(const T *__restrict__ x, int64_t ldx, int64_t rows, int cols, const float *__restrict__ gamma,
+                       const float *__restrict__ beta, float eps, T *__restrict__ y, int64_t ldy, uint8_t *__restrict__ codes,
+                       int64_t ld_codes, uint8_t *__restrict__ scales, int64_t ld_scales, float *__restrict__ mean_out,
+                       float *__restrict__ rstd_out)
+{
+    extern __shared__ float4 gb[];                               // [gamma, beta][unit][piece][thread of the row]
+    __shared__ float shared[2][kRowThreads / 32];
+    constexpr int TPR = 32 * WPR, kWide = TPR * 16;              // threads of a row, entries of a unit
+    const int t = threadIdx.x % TPR;
+    for (int i = threadIdx.x; i < 2 * UNITS * kWide; i += kRowThreads) {
+        const int c = i % (UNITS * kWide), unit = c / kWide, l = c % kWide / 16, piece = c % 16 / 4;
+        const float *from = i < UNITS * kWide ? gamma : beta;
+        reinterpret_cast<float *>(gb)[((i / (UNITS * kWide) * UNITS + unit) * 4 + piece) * TPR * 4 + l * 4 + c % 4] = c < cols ? __ldg(from + c) : 0.0f;
+    }
+    __syncthreads();
+    const float inverse = __fdiv_rn(1.0f, (float)cols);
+    constexpr int kGroups = kRowThreads / TPR;
+    for (int64_t row = (int64_t)blockIdx.x * kGroups + threadIdx.x / TPR; row < rows; row += (int64_t)gridDim.x * kGroups) {
+        const T *xr = x + row * ldx;
+        Raw16<T> raw[UNITS];
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u)
+            if (u * kWide < cols) load16<AL>(xr, u * kWide + t * 16, cols, raw[u]);
+        f2 part[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u)
+            if (u * kWide < cols)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) part[i & 3] = f2_add(part[i & 3], raw_pair(raw[u], i));
+        const float mean = __fmul_rn(group_sum<WPR>(part, shared[0]), inverse);
+        const f2 minus = f2_of(-mean, -mean);
+        keep_raw(raw);
+        part[0] = part[1] = part[2] = part[3] = 0;
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+            if ((u + 1) * kWide <= cols) {                        // (the same for every thread)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const f2 d = f2_add(raw_pair(raw[u], i), minus);
+                    part[i & 3] = f2_fma(d, d, part[i & 3]);
+                }
+            } else if (u * kWide < cols) {
+                const int c = u * kWide + t * 16;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    f2 d = f2_add(raw_pair(raw[u], i), minus);
+                    d = f2_of(c + 2 * i < cols ? f2_lo(d) : 0.0f, c + 2 * i + 1 < cols ? f2_hi(d) : 0.0f);
+                    part[i & 3] = f2_fma(d, d, part[i & 3]);
+                }
+            }
+        }
+        const float rstd = __frsqrt_rn(__fmaf_rn(group_sum<WPR>(part, shared[1]), inverse, eps));
+        if (t == 0) {
+            mean_out[row] = mean;
+            rstd_out[row] = rstd;
+        }
+        const f2 rr = f2_of(rstd, rstd);
+        keep_raw(raw);
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+            const int c = u * kWide + t * 16;
+            if (u * kWide + (t & ~31) * 16 >= cols) break;        // the whole warp is past the row's end
+            const bool full = (u + 1) * kWide <= cols;
+            f2 v[8];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float4 g = gb[(u * 4 + k) * TPR + t], b = gb[((UNITS + u) * 4 + k) * TPR + t];
+                v[2 * k] = f2_fma(f2_mul(f2_add(raw_pair(raw[u], 2 * k), minus), rr), f2_of(g.x, g.y), f2_of(b.x, b.y));
+                v[2 * k + 1] = f2_fma(f2_mul(f2_add(raw_pair(raw[u], 2 * k + 1), minus), rr), f2_of(g.z, g.w), f2_of(b.z, b.w));
+            }
+            if (!full)                                            // (gamma = beta = 0 there, but rstd may be infinite or NaN)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = f2_of(c + 2 * i < cols ? f2_lo(v[i]) : 0.0f, c + 2 * i + 1 < cols ? f2_hi(v[i]) : 0.0f);
+            const int upto = full ? c + 16 : cols;                // (a whole unit: no checks)
+            if (y) store16<YAL>(y + row * ldy, c, upto, v);
+            if (codes) {
+                uint32_t q[4];
+                const uint32_t s = codes16(v, q);
+                store_codes16(codes + row * ld_codes, c, upto, q);
+                if ((t & 7) == 0 && c < cols) scales[row * ld_scales + c / kBlock] = (uint8_t)s;
+            }
         }
     }
 }
@@ -283,22 +431,71 @@ int64_t max_chunks_for(int64_t rows, int32_t nodes)
     return (rows + r - 1) / r + nodes;
 }
 
+struct ForwardArgs {
+    const Matrix &x;
+    int64_t rows, cols;
+    const float *gamma, *beta;
+    float eps;
+    void *y;
+    int64_t ldy;
+    const lgc_packed *p;
+    float *mean, *rstd;
+    cudaStream_t s;
+};
+
 template <typename T, bool VEC>
-cudaError_t norm_type(const Matrix &x, int64_t rows, int64_t cols, const float *gamma, const float *beta, float eps, T *y, int64_t ldy,
-                      const lgc_packed *p, float *mean, float *rstd, cudaStream_t s)
+void forward_shared_rows(const ForwardArgs &a)
 {
-    const bool y_vec = matrix_rows_aligned(y, ldy, sizeof(T)), gb_vec = matrix_rows_aligned(gamma, 4, 4) && matrix_rows_aligned(beta, 4, 4);
+    const bool y_vec = matrix_rows_aligned(a.y, a.ldy, sizeof(T)), gb_vec = matrix_rows_aligned(a.gamma, 4, 4) && matrix_rows_aligned(a.beta, 4, 4);
     auto launch = [&](auto kern, int64_t ctas, int threads) {
-        kern<<<(unsigned)ctas, threads, 0, s>>>(static_cast<const T *>(x.p), x.ld, rows, cols, gamma, beta, eps, y, ldy, y_vec,
-                                                p ? p->codes : nullptr, p ? p->ld : 0, p ? p->scales : nullptr, p ? p->ld_scales : 0, mean,
-                                                rstd, gb_vec);
+        kern<<<(unsigned)ctas, threads, 0, a.s>>>(static_cast<const T *>(a.x.p), a.x.ld, a.rows, (int)a.cols, a.gamma, a.beta, a.eps,
+                                                  static_cast<T *>(a.y), a.ldy, y_vec, a.p ? a.p->codes : nullptr, a.p ? a.p->ld : 0,
+                                                  a.p ? a.p->scales : nullptr, a.p ? a.p->ld_scales : 0, a.mean, a.rstd, gb_vec);
     };
-    if (cols <= 1024) launch(layer_norm_kernel<T, VEC, 32, 4>, (rows + 3) / 4, 128);
-    else if (cols <= 4096) launch(layer_norm_kernel<T, VEC, 128, 4>, rows, 128);
-    else if (cols <= 8192) launch(layer_norm_kernel<T, VEC, 256, 4>, rows, 256);
-    else launch(layer_norm_kernel<T, VEC, 512, 4>, rows, 512);
+    if (a.cols <= 1024) launch(layer_norm_kernel<T, VEC, 128, 1>, a.rows, 128);
+    else if (a.cols <= 4096) launch(layer_norm_kernel<T, VEC, 128, 4>, a.rows, 128);
+    else if (a.cols <= 8192) launch(layer_norm_kernel<T, VEC, 256, 4>, a.rows, 256);
+    else launch(layer_norm_kernel<T, VEC, 512, 4>, a.rows, 512);
+}
+
+template <typename T, int AL, int YAL, int UNITS, int WPR>
+cudaError_t forward_rows(const ForwardArgs &a)
+{
+    auto kern = layer_norm_rows_kernel<T, AL, YAL, UNITS, WPR>;
+    constexpr int kSmem = 2 * UNITS * WPR * 512 * 4, kGroups = kRowThreads / 32 / WPR;
+    static OncePerDevice configured;
+    if (kSmem > 48 * 1024) {
+        const cudaError_t e = configured.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem); });
+        if (e != cudaSuccess) return e;
+    }
+    const int64_t need = (a.rows + kGroups - 1) / kGroups, most = (int64_t)row_ctas<T, UNITS>() * sm_count();
+    kern<<<(unsigned)(need < most ? need : most), kRowThreads, kSmem, a.s>>>(
+        static_cast<const T *>(a.x.p), a.x.ld, a.rows, (int)a.cols, a.gamma, a.beta, a.eps, static_cast<T *>(a.y), a.ldy, a.p ? a.p->codes : nullptr,
+        a.p ? a.p->ld : 0, a.p ? a.p->scales : nullptr, a.p ? a.p->ld_scales : 0, a.mean, a.rstd);
+    return cudaSuccess;
+}
+
+template <typename T, int AL, int YAL>
+cudaError_t forward_units(const ForwardArgs &a)
+{
+    if (a.cols <= 512) return forward_rows<T, AL, YAL, 1, 1>(a);
+    if (a.cols <= 1024) return forward_rows<T, AL, YAL, 2, 1>(a);
+    if (a.cols <= 2048) return forward_rows<T, AL, YAL, 1, 4>(a);
+    if (a.cols <= 4096) return forward_rows<T, AL, YAL, 2, 4>(a);
+    if (a.cols <= 8192) return forward_rows<T, AL, YAL, 4, 4>(a);
+    return forward_rows<T, AL, YAL, 8, 4>(a);
+}
+
+template <typename T>
+cudaError_t forward_type(const ForwardArgs &a)
+{
+    const int al = matrix_alignment(a.x.p, a.x.ld, sizeof(T)), yal = a.y ? matrix_alignment(a.y, a.ldy, sizeof(T)) : 32;
+    cudaError_t e = cudaSuccess;
+    if (al >= 16 && a.rows >= 4 * sm_count()) e = al == 32 && yal == 32 ? forward_units<T, 32, 32>(a) : forward_units<T, 16, 0>(a);
+    else if (al >= 16) forward_shared_rows<T, true>(a);
+    else forward_shared_rows<T, false>(a);
     ++g_kernel_launches;
-    return cudaGetLastError();
+    return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 struct BackwardArgs {
@@ -351,14 +548,8 @@ void backward_type(const BackwardArgs &a)
 cudaError_t launch_layer_norm(const Matrix &x, int64_t rows, int64_t cols, const float *gamma, const float *beta, float eps, void *y,
                               int64_t ldy, const lgc_packed *packed, float *mean, float *rstd, cudaStream_t s)
 {
-    if (x.type == LGC_TYPE_FP32) {
-        float *yf = static_cast<float *>(y);
-        return matrix_rows_aligned(x.p, x.ld, 4) ? norm_type<float, true>(x, rows, cols, gamma, beta, eps, yf, ldy, packed, mean, rstd, s)
-                                                 : norm_type<float, false>(x, rows, cols, gamma, beta, eps, yf, ldy, packed, mean, rstd, s);
-    }
-    __nv_bfloat16 *yb = static_cast<__nv_bfloat16 *>(y);
-    return matrix_rows_aligned(x.p, x.ld, 2) ? norm_type<__nv_bfloat16, true>(x, rows, cols, gamma, beta, eps, yb, ldy, packed, mean, rstd, s)
-                                             : norm_type<__nv_bfloat16, false>(x, rows, cols, gamma, beta, eps, yb, ldy, packed, mean, rstd, s);
+    const ForwardArgs a{x, rows, cols, gamma, beta, eps, y, ldy, packed, mean, rstd, s};
+    return x.type == LGC_TYPE_FP32 ? forward_type<float>(a) : forward_type<__nv_bfloat16>(a);
 }
 
 size_t layer_norm_backward_scratch(int64_t rows, int64_t cols, int32_t num_nodes)

@@ -2,44 +2,50 @@
 //
 // Both directions only stream: an entry is read once and written once, with an exponent comparison and a conversion in
 // between, so DRAM bounds them.
+#include <type_traits>
+
 #include "lgc_layers.cuh"
 
 namespace lgc {
 
 namespace {
 
-// Blocks of one row: 16 consecutive lanes hold a block of 128 entries, eight each, and find its largest magnitude with
-// four shuffles.  Item = (row, block).
-template <typename T, bool VEC, bool GATE>
+// Blocks of one row: eight consecutive lanes hold a block, sixteen entries each.  Item = (row, block).
+// AL, YAL: alignment of the rows of x and y.
+template <typename T, int AL, bool GATE, int YAL>
 __global__ void __launch_bounds__(256)
-pack_rows_kernel(const T *__restrict__ x, int64_t ldx, int64_t rows, int64_t cols, uint32_t blocks_per_row, float slope,
+pack_rows_kernel(const T *__restrict__ x, int64_t ldx, int64_t rows, int cols, uint32_t blocks_per_row, float slope,
                  const uint8_t *__restrict__ gate, int64_t ld_gate, uint8_t *__restrict__ codes, int64_t ld_codes,
-                 uint8_t *__restrict__ scales, int64_t ld_scales, __nv_bfloat16 *__restrict__ y, int64_t ldy, bool y_vec)
+                 uint8_t *__restrict__ scales, int64_t ld_scales, __nv_bfloat16 *__restrict__ y, int64_t ldy)
 {
     const int64_t items = rows * blocks_per_row;
-    const int64_t item = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 4;
-    const int part = threadIdx.x & 15;
-    const bool live = item < items;                              // whole groups of 16 lanes
+    const int64_t item = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 3;
+    const int part = threadIdx.x & 7;
+    const bool live = item < items;                              // whole groups of eight lanes
     const int64_t row = live ? item / blocks_per_row : 0;
-    const int64_t block = live ? item - row * blocks_per_row : 0;
-    const int64_t c = live ? block * kBlock + part * 8 : cols;   // (a dead group reads and writes nothing)
-    float v[8];
-    load8<T, VEC>(x + row * ldx, c, cols, v);
-    if (GATE) {
-        const uint2 q = load_codes8(gate + row * ld_gate, c, cols);
+    const int block = live ? (int)(item - row * blocks_per_row) : 0;
+    const int c = live ? block * kBlock + part * 16 : cols;      // (a dead group reads and writes nothing)
+    Raw16<T> raw;
+    load16<AL>(x + row * ldx, c, cols, raw);
+    uint32_t g[4];
+    if (GATE) load_codes16(gate + row * ld_gate, c, cols, g);
+    f2 v[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if ((i < 4 ? q.x >> (8 * i) : q.y >> (8 * (i - 4))) & 0x80u) v[i] = __fmul_rn(slope, v[i]);
+    for (int i = 0; i < 8; ++i) v[i] = raw_pair(raw, i);
+    if (GATE) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t w = g[i / 2] >> (16 * (i & 1));
+            v[i] = f2_mul(v[i], f2_of(w & 0x80u ? slope : 1.0f, w & 0x8000u ? slope : 1.0f));
+        }
     } else if (slope != 1.0f) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = leaky_slope(v[i], slope);
+        for (int i = 0; i < 8; ++i) v[i] = f2_mul(v[i], f2_of(f2_lo(v[i]) > 0.0f ? 1.0f : slope, f2_hi(v[i]) > 0.0f ? 1.0f : slope));
     }
-    const uint32_t s = block_scale(most_of_block(v));
-    if (y) {
-        if (y_vec) store8<__nv_bfloat16, true>(y + row * ldy, c, cols, v);
-        else store8<__nv_bfloat16, false>(y + row * ldy, c, cols, v);
-    }
-    store_codes8(codes + row * ld_codes, c, cols, codes4(v[0], v[1], v[2], v[3], s), codes4(v[4], v[5], v[6], v[7], s));
+    uint32_t q[4];
+    const uint32_t s = codes16(v, q);
+    if (y) store16<YAL>(y + row * ldy, c, cols, v);
+    store_codes16(codes + row * ld_codes, c, cols, q);
     if (live && part == 0) scales[row * ld_scales + block] = (uint8_t)s;
 }
 
@@ -83,23 +89,28 @@ pack_square_kernel(const T *__restrict__ x, int64_t ldx, int64_t rows, int64_t c
     }
 }
 
-template <typename T, bool VEC>
+template <typename T, int AL>
 __global__ void __launch_bounds__(256)
 unpack_kernel(const uint8_t *__restrict__ codes, int64_t ld_codes, const uint8_t *__restrict__ scales, int64_t ld_scales, int64_t rows,
-              int64_t cols, uint32_t eighths, int32_t block_rows, T *__restrict__ y, int64_t ldy)
+              int cols, uint32_t parts, int32_t block_rows, T *__restrict__ y, int64_t ldy)
 {
     const int64_t item = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (item >= rows * eighths) return;
-    const int64_t row = item / eighths;
-    const int64_t c = (item - row * eighths) * 8;
-    const uint2 q = load_codes8(codes + row * ld_codes, c, cols);
+    if (item >= rows * parts) return;
+    const int64_t row = item / parts;
+    const int c = (int)(item - row * parts) * 16;
+    uint32_t q[4];
+    load_codes16(codes + row * ld_codes, c, cols, q);
     const float f = block_factor(__ldg(scales + row / block_rows * ld_scales + c / kBlock));
-    float a[4], b[4];
-    codes_to_float4(q.x, a);
-    codes_to_float4(q.y, b);
-    const float v[8] = {__fmul_rn(a[0], f), __fmul_rn(a[1], f), __fmul_rn(a[2], f), __fmul_rn(a[3], f),
-                        __fmul_rn(b[0], f), __fmul_rn(b[1], f), __fmul_rn(b[2], f), __fmul_rn(b[3], f)};
-    store8<T, VEC>(y + row * ldy, c, cols, v);
+    const f2 ff = f2_of(f, f);
+    f2 v[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float a[4];
+        codes_to_float4(q[i], a);
+        v[2 * i] = f2_mul(f2_of(a[0], a[1]), ff);
+        v[2 * i + 1] = f2_mul(f2_of(a[2], a[3]), ff);
+    }
+    store16<AL>(y + row * ldy, c, cols, v);
 }
 
 template <typename T>
@@ -110,12 +121,21 @@ cudaError_t pack_type(const Matrix &x, int64_t rows, int64_t cols, int32_t block
     const bool vec = matrix_rows_aligned(x.p, x.ld, sizeof(T)), y_vec = matrix_rows_aligned(y, ldy, 2);
     const int64_t blocks = (cols + kBlock - 1) / kBlock;
     if (block_rows == 1) {
-        const int64_t ctas = (rows * blocks + 15) / 16;
+        const int64_t ctas = (rows * blocks + 31) / 32;
         if (ctas > 0x7fffffff) return cudaErrorInvalidConfiguration;
-        auto kern = gate ? (vec ? pack_rows_kernel<T, true, true> : pack_rows_kernel<T, false, true>)
-                         : (vec ? pack_rows_kernel<T, true, false> : pack_rows_kernel<T, false, false>);
-        kern<<<(unsigned)ctas, 256, 0, s>>>(p, x.ld, rows, cols, (uint32_t)blocks, slope, gate ? gate->codes : nullptr, gate ? gate->ld : 0,
-                                            out.codes, out.ld, out.scales, out.ld_scales, y, ldy, y_vec);
+        auto launch = [&](auto kern) {
+            kern<<<(unsigned)ctas, 256, 0, s>>>(p, x.ld, rows, (int)cols, (uint32_t)blocks, slope, gate ? gate->codes : nullptr,
+                                                gate ? gate->ld : 0, out.codes, out.ld, out.scales, out.ld_scales, y, ldy);
+        };
+        const int al = matrix_alignment(x.p, x.ld, sizeof(T)), yal = y ? matrix_alignment(y, ldy, 2) : 32;
+        auto by_alignment = [&](auto gated) {
+            constexpr bool G = decltype(gated)::value;
+            if (al == 32 && yal == 32) launch(pack_rows_kernel<T, 32, G, 32>);
+            else if (al >= 16) launch(pack_rows_kernel<T, 16, G, 0>);
+            else launch(pack_rows_kernel<T, 0, G, 0>);
+        };
+        if (gate) by_alignment(std::true_type());
+        else by_alignment(std::false_type());
     } else {
         const int64_t tall = (rows + kBlock - 1) / kBlock;
         if (tall > 65535 || blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
@@ -130,10 +150,11 @@ cudaError_t pack_type(const Matrix &x, int64_t rows, int64_t cols, int32_t block
 template <typename T>
 cudaError_t unpack_type(const lgc_packed &src, int64_t rows, int64_t cols, int32_t block_rows, T *y, int64_t ldy, cudaStream_t s)
 {
-    const int64_t eighths = (cols + 7) / 8, ctas = (rows * eighths + 255) / 256;
+    const int64_t parts = (cols + 15) / 16, ctas = (rows * parts + 255) / 256;
     if (ctas > 0x7fffffff) return cudaErrorInvalidConfiguration;
-    auto kern = matrix_rows_aligned(y, ldy, sizeof(T)) ? unpack_kernel<T, true> : unpack_kernel<T, false>;
-    kern<<<(unsigned)ctas, 256, 0, s>>>(src.codes, src.ld, src.scales, src.ld_scales, rows, cols, (uint32_t)eighths, block_rows, y, ldy);
+    const int al = matrix_alignment(y, ldy, sizeof(T));
+    auto kern = al == 32 ? unpack_kernel<T, 32> : al == 16 ? unpack_kernel<T, 16> : unpack_kernel<T, 0>;
+    kern<<<(unsigned)ctas, 256, 0, s>>>(src.codes, src.ld, src.scales, src.ld_scales, rows, (int)cols, (uint32_t)parts, block_rows, y, ldy);
     ++g_kernel_launches;
     return cudaGetLastError();
 }

@@ -139,7 +139,8 @@ def test_pack_with_the_activation_and_its_derivative(rows, cols, kind):
 
 # ---- layer norm -------------------------------------------------------------------------------------------------------
 
-NORM_SIZES = [(1, 1), (1, 4096), (5, 127), (33, 1000), (9, 1024), (17, 2049), (3, 8192), (2, 16384)]
+NORM_SIZES = [(1, 1), (1, 4096), (5, 127), (33, 1000), (9, 1024), (17, 2049), (3, 8192), (2, 16384), (700, 257), (611, 1000), (600, 2050),
+              (1201, 4096), (607, 401), (600, 5003), (593, 8200)]
 
 
 def norm_inputs(r, rows, cols, kind):
