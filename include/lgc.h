@@ -314,7 +314,7 @@ typedef struct {
     uint8_t *codes;     /* device, rows `ld` bytes apart: 16-byte aligned, ld a multiple of 16 */
     int64_t ld;
     uint8_t *scales;    /* device, [ceil(rows / block_rows)] rows of ceil(cols / 128) bytes, `ld_scales` apart: */
-    int64_t ld_scales;  /* 4-byte aligned, ld_scales a multiple of 4 */
+    int64_t ld_scales;  /* 4-byte aligned, ld_scales a multiple of 4 (they are read four at a time) */
 } lgc_packed;
 
 /* Rounds a matrix to 8 bits, a checkpoint for the backward pass or an operand of lgc_product.
@@ -374,8 +374,8 @@ lgc_status lgc_weight_gradient(const void *dy, int64_t ld_dy, const lgc_packed *
                                int64_t inner, const int64_t *node_start, int32_t num_nodes, float *dw, int64_t node_stride,
                                void *stream);
 
-/* What the kernels of lgc_product and lgc_weight_gradient recorded on the current device (a wait inside a kernel
- * that ran out): waits for `stream`, returns LGC_OK or LGC_ERR_DEVICE_CHECK and clears the record. */
+/* What the kernels of lgc_layer_norm_backward, lgc_product and lgc_weight_gradient recorded on the current device (a
+ * wait inside a kernel that ran out): waits for `stream`, returns LGC_OK or LGC_ERR_DEVICE_CHECK and clears the record. */
 lgc_status lgc_layers_check(void *stream);
 
 /* ---- inspection --------------------------------------------------------------------------- */

@@ -211,9 +211,13 @@ lgc_status lgc_layer_norm_backward(const void *dy, int32_t dy_type, int64_t ld_d
     if (!scratch || (reinterpret_cast<uintptr_t>(scratch) & 15) != 0) return refuse(where, "scratch is NULL or not 16-byte aligned");
     if (scratch_bytes < layer_norm_backward_scratch(num_rows, num_cols, num_nodes))
         return refuse(where, "scratch is smaller than lgc_layer_norm_backward_scratch says", LGC_ERR_WORKSPACE);
-    return done(where, launch_layer_norm_backward(Matrix{dy, dy_type, ld_dy}, Matrix{x, x_type, ldx}, kept ? x_packed : nullptr, num_rows,
-                                                  num_cols, gamma, mean, rstd, node_start, num_nodes, dx, ld_dx, dgamma, dbeta, node_stride,
-                                                  scratch, static_cast<cudaStream_t>(stream)));
+    int32_t *record = nullptr;
+    cudaError_t e = record_address(&record);
+    if (e == cudaSuccess)
+        e = launch_layer_norm_backward(Matrix{dy, dy_type, ld_dy}, Matrix{x, x_type, ldx}, kept ? x_packed : nullptr, num_rows, num_cols, gamma,
+                                       mean, rstd, node_start, num_nodes, dx, ld_dx, dgamma, dbeta, node_stride, scratch, record,
+                                       static_cast<cudaStream_t>(stream));
+    return done(where, e);
 }
 
 lgc_status lgc_product(const lgc_packed *a, const lgc_packed *b, int32_t across, int64_t num_rows, int64_t num_cols, int64_t inner,
@@ -267,7 +271,7 @@ lgc_status lgc_layers_check(void *stream)
     if (e == cudaSuccess && word != 0) e = cudaMemsetAsync(record, 0, sizeof word, s);
     if (e != cudaSuccess) return done(where, e);
     if (word == 0) return LGC_OK;
-    return refuse(where, "a wait inside a product kernel ran out", LGC_ERR_DEVICE_CHECK);
+    return refuse(where, "a wait inside a kernel ran out", LGC_ERR_DEVICE_CHECK);
 }
 
 }  // extern "C"

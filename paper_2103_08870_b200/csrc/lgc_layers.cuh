@@ -309,7 +309,7 @@ size_t layer_norm_backward_scratch(int64_t rows, int64_t cols, int32_t num_nodes
 cudaError_t launch_layer_norm_backward(const Matrix &dy, const Matrix &x, const lgc_packed *x_packed, int64_t rows, int64_t cols,
                                        const float *gamma, const float *mean, const float *rstd, const int64_t *node_start,
                                        int32_t num_nodes, void *dx, int64_t ld_dx, float *dgamma, float *dbeta, int64_t node_stride,
-                                       void *scratch, cudaStream_t s);
+                                       void *scratch, int32_t *errword, cudaStream_t s);
 cudaError_t launch_pack(const Matrix &x, int64_t rows, int64_t cols, int32_t block_rows, float slope, const lgc_packed *gate,
                         const lgc_packed &out, void *y, int64_t ldy, cudaStream_t s);
 cudaError_t launch_unpack(const lgc_packed &src, int64_t rows, int64_t cols, int32_t block_rows, void *y, int32_t type, int64_t ldy,

@@ -7,6 +7,7 @@
 // consecutive rows of one node; a thread keeps its columns' gradients in registers on the way, so dy and x are read once;
 // the chunks' partial sums (fp32) are added up per node, in chunk order, by a second small kernel.
 #include "lgc_layers.cuh"
+#include "lgc_tensor_core.cuh"
 
 namespace lgc {
 
@@ -289,6 +290,36 @@ __device__ __forceinline__ Chunk find_chunk(const int64_t *start, int nodes, int
     return {0, 0, -1};
 }
 
+// Eight neighbouring entries of a row in shared memory, c a multiple of 8; what lies beyond the row's end reads as zero.
+// whole: known to lie inside the row.
+template <typename T>
+__device__ __forceinline__ void slot8(const T *row, int c, int cols, bool whole, f2 (&v)[4])
+{
+    if (!whole && c >= cols) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = 0;
+        return;
+    }
+    if constexpr (sizeof(T) == 1) {
+        const uint2 q = *reinterpret_cast<const uint2 *>(row + c);
+        float a[4], b[4];
+        codes_to_float4(q.x, a);
+        codes_to_float4(q.y, b);
+        v[0] = f2_of(a[0], a[1]), v[1] = f2_of(a[2], a[3]), v[2] = f2_of(b[0], b[1]), v[3] = f2_of(b[2], b[3]);
+    } else if constexpr (sizeof(T) == 2) {
+        const uint4 q = *reinterpret_cast<const uint4 *>(row + c);
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = f2_of(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xffff0000u));
+    } else {
+        const ulonglong2 a = *reinterpret_cast<const ulonglong2 *>(row + c), b = *reinterpret_cast<const ulonglong2 *>(row + c + 4);
+        v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y;
+    }
+    if (!whole && c + 8 > cols)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = f2_of(c + 2 * j < cols ? f2_lo(v[j]) : 0.0f, c + 2 * j + 1 < cols ? f2_hi(v[j]) : 0.0f);
+}
+
 // x may be the 8-bit checkpoint (XT = uint8_t).
 template <typename XT, bool VEC>
 __device__ __forceinline__ void load_x8(const XT *x, int64_t ldx, const uint8_t *scales, int64_t ld_scales, int64_t row, int64_t c,
@@ -370,14 +401,159 @@ layer_norm_backward_kernel(const T *__restrict__ dy, int64_t ld_dy, const XT *__
     }
 }
 
-// The chunks' sums of one node, 32 columns per CTA: 16 slices of the chunks side by side, each in chunk order, then the
+// The same for rows that start on 16-byte boundaries: whole rows of dy and x (and the 8-bit form's scales) come into a ring
+// of shared-memory slots by bulk copies, so that the loads of the rows to come are always under way, whatever the registers
+// hold.  The barrier in the middle of a row's work says that every warp has read its slot, which a warp (another one each
+// row) then gives to a row to come.  A thread owns NV vectors of 8 neighbouring columns.  A row's last bytes that do not
+// fill 16 come in words of four (the last word may reach past the row's end; what it brings from there is not used).
+template <typename T, typename XT, int THREADS, int NV>
+__global__ void __launch_bounds__(THREADS, (NV == 1 ? 1024 : 512) / THREADS)
+layer_norm_backward_ring_kernel(const T *__restrict__ dy, int64_t ld_dy, const XT *__restrict__ x, int64_t ldx,
+                                const uint8_t *__restrict__ x_scales, int64_t ld_scales, int64_t rows, int cols,
+                                const float *__restrict__ gamma, const float *__restrict__ mean, const float *__restrict__ rstd,
+                                const int64_t *__restrict__ node_start, int nodes, int64_t chunk_rows, T *__restrict__ dx, int64_t ld_dx,
+                                float *__restrict__ partial, bool dx_vec, int slots, int slot_bytes, int32_t *__restrict__ errword)
+{
+    extern __shared__ __align__(16) uint8_t ring[];
+    constexpr int kWarps = THREADS / 32, kMaxSlots = 8;
+    __shared__ __align__(8) uint64_t full_bar[kMaxSlots];
+    __shared__ float2 sums_of[2][kWarps];
+    __shared__ volatile int failed;
+    const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+    grid_release_dependents();                                   // the kernel that adds up the chunks waits for this one's end
+    const Chunk ch = find_chunk(node_start, nodes, rows, chunk_rows, blockIdx.x);
+    if (ch.node < 0) return;
+    if (t == 0) {
+        failed = 0;
+        for (int s = 0; s < slots; ++s) bar_init(smem_addr(&full_bar[s]), 1 + 32);
+        bar_init_fence();
+    }
+    __syncthreads();
+    // a slot: dy's row, x's row (each from a 16-byte boundary), then mean, rstd and the scale words
+    const uint32_t dy_bytes = cols * (uint32_t)sizeof(T), x_bytes = cols * (uint32_t)sizeof(XT);
+    const uint32_t x_at = (dy_bytes + 15u) & ~15u, more_at = x_at + ((x_bytes + 15u) & ~15u);
+    const float inverse = __fdiv_rn(1.0f, (float)cols);
+    const int count = (int)(ch.end - ch.begin);
+
+    auto load_row = [&](int k, int s) {                          // by a whole warp
+        const int64_t row = ch.begin + k;
+        const uint32_t slot = smem_addr(ring) + s * slot_bytes, bar = smem_addr(&full_bar[s]);
+        const uint8_t *d = reinterpret_cast<const uint8_t *>(dy + row * ld_dy), *xr = reinterpret_cast<const uint8_t *>(x + row * ldx);
+        const uint32_t d16 = dy_bytes & ~15u, x16 = x_bytes & ~15u, words = lane * 4;
+        if (lane == 0) {
+            bar_expect(bar, d16 + x16);
+            if (d16) bulk_load(slot, d, d16, bar);
+            if (x16) bulk_load(slot + x_at, xr, x16, bar);
+        }
+        if (d16 + words < dy_bytes) word_load(slot + d16 + words, d + d16 + words);
+        if (x16 + words < x_bytes) word_load(slot + x_at + x16 + words, xr + x16 + words);
+        if (lane == 8) word_load(slot + more_at, mean + row);
+        if (lane == 9) word_load(slot + more_at + 4, rstd + row);
+        if (sizeof(XT) == 1 && lane < (cols + 4 * kBlock - 1) / (4 * kBlock))            // (at most 16 words: 8192 columns)
+            word_load(slot + more_at + 8 + words, x_scales + row * ld_scales + words);
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+    };
+    for (int k = warp; k < slots && k < count; k += kWarps) load_row(k, k);
+
+    {
+        f2 g[NV][4], dg[NV][4], db[NV][4];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float w[8];
+            load8<float, false>(gamma, (int64_t)(i * THREADS + t) * 8, cols, w);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                g[i][j] = f2_of(w[2 * j], w[2 * j + 1]);
+                dg[i][j] = db[i][j] = 0;
+            }
+        }
+        int s = 0;
+        uint32_t phase = 0, set = 0;
+        int issuer = 0;                                          // the warp that loads into this row's slot
+        T *to = dx + ch.begin * ld_dx;
+        for (int k = 0; k < count; ++k, to += ld_dx, s = s + 1 == slots ? 0 : s + 1, phase ^= s == 0, set ^= 1) {
+            bar_wait(smem_addr(&full_bar[s]), phase, &failed);   // (a wait that runs out is recorded; the warps stay together)
+            __syncwarp();
+            const uint8_t *slot = ring + s * slot_bytes;
+            const float *more = reinterpret_cast<const float *>(slot + more_at);
+            const float mu = more[0], rs = more[1];
+            f2 d[NV][4], h[NV][4];
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = (i * THREADS + t) * 8;
+                const bool whole = (i + 1) * THREADS * 8 <= cols;    // (the same for every thread)
+                slot8(reinterpret_cast<const T *>(slot), c, cols, whole, d[i]);
+                slot8(reinterpret_cast<const XT *>(slot + x_at), c, cols, whole, h[i]);
+                if (sizeof(XT) == 1) {
+                    const float f = whole || c < cols ? block_factor(reinterpret_cast<const uint8_t *>(more + 2)[c / kBlock]) : 0.0f;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) h[i][j] = f2_fma(h[i][j], f2_of(f, f), f2_of(-mu, -mu));      // (the product is exact)
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) h[i][j] = f2_add(h[i][j], f2_of(-mu, -mu));
+                }
+            }
+            f2 s0 = 0, s1 = 0;
+            const f2 rr = f2_of(rs, rs);
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    // entries beyond the row's end: d = 0, and their xh enters no sum
+                    h[i][j] = f2_mul(h[i][j], rr);
+                    dg[i][j] = f2_fma(d[i][j], h[i][j], dg[i][j]);
+                    db[i][j] = f2_add(db[i][j], d[i][j]);
+                    d[i][j] = f2_mul(d[i][j], g[i][j]);
+                    s0 = f2_add(s0, d[i][j]);
+                    s1 = f2_fma(d[i][j], h[i][j], s1);
+                }
+            float sums[2] = {__fadd_rn(f2_lo(s0), f2_hi(s0)), __fadd_rn(f2_lo(s1), f2_hi(s1))};
+            row_sums<32>(sums, nullptr);
+            if (kWarps > 1) {
+                float2 *part = sums_of[set];                  // two sets: a fast warp may be a row ahead of a slow one
+                if (lane == 0) part[warp] = make_float2(sums[0], sums[1]);
+                asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory");
+                f2 total = reinterpret_cast<const f2 *>(part)[0];
+#pragma unroll
+                for (int i = 1; i < kWarps; ++i) total = f2_add(total, reinterpret_cast<const f2 *>(part)[i]);
+                sums[0] = f2_lo(total), sums[1] = f2_hi(total);
+            }
+            if (warp == issuer && k + slots < count) load_row(k + slots, s);     // (one warp: row_sums' shuffles are its barrier)
+            issuer = issuer + 1 == kWarps ? 0 : issuer + 1;
+            const float m1 = __fmul_rn(sums[0], -inverse), m2 = __fmul_rn(sums[1], -inverse);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = (i * THREADS + t) * 8;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) d[i][j] = f2_mul(rr, f2_fma(h[i][j], f2_of(m2, m2), f2_add(d[i][j], f2_of(m1, m1))));
+                const float w[8] = {f2_lo(d[i][0]), f2_hi(d[i][0]), f2_lo(d[i][1]), f2_hi(d[i][1]),
+                                    f2_lo(d[i][2]), f2_hi(d[i][2]), f2_lo(d[i][3]), f2_hi(d[i][3])};
+                if (dx_vec) store8<T, true>(to, c, (i + 1) * THREADS * 8 <= cols ? c + 8 : cols, w);
+                else store8<T, false>(to, c, cols, w);
+            }
+        }
+        float *out = partial + (int64_t)blockIdx.x * 2 * cols;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * THREADS + t) * 8;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (c + 2 * j < cols) out[c + 2 * j] = f2_lo(dg[i][j]), out[cols + c + 2 * j] = f2_lo(db[i][j]);
+                if (c + 2 * j + 1 < cols) out[c + 2 * j + 1] = f2_hi(dg[i][j]), out[cols + c + 2 * j + 1] = f2_hi(db[i][j]);
+            }
+        }
+        if (t == 0 && failed) atomicExch(errword, 3);
+    }
+}
+
+// The chunks' sums of one node, 32 columns per CTA: 8 slices of the chunks side by side, each in chunk order, then the
 // slices in order.
-__global__ void __launch_bounds__(512)
+__global__ void __launch_bounds__(256)
 layer_norm_gradient_kernel(const float *__restrict__ partial, int64_t rows, int64_t cols, const int64_t *__restrict__ node_start,
                            int64_t chunk_rows, int64_t max_chunks, float *__restrict__ dgamma, float *__restrict__ dbeta,
                            int64_t node_stride)
 {
-    __shared__ float part[2][16][33];
+    __shared__ float part[2][8][33];
     const int node = blockIdx.y, lane = threadIdx.x & 31, slice = threadIdx.x >> 5;
     // this node's chunks: those of the nodes in front come first
     int64_t first = 0;
@@ -395,12 +571,13 @@ layer_norm_gradient_kernel(const float *__restrict__ partial, int64_t rows, int6
     const int64_t lo = node_first_row(node_start, node, rows), hi = node_first_row(node_start, node + 1, rows);
     int64_t count = hi > lo ? (hi - lo + chunk_rows - 1) / chunk_rows : 0;
     if (first + count > max_chunks) count = first < max_chunks ? max_chunks - first : 0;   // (only if node_start does not ascend)
-    const int64_t each = (count + 15) / 16;
+    grid_wait();                                                 // the chunks' sums come from the launch in front
+    const int64_t each = (count + 7) / 8;
     const int64_t c = (int64_t)blockIdx.x * 32 + lane;
     float g = 0.0f, b = 0.0f;
     if (c < cols) {
         const int64_t end = (slice + 1) * each < count ? (slice + 1) * each : count;
-#pragma unroll 4
+#pragma unroll 8
         for (int64_t i = slice * each; i < end; ++i) {
             const float *p = partial + (first + i) * 2 * cols + c;
             g = __fadd_rn(g, __ldg(p));
@@ -413,21 +590,23 @@ layer_norm_gradient_kernel(const float *__restrict__ partial, int64_t rows, int6
     if (slice < 2 && c < cols) {
         float t = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) t = __fadd_rn(t, part[slice][i][lane]);
+        for (int i = 0; i < 8; ++i) t = __fadd_rn(t, part[slice][i][lane]);
         (slice == 0 ? dgamma : dbeta)[(int64_t)node * node_stride + c] = t;
     }
 }
 
-// Rows per chunk: about four chunks per SM, at least eight rows, so that a chunk's 2 * cols partial sums stay small
-// beside its rows.
-int64_t chunk_rows_for(int64_t rows)
+// Rows per chunk, at least four: as many chunks as there is room for CTAs at a time (two per SM for rows of 4096 and more,
+// up to sixteen for narrow ones), the nodes' rounding included, since a chunk too many costs a second round of CTAs.  The
+// chunks' 2 * cols partial sums stay small beside their rows.
+int64_t chunk_rows_for(int64_t rows, int64_t cols, int32_t nodes)
 {
-    const int64_t r = (rows + 4 * 148 - 1) / (4 * 148);
-    return r < 8 ? 8 : r;
+    const int64_t per_sm = cols > 4096 ? 1 : cols > 2048 ? 2 : cols > 1024 ? 4 : cols > 512 ? 8 : 16;
+    const int64_t room = per_sm * 148 - nodes, r = (rows + (room < 148 ? 148 : room) - 1) / (room < 148 ? 148 : room);
+    return r < 4 ? 4 : r;
 }
-int64_t max_chunks_for(int64_t rows, int32_t nodes)
+int64_t max_chunks_for(int64_t rows, int64_t cols, int32_t nodes)
 {
-    const int64_t r = chunk_rows_for(rows);
+    const int64_t r = chunk_rows_for(rows, cols, nodes);
     return (rows + r - 1) / r + nodes;
 }
 
@@ -508,39 +687,67 @@ struct BackwardArgs {
     void *dx;
     int64_t ld_dx;
     float *partial;
+    int32_t *errword;
     cudaStream_t s;
 };
 
-template <typename T, typename XT, bool VEC>
-void backward_kernel(const BackwardArgs &a)
+// Rows that start anywhere, or wider than the ring kernel's threads can own.
+template <typename T, typename XT>
+void backward_any(const BackwardArgs &a)
 {
-    const int64_t chunk = chunk_rows_for(a.rows), ctas = max_chunks_for(a.rows, a.nodes);
+    const int64_t chunk = chunk_rows_for(a.rows, a.cols, a.nodes), ctas = max_chunks_for(a.rows, a.cols, a.nodes);
     auto launch = [&](auto kern, int threads) {
         kern<<<(unsigned)ctas, threads, 0, a.s>>>(static_cast<const T *>(a.dy.p), a.dy.ld,
                                                   static_cast<const XT *>(a.xp ? a.xp->codes : a.x.p), a.xp ? a.xp->ld : a.x.ld,
                                                   a.xp ? a.xp->scales : nullptr, a.xp ? a.xp->ld_scales : 0, a.rows, a.cols, a.gamma, a.mean,
                                                   a.rstd, a.node_start, a.nodes, chunk, static_cast<T *>(a.dx), a.ld_dx, a.partial);
     };
-    if (a.cols <= 512) launch(layer_norm_backward_kernel<T, XT, VEC, 32, 2>, 32);
-    else if (a.cols <= 2048) launch(layer_norm_backward_kernel<T, XT, VEC, 128, 2>, 128);
-    else if (a.cols <= 4096) launch(layer_norm_backward_kernel<T, XT, VEC, 256, 2>, 256);
-    else if (a.cols <= 8192) launch(layer_norm_backward_kernel<T, XT, VEC, 512, 2>, 512);
-    else launch(layer_norm_backward_kernel<T, XT, VEC, 1024, 2>, 1024);
+    if (a.cols <= 2048) launch(layer_norm_backward_kernel<T, XT, false, 128, 2>, 128);
+    else if (a.cols <= 8192) launch(layer_norm_backward_kernel<T, XT, false, 512, 2>, 512);
+    else launch(layer_norm_backward_kernel<T, XT, false, 1024, 2>, 1024);
+}
+
+template <typename T, typename XT, int THREADS, int NV>
+cudaError_t backward_ring(const BackwardArgs &a)
+{
+    auto kern = layer_norm_backward_ring_kernel<T, XT, THREADS, NV>;
+    const int64_t cols = a.cols;
+    const int slot = (int)((cols * sizeof(T) + 15) / 16 * 16 + (cols * sizeof(XT) + 15) / 16 * 16 +
+                           (8 + (sizeof(XT) == 1 ? (cols + 511) / 512 * 4 : 0) + 15) / 16 * 16);
+    constexpr int kMost = 200 * 1024;
+    // three CTAs per SM if three slots each leave room for that, else as many slots as one CTA can have
+    int slots = 70 * 1024 / slot;
+    if (slots < 3) slots = 105 * 1024 / slot;
+    if (slots < 3) slots = kMost / slot;
+    slots = slots > 8 ? 8 : slots < 2 ? 2 : slots;
+    static OncePerDevice configured;
+    const cudaError_t e = configured.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost); });
+    if (e != cudaSuccess) return e;
+    kern<<<(unsigned)max_chunks_for(a.rows, cols, a.nodes), THREADS, (size_t)slots * slot, a.s>>>(
+        static_cast<const T *>(a.dy.p), a.dy.ld, static_cast<const XT *>(a.xp ? a.xp->codes : a.x.p), a.xp ? a.xp->ld : a.x.ld,
+        a.xp ? a.xp->scales : nullptr, a.xp ? a.xp->ld_scales : 0, a.rows, (int)cols, a.gamma, a.mean, a.rstd, a.node_start, a.nodes,
+        chunk_rows_for(a.rows, cols, a.nodes), static_cast<T *>(a.dx), a.ld_dx, a.partial, matrix_rows_aligned(a.dx, a.ld_dx, sizeof(T)), slots, slot, a.errword);
+    return cudaSuccess;
 }
 template <typename T, typename XT>
-void backward_aligned(const BackwardArgs &a)
+cudaError_t backward_aligned(const BackwardArgs &a)
 {
-    const bool vec = matrix_rows_aligned(a.dy.p, a.dy.ld, sizeof(T)) && matrix_rows_aligned(a.dx, a.ld_dx, sizeof(T)) &&
-                     (sizeof(XT) == 1 || matrix_rows_aligned(a.x.p, a.x.ld, sizeof(XT)));
-    if (vec) backward_kernel<T, XT, true>(a);
-    else backward_kernel<T, XT, false>(a);
+    const bool vec = matrix_rows_aligned(a.dy.p, a.dy.ld, sizeof(T)) && (sizeof(XT) == 1 || matrix_rows_aligned(a.x.p, a.x.ld, sizeof(XT)));
+    if (!vec || a.cols > 8192) {
+        backward_any<T, XT>(a);
+        return cudaSuccess;
+    }
+    if (a.cols <= 512) return backward_ring<T, XT, 64, 1>(a);
+    if (a.cols <= 1024) return backward_ring<T, XT, 128, 1>(a);
+    if (a.cols <= 2048) return backward_ring<T, XT, 256, 1>(a);
+    if (a.cols <= 4096) return backward_ring<T, XT, 256, 2>(a);
+    return backward_ring<T, XT, 512, 2>(a);
 }
 template <typename T>
-void backward_type(const BackwardArgs &a)
+cudaError_t backward_type(const BackwardArgs &a)
 {
-    if (a.xp) backward_aligned<T, uint8_t>(a);
-    else if (a.x.type == LGC_TYPE_FP32) backward_aligned<T, float>(a);
-    else backward_aligned<T, __nv_bfloat16>(a);
+    if (a.xp) return backward_aligned<T, uint8_t>(a);
+    return a.x.type == LGC_TYPE_FP32 ? backward_aligned<T, float>(a) : backward_aligned<T, __nv_bfloat16>(a);
 }
 
 }  // namespace
@@ -554,24 +761,26 @@ cudaError_t launch_layer_norm(const Matrix &x, int64_t rows, int64_t cols, const
 
 size_t layer_norm_backward_scratch(int64_t rows, int64_t cols, int32_t num_nodes)
 {
-    return (size_t)max_chunks_for(rows, num_nodes) * 2 * (size_t)cols * sizeof(float);
+    return (size_t)max_chunks_for(rows, cols, num_nodes) * 2 * (size_t)cols * sizeof(float);
 }
 
 cudaError_t launch_layer_norm_backward(const Matrix &dy, const Matrix &x, const lgc_packed *x_packed, int64_t rows, int64_t cols,
                                        const float *gamma, const float *mean, const float *rstd, const int64_t *node_start,
                                        int32_t num_nodes, void *dx, int64_t ld_dx, float *dgamma, float *dbeta, int64_t node_stride,
-                                       void *scratch, cudaStream_t s)
+                                       void *scratch, int32_t *errword, cudaStream_t s)
 {
-    const BackwardArgs a{dy, x, x_packed, rows, cols, gamma, mean, rstd, node_start, num_nodes, dx, ld_dx, static_cast<float *>(scratch), s};
+    const BackwardArgs a{dy, x, x_packed, rows, cols, gamma, mean, rstd, node_start, num_nodes, dx, ld_dx, static_cast<float *>(scratch),
+                         errword, s};
     if (rows > 0) {
-        if (dy.type == LGC_TYPE_FP32) backward_type<float>(a);
-        else backward_type<__nv_bfloat16>(a);
+        cudaError_t e = dy.type == LGC_TYPE_FP32 ? backward_type<float>(a) : backward_type<__nv_bfloat16>(a);
         ++g_kernel_launches;
-        const cudaError_t e = cudaGetLastError();
+        if (e == cudaSuccess) e = cudaGetLastError();
         if (e != cudaSuccess) return e;
     }
-    layer_norm_gradient_kernel<<<dim3((unsigned)((cols + 31) / 32), (unsigned)num_nodes), 512, 0, s>>>(
-        a.partial, rows, cols, node_start, chunk_rows_for(rows), max_chunks_for(rows, num_nodes), dgamma, dbeta, node_stride);
+    const cudaError_t e = launch_dependent(layer_norm_gradient_kernel, dim3((unsigned)((cols + 31) / 32), (unsigned)num_nodes), dim3(256), s, a.partial,
+                                           rows, cols, node_start, chunk_rows_for(rows, cols, num_nodes), max_chunks_for(rows, cols, num_nodes),
+                                           dgamma, dbeta, node_stride);
+    if (e != cudaSuccess) return e;
     ++g_kernel_launches;
     return cudaGetLastError();
 }

@@ -178,9 +178,7 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_
                 for (int j = 0; j < kRows / 32; ++j) {
                     const int64_t row = w.begin + (int64_t)i * kRows + 32 * j + lane;
                     if (row < w.end && block * kBlock < p.inner)
-                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(scale_words + (s * kRows + 32 * j + lane) * 4),
-                                     "l"(p.scales + row * p.ld_scales + (block & ~(int64_t)3))
-                                     : "memory");
+                        word_load(scale_words + (s * kRows + 32 * j + lane) * 4, p.scales + row * p.ld_scales + (block & ~(int64_t)3));
                 }
                 asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_addr(&full_bar[s])) : "memory");
             }

@@ -228,6 +228,6 @@ def weight_gradient(dy: torch.Tensor, x: Packed, dw: torch.Tensor, node_start: O
 
 
 def check(stream: Optional[torch.cuda.Stream] = None) -> None:
-    """Waits for the stream and raises if a kernel of product or weight_gradient recorded a failure."""
+    """Waits for the stream and raises if a kernel recorded a failure (a wait that ran out)."""
     s = stream if stream is not None else torch.cuda.current_stream()
     _done(lgc.lib().lgc_layers_check(s.cuda_stream), "lgc_layers_check")
