@@ -197,43 +197,45 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 else tma_load(st + kM * kBlock, &map_b, bar, kb * kBlock, n * kN);
             }
         }
-    } else if (threadIdx.x == 32) {
+    } else if (warp == 1) {
         // e4m3 x e4m3, scales in e8m0; B K-major or (across) N-major
         constexpr uint32_t idesc = (ACROSS ? 1u << 16 : 0u) | (uint32_t)(kN >> 3) << 17 | 1u << 23 | (uint32_t)(kM >> 4) << 24;
-        int it = 0, quads = 0, acc = 0;
-        for (int64_t tile = blockIdx.x; tile < total && !failed; tile += gridDim.x, ++acc) {
+        const bool issuer = elect_one();
+        int s = 0, quads = 0, acc = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        for (int64_t tile = blockIdx.x; tile < total && ok; tile += gridDim.x, ++acc) {
             const int buf = acc & 1;
-            if (acc >= 2 && !bar_wait(smem_addr(&tempty_bar[buf]), ((acc >> 1) & 1) ^ 1, &failed)) break;
+            if (acc >= 2 && !bar_wait_together(smem_addr(&tempty_bar[buf]), ((acc >> 1) & 1) ^ 1, &failed)) break;
             tc_fence_after();
-            bool ok = true;
-            for (int kb = 0; kb < blocks; ++kb, ++it) {
-                const int s = it % kStages;
+            for (int kb = 0; kb < blocks; ++kb) {
                 const int q = quads & 1;
                 const uint32_t sa = tmem + kScaleCol + q * kScaleCols, sb = sa + kM / 32;
-                if ((kb & 3) == 0) {
-                    // full means that the set's last user has finished: its shared memory and its columns are free
-                    if (!bar_wait(smem_addr(&sfull_bar[q]), (quads >> 1) & 1, &failed)) { ok = false; break; }
-                    tc_fence_after();
-                    copy_scales(sa, scales + q * kScaleBytes);
-                    copy_scales(sb, scales + q * kScaleBytes + kM * 4);
-                }
-                if (!bar_wait(smem_addr(&full_bar[s]), (it / kStages) & 1, &failed)) { ok = false; break; }
+                // full means that the set's last user has finished: its shared memory and its columns are free
+                if ((kb & 3) == 0 && !bar_wait_together(smem_addr(&sfull_bar[q]), (quads >> 1) & 1, &failed)) { ok = false; break; }
+                if (!bar_wait_together(smem_addr(&full_bar[s]), phase, &failed)) { ok = false; break; }
                 tc_fence_after();
                 const uint32_t st = tiles + s * kStageBytes;
                 const uint32_t id = idesc | (uint32_t)(kb & 3) << 4 | (uint32_t)(kb & 3) << 29;    // which byte of the scale words
                 const uint64_t a = tc_desc_k(st), b = ACROSS ? tc_desc(st + kM * kBlock, kN * kBlock) : tc_desc_k(st + kM * kBlock);
+                const bool last = (kb & 3) == 3 || kb == blocks - 1;
+                if (issuer) {
+                    if ((kb & 3) == 0) {
+                        copy_scales(sa, scales + q * kScaleBytes);
+                        copy_scales(sb, scales + q * kScaleBytes + kM * 4);
+                    }
 #pragma unroll
-                for (int ks = 0; ks < 4; ++ks)                     // 32 along the contraction: 32 bytes, or 32 rows of 128 bytes
-                    mma_block_scaled(tmem + buf * kN, a + (uint64_t)(ks * 32 >> 4), b + (uint64_t)((ACROSS ? ks * 4096 : ks * 32) >> 4), id,
-                                     sa, sb, kb > 0 || ks > 0);
-                tc_commit(smem_addr(&empty_bar[s]));
-                if ((kb & 3) == 3 || kb == blocks - 1) {
-                    tc_commit(smem_addr(&sempty_bar[q]));
-                    ++quads;
+                    for (int ks = 0; ks < 4; ++ks)                 // 32 along the contraction: 32 bytes, or 32 rows of 128 bytes
+                        mma_block_scaled(tmem + buf * kN, a + (uint64_t)(ks * 32 >> 4), b + (uint64_t)((ACROSS ? ks * 4096 : ks * 32) >> 4), id,
+                                         sa, sb, kb > 0 || ks > 0);
+                    tc_commit(smem_addr(&empty_bar[s]));
+                    if (last) tc_commit(smem_addr(&sempty_bar[q]));
+                    if (kb == blocks - 1) tc_commit(smem_addr(&tfull_bar[buf]));
                 }
+                __syncwarp();
+                if (++s == kStages) s = 0, phase ^= 1;
+                quads += last;
             }
-            if (!ok) break;
-            tc_commit(smem_addr(&tfull_bar[buf]));
         }
     } else if (warp == 2) {
         // scale words of four blocks along the contraction: lane l serves rows l, l + 32, l + 64, l + 96 of the tile
@@ -404,44 +406,46 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                 if (++s == kStages) s = 0, phase ^= 1;
             }
         }
-    } else if (threadIdx.x == 32 && rank == 0) {
+    } else if (warp == 1) {
         constexpr uint32_t idesc = (ACROSS ? 1u << 16 : 0u) | (uint32_t)(kTile >> 3) << 17 | 1u << 23 | (uint32_t)(kTile >> 4) << 24;
+        const bool issuer = elect_one();
         int s = 0, quads = 0, acc = 0;
         uint32_t phase = 0;
-        for (int64_t tile = first; tile < total && !failed; tile += step, ++acc) {
+        bool ok = rank == 0;
+        for (int64_t tile = first; tile < total && ok; tile += step, ++acc) {
             const uint32_t d = tmem + ((acc & 1) ? kSecond : 0);
-            if (acc >= 1 && !bar_wait(smem_addr(&drained_bar), (acc - 1) & 1, &failed)) break;
+            if (acc >= 1 && !bar_wait_together(smem_addr(&drained_bar), (acc - 1) & 1, &failed)) break;
             tc_fence_after();
-            bool ok = true;
             for (int kb = 0; kb < blocks; ++kb) {
                 const int q = quads & 1;
                 const uint32_t sa = tmem + kScaleCol + q * kScaleCols, sb = sa + kHalf / 32;
-                if ((kb & 3) == 0) {
-                    // full means that the set's last user has finished: its shared memory and its columns are free
-                    if (!bar_wait(smem_addr(&sfull_bar[q]), (quads >> 1) & 1, &failed)) { ok = false; break; }
-                    tc_fence_after();
-                    const uint32_t at = scales + q * kScaleBytes;
-                    copy_scales(sa, at);
-                    copy_scales(sb, at + kHalf * 4);
-                    copy_scales(sb + 4, at + kHalf * 8);
-                }
-                if (!bar_wait(smem_addr(&full_bar[s]), phase, &failed)) { ok = false; break; }
+                // full means that the set's last user has finished: its shared memory and its columns are free
+                if ((kb & 3) == 0 && !bar_wait_together(smem_addr(&sfull_bar[q]), (quads >> 1) & 1, &failed)) { ok = false; break; }
+                if (!bar_wait_together(smem_addr(&full_bar[s]), phase, &failed)) { ok = false; break; }
                 tc_fence_after();
                 const uint32_t st = tiles + s * kStageBytes;
                 const uint32_t id = idesc | (uint32_t)(kb & 3) << 4 | (uint32_t)(kb & 3) << 29;    // which byte of the scale words
                 const uint64_t a = tc_desc_k(st), b = ACROSS ? tc_desc(st + kHalf * kBlock, kHalf * kBlock) : tc_desc_k(st + kHalf * kBlock);
+                const bool last = (kb & 3) == 3 || kb == blocks - 1;
+                if (issuer) {
+                    if ((kb & 3) == 0) {
+                        const uint32_t at = scales + q * kScaleBytes;
+                        copy_scales(sa, at);
+                        copy_scales(sb, at + kHalf * 4);
+                        copy_scales(sb + 4, at + kHalf * 8);
+                    }
 #pragma unroll
-                for (int ks = 0; ks < 4; ++ks)                     // 32 along the contraction: 32 bytes, or 32 rows of 128 bytes
-                    mma_block_scaled(d, a + (uint64_t)(ks * 32 >> 4), b + (uint64_t)((ACROSS ? ks * 4096 : ks * 32) >> 4), id, sa, sb, kb > 0 || ks > 0);
-                tc_commit_pair(smem_addr(&empty_bar[s]));
-                if (++s == kStages) s = 0, phase ^= 1;
-                if ((kb & 3) == 3 || kb == blocks - 1) {
-                    tc_commit_pair(smem_addr(&sempty_bar[q]));
-                    ++quads;
+                    for (int ks = 0; ks < 4; ++ks)                 // 32 along the contraction: 32 bytes, or 32 rows of 128 bytes
+                        mma_block_scaled(d, a + (uint64_t)(ks * 32 >> 4), b + (uint64_t)((ACROSS ? ks * 4096 : ks * 32) >> 4), id, sa, sb,
+                                         kb > 0 || ks > 0);
+                    tc_commit_pair(smem_addr(&empty_bar[s]));
+                    if (last) tc_commit_pair(smem_addr(&sempty_bar[q]));
+                    if (kb == blocks - 1) tc_commit_pair(smem_addr(&tfull_bar[acc & 1]));
                 }
+                __syncwarp();
+                if (++s == kStages) s = 0, phase ^= 1;
+                quads += last;
             }
-            if (!ok) break;
-            tc_commit_pair(smem_addr(&tfull_bar[acc & 1]));
         }
     } else if (warp == 2) {
         // scale words of four blocks along the contraction: lane l serves rows l, l + 32, l + 64, l + 96 of a group of 128

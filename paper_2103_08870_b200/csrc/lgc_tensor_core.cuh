@@ -52,6 +52,43 @@ __device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity, vol
     if ((threadIdx.x & 31) == 0) have = bar_wait(bar, parity, failed) ? 1 : 0;
     return __shfl_sync(0xffffffffu, have, 0) != 0;
 }
+// The same for a whole warp that stays together: every lane polls, and the result is the same for all.  The warps that
+// issue tensor-core work run this way: their descriptors and addresses then are uniform values, which the instructions
+// want; from a branch that one thread takes alone each of them costs a move (0.2 us per stage of four MMAs).
+__device__ __forceinline__ bool bar_wait_together(uint32_t bar, uint32_t parity, volatile int *failed)
+{
+    long long begin = 0;
+    for (;;) {
+        uint32_t done;
+        asm volatile(
+            "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\t"
+            "mov.u32 n, 0;\n\t"
+            "POLL:\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+            "@p bra DONE;\n\t"
+            "add.u32 n, n, 1;\n\t"
+            "setp.lt.u32 q, n, 256;\n\t"
+            "@q bra POLL;\n\t"
+            "DONE:\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(done)
+            : "r"(bar), "r"(parity)
+            : "memory");
+        if (__all_sync(0xffffffffu, done)) return true;
+        const long long now = clock64();
+        if (begin == 0) begin = now;
+        if (__any_sync(0xffffffffu, *failed || now - begin > kWaitCycles)) break;
+    }
+    *failed = 1;
+    return false;
+}
+// One lane of a warp that is together, always the same.
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t e;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
+    return e != 0;
+}
 
 // ---- pairs of CTAs (clusters of two) ---------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t cluster_rank()

@@ -138,31 +138,35 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_
                 }
             }
         }
-    } else if (threadIdx.x == 32 && rank == 0) {
+    } else if (warp == 1) {
         // fp32 sums, bf16 x bf16, both operands MN-major
         constexpr uint32_t idesc = 1u << 4 | 1u << 7 | 1u << 10 | 1u << 15 | 1u << 16 | (uint32_t)(kN >> 3) << 17 | (uint32_t)(kM >> 4) << 24;
-        int it = 0, acc = 0;
-        for (int64_t t = first; t < total && !failed; t += step) {
-            const Tile w = tile_of(p, t);
-            bool ok = true;
-            for (int i = 0; i < w.steps; ++i, ++it) {
-                const int s = it % kStages, buf = acc & 1;
-                const bool begin = i % kFlushSteps == 0;
-                if (begin && acc >= 2 && !bar_wait(smem_addr(&tempty_bar[buf]), ((acc >> 1) & 1) ^ 1, &failed)) { ok = false; break; }
+        const bool issuer = elect_one();
+        int s = 0, acc = 0;
+        uint32_t phase = 0;
+        bool ok = rank == 0;
+        for (int64_t t = first; t < total && ok; t += step) {
+            const int steps = __shfl_sync(0xffffffffu, tile_of(p, t).steps, 0);
+            for (int i = 0; i < steps; ++i) {
+                const int buf = acc & 1;
+                const bool begin = i % kFlushSteps == 0, end = i % kFlushSteps == kFlushSteps - 1 || i == steps - 1;
+                if (begin && acc >= 2 && !bar_wait_together(smem_addr(&tempty_bar[buf]), ((acc >> 1) & 1) ^ 1, &failed)) { ok = false; break; }
                 // the warps that make B wait for the loads of their CTA, dY among them
-                if (!bar_wait(smem_addr(&ready_bar[s]), (it / kStages) & 1, &failed)) { ok = false; break; }
+                if (!bar_wait_together(smem_addr(&ready_bar[s]), phase, &failed)) { ok = false; break; }
                 tc_fence_after();
                 const uint32_t st = base + s * kStageBytes;
+                const uint64_t a = tc_desc(st, kPiece), b = tc_desc(st + kABytes, kPiece);
+                if (issuer) {
 #pragma unroll
-                for (int ks = 0; ks < kRows / 16; ++ks)           // 16 rows of 128 bytes per step
-                    mma_bf16(tmem + buf * kN, tc_desc(st + ks * 2048, kPiece), tc_desc(st + kABytes + ks * 2048, kPiece), idesc, !begin || ks > 0);
-                tc_commit_pair(smem_addr(&empty_bar[s]));
-                if (i % kFlushSteps == kFlushSteps - 1 || i == w.steps - 1) {
-                    tc_commit_pair(smem_addr(&tfull_bar[buf]));
-                    ++acc;
+                    for (int ks = 0; ks < kRows / 16; ++ks)       // 16 rows of 128 bytes per step
+                        mma_bf16(tmem + buf * kN, a + (uint64_t)(ks * 2048 >> 4), b + (uint64_t)(ks * 2048 >> 4), idesc, !begin || ks > 0);
+                    tc_commit_pair(smem_addr(&empty_bar[s]));
+                    if (end) tc_commit_pair(smem_addr(&tfull_bar[buf]));
                 }
+                __syncwarp();
+                if (++s == kStages) s = 0, phase ^= 1;
+                acc += end;
             }
-            if (!ok) break;
         }
     } else if (warp == 2) {
         // scale words of the stage's rows (four blocks each; this CTA's columns are one of them)
