@@ -260,7 +260,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 } else {
                     wb = __ldg(reinterpret_cast<const uint32_t *>(p.b_scales + (int64_t)n * p.ld_bs + kb));
                 }
-                if (quads >= 2 && !bar_wait_warp(smem_addr(&sempty_bar[q]), ((quads >> 1) & 1) ^ 1, &failed)) { ok = false; break; }
+                if (quads >= 2 && !bar_wait_together(smem_addr(&sempty_bar[q]), ((quads >> 1) & 1) ^ 1, &failed)) { ok = false; break; }
                 const uint32_t at = scales + q * kScaleBytes + lane * 16;
                 asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(wa[0]), "r"(wa[1]), "r"(wa[2]), "r"(wa[3]) : "memory");
                 asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + kM * 4), "r"(wb) : "memory");
@@ -275,7 +275,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             int m, n;
             tile_of(tile, p.tiles_m, p.tiles_n, m, n);
             const int buf = acc & 1;
-            if (!bar_wait_warp(smem_addr(&tfull_bar[buf]), (acc >> 1) & 1, &failed)) break;
+            if (!bar_wait_together(smem_addr(&tfull_bar[buf]), (acc >> 1) & 1, &failed)) break;
             tc_fence_after();
             const uint32_t at = tmem + buf * kN + ((uint32_t)(q * 32) << 16);
             float v[kN];
@@ -476,7 +476,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                         wb[g] = __ldg(reinterpret_cast<const uint32_t *>(p.b_scales + group * p.ld_bs + kb));
                     }
                 }
-                if (quads >= 2 && !bar_wait_warp(smem_addr(&sempty_bar[q]), ((quads >> 1) & 1) ^ 1, &failed)) { ok = false; break; }
+                if (quads >= 2 && !bar_wait_together(smem_addr(&sempty_bar[q]), ((quads >> 1) & 1) ^ 1, &failed)) { ok = false; break; }
                 const uint32_t at = scales + q * kScaleBytes + lane * 16;
                 asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(wa[0]), "r"(wa[1]), "r"(wa[2]), "r"(wa[3]) : "memory");
                 asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + kHalf * 4), "r"(wb[0]) : "memory");
@@ -495,7 +495,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
             int m, n;
             tile_at(tile, p, m, n);
             const int buf = acc & 1;
-            if (!bar_wait_warp(smem_addr(&tfull_bar[buf]), (acc >> 1) & 1, &failed)) break;
+            if (!bar_wait_together(smem_addr(&tfull_bar[buf]), (acc >> 1) & 1, &failed)) break;
             tc_fence_after();
             const uint32_t at = tmem + (buf ? kSecond : 0) + ((uint32_t)(q * 32) << 16);
 #pragma unroll 1

@@ -45,13 +45,6 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
     *failed = 1;
     return false;
 }
-// The same for a whole warp: one lane polls.
-__device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity, volatile int *failed)
-{
-    int have = 0;
-    if ((threadIdx.x & 31) == 0) have = bar_wait(bar, parity, failed) ? 1 : 0;
-    return __shfl_sync(0xffffffffu, have, 0) != 0;
-}
 // The same for a whole warp that stays together: every lane polls, and the result is the same for all.  The warps that
 // issue tensor-core work run this way: their descriptors and addresses then are uniform values, which the instructions
 // want; from a branch that one thread takes alone each of them costs a move (0.2 us per stage of four MMAs).

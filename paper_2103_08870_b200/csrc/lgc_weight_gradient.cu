@@ -177,7 +177,7 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_
             const int64_t block = (int64_t)w.n * 2 + rank;
             for (int i = 0; i < w.steps; ++i, ++it) {
                 const int s = it % kStages;
-                if (it >= kStages && !bar_wait_warp(smem_addr(&empty_bar[s]), ((it / kStages) & 1) ^ 1, &failed)) { ok = false; break; }
+                if (it >= kStages && !bar_wait_together(smem_addr(&empty_bar[s]), ((it / kStages) & 1) ^ 1, &failed)) { ok = false; break; }
 #pragma unroll
                 for (int j = 0; j < kRows / 32; ++j) {
                     const int64_t row = w.begin + (int64_t)i * kRows + 32 * j + lane;
@@ -205,7 +205,7 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_
                 const int s = it % kStages;
                 const uint32_t st = base + s * kStageBytes;
                 const bool live = r < w.end - (w.begin + (int64_t)i * kRows);        // the row is this node's
-                if (!bar_wait_warp(smem_addr(&full_bar[s]), (it / kStages) & 1, &failed)) { ok = false; break; }
+                if (!bar_wait_together(smem_addr(&full_bar[s]), (it / kStages) & 1, &failed)) { ok = false; break; }
                 uint32_t q[2][4], word;
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
@@ -263,7 +263,7 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_
             for (int i = 0; i == 0 || i < w.steps; i += kFlushSteps) {
                 const int buf = acc & 1;
                 if (w.steps > 0) {
-                    if (!bar_wait_warp(smem_addr(&tfull_bar[buf]), (acc >> 1) & 1, &failed)) { ok = false; break; }
+                    if (!bar_wait_together(smem_addr(&tfull_bar[buf]), (acc >> 1) & 1, &failed)) { ok = false; break; }
                     tc_fence_after();
                     ++acc;
                 }
