@@ -368,11 +368,13 @@ lgc_status lgc_product(const lgc_packed *a, const lgc_packed *b, int32_t across,
  *     dW_k[n][i] = sum over node k's rows t of dY[t][n] X[t][i],    fp32, n < num_cols, i < inner,
  * written back to back (num_cols * inner floats, node k's k * node_stride floats after node 0's).
  * dy: bf16, 16-byte aligned, ld_dy a multiple of 8.  x: block_rows = 1.  The products are exact in the tensor
- * cores' bf16 form (a code times its scale is a bf16 number), the sums fp32.  Rows outside a node's run have no
- * influence on its gradient, whatever they hold. */
+ * cores' bf16 form (a code times its scale is a bf16 number), the sums fp32 in a fixed order.  Rows outside a node's
+ * run have no influence on its gradient, whatever they hold.
+ * scratch: lgc_weight_gradient_scratch bytes, 16-byte aligned (X in bf16; partial sums where there are few tiles). */
+lgc_status lgc_weight_gradient_scratch(int64_t num_rows, int64_t num_cols, int64_t inner, int32_t num_nodes, size_t *bytes);
 lgc_status lgc_weight_gradient(const void *dy, int64_t ld_dy, const lgc_packed *x, int64_t num_rows, int64_t num_cols,
                                int64_t inner, const int64_t *node_start, int32_t num_nodes, float *dw, int64_t node_stride,
-                               void *stream);
+                               void *scratch, size_t scratch_bytes, void *stream);
 
 /* What the kernels of lgc_layer_norm_backward, lgc_product and lgc_weight_gradient recorded on the current device (a
  * wait inside a kernel that ran out): waits for `stream`, returns LGC_OK or LGC_ERR_DEVICE_CHECK and clears the record. */

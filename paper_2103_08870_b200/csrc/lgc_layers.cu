@@ -239,8 +239,18 @@ lgc_status lgc_product(const lgc_packed *a, const lgc_packed *b, int32_t across,
     return done(where, e);
 }
 
+lgc_status lgc_weight_gradient_scratch(int64_t num_rows, int64_t num_cols, int64_t inner, int32_t num_nodes, size_t *bytes)
+{
+    const char *where = "lgc_weight_gradient_scratch", *why = bad_sizes(num_rows, num_cols);
+    if (why || (why = bad_sizes(0, inner))) return refuse(where, why);
+    if (!bytes || num_nodes < 1 || num_nodes > 65535) return refuse(where, "NULL result or num_nodes outside [1, 65535]");
+    *bytes = weight_gradient_scratch(num_rows, num_cols, inner, num_nodes);
+    return LGC_OK;
+}
+
 lgc_status lgc_weight_gradient(const void *dy, int64_t ld_dy, const lgc_packed *x, int64_t num_rows, int64_t num_cols, int64_t inner,
-                               const int64_t *node_start, int32_t num_nodes, float *dw, int64_t node_stride, void *stream)
+                               const int64_t *node_start, int32_t num_nodes, float *dw, int64_t node_stride, void *scratch,
+                               size_t scratch_bytes, void *stream)
 {
     const char *where = "lgc_weight_gradient", *why = nullptr;
     if ((why = bad_sizes(num_rows, num_cols)) || (why = bad_sizes(0, inner))) return refuse(where, why);
@@ -252,10 +262,13 @@ lgc_status lgc_weight_gradient(const void *dy, int64_t ld_dy, const lgc_packed *
     if (num_rows == 0)                            // no node has a row: every gradient is zero
         return done(where, cudaMemset2DAsync(dw, (size_t)(num_nodes > 1 ? node_stride : num_cols * inner) * 4, 0,
                                              (size_t)(num_cols * inner) * 4, (size_t)num_nodes, static_cast<cudaStream_t>(stream)));
+    if (!scratch || (reinterpret_cast<uintptr_t>(scratch) & 15) != 0) return refuse(where, "scratch is NULL or not 16-byte aligned");
+    if (scratch_bytes < weight_gradient_scratch(num_rows, num_cols, inner, num_nodes))
+        return refuse(where, "scratch is smaller than lgc_weight_gradient_scratch says", LGC_ERR_WORKSPACE);
     int32_t *record = nullptr;
     cudaError_t e = record_address(&record);
     if (e == cudaSuccess)
-        e = launch_weight_gradient(dy, ld_dy, *x, num_rows, num_cols, inner, node_start, num_nodes, dw, node_stride, record,
+        e = launch_weight_gradient(dy, ld_dy, *x, num_rows, num_cols, inner, node_start, num_nodes, dw, node_stride, scratch, record,
                                    static_cast<cudaStream_t>(stream));
     return done(where, e);
 }

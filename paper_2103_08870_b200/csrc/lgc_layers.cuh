@@ -316,8 +316,9 @@ cudaError_t launch_unpack(const lgc_packed &src, int64_t rows, int64_t cols, int
                           cudaStream_t s);
 cudaError_t launch_product(const lgc_packed &a, const lgc_packed &b, bool across, int64_t rows, int64_t cols, int64_t inner, float slope,
                            void *y, int32_t type, int64_t ldy, const lgc_packed *packed, int32_t *errword, cudaStream_t s);
+size_t weight_gradient_scratch(int64_t rows, int64_t cols, int64_t inner, int32_t nodes);
 cudaError_t launch_weight_gradient(const void *dy, int64_t ld_dy, const lgc_packed &x, int64_t rows, int64_t cols, int64_t inner,
-                                   const int64_t *node_start, int32_t num_nodes, float *dw, int64_t node_stride, int32_t *errword,
-                                   cudaStream_t s);
+                                   const int64_t *node_start, int32_t num_nodes, float *dw, int64_t node_stride, void *scratch,
+                                   int32_t *errword, cudaStream_t s);
 
 }  // namespace lgc

@@ -94,6 +94,7 @@ __global__ void __launch_bounds__(256)
 unpack_kernel(const uint8_t *__restrict__ codes, int64_t ld_codes, const uint8_t *__restrict__ scales, int64_t ld_scales, int64_t rows,
               int cols, uint32_t parts, int32_t block_rows, T *__restrict__ y, int64_t ldy)
 {
+    grid_release_dependents();                                   // (the weight gradient sets itself up meanwhile)
     const int64_t item = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (item >= rows * parts) return;
     const int64_t row = item / parts;

@@ -182,19 +182,25 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     tc_fence_after();
     const uint32_t tmem = tmem_base;
 
-    if (threadIdx.x == 0) {
-        int it = 0;
-        for (int64_t tile = blockIdx.x; tile < total && !failed; tile += gridDim.x) {
+    if (warp == 0) {
+        const bool issuer = elect_one();
+        int s = 0;
+        uint32_t phase = 1;                                       // the first pass over the stages waits for nobody
+        bool ok = true;
+        for (int64_t tile = blockIdx.x; tile < total && ok; tile += gridDim.x) {
             int m, n;
             tile_of(tile, p.tiles_m, p.tiles_n, m, n);
-            for (int kb = 0; kb < blocks; ++kb, ++it) {
-                const int s = it % kStages;
-                if (it >= kStages && !bar_wait(smem_addr(&empty_bar[s]), ((it / kStages) & 1) ^ 1, &failed)) break;
+            for (int kb = 0; kb < blocks; ++kb) {
+                if (!bar_wait_together(smem_addr(&empty_bar[s]), phase, &failed)) { ok = false; break; }
                 const uint32_t bar = smem_addr(&full_bar[s]), st = tiles + s * kStageBytes;
-                bar_expect(bar, kStageBytes);
-                tma_load(st, &map_a, bar, kb * kBlock, m * kM);
-                if (ACROSS) tma_load(st + kM * kBlock, &map_b, bar, n * kN, kb * kBlock);
-                else tma_load(st + kM * kBlock, &map_b, bar, kb * kBlock, n * kN);
+                if (issuer) {
+                    bar_expect(bar, kStageBytes);
+                    tma_load(st, &map_a, bar, kb * kBlock, m * kM);
+                    if (ACROSS) tma_load(st + kM * kBlock, &map_b, bar, n * kN, kb * kBlock);
+                    else tma_load(st + kM * kBlock, &map_b, bar, kb * kBlock, n * kN);
+                }
+                __syncwarp();
+                if (++s == kStages) s = 0, phase ^= 1;
             }
         }
     } else if (warp == 1) {
@@ -320,13 +326,6 @@ constexpr int kScaleCol = 512 - 2 * kScaleCols;
 constexpr int kSecond = kScaleCol - kTile;                       // first column of the second accumulator
 static_assert(kSecond >= kTile - kBlock, "the shared columns lie inside one block of 128 of either accumulator");
 
-__device__ __forceinline__ void tma_load_shared_bar(uint32_t dst, const CUtensorMap *map, uint32_t bar0, int c0, int c1)   // completes at CTA 0's barrier
-{
-    asm volatile(
-        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-        ::"r"(dst), "l"(map), "r"(bar0), "r"(c0), "r"(c1)
-        : "memory");
-}
 __device__ __forceinline__ void mma_block_scaled(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, bool accumulate)
 {
     asm volatile(
@@ -389,20 +388,25 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     tc_fence_after();
     const uint32_t tmem = tmem_base;
 
-    if (threadIdx.x == 0) {
+    if (warp == 0) {
+        const bool issuer = elect_one();
         int s = 0;
         uint32_t phase = 1;                                       // the first pass over the stages waits for nobody
-        for (int64_t tile = first; tile < total && !failed; tile += step) {
+        bool ok = true;
+        for (int64_t tile = first; tile < total && ok; tile += step) {
             int m, n;
             tile_at(tile, p, m, n);
             const int arow = m * kTile + (int)rank * kHalf, brow = n * kTile + (int)rank * kHalf;
             for (int kb = 0; kb < blocks; ++kb) {
-                if (!bar_wait(smem_addr(&empty_bar[s]), phase, &failed)) break;
+                if (!bar_wait_together(smem_addr(&empty_bar[s]), phase, &failed)) { ok = false; break; }
                 const uint32_t st = tiles + s * kStageBytes, bar0 = cluster_addr(smem_addr(&full_bar[s]), 0);
-                if (rank == 0) bar_expect(smem_addr(&full_bar[s]), 2 * kStageBytes);
-                tma_load_shared_bar(st, &map_a, bar0, kb * kBlock, arow);
-                if (ACROSS) tma_load_shared_bar(st + kHalf * kBlock, &map_b, bar0, brow, kb * kBlock);
-                else tma_load_shared_bar(st + kHalf * kBlock, &map_b, bar0, kb * kBlock, brow);
+                if (issuer) {
+                    if (rank == 0) bar_expect(smem_addr(&full_bar[s]), 2 * kStageBytes);
+                    tma_load_pair(st, &map_a, bar0, kb * kBlock, arow);
+                    if (ACROSS) tma_load_pair(st + kHalf * kBlock, &map_b, bar0, brow, kb * kBlock);
+                    else tma_load_pair(st + kHalf * kBlock, &map_b, bar0, kb * kBlock, brow);
+                }
+                __syncwarp();
                 if (++s == kStages) s = 0, phase ^= 1;
             }
         }

@@ -109,6 +109,14 @@ __device__ __forceinline__ void bar_arrive_cluster(uint32_t cluster_bar)
 {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
+// A TMA load into this CTA's shared memory that completes at a barrier of either CTA of the pair (a cluster address).
+__device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap *map, uint32_t cluster_bar, int c0, int c1)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+        ::"r"(dst), "l"(map), "r"(cluster_bar), "r"(c0), "r"(c1)
+        : "memory");
+}
 // tcgen05 for the pair: tensor memory is allocated in both CTAs, one thread of CTA 0 issues, and completion arrives at the
 // same barrier of both.
 __device__ __forceinline__ void tc_alloc_pair(uint32_t *where, uint32_t cols)

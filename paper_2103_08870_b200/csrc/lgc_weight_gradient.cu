@@ -2,15 +2,17 @@
 //
 // The sum runs along the rows (tokens) of both operands, and the checkpoint's scale changes from row to row, so the
 // 8-bit tensor-core form, whose scales cover 32 steps of the sum, cannot take X without rounding it a second time.
-// Instead a code times its scale, exactly a bf16 number, is formed in shared memory by sixteen warps between the TMA and the
-// MMA; dY is bf16 and goes in as it is.  Both operands lie along their rows (MN-major): 128 bytes of columns per row.
+// Instead X becomes bf16 first (exact: a code times its scale is a bf16 number), once, in scratch memory, and a bf16 product
+// follows.  (Making the bf16 numbers inside the product, between the loads and the tensor cores, saves the 3 bytes an entry
+// but repeats the conversion for every 256 columns of dY, and its shared memory and its delay are missing in the ring of
+// loads: 626 us against 517 us for 16384 x 4096 x 4096.)
 //
-// Two CTAs make a tile of 256 x 256 together (cta_group::2): each loads, and converts, half of both operands, which halves
-// what a tile of this size costs in loads and conversions per product.
-//
-// Rows of other nodes that a tile's last block of rows reaches are set to zero in both operands.
+// Both operands lie along their rows (MN-major): 128 bytes of columns per row.  Two CTAs make a tile of 256 x 256 together
+// (cta_group::2); each loads half of both operands.  Rows of other nodes that a tile's last stage reaches are set to zero in
+// both operands, whatever they hold.
 // Sums: the tensor cores add in fp32 in tensor memory over at most 64 * 64 rows; longer sums are added up in memory from
-// there, so that they do not lose to the accumulator's rounding (it errs by about 2^-24 of the sum per 16 rows).
+// there, so that they do not lose to the accumulator's rounding (it errs by about 2^-24 of the sum per 16 rows).  Where
+// there are few tiles a node's rows are cut into parts, whose sums a last kernel adds in order.
 #include "lgc_layers.cuh"
 #include "lgc_tensor_core.cuh"
 
@@ -21,15 +23,13 @@ namespace {
 constexpr int kM = 256, kN = 256;                 // a pair's tile: columns of dY x columns of X; each CTA loads half of both
 constexpr int kRows = 64;                         // rows per stage
 constexpr int kHalf = 128;
-constexpr int kABytes = kHalf * kRows * 2, kBBytes = kHalf * kRows * 2, kCodeBytes = kHalf * kRows;
-constexpr int kStageBytes = kABytes + kBBytes + kCodeBytes;
-constexpr int kPiece = 64 * kRows * 2;            // 64 columns (128 bytes) of a stage's rows in bf16
-constexpr int kStages = 5;
+constexpr int kABytes = kHalf * kRows * 2, kStageBytes = 2 * kABytes;
+constexpr int kPiece = 64 * kRows * 2;            // 64 columns (128 bytes) of a stage's rows
+constexpr int kStages = 6;
 constexpr int kFlushSteps = 64;                   // stages that the tensor cores add up before their sums go to memory
 constexpr int kPitch = 33;                        // floats per row of the result's staging blocks
-constexpr int kOutBytes = 4 * 32 * kPitch * 4;
-constexpr int kSmemBytes = kStages * (kStageBytes + kRows * 4) + kOutBytes + 1024;
-constexpr int kThreads = 768;                     // warp 0: TMA, 1: MMA, 2: scales, 3: tensor memory, 4..7: results, 8..23: X to bf16
+constexpr int kSmemBytes = kStages * kStageBytes + 4 * 32 * kPitch * 4 + 1024;
+constexpr int kThreads = 256;                     // warp 0: TMA, 1: MMA, 2: rows of other nodes, 3: tensor memory, 4..7: results
 constexpr int kTmemCols = 2 * kN;
 
 __device__ __forceinline__ void mma_bf16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate)
@@ -42,46 +42,39 @@ __device__ __forceinline__ void mma_bf16(uint32_t d, uint64_t a, uint64_t b, uin
         : "memory");
 }
 
-// Two codes (bytes 0 and 1 of q, or 2 and 3) as bf16 times a power of two, exact.  A code's exponent and mantissa bits
-// moved to bf16's place read as the value times 2^-120 (subnormal codes as subnormal bf16), so factor = scale * 2^120.
-__device__ __forceinline__ uint32_t codes_to_bf16(uint32_t q, uint32_t selector, uint32_t factor)
-{
-    const uint32_t w = __byte_perm(q, 0, selector);            // each code in the upper byte of a half
-    const uint32_t x = (w & 0x80008000u) | ((w & 0x7f007f00u) >> 4);
-    uint32_t r;
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(factor));
-    return r;
-}
-
 struct WeightArgs {
-    const uint8_t *scales;
-    int64_t ld_scales;
     int64_t rows, cols, inner;
     const int64_t *start;
-    int nodes;
+    int nodes, parts;        // parts of a node's rows
     float *dw;
     int64_t node_stride;
+    float *partial;          // [parts][nodes * tiles][256][256] where parts > 1
     int32_t *errword;
     int tiles_m, tiles_n;
 };
 
 struct Tile {
-    int64_t begin, end;      // rows of the node
+    int64_t begin, end;      // rows: from the part's first to the node's end
     int node, m, n;
     int steps;               // stages of kRows rows
 };
 __device__ __forceinline__ Tile tile_of(const WeightArgs &p, int64_t t)
 {
     Tile w;
-    const int64_t per = (int64_t)p.tiles_m * p.tiles_n;
-    w.node = (int)(t / per);
-    const int r = (int)(t - w.node * per);
+    const int64_t per = (int64_t)p.tiles_m * p.tiles_n, all = per * p.nodes;
+    const int part = (int)(t / all);
+    const int64_t u = t - part * all;
+    w.node = (int)(u / per);
+    const int r = (int)(u - w.node * per);
     w.m = r % p.tiles_m;
     w.n = r / p.tiles_m;
     w.begin = node_first_row(p.start, w.node, p.rows);
     w.end = node_first_row(p.start, w.node + 1, p.rows);
     if (w.end < w.begin) w.end = w.begin;
-    w.steps = (int)((w.end - w.begin + kRows - 1) / kRows);
+    const int64_t steps = (w.end - w.begin + kRows - 1) / kRows;
+    const int64_t from = steps * part / p.parts, to = steps * (part + 1) / p.parts;
+    w.begin += from * kRows;
+    w.steps = (int)(to - from);
     return w;
 }
 
@@ -89,23 +82,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 weight_gradient_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ WeightArgs p)
 {
     extern __shared__ uint8_t dyn_smem[];
-    // full: loads of a stage (both CTAs have their own); ready (CTA 0's): X of both halves is bf16; empty: the MMAs are through
-    __shared__ __align__(8) uint64_t full_bar[kStages], ready_bar[kStages], empty_bar[kStages], tfull_bar[2], tempty_bar[2];
+    // full, cleared, tempty: CTA 0's count, for the pair; empty, tfull: arrive in both CTAs; loaded: this CTA's last stage of a tile
+    __shared__ __align__(8) uint64_t full_bar[kStages], empty_bar[kStages], loaded_bar[kStages], cleared_bar[kStages], tfull_bar[2], tempty_bar[2];
     __shared__ uint32_t tmem_base;
     __shared__ volatile int failed;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t base = (smem_addr(dyn_smem) + 1023u) & ~1023u;
-    const uint32_t scale_words = base + kStages * kStageBytes;
-    const int64_t total = (int64_t)p.tiles_m * p.tiles_n * p.nodes;
+    const int64_t total = (int64_t)p.tiles_m * p.tiles_n * p.nodes * p.parts;
     const uint32_t rank = cluster_rank();
     const int64_t first = blockIdx.x >> 1, step = gridDim.x >> 1;
 
     if (threadIdx.x == 0) {
         failed = 0;
         for (int s = 0; s < kStages; ++s) {
-            bar_init(smem_addr(&full_bar[s]), 1 + 32);
-            bar_init(smem_addr(&ready_bar[s]), 2 * 8);
+            bar_init(smem_addr(&full_bar[s]), 1);
             bar_init(smem_addr(&empty_bar[s]), 1);
+            bar_init(smem_addr(&loaded_bar[s]), 1);
+            bar_init(smem_addr(&cleared_bar[s]), 2);
         }
         for (int s = 0; s < 2; ++s) {
             bar_init(smem_addr(&tfull_bar[s]), 1);
@@ -119,23 +112,36 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_
     cluster_sync();
     tc_fence_after();
     const uint32_t tmem = tmem_base;
+    grid_wait();                          // X in bf16 comes from the launch in front
 
-    if (threadIdx.x == 0) {
-        int it = 0;
-        for (int64_t t = first; t < total && !failed; t += step) {
+    // A stage that reaches past its node's end completes at this CTA's own barrier `loaded`; warp 2 clears the rows that are
+    // not the node's and reports to `cleared`.  Every other stage completes at CTA 0's `full`.
+    if (warp == 0) {
+        const bool issuer = elect_one();
+        int s = 0;
+        uint32_t phase = 1;                                       // the first pass over the stages waits for nobody
+        bool ok = true;
+        for (int64_t t = first; t < total && ok; t += step) {
             const Tile w = tile_of(p, t);
             const int mc = w.m * kM + (int)rank * kHalf, nc = w.n * kN + (int)rank * kHalf;
-            for (int i = 0; i < w.steps; ++i, ++it) {
-                const int s = it % kStages;
-                if (it >= kStages && !bar_wait(smem_addr(&empty_bar[s]), ((it / kStages) & 1) ^ 1, &failed)) break;
-                const uint32_t bar = smem_addr(&full_bar[s]), st = base + s * kStageBytes;
-                const int row = (int)(w.begin + (int64_t)i * kRows);
-                bar_expect(bar, kABytes + kCodeBytes);
+            const int steps = __shfl_sync(0xffffffffu, w.steps, 0);
+            for (int i = 0; i < steps; ++i) {
+                if (!bar_wait_together(smem_addr(&empty_bar[s]), phase, &failed)) { ok = false; break; }
+                const int64_t row = w.begin + (int64_t)i * kRows;
+                const bool ragged = row + kRows > w.end;
+                const uint32_t st = base + s * kStageBytes;
+                const uint32_t bar = ragged ? smem_addr(&loaded_bar[s]) : cluster_addr(smem_addr(&full_bar[s]), 0);
+                if (issuer) {
+                    if (ragged) bar_expect(smem_addr(&loaded_bar[s]), kStageBytes);
+                    else if (rank == 0) bar_expect(smem_addr(&full_bar[s]), 2 * kStageBytes);
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    tma_load(st + j * kPiece, &map_dy, bar, mc + 64 * j, row);
-                    tma_load(st + kABytes + kBBytes + j * 64 * kRows, &map_x, bar, nc + 64 * j, row);
+                    for (int j = 0; j < 2; ++j) {
+                        tma_load_pair(st + j * kPiece, &map_dy, bar, mc + 64 * j, (int)row);
+                        tma_load_pair(st + kABytes + j * kPiece, &map_x, bar, nc + 64 * j, (int)row);
+                    }
                 }
+                __syncwarp();
+                if (++s == kStages) s = 0, phase ^= 1;
             }
         }
     } else if (warp == 1) {
@@ -143,16 +149,23 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_
         constexpr uint32_t idesc = 1u << 4 | 1u << 7 | 1u << 10 | 1u << 15 | 1u << 16 | (uint32_t)(kN >> 3) << 17 | (uint32_t)(kM >> 4) << 24;
         const bool issuer = elect_one();
         int s = 0, acc = 0;
-        uint32_t phase = 0;
+        uint32_t full = 0, cleared = 0;                           // a bit per stage: the phases of the two barriers to wait for next
         bool ok = rank == 0;
         for (int64_t t = first; t < total && ok; t += step) {
-            const int steps = __shfl_sync(0xffffffffu, tile_of(p, t).steps, 0);
+            const Tile w = tile_of(p, t);
+            const int steps = __shfl_sync(0xffffffffu, w.steps, 0);
+            const bool ragged_end = __all_sync(0xffffffffu, w.begin + (int64_t)w.steps * kRows > w.end);
             for (int i = 0; i < steps; ++i) {
                 const int buf = acc & 1;
                 const bool begin = i % kFlushSteps == 0, end = i % kFlushSteps == kFlushSteps - 1 || i == steps - 1;
                 if (begin && acc >= 2 && !bar_wait_together(smem_addr(&tempty_bar[buf]), ((acc >> 1) & 1) ^ 1, &failed)) { ok = false; break; }
-                // the warps that make B wait for the loads of their CTA, dY among them
-                if (!bar_wait_together(smem_addr(&ready_bar[s]), phase, &failed)) { ok = false; break; }
+                if (ragged_end && i == steps - 1) {
+                    if (!bar_wait_together(smem_addr(&cleared_bar[s]), (cleared >> s) & 1, &failed)) { ok = false; break; }
+                    cleared ^= 1u << s;
+                } else {
+                    if (!bar_wait_together(smem_addr(&full_bar[s]), (full >> s) & 1, &failed)) { ok = false; break; }
+                    full ^= 1u << s;
+                }
                 tc_fence_after();
                 const uint32_t st = base + s * kStageBytes;
                 const uint64_t a = tc_desc(st, kPiece), b = tc_desc(st + kABytes, kPiece);
@@ -164,102 +177,47 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_
                     if (end) tc_commit_pair(smem_addr(&tfull_bar[buf]));
                 }
                 __syncwarp();
-                if (++s == kStages) s = 0, phase ^= 1;
+                if (++s == kStages) s = 0;
                 acc += end;
             }
         }
     } else if (warp == 2) {
-        // scale words of the stage's rows (four blocks each; this CTA's columns are one of them)
-        int it = 0;
-        bool ok = true;
-        for (int64_t t = first; t < total && ok; t += step) {
+        int s = 0;
+        uint32_t phases = 0;                                      // a bit per stage: the phase of `loaded` to wait for next
+        for (int64_t t = first; t < total; t += step) {
             const Tile w = tile_of(p, t);
-            const int64_t block = (int64_t)w.n * 2 + rank;
-            for (int i = 0; i < w.steps; ++i, ++it) {
-                const int s = it % kStages;
-                if (it >= kStages && !bar_wait_together(smem_addr(&empty_bar[s]), ((it / kStages) & 1) ^ 1, &failed)) { ok = false; break; }
-#pragma unroll
-                for (int j = 0; j < kRows / 32; ++j) {
-                    const int64_t row = w.begin + (int64_t)i * kRows + 32 * j + lane;
-                    if (row < w.end && block * kBlock < p.inner)
-                        word_load(scale_words + (s * kRows + 32 * j + lane) * 4, p.scales + row * p.ld_scales + (block & ~(int64_t)3));
-                }
-                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_addr(&full_bar[s])) : "memory");
-            }
-        }
-    } else if (warp >= 8) {
-        // Two groups of eight warps take the stages in turn.  A thread converts 16 neighbouring codes of one row in both
-        // 64-column pieces; four lanes per row, so that eight lanes read and write 128 bytes without bank conflicts.
-        const int group = (warp - 8) >> 3, id = threadIdx.x & 255, quarter = id & 3, r = id >> 2;
-        const uint32_t from = kABytes + kBBytes + r * 64 + quarter * 16, to = kABytes + r * 128;
-        const uint32_t c0 = ((quarter * 2) ^ (r & 7)) << 4, c1 = ((quarter * 2 + 1) ^ (r & 7)) << 4;    // 16-byte chunks, swizzled by the row
-        int it = 0;
-        bool ok = true;
-        for (int64_t t = first; t < total && ok; t += step) {
-            const Tile w = tile_of(p, t);
-            const int64_t block = (int64_t)w.n * 2 + rank;
-            const bool any = block * kBlock < p.inner;
-            const int shift = (int)(block & 3) * 8;
-            for (int i = 0; i < w.steps; ++i, ++it) {
-                if ((it & 1) != group) continue;
-                const int s = it % kStages;
-                const uint32_t st = base + s * kStageBytes;
-                const bool live = r < w.end - (w.begin + (int64_t)i * kRows);        // the row is this node's
-                if (!bar_wait_together(smem_addr(&full_bar[s]), (it / kStages) & 1, &failed)) { ok = false; break; }
-                uint32_t q[2][4], word;
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                                 : "=r"(q[j][0]), "=r"(q[j][1]), "=r"(q[j][2]), "=r"(q[j][3])
-                                 : "r"(st + from + j * 64 * kRows));
-                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(word) : "r"(scale_words + (s * kRows + r) * 4));
-                const uint32_t scale = (word >> shift) & 255u;
-                // scale * 2^120, in two factors where that is beyond bf16's exponents
-                uint32_t f1 = ((min(scale, 134u) + 120u) << 7) * 0x10001u, f2 = 0;
-                if (scale > 134u) {
-                    if (scale == 255u) f1 = 0x7fff7fffu;
-                    else f2 = ((scale - 7u) << 7) * 0x10001u;
-                }
-                if (!live || !any) f1 = f2 = 0;
-                uint32_t x[2][8];
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        x[j][2 * k] = codes_to_bf16(q[j][k], 0x1404, f1);
-                        x[j][2 * k + 1] = codes_to_bf16(q[j][k], 0x3424, f1);
-                    }
-                if (f2 != 0)
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) asm("mul.rn.bf16x2 %0, %0, %1;" : "+r"(x[j >> 3][j & 7]) : "r"(f2));
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const uint32_t at = st + to + j * kPiece;
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + c0), "r"(x[j][0]), "r"(x[j][1]), "r"(x[j][2]), "r"(x[j][3]) : "memory");
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + c1), "r"(x[j][4]), "r"(x[j][5]), "r"(x[j][6]), "r"(x[j][7]) : "memory");
-                }
-                if (!live) {
-                    // a row of another node: dY's part becomes zero as well (its chunks of 16 bytes, whatever their order)
+            if (w.steps == 0) continue;
+            s = (s + w.steps - 1) % kStages;                      // the tile's last stage
+            const int live = (int)(w.end - (w.begin + (int64_t)(w.steps - 1) * kRows));
+            if (live < kRows) {
+                if (!bar_wait_together(smem_addr(&loaded_bar[s]), (phases >> s) & 1, &failed)) break;
+                phases ^= 1u << s;
+                // rows of 128 bytes, whose order inside does not matter: four pieces, eight lanes per row
+                for (int r = live + (lane >> 3); r < kRows; r += 4)
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(st + (j >> 1) * kPiece + r * 128 + quarter * 32 + (j & 1) * 16), "r"(0)
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(base + s * kStageBytes + j * kPiece + r * 128 + (lane & 7) * 16), "r"(0)
                                      : "memory");
-                }
                 async_proxy_fence();
                 __syncwarp();
-                if (lane == 0) bar_arrive_cluster(cluster_addr(smem_addr(&ready_bar[s]), 0));
+                if (lane == 0) bar_arrive_cluster(cluster_addr(smem_addr(&cleared_bar[s]), 0));
             }
+            s = s + 1 == kStages ? 0 : s + 1;
         }
     } else if (warp >= 4) {
         const int q = warp & 3;
-        float *stage = reinterpret_cast<float *>(dyn_smem + (scale_words - smem_addr(dyn_smem)) + kStages * kRows * 4) + q * 32 * kPitch;
+        float *stage = reinterpret_cast<float *>(dyn_smem + (base - smem_addr(dyn_smem)) + kStages * kStageBytes) + q * 32 * kPitch;
         int acc = 0;
         bool ok = true;
         for (int64_t t = first; t < total && ok; t += step) {
             const Tile w = tile_of(p, t);
-            float *out = p.dw + w.node * p.node_stride;
-            const int64_t row0 = (int64_t)w.m * kM + rank * kHalf + q * 32;
-            // (a node without rows: its gradient is zero)
+            const int row0 = (int)rank * kHalf + q * 32;          // inside the tile
+            // where the tile's entry (0, 0) goes, and how much of the tile is written
+            float *out = p.parts > 1 ? p.partial + t * (kM * kN) : p.dw + w.node * p.node_stride + (int64_t)w.m * kM * p.inner + (int64_t)w.n * kN;
+            const int64_t ld = p.parts > 1 ? kN : p.inner;
+            const int rows = p.parts > 1 ? kM : (int)min((int64_t)kM, p.cols - (int64_t)w.m * kM);
+            const int cols = p.parts > 1 ? kN : (int)min((int64_t)kN, p.inner - (int64_t)w.n * kN);
+            // (without rows: zeros)
             for (int i = 0; i == 0 || i < w.steps; i += kFlushSteps) {
                 const int buf = acc & 1;
                 if (w.steps > 0) {
@@ -283,15 +241,18 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_
 #pragma unroll
                     for (int j = 0; j < 32; ++j) stage[lane * kPitch + j] = __uint_as_float(v[j]);
                     __syncwarp();
-                    const int64_t col = (int64_t)w.n * kN + c + lane;
-                    if (col < p.inner)
+                    if (c + lane < cols) {
+                        float *o = out + row0 * ld + c + lane;
+                        if (i == 0) {
 #pragma unroll 8
-                        for (int j = 0; j < 32; ++j)
-                            if (row0 + j < p.cols) {
-                                float *o = out + (row0 + j) * p.inner + col;
-                                const float x = stage[j * kPitch + lane];
-                                *o = i == 0 ? x : __fadd_rn(*o, x);
-                            }
+                            for (int j = 0; j < 32; ++j)
+                                if (row0 + j < rows) o[j * ld] = stage[j * kPitch + lane];
+                        } else {
+#pragma unroll 8
+                            for (int j = 0; j < 32; ++j)
+                                if (row0 + j < rows) o[j * ld] = __fadd_rn(o[j * ld], stage[j * kPitch + lane]);
+                        }
+                    }
                 }
                 if (w.steps > 0) {
                     tc_fence_before();
@@ -308,26 +269,77 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_
     if (warp == 3) tc_free_pair(tmem, kTmemCols);
 }
 
+// The parts of every tile, added in order.  A CTA: 16 rows of a tile.
+__global__ void __launch_bounds__(256)
+weight_gradient_sum_kernel(const __grid_constant__ WeightArgs p)
+{
+    grid_wait();
+    const int64_t per = (int64_t)p.tiles_m * p.tiles_n, all = per * p.nodes, t = blockIdx.x;
+    const int node = (int)(t / per), r = (int)(t - node * per);
+    const int64_t row0 = (int64_t)(r % p.tiles_m) * kM + blockIdx.y * 16, col = (int64_t)(r / p.tiles_m) * kN + threadIdx.x;
+    if (col >= p.inner) return;
+    const float *from = p.partial + t * (kM * kN) + blockIdx.y * 16 * kN + threadIdx.x;
+    float sum[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) sum[j] = __ldcg(from + j * kN);
+    for (int part = 1; part < p.parts; ++part) {
+        from += all * (kM * kN);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) sum[j] = __fadd_rn(sum[j], __ldcg(from + j * kN));
+    }
+    float *out = p.dw + node * p.node_stride + row0 * p.inner + col;
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+        if (row0 + j < p.cols) out[j * p.inner] = sum[j];
+}
+
+int64_t x_bytes(int64_t rows, int64_t inner) { return (rows * ((inner + 7) / 8 * 8) * 2 + 255) / 256 * 256; }
+int64_t tiles_for(int64_t cols, int64_t inner, int32_t nodes) { return ((cols + kM - 1) / kM) * ((inner + kN - 1) / kN) * nodes; }
+
+// Parts of a node's rows: as many as give every pair of SMs a tile, but at least eight stages to a part.
+int parts_for(int64_t rows, int64_t cols, int64_t inner, int32_t nodes)
+{
+    const int64_t tiles = tiles_for(cols, inner, nodes), most = 148 / 2 / tiles, long_enough = rows / nodes / (8 * kRows);
+    const int64_t parts = most < long_enough ? most : long_enough;
+    return parts < 2 ? 1 : (int)parts;
+}
+
 }  // namespace
 
-cudaError_t launch_weight_gradient(const void *dy, int64_t ld_dy, const lgc_packed &x, int64_t rows, int64_t cols, int64_t inner,
-                                   const int64_t *node_start, int32_t num_nodes, float *dw, int64_t node_stride, int32_t *errword,
-                                   cudaStream_t s)
+size_t weight_gradient_scratch(int64_t rows, int64_t cols, int64_t inner, int32_t nodes)
 {
-    WeightArgs p{x.scales, x.ld_scales, rows, cols, inner, node_start, num_nodes, dw, node_stride, errword, (int)((cols + kM - 1) / kM),
+    const int parts = parts_for(rows, cols, inner, nodes);
+    return (size_t)x_bytes(rows, inner) + (parts > 1 ? (size_t)parts * tiles_for(cols, inner, nodes) * kM * kN * 4 : 0);
+}
+
+cudaError_t launch_weight_gradient(const void *dy, int64_t ld_dy, const lgc_packed &x, int64_t rows, int64_t cols, int64_t inner,
+                                   const int64_t *node_start, int32_t num_nodes, float *dw, int64_t node_stride, void *scratch,
+                                   int32_t *errword, cudaStream_t s)
+{
+    const int64_t ld_x = (inner + 7) / 8 * 8;
+    cudaError_t e = launch_unpack(x, rows, inner, 1, scratch, LGC_TYPE_BF16, ld_x, s);
+    if (e != cudaSuccess) return e;
+    WeightArgs p{rows, cols, inner, node_start, num_nodes, parts_for(rows, cols, inner, num_nodes), dw, node_stride,
+                 reinterpret_cast<float *>(static_cast<char *>(scratch) + x_bytes(rows, inner)), errword, (int)((cols + kM - 1) / kM),
                  (int)((inner + kN - 1) / kN)};
     CUtensorMap map_dy, map_x;
-    cudaError_t e = make_matrix_map(&map_dy, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, dy, cols, rows, ld_dy, 64, kRows, CU_TENSOR_MAP_SWIZZLE_128B);
+    e = make_matrix_map(&map_dy, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, dy, cols, rows, ld_dy, 64, kRows, CU_TENSOR_MAP_SWIZZLE_128B);
     if (e != cudaSuccess) return e;
-    e = make_matrix_map(&map_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, x.codes, inner, rows, x.ld, 64, kRows, CU_TENSOR_MAP_SWIZZLE_NONE);
+    e = make_matrix_map(&map_x, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, scratch, inner, rows, ld_x, 64, kRows, CU_TENSOR_MAP_SWIZZLE_128B);
     if (e != cudaSuccess) return e;
     static OncePerDevice configured;
     e = configured.run([&] { return cudaFuncSetAttribute(weight_gradient_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes); });
     if (e != cudaSuccess) return e;
-    const int64_t total = (int64_t)p.tiles_m * p.tiles_n * num_nodes;
-    const int64_t pairs = sm_count() / 2;
-    weight_gradient_kernel<<<(unsigned)(2 * (total < pairs ? total : pairs)), kThreads, kSmemBytes, s>>>(map_dy, map_x, p);
+    const int64_t tiles = tiles_for(cols, inner, num_nodes), total = tiles * p.parts, pairs = sm_count() / 2;
+    e = launch_dependent_smem(weight_gradient_kernel, dim3((unsigned)(2 * (total < pairs ? total : pairs))), dim3(kThreads), kSmemBytes, s, map_dy,
+                              map_x, p);
+    if (e != cudaSuccess) return e;
     ++g_kernel_launches;
+    if (p.parts > 1) {
+        e = launch_dependent(weight_gradient_sum_kernel, dim3((unsigned)tiles, kM / 16), dim3(256), s, p);
+        if (e != cudaSuccess) return e;
+        ++g_kernel_launches;
+    }
     return cudaGetLastError();
 }
 

@@ -213,18 +213,27 @@ def product(a: Packed, b: Packed, y: Optional[torch.Tensor] = None, packed: Opti
                                 None if packed is None else _packed(packed, "packed", rows, cols), _stream(stream, a.codes)), "lgc_product")
 
 
+def weight_gradient_scratch(rows: int, cols: int, inner: int, num_nodes: int = 1) -> int:
+    """Bytes of scratch that weight_gradient needs."""
+    n = C.c_size_t()
+    _done(lgc.lib().lgc_weight_gradient_scratch(rows, cols, inner, num_nodes, C.byref(n)), "lgc_weight_gradient_scratch")
+    return n.value
+
+
 def weight_gradient(dy: torch.Tensor, x: Packed, dw: torch.Tensor, node_start: Optional[torch.Tensor] = None,
-                    stream: Optional[torch.cuda.Stream] = None) -> None:
+                    scratch: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
     """dw[k] = the sum over node k's rows of dy^T x ([dy's columns][x's columns], flat), from the bf16 gradient `dy` (rows
-    16-byte aligned) and the 8-bit checkpoint `x`.  `dw`: a [nodes][n] fp32 view (columns of the nodes' gradients)."""
+    16-byte aligned) and the 8-bit checkpoint `x`.  `dw`: a [nodes][n] fp32 view (columns of the nodes' gradients).
+    `scratch`: a uint8 tensor of weight_gradient_scratch bytes; without one it comes from PyTorch's allocator."""
     rows, cols, ld_dy, kind = _matrix(dy, "dy")
     if kind != TYPE_BF16:
         raise ValueError("dy: need a bf16 tensor")
     inner = x.cols
     xp = _packed(x, "x", rows, inner)
     start, K, stride = _nodes(node_start, dw, cols * inner, "dw")
-    _done(lgc.lib().lgc_weight_gradient(dy.data_ptr(), ld_dy, xp, rows, cols, inner, start, K, dw.data_ptr(), stride, _stream(stream, dy)),
-          "lgc_weight_gradient")
+    scratch, size = _scratch(weight_gradient_scratch(rows, cols, inner, K), scratch, stream, dy)
+    _done(lgc.lib().lgc_weight_gradient(dy.data_ptr(), ld_dy, xp, rows, cols, inner, start, K, dw.data_ptr(), stride, scratch.data_ptr(), size,
+                                        _stream(stream, dy)), "lgc_weight_gradient")
 
 
 def check(stream: Optional[torch.cuda.Stream] = None) -> None:

@@ -29,7 +29,7 @@ EXPORTS = (
     "lgc_check", "lgc_status_string", "lgc_last_error", "lgc_topk_noalloc", "lgc_topk_noalloc_check", "lgc_kernel_launches",
     "lgc_selection_stats",
     "lgc_pack", "lgc_unpack", "lgc_layer_norm", "lgc_layer_norm_backward_scratch", "lgc_layer_norm_backward", "lgc_product",
-    "lgc_weight_gradient", "lgc_layers_check",
+    "lgc_weight_gradient_scratch", "lgc_weight_gradient", "lgc_layers_check",
 )
 NOALLOC_MAX_N = 16777216
 
@@ -99,7 +99,8 @@ def lib() -> C.CDLL:
         l.lgc_layer_norm_backward_scratch.argtypes = [i64, i64, i32, C.POINTER(sz)]
         l.lgc_layer_norm_backward.argtypes = [vp, i32, i64, vp, i32, i64, pk, i64, i64, vp, vp, vp, vp, i32, vp, i64, vp, vp, i64, vp, sz, vp]
         l.lgc_product.argtypes = [pk, pk, i32, i64, i64, i64, f32, vp, i32, i64, pk, vp]
-        l.lgc_weight_gradient.argtypes = [vp, i64, pk, i64, i64, i64, vp, i32, vp, i64, vp]
+        l.lgc_weight_gradient_scratch.argtypes = [i64, i64, i64, i32, C.POINTER(sz)]
+        l.lgc_weight_gradient.argtypes = [vp, i64, pk, i64, i64, i64, vp, i32, vp, i64, vp, sz, vp]
         l.lgc_layers_check.argtypes = [vp]
         for name in EXPORTS:            # every declared entry point must be exported
             getattr(l, name)

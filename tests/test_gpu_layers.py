@@ -333,7 +333,7 @@ def test_product_of_extreme_scales_and_of_blocks_that_are_not_numbers():
 
 
 @pytest.mark.parametrize("rows,cols,inner,nodes", [(1, 1, 1, 1), (1, 130, 70, 3), (64, 128, 128, 1), (65, 128, 129, 3), (300, 257, 513, 5), (2500, 40, 200, 3),
-                                                   (1100, 300, 64, 5), (0, 30, 20, 3)])
+                                                   (1100, 300, 64, 5), (0, 30, 20, 3), (9000, 70, 300, 1), (6000, 513, 90, 3)])
 @pytest.mark.parametrize("stride_extra", [0, 5])
 def test_weight_gradient(rows, cols, inner, nodes, stride_extra):
     r = rng("weights", rows, cols, inner, nodes)
@@ -343,7 +343,8 @@ def test_weight_gradient(rows, cols, inner, nodes, stride_extra):
     start = np.minimum([rows if s is None else s for s in NODES[nodes]], rows)
     n = cols * inner
     grads = torch.full((nodes, n + stride_extra), 3.0, device="cuda")
-    layers.weight_gradient(dy, x, grads[:, :n], node_start=torch.from_numpy(start).cuda() if nodes > 1 else None)
+    scratch = torch.full((layers.weight_gradient_scratch(rows, cols, inner, nodes),), 0xff, dtype=torch.uint8, device="cuda")
+    layers.weight_gradient(dy, x, grads[:, :n], node_start=torch.from_numpy(start).cuda() if nodes > 1 else None, scratch=scratch)
     X, D = R.unpack(codes, scales) if rows else np.zeros((0, inner)), host(dy)
     for k in range(nodes):
         part = slice(start[k], start[k + 1])
@@ -467,6 +468,7 @@ def test_refusals():
         (lambda: layers.product(p, w), 1),
         (lambda: layers.pack(torch.zeros(4, 200, device="cuda"), layers.Packed(torch.zeros(4, 200, dtype=torch.uint8, device="cuda"), p.scales, 200)), 1),
         (lambda: layers.weight_gradient(torch.zeros(4, 257, dtype=torch.bfloat16, device="cuda"), p, torch.zeros(1, 257 * 256, device="cuda")), 1),
+        (lambda: layers.weight_gradient(f.bfloat16(), p, torch.zeros(1, 256 * 256, device="cuda"), scratch=torch.zeros(16, dtype=torch.uint8, device="cuda")), 3),
         (lambda: layers.layer_norm_backward(f, f, v256, v4, v4, f, torch.zeros(1, 256, device="cuda"), torch.zeros(1, 256, device="cuda"),
                                             scratch=torch.zeros(16, dtype=torch.uint8, device="cuda")), 3),
     ]

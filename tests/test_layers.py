@@ -83,8 +83,11 @@ def test_refused_on_the_host(lib):
     prod = lambda a=packed(), b=packed(), across=0, r=4, c=256, i=256, y=P, t=0: lib.lgc_product(a, b, across, r, c, i, 1.0, y, t, 256, None, None)  # noqa: E731
     assert prod(a=None) == INVALID and prod(b=None) == INVALID and prod(across=2) == INVALID and prod(i=0) == INVALID and prod(y=None) == INVALID
     assert prod(i=257) == INVALID and prod(t=9) == INVALID and prod(r=0) == OK
-    grad = lambda dy=P, ld=256, x=packed(), r=4, c=256, i=256, start=None, K=1, dw=P, stride=0: lib.lgc_weight_gradient(dy, ld, x, r, c, i, start, K, dw, stride, None)  # noqa: E731
+    grad = lambda dy=P, ld=256, x=packed(), r=4, c=256, i=256, start=None, K=1, dw=P, stride=0, scratch=P, size=1 << 40: lib.lgc_weight_gradient(dy, ld, x, r, c, i, start, K, dw, stride, scratch, size, None)  # noqa: E731
     assert grad(dy=P + 2) == INVALID and grad(ld=260) == INVALID and grad(x=None) == INVALID and grad(K=2) == INVALID
+    assert lib.lgc_weight_gradient_scratch(4, 256, 0, 1, C.byref(n)) == INVALID and lib.lgc_weight_gradient_scratch(4, 256, 256, 1, None) == INVALID
+    assert lib.lgc_weight_gradient_scratch(4, 256, 256, 1, C.byref(n)) == OK and n.value >= 4 * 256 * 2
+    assert grad(size=n.value - 1) == WORKSPACE and grad(scratch=None) == INVALID and grad(scratch=P + 8) == INVALID
     assert grad(start=P, K=2, stride=65535) == INVALID and grad(dw=None) == INVALID and grad(c=1 << 30, ld=1 << 30, i=2048, x=packed(ld=2048, ld_scales=16)) == INVALID
 
 
