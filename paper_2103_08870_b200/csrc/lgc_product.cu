@@ -182,8 +182,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     tc_fence_after();
     const uint32_t tmem = tmem_base;
 
-    if (warp == 0) {
-        const bool issuer = elect_one();
+    if (threadIdx.x == 0) {
         int s = 0;
         uint32_t phase = 1;                                       // the first pass over the stages waits for nobody
         bool ok = true;
@@ -191,15 +190,12 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             int m, n;
             tile_of(tile, p.tiles_m, p.tiles_n, m, n);
             for (int kb = 0; kb < blocks; ++kb) {
-                if (!bar_wait_together(smem_addr(&empty_bar[s]), phase, &failed)) { ok = false; break; }
+                if (!bar_wait(smem_addr(&empty_bar[s]), phase, &failed)) { ok = false; break; }
                 const uint32_t bar = smem_addr(&full_bar[s]), st = tiles + s * kStageBytes;
-                if (issuer) {
-                    bar_expect(bar, kStageBytes);
-                    tma_load(st, &map_a, bar, kb * kBlock, m * kM);
-                    if (ACROSS) tma_load(st + kM * kBlock, &map_b, bar, n * kN, kb * kBlock);
-                    else tma_load(st + kM * kBlock, &map_b, bar, kb * kBlock, n * kN);
-                }
-                __syncwarp();
+                bar_expect(bar, kStageBytes);
+                tma_load(st, &map_a, bar, kb * kBlock, m * kM);
+                if (ACROSS) tma_load(st + kM * kBlock, &map_b, bar, n * kN, kb * kBlock);
+                else tma_load(st + kM * kBlock, &map_b, bar, kb * kBlock, n * kN);
                 if (++s == kStages) s = 0, phase ^= 1;
             }
         }
@@ -388,8 +384,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     tc_fence_after();
     const uint32_t tmem = tmem_base;
 
-    if (warp == 0) {
-        const bool issuer = elect_one();
+    if (threadIdx.x == 0) {
         int s = 0;
         uint32_t phase = 1;                                       // the first pass over the stages waits for nobody
         bool ok = true;
@@ -398,15 +393,12 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
             tile_at(tile, p, m, n);
             const int arow = m * kTile + (int)rank * kHalf, brow = n * kTile + (int)rank * kHalf;
             for (int kb = 0; kb < blocks; ++kb) {
-                if (!bar_wait_together(smem_addr(&empty_bar[s]), phase, &failed)) { ok = false; break; }
+                if (!bar_wait(smem_addr(&empty_bar[s]), phase, &failed)) { ok = false; break; }
                 const uint32_t st = tiles + s * kStageBytes, bar0 = cluster_addr(smem_addr(&full_bar[s]), 0);
-                if (issuer) {
-                    if (rank == 0) bar_expect(smem_addr(&full_bar[s]), 2 * kStageBytes);
-                    tma_load_pair(st, &map_a, bar0, kb * kBlock, arow);
-                    if (ACROSS) tma_load_pair(st + kHalf * kBlock, &map_b, bar0, brow, kb * kBlock);
-                    else tma_load_pair(st + kHalf * kBlock, &map_b, bar0, kb * kBlock, brow);
-                }
-                __syncwarp();
+                if (rank == 0) bar_expect(smem_addr(&full_bar[s]), 2 * kStageBytes);
+                tma_load_pair(st, &map_a, bar0, kb * kBlock, arow);
+                if (ACROSS) tma_load_pair(st + kHalf * kBlock, &map_b, bar0, brow, kb * kBlock);
+                else tma_load_pair(st + kHalf * kBlock, &map_b, bar0, kb * kBlock, brow);
                 if (++s == kStages) s = 0, phase ^= 1;
             }
         }
