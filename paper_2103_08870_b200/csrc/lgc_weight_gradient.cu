@@ -243,10 +243,13 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_
 #pragma unroll 8
                             for (int j = 0; j < 32; ++j)
                                 if (row0 + j < rows) o[j * ld] = stage[j * kPitch + lane];
-                        } else {
-#pragma unroll 8
+                        } else {                                  // all of what is there first: a load behind a store would wait for it
+                            float old[32];
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) old[j] = row0 + j < rows ? o[j * ld] : 0.0f;
+#pragma unroll
                             for (int j = 0; j < 32; ++j)
-                                if (row0 + j < rows) o[j * ld] = __fadd_rn(o[j * ld], stage[j * kPitch + lane]);
+                                if (row0 + j < rows) o[j * ld] = __fadd_rn(old[j], stage[j * kPitch + lane]);
                         }
                     }
                 }

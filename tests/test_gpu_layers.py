@@ -275,7 +275,7 @@ def test_layer_norm_gradient_agrees_with_differences():
 # ---- products -----------------------------------------------------------------------------------------------------------
 
 PRODUCTS = [(1, 1, 1), (1, 4096, 512), (2, 130, 40), (7, 1000, 513), (128, 128, 128), (129, 129, 640), (300, 777, 1160), (33, 260, 2100),
-            (513, 384, 96), (17, 64, 4224), (1500, 1900, 200), (2304, 1024, 1100), (1025, 2560, 130), (2600, 2700, 520)]
+            (513, 384, 96), (17, 64, 4224), (1500, 1900, 200), (2304, 1024, 1100), (1025, 2560, 130), (2600, 2700, 520), (3, 384, 8192), (4, 129, 8193), (1, 2043, 1160)]
 
 
 @pytest.mark.parametrize("rows,cols,inner", PRODUCTS)
