@@ -10,9 +10,10 @@
 // Both operands lie along their rows (MN-major): 128 bytes of columns per row.  Two CTAs make a tile of 256 x 256 together
 // (cta_group::2); each loads half of both operands.  Rows of other nodes that a tile's last stage reaches are set to zero in
 // both operands, whatever they hold.
-// Sums: the tensor cores add in fp32 in tensor memory over at most 64 * 64 rows; longer sums are added up in memory from
-// there, so that they do not lose to the accumulator's rounding (it errs by about 2^-24 of the sum per 16 rows).  Where
-// there are few tiles a node's rows are cut into parts, whose sums a last kernel adds in order.
+// Sums: the tensor cores' additions round towards zero (after 4096 rows a sum is 1.8e-6 of its size too small, and the error
+// grows with the rows), so their accumulator takes only 8 * 64 rows at a time; eight warps add those sums up in registers
+// while the other accumulator fills.  Where there are few tiles a node's rows are cut into parts, whose sums a last kernel
+// adds in order.
 #include "lgc_layers.cuh"
 #include "lgc_tensor_core.cuh"
 
@@ -26,10 +27,10 @@ constexpr int kHalf = 128;
 constexpr int kABytes = kHalf * kRows * 2, kStageBytes = 2 * kABytes;
 constexpr int kPiece = 64 * kRows * 2;            // 64 columns (128 bytes) of a stage's rows
 constexpr int kStages = 6;
-constexpr int kFlushSteps = 64;                   // stages that the tensor cores add up before their sums go to memory
+constexpr int kFlushSteps = 8;                    // stages that the tensor cores add up before their sums go to registers
 constexpr int kPitch = 33;                        // floats per row of the result's staging blocks
-constexpr int kSmemBytes = kStages * kStageBytes + 4 * 32 * kPitch * 4 + 1024;
-constexpr int kThreads = 256;                     // warp 0: TMA, 1: MMA, 2: rows of other nodes, 3: tensor memory, 4..7: results
+constexpr int kSmemBytes = kStages * kStageBytes + 8 * 32 * kPitch * 4 + 1024;
+constexpr int kThreads = 384;                     // warp 0: TMA, 1: MMA, 2: rows of other nodes, 3: tensor memory, 4..11: results
 constexpr int kTmemCols = 2 * kN;
 
 __device__ __forceinline__ void mma_bf16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate)
@@ -102,7 +103,7 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_
         }
         for (int s = 0; s < 2; ++s) {
             bar_init(smem_addr(&tfull_bar[s]), 1);
-            bar_init(smem_addr(&tempty_bar[s]), 2 * 4);
+            bar_init(smem_addr(&tempty_bar[s]), 2 * 8);
         }
         bar_init_fence();
     }
@@ -201,62 +202,52 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_
             s = s + 1 == kStages ? 0 : s + 1;
         }
     } else if (warp >= 4) {
-        const int q = warp & 3;
-        float *stage = reinterpret_cast<float *>(dyn_smem + (base - smem_addr(dyn_smem)) + kStages * kStageBytes) + q * 32 * kPitch;
+        // a warp: 32 rows, half of the columns
+        const int q = warp & 3, half = (warp - 4) >> 2;
+        float *stage = reinterpret_cast<float *>(dyn_smem + (base - smem_addr(dyn_smem)) + kStages * kStageBytes) + (warp - 4) * 32 * kPitch;
+        const uint32_t drained[2] = {cluster_addr(smem_addr(&tempty_bar[0]), 0), cluster_addr(smem_addr(&tempty_bar[1]), 0)};
         int acc = 0;
         bool ok = true;
         for (int64_t t = first; t < total && ok; t += step) {
             const Tile w = tile_of(p, t);
-            const int row0 = (int)rank * kHalf + q * 32;          // inside the tile
+            float v[kHalf];                                       // (without rows: zeros)
+#pragma unroll
+            for (int c = 0; c < kHalf; ++c) v[c] = 0.0f;
+            for (int i = 0; i < w.steps; i += kFlushSteps, ++acc) {
+                const int buf = acc & 1;
+                if (!bar_wait_together(smem_addr(&tfull_bar[buf]), (acc >> 1) & 1, &failed)) { ok = false; break; }
+                tc_fence_after();
+                const uint32_t at = tmem + buf * kN + half * kHalf + ((uint32_t)(q * 32) << 16);
+#pragma unroll
+                for (int c = 0; c < kHalf; c += 16) {
+                    uint32_t r[16];
+                    tc_read16(at + c, r);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) v[c + j] = __fadd_rn(v[c + j], __uint_as_float(r[j]));
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive_cluster(drained[buf]);
+            }
+            if (!ok) break;
             // where the tile's entry (0, 0) goes, and how much of the tile is written
             float *out = p.parts > 1 ? p.partial + t * (kM * kN) : p.dw + w.node * p.node_stride + (int64_t)w.m * kM * p.inner + (int64_t)w.n * kN;
             const int64_t ld = p.parts > 1 ? kN : p.inner;
-            const int rows = p.parts > 1 ? kM : (int)min((int64_t)kM, p.cols - (int64_t)w.m * kM);
+            const int row0 = (int)rank * kHalf + q * 32;
+            const int rows = p.parts > 1 ? 32 : (int)min((int64_t)32, p.cols - (int64_t)w.m * kM - row0);
             const int cols = p.parts > 1 ? kN : (int)min((int64_t)kN, p.inner - (int64_t)w.n * kN);
-            // (without rows: zeros)
-            for (int i = 0; i == 0 || i < w.steps; i += kFlushSteps) {
-                const int buf = acc & 1;
-                if (w.steps > 0) {
-                    if (!bar_wait_together(smem_addr(&tfull_bar[buf]), (acc >> 1) & 1, &failed)) { ok = false; break; }
-                    tc_fence_after();
-                    ++acc;
-                }
-                const uint32_t at = tmem + buf * kN + ((uint32_t)(q * 32) << 16);
-#pragma unroll 1
-                for (int c = 0; c < kN; c += 32) {
-                    uint32_t v[32];
-                    if (w.steps > 0) {
-                        tc_read32(at + c, v);
-                        tc_read_wait(v);
-                    } else {
+            // 32 x 32 entries at a time through shared memory: a warp writes 32 neighbours of a row, wherever the row starts
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = 0;
-                    }
-                    // 32 x 32 entries through shared memory: a warp writes 32 neighbours of a row, wherever the row starts
-                    __syncwarp();
+            for (int c = 0; c < kHalf; c += 32) {
+                __syncwarp();
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) stage[lane * kPitch + j] = __uint_as_float(v[j]);
-                    __syncwarp();
-                    if (c + lane < cols) {
-                        float *o = out + row0 * ld + c + lane;
-                        if (i == 0) {
+                for (int j = 0; j < 32; ++j) stage[lane * kPitch + j] = v[c + j];
+                __syncwarp();
+                if (half * kHalf + c + lane < cols) {
+                    float *o = out + row0 * ld + half * kHalf + c + lane;
 #pragma unroll 8
-                            for (int j = 0; j < 32; ++j)
-                                if (row0 + j < rows) o[j * ld] = stage[j * kPitch + lane];
-                        } else {                                  // all of what is there first: a load behind a store would wait for it
-                            float old[32];
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) old[j] = row0 + j < rows ? o[j * ld] : 0.0f;
-#pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if (row0 + j < rows) o[j * ld] = __fadd_rn(old[j], stage[j * kPitch + lane]);
-                        }
-                    }
-                }
-                if (w.steps > 0) {
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) bar_arrive_cluster(cluster_addr(smem_addr(&tempty_bar[buf]), 0));
+                    for (int j = 0; j < 32; ++j, o += ld)
+                        if (j < rows) *o = stage[j * kPitch + lane];
                 }
             }
         }
