@@ -418,6 +418,7 @@ layer_norm_backward_ring_kernel(const T *__restrict__ dy, int64_t ld_dy, const X
     constexpr int kWarps = THREADS / 32, kMaxSlots = 8;
     __shared__ __align__(8) uint64_t full_bar[kMaxSlots];
     __shared__ float2 sums_of[2][kWarps];
+    __shared__ __align__(16) T stage[kWarps][256];
     __shared__ volatile int failed;
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
     grid_release_dependents();                                   // the kernel that adds up the chunks waits for this one's end
@@ -528,8 +529,19 @@ layer_norm_backward_ring_kernel(const T *__restrict__ dy, int64_t ld_dy, const X
                 for (int j = 0; j < 4; ++j) d[i][j] = f2_mul(rr, f2_fma(h[i][j], f2_of(m2, m2), f2_add(d[i][j], f2_of(m1, m1))));
                 const float w[8] = {f2_lo(d[i][0]), f2_hi(d[i][0]), f2_lo(d[i][1]), f2_hi(d[i][1]),
                                     f2_lo(d[i][2]), f2_hi(d[i][2]), f2_lo(d[i][3]), f2_hi(d[i][3])};
-                if (dx_vec) store8<T, true>(to, c, (i + 1) * THREADS * 8 <= cols ? c + 8 : cols, w);
-                else store8<T, false>(to, c, cols, w);
+                if (dx_vec) {
+                    store8<T, true>(to, c, (i + 1) * THREADS * 8 <= cols ? c + 8 : cols, w);
+                } else {                                          // rows that start anywhere: neighbouring lanes write neighbours
+                    __syncwarp();
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) stage[warp][lane * 8 + j] = (T)w[j];
+                    __syncwarp();
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int at = (i * THREADS + warp * 32) * 8 + j * 32 + lane;
+                        if (at < cols) to[at] = stage[warp][j * 32 + lane];
+                    }
+                }
             }
         }
         float *out = partial + (int64_t)blockIdx.x * 2 * cols;
@@ -714,11 +726,11 @@ cudaError_t backward_ring(const BackwardArgs &a)
     const int64_t cols = a.cols;
     const int slot = (int)((cols * sizeof(T) + 15) / 16 * 16 + (cols * sizeof(XT) + 15) / 16 * 16 +
                            (8 + (sizeof(XT) == 1 ? (cols + 511) / 512 * 4 : 0) + 15) / 16 * 16);
-    constexpr int kMost = 200 * 1024;
-    // three CTAs per SM if three slots each leave room for that, else as many slots as one CTA can have
-    int slots = 70 * 1024 / slot;
-    if (slots < 3) slots = 105 * 1024 / slot;
-    if (slots < 3) slots = kMost / slot;
+    constexpr int kMost = 192 * 1024;
+    // as many slots as leave room for the CTAs that the registers allow (narrow rows: more CTAs count for more than more slots)
+    constexpr int kCtas = (NV == 1 ? 1024 : 512) / THREADS;
+    int slots = kMost / kCtas / slot;
+    if (slots < 2) slots = kMost / slot;
     slots = slots > 8 ? 8 : slots < 2 ? 2 : slots;
     static OncePerDevice configured;
     const cudaError_t e = configured.run([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost); });
