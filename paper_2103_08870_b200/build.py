@@ -14,6 +14,7 @@ LIB = os.path.join(HERE, "liblgc.so")
 NVCC_FLAGS = [
     "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
     "-fmad=false",            # every fused multiply-add in the kernels is written explicitly
+    "-t", str(os.cpu_count() or 1),     # the files side by side
     "-Xcompiler", "-fPIC", "-shared", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
 ]
 
