@@ -43,20 +43,19 @@ __device__ __forceinline__ void row_sums(float (&v)[COUNT], float *shared)
     }
 }
 
-// Few rows, wide rows, rows that start anywhere: TPR threads share a row, NV vectors of eight entries each.  Lanes hold
-// neighbouring vectors, so that 16 lanes hold a block of the 8-bit form.
+// Few rows (less than four per SM), wide rows, rows that start anywhere: a CTA of TPR threads per row, NV vectors of eight
+// entries each.  Lanes hold neighbouring vectors, so that 16 lanes hold a block of the 8-bit form.  One row of 4096: 8 us
+// from cold caches.
 template <typename T, bool VEC, int TPR, int NV>
-__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR)
-layer_norm_kernel(const T *__restrict__ x, int64_t ldx, int64_t rows, int cols, const float *__restrict__ gamma,
+__global__ void __launch_bounds__(TPR)
+layer_norm_kernel(const T *__restrict__ x, int64_t ldx, int cols, const float *__restrict__ gamma,
                   const float *__restrict__ beta, float eps, T *__restrict__ y, int64_t ldy, bool y_vec, uint8_t *__restrict__ codes,
                   int64_t ld_codes, uint8_t *__restrict__ scales, int64_t ld_scales, float *__restrict__ mean_out,
                   float *__restrict__ rstd_out, bool gb_vec)
 {
     __shared__ float shared[2][TPR / 32];
-    constexpr int kRows = TPR < 128 ? 128 / TPR : 1;
-    const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
-    const int t = threadIdx.x % TPR;
-    if (row >= rows) return;                                    // a whole warp (TPR = 32): no barrier follows
+    const int64_t row = blockIdx.x;
+    const int t = threadIdx.x;
     const T *xr = x + row * ldx;
     float v[NV][8];
 #pragma unroll
@@ -137,7 +136,9 @@ __device__ __forceinline__ void keep_raw(Raw16<T> (&raw)[UNITS])
 
 // Many rows: WPR warps per row, walking from row to row.  The row stays as it was loaded (bf16: half the registers of fp32
 // numbers), UNITS times 16 neighbouring entries per lane; gamma and beta lie in shared memory in the order in which lanes
-// read them, one 16-byte piece per lane without bank conflicts.
+// read them, one 16-byte piece per lane without bank conflicts.  16384 x 4096 bf16 to 8 bits: 58 us, 3.5 TB/s; the issue
+// rate bounds it (17 instructions an entry), so four warps a row (32 per SM) beat one warp a row (76 us), and the next
+// row's loads, ahead in registers or in shared memory, gained nothing (61 and 73 us).
 constexpr int kRowThreads = 256;
 
 // A sum over the WPR warps of a row; the groups of a CTA have a named barrier each.
@@ -321,7 +322,7 @@ __device__ __forceinline__ void slot8(const T *row, int c, int cols, bool whole,
 }
 
 // x may be the 8-bit checkpoint (XT = uint8_t).
-template <typename XT, bool VEC>
+template <typename XT>
 __device__ __forceinline__ void load_x8(const XT *x, int64_t ldx, const uint8_t *scales, int64_t ld_scales, int64_t row, int64_t c,
                                         int64_t cols, float (&v)[8])
 {
@@ -337,12 +338,12 @@ __device__ __forceinline__ void load_x8(const XT *x, int64_t ldx, const uint8_t 
             v[4 + j] = __fmul_rn(b[j], f);
         }
     } else {
-        load8<XT, VEC>(x + row * ldx, c, cols, v);
+        load8<XT, false>(x + row * ldx, c, cols, v);
     }
 }
 
 // partial: [chunks][2][cols], the weight's then the bias's gradient over the chunk's rows.
-template <typename T, typename XT, bool VEC, int TPR, int NV>
+template <typename T, typename XT, int TPR, int NV>
 __global__ void __launch_bounds__(TPR)
 layer_norm_backward_kernel(const T *__restrict__ dy, int64_t ld_dy, const XT *__restrict__ x, int64_t ldx,
                            const uint8_t *__restrict__ x_scales, int64_t ld_scales, int64_t rows, int64_t cols,
@@ -369,8 +370,8 @@ layer_norm_backward_kernel(const T *__restrict__ dy, int64_t ld_dy, const XT *__
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int64_t c = (int64_t)(i * TPR + t) * 8;
-            load8<T, VEC>(dy + row * ld_dy, c, cols, d[i]);
-            load_x8<XT, VEC>(x, ldx, x_scales, ld_scales, row, c, cols, h[i]);
+            load8<T, false>(dy + row * ld_dy, c, cols, d[i]);
+            load_x8<XT>(x, ldx, x_scales, ld_scales, row, c, cols, h[i]);
         }
 #pragma unroll
         for (int i = 0; i < NV; ++i)
@@ -390,7 +391,7 @@ layer_norm_backward_kernel(const T *__restrict__ dy, int64_t ld_dy, const XT *__
         for (int i = 0; i < NV; ++i) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) d[i][j] = __fmul_rn(rs, __fsub_rn(__fsub_rn(d[i][j], m1), __fmul_rn(h[i][j], m2)));
-            store8<T, VEC>(dx + row * ld_dx, (int64_t)(i * TPR + t) * 8, cols, d[i]);
+            store8<T, false>(dx + row * ld_dx, (int64_t)(i * TPR + t) * 8, cols, d[i]);
         }
     }
     float *out = partial + (int64_t)blockIdx.x * 2 * cols;
@@ -403,7 +404,7 @@ layer_norm_backward_kernel(const T *__restrict__ dy, int64_t ld_dy, const XT *__
 
 // The same for rows that start on 16-byte boundaries: whole rows of dy and x (and the 8-bit form's scales) come into a ring
 // of shared-memory slots by bulk copies, so that the loads of the rows to come are always under way, whatever the registers
-// hold.  The barrier in the middle of a row's work says that every warp has read its slot, which a warp (another one each
+// hold (16384 x 4096 bf16, x in 8 bits: 98 us against 196 with plain loads).  The barrier in the middle of a row's work says that every warp has read its slot, which a warp (another one each
 // row) then gives to a row to come.  A thread owns NV vectors of 8 neighbouring columns.  A row's last bytes that do not
 // fill 16 come in words of four (the last word may reach past the row's end; what it brings from there is not used).
 template <typename T, typename XT, int THREADS, int NV>
@@ -554,6 +555,7 @@ layer_norm_backward_ring_kernel(const T *__restrict__ dy, int64_t ld_dy, const X
                 if (c + 2 * j + 1 < cols) out[c + 2 * j + 1] = f2_hi(dg[i][j]), out[cols + c + 2 * j + 1] = f2_hi(db[i][j]);
             }
         }
+        let_copies_land(&failed);
         if (t == 0 && failed) atomicExch(errword, 3);
     }
 }
@@ -639,7 +641,7 @@ void forward_shared_rows(const ForwardArgs &a)
 {
     const bool y_vec = matrix_rows_aligned(a.y, a.ldy, sizeof(T)), gb_vec = matrix_rows_aligned(a.gamma, 4, 4) && matrix_rows_aligned(a.beta, 4, 4);
     auto launch = [&](auto kern, int64_t ctas, int threads) {
-        kern<<<(unsigned)ctas, threads, 0, a.s>>>(static_cast<const T *>(a.x.p), a.x.ld, a.rows, (int)a.cols, a.gamma, a.beta, a.eps,
+        kern<<<(unsigned)ctas, threads, 0, a.s>>>(static_cast<const T *>(a.x.p), a.x.ld, (int)a.cols, a.gamma, a.beta, a.eps,
                                                   static_cast<T *>(a.y), a.ldy, y_vec, a.p ? a.p->codes : nullptr, a.p ? a.p->ld : 0,
                                                   a.p ? a.p->scales : nullptr, a.p ? a.p->ld_scales : 0, a.mean, a.rstd, gb_vec);
     };
@@ -714,9 +716,9 @@ void backward_any(const BackwardArgs &a)
                                                   a.xp ? a.xp->scales : nullptr, a.xp ? a.xp->ld_scales : 0, a.rows, a.cols, a.gamma, a.mean,
                                                   a.rstd, a.node_start, a.nodes, chunk, static_cast<T *>(a.dx), a.ld_dx, a.partial);
     };
-    if (a.cols <= 2048) launch(layer_norm_backward_kernel<T, XT, false, 128, 2>, 128);
-    else if (a.cols <= 8192) launch(layer_norm_backward_kernel<T, XT, false, 512, 2>, 512);
-    else launch(layer_norm_backward_kernel<T, XT, false, 1024, 2>, 1024);
+    if (a.cols <= 2048) launch(layer_norm_backward_kernel<T, XT, 128, 2>, 128);
+    else if (a.cols <= 8192) launch(layer_norm_backward_kernel<T, XT, 512, 2>, 512);
+    else launch(layer_norm_backward_kernel<T, XT, 1024, 2>, 1024);
 }
 
 template <typename T, typename XT, int THREADS, int NV>

@@ -1,7 +1,7 @@
 // 8-bit checkpoints: matrices to e4m3 codes with a power of two per block of 128 (or 128 x 128) entries, and back.
 //
 // Both directions only stream: an entry is read once and written once, with an exponent comparison and a conversion in
-// between, so DRAM bounds them.
+// between, so DRAM bounds them: 16384 x 8192 bf16 66 and 65 us (6.1 and 6.2 TB/s), the gated form 120 us (6.7 TB/s).
 #include <type_traits>
 
 #include "lgc_layers.cuh"

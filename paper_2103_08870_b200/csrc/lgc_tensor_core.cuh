@@ -45,7 +45,15 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
     *failed = 1;
     return false;
 }
-// The same for a whole warp that stays together: every lane polls, and the result is the same for all.  The warps that
+// After a wait that ran out: copies of this CTA may still be on their way into its shared memory.  Gives them a millisecond
+// (a copy takes microseconds) before the CTA ends.
+__device__ __forceinline__ void let_copies_land(volatile int *failed)
+{
+    if (!*failed) return;
+    for (const long long begin = clock64(); clock64() - begin < kWaitCycles / 1000;) {}
+}
+
+// bar_wait for a whole warp that stays together: every lane polls, and the result is the same for all.  The warps that
 // issue tensor-core work run this way: their descriptors and addresses then are uniform values, which the instructions
 // want; from a branch that one thread takes alone each of them costs a move (0.2 us per stage of four MMAs).
 __device__ __forceinline__ bool bar_wait_together(uint32_t bar, uint32_t parity, volatile int *failed)

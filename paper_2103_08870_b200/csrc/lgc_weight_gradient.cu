@@ -252,6 +252,7 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_
             }
         }
     }
+    let_copies_land(&failed);
     tc_fence_before();
     __syncthreads();
     cluster_sync();                       // the other CTA's MMAs read this one's shared memory
