@@ -203,7 +203,7 @@ layer_norm_rows_kernel(const T *__restrict__ x, int64_t ldx, int64_t rows, int c
         part[0] = part[1] = part[2] = part[3] = 0;
 #pragma unroll
         for (int u = 0; u < UNITS; ++u) {
-            if ((u + 1) * kWide <= cols) {                        // (the same for every thread)
+            if (u * kWide + ((t | 31) + 1) * 16 <= cols) {        // (the same for a warp)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const f2 d = f2_add(raw_pair(raw[u], i), minus);
@@ -230,7 +230,7 @@ layer_norm_rows_kernel(const T *__restrict__ x, int64_t ldx, int64_t rows, int c
         for (int u = 0; u < UNITS; ++u) {
             const int c = u * kWide + t * 16;
             if (u * kWide + (t & ~31) * 16 >= cols) break;        // the whole warp is past the row's end
-            const bool full = (u + 1) * kWide <= cols;
+            const bool full = u * kWide + ((t | 31) + 1) * 16 <= cols;
             f2 v[8];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
@@ -483,7 +483,7 @@ layer_norm_backward_ring_kernel(const T *__restrict__ dy, int64_t ld_dy, const X
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int c = (i * THREADS + t) * 8;
-                const bool whole = (i + 1) * THREADS * 8 <= cols;    // (the same for every thread)
+                const bool whole = (i * THREADS + (t | 31) + 1) * 8 <= cols;    // (the same for a warp)
                 slot8(reinterpret_cast<const T *>(slot), c, cols, whole, d[i]);
                 slot8(reinterpret_cast<const XT *>(slot + x_at), c, cols, whole, h[i]);
                 if (sizeof(XT) == 1) {
@@ -531,7 +531,7 @@ layer_norm_backward_ring_kernel(const T *__restrict__ dy, int64_t ld_dy, const X
                 const float w[8] = {f2_lo(d[i][0]), f2_hi(d[i][0]), f2_lo(d[i][1]), f2_hi(d[i][1]),
                                     f2_lo(d[i][2]), f2_hi(d[i][2]), f2_lo(d[i][3]), f2_hi(d[i][3])};
                 if (dx_vec) {
-                    store8<T, true>(to, c, (i + 1) * THREADS * 8 <= cols ? c + 8 : cols, w);
+                    store8<T, true>(to, c, (i * THREADS + (t | 31) + 1) * 8 <= cols ? c + 8 : cols, w);
                 } else {                                          // rows that start anywhere: neighbouring lanes write neighbours
                     __syncwarp();
 #pragma unroll

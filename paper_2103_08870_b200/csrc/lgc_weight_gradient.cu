@@ -260,27 +260,32 @@ weight_gradient_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_
     if (warp == 3) tc_free_pair(tmem, kTmemCols);
 }
 
-// The parts of every tile, added in order.  A CTA: 16 rows of a tile.
+// The parts of every tile, added in order.  A CTA: four rows of a tile; the loads of four parts are under way together.
+constexpr int kSumRows = 4;
 __global__ void __launch_bounds__(256)
 weight_gradient_sum_kernel(const __grid_constant__ WeightArgs p)
 {
     grid_wait();
-    const int64_t per = (int64_t)p.tiles_m * p.tiles_n, all = per * p.nodes, t = blockIdx.x;
+    const int64_t per = (int64_t)p.tiles_m * p.tiles_n, step = per * p.nodes * (kM * kN), t = blockIdx.x;
     const int node = (int)(t / per), r = (int)(t - node * per);
-    const int64_t row0 = (int64_t)(r % p.tiles_m) * kM + blockIdx.y * 16, col = (int64_t)(r / p.tiles_m) * kN + threadIdx.x;
-    if (col >= p.inner) return;
-    const float *from = p.partial + t * (kM * kN) + blockIdx.y * 16 * kN + threadIdx.x;
-    float sum[16];
+    const int64_t row0 = (int64_t)(r % p.tiles_m) * kM + blockIdx.y * kSumRows, col = (int64_t)(r / p.tiles_m) * kN + threadIdx.x;
+    if (col >= p.inner || row0 >= p.cols) return;
+    const float *from = p.partial + t * (kM * kN) + blockIdx.y * kSumRows * kN + threadIdx.x;
+    float sum[kSumRows] = {};
+    for (int part = 0; part < p.parts; part += 4, from += 4 * step) {
+        float v[4][kSumRows];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) sum[j] = __ldcg(from + j * kN);
-    for (int part = 1; part < p.parts; ++part) {
-        from += all * (kM * kN);
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) sum[j] = __fadd_rn(sum[j], __ldcg(from + j * kN));
+            for (int j = 0; j < kSumRows; ++j) v[i][j] = part + i < p.parts ? __ldcg(from + i * step + j * kN) : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < kSumRows; ++j) sum[j] = __fadd_rn(sum[j], v[i][j]);
     }
     float *out = p.dw + node * p.node_stride + row0 * p.inner + col;
 #pragma unroll
-    for (int j = 0; j < 16; ++j)
+    for (int j = 0; j < kSumRows; ++j)
         if (row0 + j < p.cols) out[j * p.inner] = sum[j];
 }
 
@@ -327,7 +332,7 @@ cudaError_t launch_weight_gradient(const void *dy, int64_t ld_dy, const lgc_pack
     if (e != cudaSuccess) return e;
     ++g_kernel_launches;
     if (p.parts > 1) {
-        e = launch_dependent(weight_gradient_sum_kernel, dim3((unsigned)tiles, kM / 16), dim3(256), s, p);
+        e = launch_dependent(weight_gradient_sum_kernel, dim3((unsigned)tiles, kM / kSumRows), dim3(256), s, p);
         if (e != cudaSuccess) return e;
         ++g_kernel_launches;
     }
