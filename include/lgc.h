@@ -358,7 +358,8 @@ lgc_status lgc_layer_norm_backward(const void *dy, int32_t dy_type, int64_t ld_d
  *     across = 0:  Y[t][n] = act(sum_i A[t][i] B[n][i])     (a linear layer: A activations, B weights)
  *     across = 1:  Y[t][n] = act(sum_i A[t][i] B[i][n])     (the gradient at its input: the same weights, A the
  *                                                            gradient at its output)
- * for t < num_rows, n < num_cols, i < inner.  A has block_rows = 1, B block_rows = 128.
+ * for t < num_rows, n < num_cols, i < inner.  A has block_rows = 1, B block_rows = 128.  The tensor cores add up at most 2048
+ * terms of a sum (their additions round towards zero), the rest is fp32 additions to nearest in a fixed order.
  * act is the leaky ReLU with `slope` (1 = none).  y: NULL, or fp32 / bf16 (type); packed: NULL, or Y in 8 bits
  * (block_rows = 1), rounded from the fp32 sums.  At least one of the two. */
 lgc_status lgc_product(const lgc_packed *a, const lgc_packed *b, int32_t across, int64_t num_rows, int64_t num_cols,
@@ -368,8 +369,9 @@ lgc_status lgc_product(const lgc_packed *a, const lgc_packed *b, int32_t across,
  *     dW_k[n][i] = sum over node k's rows t of dY[t][n] X[t][i],    fp32, n < num_cols, i < inner,
  * written back to back (num_cols * inner floats, node k's k * node_stride floats after node 0's).
  * dy: bf16, 16-byte aligned, ld_dy a multiple of 8.  x: block_rows = 1.  The products are exact in the tensor
- * cores' bf16 form (a code times its scale is a bf16 number), the sums fp32 in a fixed order.  Rows outside a node's
- * run have no influence on its gradient, whatever they hold.
+ * cores' bf16 form (a code times its scale is a bf16 number), the sums fp32 in a fixed order: the tensor cores add up at most
+ * 512 rows (their additions round towards zero), the rest is additions to nearest.  Rows outside a node's run have no
+ * influence on its gradient, whatever they hold.
  * scratch: lgc_weight_gradient_scratch bytes, 16-byte aligned (X in bf16; partial sums where there are few tiles). */
 lgc_status lgc_weight_gradient_scratch(int64_t num_rows, int64_t num_cols, int64_t inner, int32_t num_nodes, size_t *bytes);
 lgc_status lgc_weight_gradient(const void *dy, int64_t ld_dy, const lgc_packed *x, int64_t num_rows, int64_t num_cols,

@@ -390,6 +390,54 @@ def test_weight_gradient_of_every_code_and_scale():
     assert (np.abs(host(grads) - want)[~big] <= np.abs(want)[~big]).all()
 
 
+# ---- long sums ----------------------------------------------------------------------------------------------------------
+
+# The tensor cores' additions round towards zero: a step (32 terms of the product, 16 of the weight gradient) loses less than a
+# unit in the last place of the sum so far, 2^-23 of it.  Terms of one sign and one distribution: after step j of n the sum is
+# j / n of the segment's, so a segment loses less than (n + 1) / 2 * 2^-23 of itself (and a tenth for the terms' scatter), in
+# the mean half of that; every addition of a segment in fp32 registers, to nearest, 2^-24 of the sum.
+def one_sign_bounds(steps, segments):
+    lost = 1.1 * (steps + 1) / 2 * 2.0 ** -23
+    return lost + segments * U32, lost / 2 + segments * U32
+
+
+@pytest.mark.parametrize("rows,cols,inner", [(1, 384, 16384), (130, 200, 8192), (130, 200, 16384), (1300, 2000, 16384)])
+@pytest.mark.parametrize("across", [False, True])
+def test_product_of_long_sums_of_one_sign(rows, cols, inner, across):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(inner + rows)
+    a, b = layers.packed_empty(rows, inner), layers.packed_empty(*((inner, cols) if across else (cols, inner)), 128)
+    layers.pack(torch.rand(rows, inner, generator=g, device="cuda"), a)
+    layers.pack(torch.rand(b.rows, b.cols, generator=g, device="cuda"), b)
+    A, B = (torch.empty(p.rows, p.cols, device="cuda") for p in (a, b))
+    layers.unpack(a, A)
+    layers.unpack(b, B)
+    want = A.double() @ (B.double() if across else B.double().t())
+    y = torch.empty(rows, cols, device="cuda")
+    layers.product(a, b, y=y, across=across)
+    lost = (want - y.double()) / want
+    most, mean = one_sign_bounds(2048 // 32, inner / 2048)          # at most 2048 terms are added up in tensor memory
+    assert lost.abs().max() <= most and lost.mean().abs() <= mean
+    layers.check()
+
+
+@pytest.mark.parametrize("rows,cols,inner", [(16384, 128, 264), (16384, 1032, 1032)])
+def test_weight_gradient_of_long_sums_of_one_sign(rows, cols, inner):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(cols)
+    dy, x = torch.rand(rows, cols, generator=g, device="cuda").bfloat16(), layers.packed_empty(rows, inner)
+    layers.pack(torch.rand(rows, inner, generator=g, device="cuda"), x)
+    X = torch.empty(rows, inner, device="cuda")
+    layers.unpack(x, X)
+    want = dy.double().t() @ X.double()
+    dw = torch.empty(1, cols * inner, device="cuda")
+    layers.weight_gradient(dy, x, dw)
+    lost = (want - dw.view(cols, inner).double()) / want
+    most, mean = one_sign_bounds(512 // 16, rows / 512)             # at most 512 rows are added up in tensor memory
+    assert lost.abs().max() <= most and lost.mean().abs() <= mean
+    layers.check()
+
+
 # ---- streams, refusals ---------------------------------------------------------------------------------------------------
 
 def test_calls_run_on_the_stream_they_are_given():
