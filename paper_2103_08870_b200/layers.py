@@ -14,10 +14,13 @@ Gradients of weights come out per node, in views of the ``[K][N]`` gradients tha
     layers.weight_gradient(dz, h8, grads[:, at:at + n], node_start=starts)   # dW of every node into its row
     layers.layer_norm_backward(dh, x, gamma, mean, rstd, dx, grads[:, g0:g1], grads[:, b0:b1], node_start=starts)
 
-Outputs are the caller's tensors; a call enqueues on ``stream`` (default: the current stream) and returns.
+Outputs are the caller's tensors; a call enqueues on ``stream`` (default: the current stream) and returns.  With a ``stream``
+of the caller's, the order against other streams and the tensors' lifetime until the stream is done (``record_stream``) are
+the caller's too; scratch that a call allocates belongs to that stream.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 from typing import Optional, Union
 
@@ -162,10 +165,9 @@ def layer_norm_backward_scratch(rows: int, cols: int, num_nodes: int = 1) -> int
 def _scratch(need: int, scratch: Optional[torch.Tensor], stream: Optional[torch.cuda.Stream], like: torch.Tensor):
     """(tensor, bytes) of a call's scratch: the caller's, or from PyTorch's allocator."""
     if scratch is None:
-        scratch = torch.empty(need, dtype=torch.uint8, device=like.device)
-        if stream is not None:
-            scratch.record_stream(stream)
-        return scratch, need
+        # of the pool of the stream that uses it: in another pool's block earlier work of that pool's stream may be under way
+        with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+            return torch.empty(need, dtype=torch.uint8, device=like.device), need
     if not (scratch.is_cuda and scratch.dtype is torch.uint8 and scratch.is_contiguous()):
         raise ValueError("scratch: need a contiguous uint8 CUDA tensor")
     return scratch, scratch.numel()

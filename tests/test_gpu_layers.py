@@ -472,6 +472,42 @@ def test_calls_run_on_the_stream_they_are_given():
         assert torch.equal(a, b)
 
 
+def test_scratch_of_calls_on_two_streams_at_a_time():
+    """Without a scratch of the caller's: two calls of one size, on streams that do not wait for each other."""
+    r = rng("two streams")
+    rows, cols, inner = 8192, 512, 1024
+    side = torch.cuda.Stream()
+    dy = [dev(r.randn(rows, cols), torch.bfloat16) for _ in range(2)]
+    x = [layers.packed_empty(rows, inner) for _ in range(2)]
+    for p in x:
+        layers.pack(dev(r.randn(rows, inner)), p)
+    h = [dev(r.randn(rows, cols)) for _ in range(2)]
+    gamma, mean, rstd = torch.ones(cols, device="cuda"), torch.zeros(rows, device="cuda"), torch.ones(rows, device="cuda")
+
+    def run(i, stream=None):
+        layers.weight_gradient(dy[i], x[i], dw[i], stream=stream)
+        layers.layer_norm_backward(dy[i], h[i], gamma, mean, rstd, dx[i], dgb[i][:, :cols], dgb[i][:, cols:], stream=stream)
+
+    def outputs():
+        return ([torch.zeros(1, cols * inner, device="cuda") for _ in range(2)], [torch.zeros_like(d) for d in dy],
+                [torch.zeros(1, 2 * cols, device="cuda") for _ in range(2)])
+
+    dw, dx, dgb = want = outputs()
+    for i in range(2):
+        run(i)
+        torch.cuda.synchronize()
+    for _ in range(20):
+        dw, dx, dgb = got = outputs()
+        torch.cuda.synchronize()
+        run(0)
+        run(1, side)
+        run(0)
+        torch.cuda.synchronize()
+        for a, b in zip(want, got):
+            assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    layers.check()
+
+
 def test_no_rows():
     gamma = torch.ones(40, device="cuda")
     x, empty = torch.empty(0, 40, device="cuda"), torch.empty(0, device="cuda")

@@ -1,5 +1,6 @@
 """Layer operators without a GPU: the plain 64-bit forms that the kernels are tested against, and what the library
 refuses on the host before it enqueues anything."""
+import contextlib
 import ctypes as C
 
 import numpy as np
@@ -95,3 +96,58 @@ def test_binding_refuses_host_tensors():
     from paper_2103_08870_b200 import layers
     with pytest.raises(ValueError):
         layers.Packed(torch.zeros(4, 256, dtype=torch.uint8), torch.zeros(4, 4, dtype=torch.uint8))
+
+
+class Stub:
+    """What the binding asks of a CUDA tensor; there is no memory behind it."""
+
+    is_cuda = True
+
+    def __init__(self, *shape, dtype=torch.float32, device=0, ptr=4096):
+        self.shape, self.dtype, self.device_index, self.ptr = shape, dtype, device, ptr
+        self.device = torch.device("cuda", device)
+
+    def get_device(self):
+        return self.device_index
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        return int(np.prod(self.shape))
+
+    def stride(self, axis=None):
+        s = tuple(int(np.prod(self.shape[i + 1:])) for i in range(len(self.shape)))
+        return s if axis is None else s[axis]
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return self.ptr
+
+
+def test_scratch_is_allocated_on_the_stream_that_uses_it(monkeypatch):
+    """The allocator hands out a block whose last user may still be queued on the stream that the block is allocated on."""
+    from paper_2103_08870_b200 import layers
+    current, at = ["current"], []
+
+    @contextlib.contextmanager
+    def on(stream):
+        current.append(stream)
+        yield
+        current.pop()
+
+    class Block(Stub):
+        def record_stream(self, stream):
+            pass
+
+    def empty(n, **kw):
+        at.append(current[-1])
+        return Block(n, dtype=torch.uint8)
+
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch, "empty", empty)
+    assert layers._scratch(64, None, None, Stub(4, 8))[1] == 64
+    assert layers._scratch(64, None, "side", Stub(4, 8))[1] == 64
+    assert at == ["current", "side"]
