@@ -29,6 +29,7 @@ class ResidualBlock:
         if width % 8 or hidden % 8:
             raise ValueError("width and hidden: multiples of 8 (rows of the activations start 16-byte aligned)")
         dev = torch.device(device if device is not None else "cuda:0")
+        torch.cuda.set_device(dev)                                        # (the calls run on the current device)
         self.rows, self.width, self.hidden, self.K = rows, width, hidden, num_nodes
         self.numel = [width, width, hidden * width, width * hidden]       # the layer table of the compression context
         at = [0]

@@ -16,7 +16,8 @@ Gradients of weights come out per node, in views of the ``[K][N]`` gradients tha
 
 Outputs are the caller's tensors; a call enqueues on ``stream`` (default: the current stream) and returns.  With a ``stream``
 of the caller's, the order against other streams and the tensors' lifetime until the stream is done (``record_stream``) are
-the caller's too; scratch that a call allocates belongs to that stream.
+the caller's too; scratch that a call allocates belongs to that stream.  A call runs on the current device and refuses
+operands and streams of another one.
 """
 from __future__ import annotations
 
@@ -38,11 +39,11 @@ class Packed:
     """An 8-bit matrix: e4m3 `codes` (uint8 [rows][ld], unit column stride, 16-byte aligned rows) and the blocks' scale
     bytes (uint8 [ceil(rows / block_rows)][..]); `cols` of the codes' columns belong to it."""
 
-    __slots__ = ("codes", "scales", "rows", "cols", "block_rows", "_c")
+    __slots__ = ("codes", "scales", "rows", "cols", "block_rows", "device_index", "_c")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, cols: Optional[int] = None, block_rows: int = 1):
-        if not (codes.is_cuda and scales.is_cuda and codes.dtype is torch.uint8 and scales.dtype is torch.uint8):
-            raise ValueError("codes and scales: need 2-D uint8 CUDA tensors")
+        if not (codes.is_cuda and scales.get_device() == codes.get_device() and codes.dtype is torch.uint8 and scales.dtype is torch.uint8):
+            raise ValueError("codes and scales: need 2-D uint8 CUDA tensors of one device")
         shape, tall, ld, lds = codes.shape, scales.shape, codes.stride(), scales.stride()
         if len(shape) != 2 or len(tall) != 2:
             raise ValueError("codes and scales: need 2-D uint8 CUDA tensors")
@@ -54,6 +55,7 @@ class Packed:
         if not (0 < cols <= width and ld[1] == 1 and lds[1] == 1 and tall[0] == -(-rows // block_rows) and tall[1] * BLOCK >= cols):
             raise ValueError("codes need unit column stride and `cols` columns, scales a row per row of blocks and a byte per block")
         self.codes, self.scales, self.rows, self.cols, self.block_rows = codes, scales, rows, cols, block_rows
+        self.device_index = codes.get_device()
         # (the row stride of a tensor with one row may be anything)
         self._c = lgc.lgc_packed(codes.data_ptr(), ld[0] if rows > 1 else -(-width // 16) * 16,
                                  scales.data_ptr(), lds[0] if tall[0] > 1 else -(-tall[1] // 4) * 4)
@@ -66,50 +68,64 @@ def packed_empty(rows: int, cols: int, block_rows: int = 1, device: Optional[tor
                   torch.empty(-(-rows // block_rows), -(-cols // (4 * BLOCK)) * 4, dtype=torch.uint8, device=dev), cols, block_rows)
 
 
-def _stream(stream: Optional[torch.cuda.Stream], t: torch.Tensor) -> int:
+def _device(index: int, stream: Optional[torch.cuda.Stream]) -> int:
+    """The device that a call runs on, given its first operand's: the current one, since the library launches there."""
+    if index < 0:
+        raise ValueError("need CUDA tensors")
+    current = torch._C._cuda_getDevice()
+    if index != current:
+        raise ValueError(f"the operands are on cuda:{index}, the current device is cuda:{current} (set it with torch.cuda.device)")
+    if stream is not None and stream.device_index != index:
+        raise ValueError(f"stream: of cuda:{stream.device_index}, the operands are on cuda:{index}")
+    return index
+
+
+def _stream(stream: Optional[torch.cuda.Stream], device: int) -> int:
     # (torch.cuda.current_stream builds a Stream object: 2 us, as much as the launch)
-    return torch._C._cuda_getCurrentRawStream(t.get_device()) if stream is None else stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
-def _matrix(t: torch.Tensor, name: str, want: Optional[tuple] = None):
+def _matrix(t: torch.Tensor, name: str, device: int, want: Optional[tuple] = None):
     """(rows, columns, row stride, type) of a matrix argument, after the checks that need the tensor (the library checks the
     numbers)."""
     shape, kind = t.shape, _TYPES.get(t.dtype)
-    if kind is None or len(shape) != 2 or not t.is_cuda:
-        raise ValueError(f"{name}: need a 2-D fp32 or bf16 CUDA tensor with unit column stride")
+    if kind is None or len(shape) != 2 or t.get_device() != device:
+        raise ValueError(f"{name}: need a 2-D fp32 or bf16 tensor with unit column stride on cuda:{device}")
     ld, unit = t.stride()
     rows, cols = shape
     if unit != 1 and cols > 1:
-        raise ValueError(f"{name}: need a 2-D fp32 or bf16 CUDA tensor with unit column stride")
+        raise ValueError(f"{name}: need a 2-D fp32 or bf16 tensor with unit column stride on cuda:{device}")
     if want is not None and (rows, cols) != want:
         raise ValueError(f"{name}: need {want[0]} x {want[1]} elements, got {rows} x {cols}")
     # a single row may have any stride: report one that the library accepts
     return rows, cols, (ld if rows > 1 else -(-cols // 8) * 8), kind
 
 
-def _vector(t: torch.Tensor, n: int, name: str) -> int:
-    if not (t.dtype is torch.float32 and t.is_cuda and t.numel() == n and t.is_contiguous()):
-        raise ValueError(f"{name}: need a contiguous fp32 CUDA tensor of {n} elements")
+def _vector(t: torch.Tensor, n: int, name: str, device: int) -> int:
+    if not (t.dtype is torch.float32 and t.get_device() == device and t.numel() == n and t.is_contiguous()):
+        raise ValueError(f"{name}: need a contiguous fp32 tensor of {n} elements on cuda:{device}")
     return t.data_ptr()
 
 
-def _packed(p: Packed, name: str, rows: int, cols: int, block_rows: int = 1):
+def _packed(p: Packed, name: str, device: int, rows: int, cols: int, block_rows: int = 1):
+    if p.device_index != device:
+        raise ValueError(f"{name}: need an 8-bit matrix on cuda:{device}")
     if p.rows != rows or p.cols != cols or p.block_rows != block_rows:
         raise ValueError(f"{name}: need a {rows} x {cols} 8-bit matrix with block_rows {block_rows}, got {p.rows} x {p.cols}, {p.block_rows}")
     return C.byref(p._c)
 
 
-def _nodes(node_start: Optional[torch.Tensor], out: torch.Tensor, n: int, name: str):
+def _nodes(node_start: Optional[torch.Tensor], out: torch.Tensor, n: int, name: str, device: int):
     """(pointer to node_start, number of nodes, node stride) for per-node results in `out` [K][n]."""
-    if not (out.is_cuda and out.dtype == torch.float32 and out.dim() == 2 and out.shape[1] == n and (n == 1 or out.stride(1) == 1)):
-        raise ValueError(f"{name}: need a [nodes][{n}] fp32 CUDA view with unit column stride")
+    if not (out.get_device() == device and out.dtype == torch.float32 and out.dim() == 2 and out.shape[1] == n and (n == 1 or out.stride(1) == 1)):
+        raise ValueError(f"{name}: need a [nodes][{n}] fp32 view with unit column stride on cuda:{device}")
     K = out.shape[0]
     if node_start is None:
         if K != 1:
             raise ValueError("node_start: needed with more than one node")
         return None, 1, n
-    if not (node_start.is_cuda and node_start.dtype == torch.int64 and node_start.is_contiguous() and node_start.numel() == K + 1):
-        raise ValueError(f"node_start: need a contiguous int64 CUDA tensor of {K + 1} elements")
+    if not (node_start.get_device() == device and node_start.dtype == torch.int64 and node_start.is_contiguous() and node_start.numel() == K + 1):
+        raise ValueError(f"node_start: need a contiguous int64 tensor of {K + 1} elements on cuda:{device}")
     return node_start.data_ptr(), K, (out.stride(0) if K > 1 else n)
 
 
@@ -122,37 +138,40 @@ def pack(x: torch.Tensor, out: Packed, slope: float = 1.0, gate: Optional[Packed
          stream: Optional[torch.cuda.Stream] = None) -> None:
     """`x` (fp32 or bf16), through a leaky ReLU of `slope` (1: none), to 8 bits.  With `gate` (the 8-bit result of that
     leaky ReLU) `x` is a gradient and gets its derivative instead.  `y` (bf16): also what was rounded."""
-    rows, cols, ldx, kind = _matrix(x, "x")
+    device = _device(x.get_device(), stream)
+    rows, cols, ldx, kind = _matrix(x, "x", device)
     yp = ldy = None
     if y is not None:
-        _, _, ldy, ykind = _matrix(y, "y", (rows, cols))
+        _, _, ldy, ykind = _matrix(y, "y", device, (rows, cols))
         if ykind != TYPE_BF16:
             raise ValueError("y: need a bf16 tensor")
         yp = y.data_ptr()
     _done(lgc.lib().lgc_pack(x.data_ptr(), kind, rows, cols, ldx, out.block_rows, slope,
-                             None if gate is None else _packed(gate, "gate", rows, cols), _packed(out, "out", rows, cols, out.block_rows),
-                             yp, ldy or 0, _stream(stream, x)), "lgc_pack")
+                             None if gate is None else _packed(gate, "gate", device, rows, cols),
+                             _packed(out, "out", device, rows, cols, out.block_rows), yp, ldy or 0, _stream(stream, device)), "lgc_pack")
 
 
 def unpack(src: Packed, y: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
     """The values of an 8-bit matrix in `y` (fp32 or bf16; exact in both)."""
-    rows, cols, ldy, kind = _matrix(y, "y", (src.rows, src.cols))
-    _done(lgc.lib().lgc_unpack(C.byref(src._c), rows, cols, src.block_rows, y.data_ptr(), kind, ldy, _stream(stream, y)), "lgc_unpack")
+    device = _device(src.device_index, stream)
+    rows, cols, ldy, kind = _matrix(y, "y", device, (src.rows, src.cols))
+    _done(lgc.lib().lgc_unpack(C.byref(src._c), rows, cols, src.block_rows, y.data_ptr(), kind, ldy, _stream(stream, device)), "lgc_unpack")
 
 
 def layer_norm(x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor, eps: float, mean: torch.Tensor, rstd: torch.Tensor,
                y: Optional[torch.Tensor] = None, packed: Optional[Packed] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
     """Layer norm of the rows of `x` into `y` (x's type) and / or, in 8 bits, `packed`; `mean` and `rstd` for the backward pass."""
-    rows, cols, ldx, kind = _matrix(x, "x")
+    device = _device(x.get_device(), stream)
+    rows, cols, ldx, kind = _matrix(x, "x", device)
     yp = ldy = None
     if y is not None:
-        _, _, ldy, ykind = _matrix(y, "y", (rows, cols))
+        _, _, ldy, ykind = _matrix(y, "y", device, (rows, cols))
         if ykind != kind:
             raise ValueError("y: need x's type")
         yp = y.data_ptr()
-    _done(lgc.lib().lgc_layer_norm(x.data_ptr(), kind, rows, cols, ldx, _vector(gamma, cols, "gamma"), _vector(beta, cols, "beta"), eps, yp,
-                                   ldy or 0, None if packed is None else _packed(packed, "packed", rows, cols),
-                                   _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"), _stream(stream, x)), "lgc_layer_norm")
+    _done(lgc.lib().lgc_layer_norm(x.data_ptr(), kind, rows, cols, ldx, _vector(gamma, cols, "gamma", device), _vector(beta, cols, "beta", device),
+                                   eps, yp, ldy or 0, None if packed is None else _packed(packed, "packed", device, rows, cols),
+                                   _vector(mean, rows, "mean", device), _vector(rstd, rows, "rstd", device), _stream(stream, device)), "lgc_layer_norm")
 
 
 def layer_norm_backward_scratch(rows: int, cols: int, num_nodes: int = 1) -> int:
@@ -168,8 +187,8 @@ def _scratch(need: int, scratch: Optional[torch.Tensor], stream: Optional[torch.
         # of the pool of the stream that uses it: in another pool's block earlier work of that pool's stream may be under way
         with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
             return torch.empty(need, dtype=torch.uint8, device=like.device), need
-    if not (scratch.is_cuda and scratch.dtype is torch.uint8 and scratch.is_contiguous()):
-        raise ValueError("scratch: need a contiguous uint8 CUDA tensor")
+    if not (scratch.get_device() == like.get_device() and scratch.dtype is torch.uint8 and scratch.is_contiguous()):
+        raise ValueError(f"scratch: need a contiguous uint8 tensor on cuda:{like.get_device()}")
     return scratch, scratch.numel()
 
 
@@ -179,40 +198,42 @@ def layer_norm_backward(dy: torch.Tensor, x: Union[torch.Tensor, Packed], gamma:
     """Backward pass of layer_norm.  `x`: the input, or its 8-bit checkpoint.  `dgamma`, `dbeta`: [nodes][cols] views with
     one row stride (columns of the nodes' gradients).  `scratch`: a uint8 tensor of layer_norm_backward_scratch bytes;
     without one it comes from PyTorch's allocator."""
-    rows, cols, ld_dy, kind = _matrix(dy, "dy")
-    _, _, ld_dx, dx_kind = _matrix(dx, "dx", (rows, cols))
+    device = _device(dy.get_device(), stream)
+    rows, cols, ld_dy, kind = _matrix(dy, "dy", device)
+    _, _, ld_dx, dx_kind = _matrix(dx, "dx", device, (rows, cols))
     if dx_kind != kind:
         raise ValueError("dx: need dy's type")
-    nodes = _nodes(node_start, dgamma, cols, "dgamma")
-    if _nodes(node_start, dbeta, cols, "dbeta") != nodes:
+    nodes = _nodes(node_start, dgamma, cols, "dgamma", device)
+    if _nodes(node_start, dbeta, cols, "dbeta", device) != nodes:
         raise ValueError("dgamma and dbeta: need the same nodes and row stride")
     start, K, stride = nodes
     if isinstance(x, Packed):
-        xp, ldx, xkind, x8 = None, 0, TYPE_PACKED, _packed(x, "x", rows, cols)
+        xp, ldx, xkind, x8 = None, 0, TYPE_PACKED, _packed(x, "x", device, rows, cols)
     else:
-        _, _, ldx, xkind = _matrix(x, "x", (rows, cols))
+        _, _, ldx, xkind = _matrix(x, "x", device, (rows, cols))
         xp, x8 = x.data_ptr(), None
     scratch, size = _scratch(layer_norm_backward_scratch(rows, cols, K), scratch, stream, dy)
     _done(lgc.lib().lgc_layer_norm_backward(
-        dy.data_ptr(), kind, ld_dy, xp, xkind, ldx, x8, rows, cols, _vector(gamma, cols, "gamma"), _vector(mean, rows, "mean"),
-        _vector(rstd, rows, "rstd"), start, K, dx.data_ptr(), ld_dx, dgamma.data_ptr(), dbeta.data_ptr(), stride, scratch.data_ptr(), size,
-        _stream(stream, dy)), "lgc_layer_norm_backward")
+        dy.data_ptr(), kind, ld_dy, xp, xkind, ldx, x8, rows, cols, _vector(gamma, cols, "gamma", device), _vector(mean, rows, "mean", device),
+        _vector(rstd, rows, "rstd", device), start, K, dx.data_ptr(), ld_dx, dgamma.data_ptr(), dbeta.data_ptr(), stride, scratch.data_ptr(), size,
+        _stream(stream, device)), "lgc_layer_norm_backward")
 
 
 def product(a: Packed, b: Packed, y: Optional[torch.Tensor] = None, packed: Optional[Packed] = None, across: bool = False,
             slope: float = 1.0, stream: Optional[torch.cuda.Stream] = None) -> None:
     """act(a b^T), or with `across` act(a b), of 8-bit matrices (`b`: weights, block_rows 128) into `y` (fp32 or bf16) and / or,
     in 8 bits, `packed`.  act: the leaky ReLU of `slope` (1: none)."""
+    device = _device(a.device_index, stream)
     rows, inner = a.rows, a.cols
     cols = b.cols if across else b.rows
-    ap = _packed(a, "a", rows, inner)
-    bp = _packed(b, "b", inner if across else cols, cols if across else inner, BLOCK)
+    ap = _packed(a, "a", device, rows, inner)
+    bp = _packed(b, "b", device, inner if across else cols, cols if across else inner, BLOCK)
     yp, ldy, kind = None, 0, TYPE_BF16
     if y is not None:
-        _, _, ldy, kind = _matrix(y, "y", (rows, cols))
+        _, _, ldy, kind = _matrix(y, "y", device, (rows, cols))
         yp = y.data_ptr()
     _done(lgc.lib().lgc_product(ap, bp, 1 if across else 0, rows, cols, inner, slope, yp, kind, ldy,
-                                None if packed is None else _packed(packed, "packed", rows, cols), _stream(stream, a.codes)), "lgc_product")
+                                None if packed is None else _packed(packed, "packed", device, rows, cols), _stream(stream, device)), "lgc_product")
 
 
 def weight_gradient_scratch(rows: int, cols: int, inner: int, num_nodes: int = 1) -> int:
@@ -227,18 +248,20 @@ def weight_gradient(dy: torch.Tensor, x: Packed, dw: torch.Tensor, node_start: O
     """dw[k] = the sum over node k's rows of dy^T x ([dy's columns][x's columns], flat), from the bf16 gradient `dy` (rows
     16-byte aligned) and the 8-bit checkpoint `x`.  `dw`: a [nodes][n] fp32 view (columns of the nodes' gradients).
     `scratch`: a uint8 tensor of weight_gradient_scratch bytes; without one it comes from PyTorch's allocator."""
-    rows, cols, ld_dy, kind = _matrix(dy, "dy")
+    device = _device(dy.get_device(), stream)
+    rows, cols, ld_dy, kind = _matrix(dy, "dy", device)
     if kind != TYPE_BF16:
         raise ValueError("dy: need a bf16 tensor")
     inner = x.cols
-    xp = _packed(x, "x", rows, inner)
-    start, K, stride = _nodes(node_start, dw, cols * inner, "dw")
+    xp = _packed(x, "x", device, rows, inner)
+    start, K, stride = _nodes(node_start, dw, cols * inner, "dw", device)
     scratch, size = _scratch(weight_gradient_scratch(rows, cols, inner, K), scratch, stream, dy)
     _done(lgc.lib().lgc_weight_gradient(dy.data_ptr(), ld_dy, xp, rows, cols, inner, start, K, dw.data_ptr(), stride, scratch.data_ptr(), size,
-                                        _stream(stream, dy)), "lgc_weight_gradient")
+                                        _stream(stream, device)), "lgc_weight_gradient")
 
 
 def check(stream: Optional[torch.cuda.Stream] = None) -> None:
     """Waits for the stream and raises if a kernel recorded a failure (a wait that ran out)."""
     s = stream if stream is not None else torch.cuda.current_stream()
+    _device(s.device_index, None)
     _done(lgc.lib().lgc_layers_check(s.cuda_stream), "lgc_layers_check")

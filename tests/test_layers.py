@@ -151,3 +151,69 @@ def test_scratch_is_allocated_on_the_stream_that_uses_it(monkeypatch):
     assert layers._scratch(64, None, None, Stub(4, 8))[1] == 64
     assert layers._scratch(64, None, "side", Stub(4, 8))[1] == 64
     assert at == ["current", "side"]
+
+
+class NothingLaunched:
+    """Stands in for the library: sizes are answered, a launch is a failure of the test."""
+
+    def __getattr__(self, name):
+        def call(*a):
+            assert name.endswith("_scratch"), f"{name} was called"
+            a[-1]._obj.value = 64
+            return OK
+        return call
+
+
+def test_operands_and_streams_of_another_device_are_refused(monkeypatch):
+    from types import SimpleNamespace
+    from paper_2103_08870_b200 import layers
+    monkeypatch.setattr(lgc, "lib", lambda: NothingLaunched())
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 0, raising=False)
+    bf, i64, u8 = torch.bfloat16, torch.int64, torch.uint8
+    R_, Cc, N = 4, 256, 256 * 256
+    f = lambda d=0: Stub(R_, Cc, device=d)                                        # noqa: E731
+    b = lambda d=0: Stub(R_, Cc, dtype=bf, device=d)                              # noqa: E731
+    v = lambda n, d=0: Stub(n, device=d)                                          # noqa: E731
+    p = lambda d=0, tall=1, rows=R_: layers.Packed(Stub(rows, Cc, dtype=u8, device=d), Stub(-(-rows // tall), 4, dtype=u8, device=d), Cc, tall)  # noqa: E731
+    w = lambda d=0: p(d, 128, 256)                                                # noqa: E731
+    g = lambda d=0, n=Cc: Stub(2, n, device=d)                                    # noqa: E731
+    start = lambda d=0: Stub(3, dtype=i64, device=d)                              # noqa: E731
+    room = lambda d=0: Stub(64, dtype=u8, device=d)                               # noqa: E731
+    calls = [      # every operand in turn on the other device; the last time all of them
+        (layers.pack, [f, p], dict(gate=p, y=b)), (layers.unpack, [p, f], {}),
+        (layers.layer_norm, [f, lambda d=0: v(Cc, d), lambda d=0: v(Cc, d), 1e-5, lambda d=0: v(R_, d), lambda d=0: v(R_, d)], dict(y=f, packed=p)),
+        (layers.layer_norm_backward, [f, f, lambda d=0: v(Cc, d), lambda d=0: v(R_, d), lambda d=0: v(R_, d), f, g, g], dict(node_start=start, scratch=room)),
+        (layers.layer_norm_backward, [b, p, lambda d=0: v(Cc, d), lambda d=0: v(R_, d), lambda d=0: v(R_, d), b, g, g], dict(node_start=start, scratch=room)),
+        (layers.product, [p, w], dict(y=f, packed=p)),
+        (layers.weight_gradient, [b, p, lambda d=0: g(d, N)], dict(node_start=start, scratch=room)),
+    ]
+    for call, args, named in calls:
+        slots = [i for i, a in enumerate(args) if callable(a)] + list(named)
+        for other in [[s] for s in slots] + [slots]:
+            at = lambda s, a: a(1 if s in other else 0) if callable(a) else a     # noqa: E731
+            with pytest.raises(ValueError):
+                call(*[at(i, a) for i, a in enumerate(args)], **{k: at(k, a) for k, a in named.items()})
+        with pytest.raises(AssertionError):                                       # all where they belong: the library is called
+            call(*[a() if callable(a) else a for a in args], **{k: a() for k, a in named.items()})
+        with pytest.raises(ValueError):
+            call(*[a() if callable(a) else a for a in args], **{k: a() for k, a in named.items()}, stream=SimpleNamespace(device_index=1, cuda_stream=0))
+    with pytest.raises(ValueError):
+        layers.Packed(Stub(R_, Cc, dtype=u8), Stub(R_, 4, dtype=u8, device=1), Cc)
+
+
+def test_the_block_makes_its_device_current(monkeypatch):
+    from paper_2103_08870_b200 import block
+    seen = []
+
+    class Stop(Exception):
+        pass
+
+    def stop(*a, **kw):
+        raise Stop
+
+    monkeypatch.setattr(torch.cuda, "set_device", seen.append)
+    monkeypatch.setattr(torch, "Generator", stop)
+    with pytest.raises(Stop):
+        block.ResidualBlock(4, 8, 8, 1, device=torch.device("cuda", 1))
+    assert seen == [torch.device("cuda", 1)]
