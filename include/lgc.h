@@ -345,7 +345,8 @@ lgc_status lgc_layer_norm(const void *x, int32_t type, int64_t num_rows, int64_t
  * dy, dx: fp32 or bf16 (dy_type); dx may be dy.  x: fp32, bf16, or (x_type = LGC_TYPE_PACKED, x_packed) the 8-bit
  * checkpoint of the input; mean and rstd are those of lgc_layer_norm.  node_start: device int64
  * [num_nodes + 1], or NULL for one node with every row; dgamma, dbeta: node k's C floats start
- * k * node_stride after node 0's.  The sums over rows are taken in a fixed order in fp32.
+ * k * node_stride after node 0's.  The sums over rows are taken in a fixed order in fp32.  Rows that lie in no node's run (in
+ * front of node_start[0], from node_start[num_nodes] on) get their dx too.
  * scratch: lgc_layer_norm_backward_scratch bytes, 16-byte aligned. */
 lgc_status lgc_layer_norm_backward_scratch(int64_t num_rows, int64_t num_cols, int32_t num_nodes, size_t *bytes);
 lgc_status lgc_layer_norm_backward(const void *dy, int32_t dy_type, int64_t ld_dy, const void *x, int32_t x_type, int64_t ldx,

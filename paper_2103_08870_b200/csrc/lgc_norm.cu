@@ -254,8 +254,9 @@ layer_norm_rows_kernel(const T *__restrict__ x, int64_t ldx, int64_t rows, int c
 }
 
 // ---- backward ---------------------------------------------------------------------------------------------------------
-// Chunk `want` of the nodes' rows, each node's rows cut into chunks of `chunk_rows`: its rows and its node.  Called by a
-// whole warp; 32 nodes at a time.
+// Chunk `want` of the nodes' rows, each node's rows cut into chunks of `chunk_rows`: its rows and its node.  After the last
+// node's come the rows in front of the first node's run (as node `nodes`) and behind the last one's (`nodes` + 1), which have a
+// dx like all others and no part in any node's sums.  Called by a whole warp; 32 nodes at a time.
 struct Chunk {
     int64_t begin, end;
     int node;
@@ -263,12 +264,12 @@ struct Chunk {
 __device__ __forceinline__ Chunk find_chunk(const int64_t *start, int nodes, int64_t rows, int64_t chunk_rows, int64_t want)
 {
     const int lane = threadIdx.x & 31;
-    for (int k0 = 0; k0 < nodes; k0 += 32) {
+    for (int k0 = 0; k0 < nodes + 2; k0 += 32) {
         const int k = k0 + lane;
         int64_t lo = 0, hi = 0;
-        if (k < nodes) {
-            lo = node_first_row(start, k, rows);
-            hi = node_first_row(start, k + 1, rows);
+        if (k < nodes + 2) {
+            if (k != nodes) lo = node_first_row(start, k < nodes ? k : nodes, rows);
+            hi = k <= nodes ? node_first_row(start, k < nodes ? k + 1 : 0, rows) : rows;
             if (hi < lo) hi = lo;
         }
         const int64_t mine = (hi - lo + chunk_rows - 1) / chunk_rows;
@@ -621,7 +622,7 @@ int64_t chunk_rows_for(int64_t rows, int64_t cols, int32_t nodes)
 int64_t max_chunks_for(int64_t rows, int64_t cols, int32_t nodes)
 {
     const int64_t r = chunk_rows_for(rows, cols, nodes);
-    return (rows + r - 1) / r + nodes;
+    return rows / r + nodes + 2;                                 // (every run, the two of no node among them, may end in part of a chunk)
 }
 
 struct ForwardArgs {

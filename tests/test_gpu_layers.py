@@ -272,6 +272,50 @@ def test_layer_norm_gradient_agrees_with_differences():
         assert abs(want[1] - host(grads)[0, cols + j]) <= 1e-4 * np.abs(host(grads)).max()
 
 
+def chunk_rows(rows, cols, nodes):
+    """Rows that one thread adds up one after the other in the backward pass (the launcher's rule)."""
+    per_sm = 1 if cols > 4096 else 2 if cols > 2048 else 4 if cols > 1024 else 8 if cols > 512 else 16
+    return max(4, -(-rows // max(148, per_sm * 148 - nodes)))
+
+
+def backward_within_bounds(ds, xs, gs, m, rs, start, bf16, dx, dg, db):
+    """Outputs of layer_norm_backward against the formula; all in 64 bits on the GPU."""
+    rows, cols = ds.shape
+    xh = (xs - m[:, None]) * rs[:, None]
+    g, gx = ds * gs, ds * gs * xh
+    want = rs[:, None] * (g - g.mean(1, keepdim=True) - xh * gx.mean(1, keepdim=True))
+    # xh: two roundings, the first relative to x - mean; a row's sums: 16 entries a thread at most, five shuffles, 16 warps, the
+    # product with 1 / cols (which is rounded itself)
+    bound = rs[:, None] * U32 * (8 * g.abs() + 40 * g.abs().mean(1, keepdim=True) + 44 * xh.abs() * gx.abs().mean(1, keepdim=True)) + 1e-30
+    assert ((dx - want).abs() <= bound * 1.01 + (UBF * 1.01 * want.abs() if bf16 else 0)).all()
+    chunk = chunk_rows(rows, cols, len(start) - 1)
+    for k, (lo, hi) in enumerate(zip(start[:-1], start[1:])):
+        # a chunk's rows, a slice's chunks (eight slices), the slices, three roundings of a term
+        tol = (chunk + -(-max(0, hi - lo) // (8 * chunk)) + 1 + 8 + 3) * U32
+        t, a = (ds * xh)[lo:hi].sum(0), (ds * xh)[lo:hi].abs().sum(0)
+        assert ((dg[k] - t).abs() <= tol * a + 1e-30).all()
+        t, a = ds[lo:hi].sum(0), ds[lo:hi].abs().sum(0)
+        assert ((db[k] - t).abs() <= tol * a + 1e-30).all()
+
+
+@pytest.mark.parametrize("rows,cols", [(50, 127), (33, 2048), (700, 257), (20, 9001)])
+@pytest.mark.parametrize("start", [[7, 20], [0, 5, 9], [30, 30, 30], [3, 3, 12, 12, 33]])
+@pytest.mark.parametrize("aligned", [True, False])
+def test_layer_norm_backward_of_rows_in_no_nodes_run(rows, cols, start, aligned):
+    r = rng("no node", rows, cols, len(start))
+    x, gamma, _ = norm_inputs(r, rows, cols, torch.float32)
+    start = [min(s, rows) for s in start]
+    K = len(start) - 1
+    ld, offset = (-(-cols // 8) * 8, 0) if aligned else (cols + 1, 1)
+    dy, xv = view(dev(r.randn(rows, cols)), ld, offset), view(x, ld, offset)
+    mean, rstd = x.mean(1), (x.var(1, correction=0) + 1e-5).rsqrt()
+    dx, grads = torch.full_like(dy, 7.0), torch.full((K, 2 * cols), 3.0, device="cuda")
+    layers.layer_norm_backward(dy, xv, gamma, mean, rstd, dx, grads[:, :cols], grads[:, cols:], node_start=torch.tensor(start, device="cuda"))
+    backward_within_bounds(dy.double(), x.double(), gamma.double(), mean.double(), rstd.double(), start, False, dx.double(),
+                           grads[:, :cols].double(), grads[:, cols:].double())
+    layers.check()
+
+
 # ---- products -----------------------------------------------------------------------------------------------------------
 
 PRODUCTS = [(1, 1, 1), (1, 4096, 512), (2, 130, 40), (7, 1000, 513), (128, 128, 128), (129, 129, 640), (300, 777, 1160), (33, 260, 2100),
