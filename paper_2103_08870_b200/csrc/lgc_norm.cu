@@ -595,8 +595,8 @@ layer_norm_gradient_kernel(const float *__restrict__ partial, int64_t rows, int6
 #pragma unroll 8
         for (int64_t i = slice * each; i < end; ++i) {
             const float *p = partial + (first + i) * 2 * cols + c;
-            g = __fadd_rn(g, __ldg(p));
-            b = __fadd_rn(b, __ldg(p + cols));
+            g = __fadd_rn(g, __ldcg(p));                          // (not __ldg: they are written while this kernel is under way)
+            b = __fadd_rn(b, __ldcg(p + cols));
         }
     }
     part[0][slice][lane] = g;

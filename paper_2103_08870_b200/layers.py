@@ -196,8 +196,8 @@ def layer_norm_backward(dy: torch.Tensor, x: Union[torch.Tensor, Packed], gamma:
                         dx: torch.Tensor, dgamma: torch.Tensor, dbeta: torch.Tensor, node_start: Optional[torch.Tensor] = None,
                         scratch: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
     """Backward pass of layer_norm.  `x`: the input, or its 8-bit checkpoint.  `dgamma`, `dbeta`: [nodes][cols] views with
-    one row stride (columns of the nodes' gradients); rows in no node's run get their `dx` too.  `scratch`: a uint8 tensor of layer_norm_backward_scratch bytes;
-    without one it comes from PyTorch's allocator."""
+    one row stride (columns of the nodes' gradients); rows in no node's run get their `dx` too.  `scratch`: a uint8 tensor of
+    layer_norm_backward_scratch bytes; without one it comes from PyTorch's allocator."""
     device = _device(dy.get_device(), stream)
     rows, cols, ld_dy, kind = _matrix(dy, "dy", device)
     _, _, ld_dx, dx_kind = _matrix(dx, "dx", device, (rows, cols))
