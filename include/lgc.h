@@ -323,6 +323,7 @@ typedef struct {
  *   gate   : NULL, or the 8-bit result of that leaky ReLU in the forward pass (block_rows = 1): x is
  *            then a gradient and is multiplied by the derivative instead, `slope` where the gate's code has its
  *            sign bit set, 1 elsewhere (the sign survives the rounding, so this is exact; +0 counts as positive)
+ *            (the sign tells the branch only for a slope of +0 or more: others are refused with a gate)
  *   y      : NULL, or bf16 [num_rows] rows `ldy` apart: what was rounded, in bf16 */
 lgc_status lgc_pack(const void *x, int32_t type, int64_t num_rows, int64_t num_cols, int64_t ldx, int32_t block_rows,
                     float slope, const lgc_packed *gate, const lgc_packed *out, void *y, int64_t ldy, void *stream);

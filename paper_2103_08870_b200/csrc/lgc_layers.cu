@@ -1,5 +1,6 @@
 // C ABI of the layer operators: argument checks and the word their kernels record failures in (see include/lgc.h for
 // the contract of each).
+#include <cmath>
 #include <mutex>
 
 #include "lgc_layers.cuh"
@@ -149,6 +150,7 @@ lgc_status lgc_pack(const void *x, int32_t type, int64_t num_rows, int64_t num_c
         return refuse(where, why);
     if (block_rows != 1 && block_rows != kBlock) return refuse(where, "block_rows must be 1 or 128");
     if (gate && block_rows != 1) return refuse(where, "a gate goes with block_rows = 1");
+    if (gate && (std::isnan(slope) || std::signbit(slope))) return refuse(where, "with a gate, slope must not be negative (nor -0)");
     if (block_rows != 1 && num_rows > 65535 * (int64_t)kBlock) return refuse(where, "too many rows for block_rows = 128", LGC_ERR_UNSUPPORTED);
     return done(where, launch_pack(Matrix{x, type, ldx}, num_rows, num_cols, block_rows, slope, gate, *out, y, ldy,
                                    static_cast<cudaStream_t>(stream)));

@@ -137,7 +137,7 @@ def _done(status: int, where: str) -> None:
 def pack(x: torch.Tensor, out: Packed, slope: float = 1.0, gate: Optional[Packed] = None, y: Optional[torch.Tensor] = None,
          stream: Optional[torch.cuda.Stream] = None) -> None:
     """`x` (fp32 or bf16), through a leaky ReLU of `slope` (1: none), to 8 bits.  With `gate` (the 8-bit result of that
-    leaky ReLU) `x` is a gradient and gets its derivative instead.  `y` (bf16): also what was rounded."""
+    leaky ReLU, `slope` not negative) `x` is a gradient and gets its derivative instead.  `y` (bf16): also what was rounded."""
     device = _device(x.get_device(), stream)
     rows, cols, ldx, kind = _matrix(x, "x", device)
     yp = ldy = None

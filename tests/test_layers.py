@@ -92,6 +92,16 @@ def test_refused_on_the_host(lib):
     assert grad(start=P, K=2, stride=65535) == INVALID and grad(dw=None) == INVALID and grad(c=1 << 30, ld=1 << 30, i=2048, x=packed(ld=2048, ld_scales=16)) == INVALID
 
 
+def test_a_gate_needs_a_slope_whose_sign_tells_the_branch(lib):
+    """With a slope below zero, or -0, the result of a negative entry has no sign bit: its derivative cannot be read off."""
+    pack = lambda slope, gate, rows=4: lib.lgc_pack(4096, 0, rows, 256, 256, 1, slope, gate, packed(), None, 0, None)  # noqa: E731
+    for slope in (-0.01, -0.0, -1.0, float("-inf"), float("nan")):
+        assert pack(slope, packed()) == INVALID
+        assert b"slope" in lib.lgc_last_error(None)
+        assert pack(slope, None, 0) == OK
+    assert pack(0.0, packed(), 0) == OK and pack(0.01, packed(), 0) == OK
+
+
 def test_binding_refuses_host_tensors():
     from paper_2103_08870_b200 import layers
     with pytest.raises(ValueError):
