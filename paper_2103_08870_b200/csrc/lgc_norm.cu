@@ -407,7 +407,7 @@ layer_norm_backward_kernel(const T *__restrict__ dy, int64_t ld_dy, const XT *__
 // of shared-memory slots by bulk copies, so that the loads of the rows to come are always under way, whatever the registers
 // hold (16384 x 4096 bf16, x in 8 bits: 98 us against 196 with plain loads).  The barrier in the middle of a row's work says that every warp has read its slot, which a warp (another one each
 // row) then gives to a row to come.  A thread owns NV vectors of 8 neighbouring columns.  A row's last bytes that do not
-// fill 16 come in words of four (the last word may reach past the row's end; what it brings from there is not used).
+// fill 16 come in words of four, the last of them perhaps in part.
 template <typename T, typename XT, int THREADS, int NV>
 __global__ void __launch_bounds__(THREADS, (NV == 1 ? 1024 : 512) / THREADS)
 layer_norm_backward_ring_kernel(const T *__restrict__ dy, int64_t ld_dy, const XT *__restrict__ x, int64_t ldx,
@@ -448,8 +448,8 @@ layer_norm_backward_ring_kernel(const T *__restrict__ dy, int64_t ld_dy, const X
             if (d16) bulk_load(slot, d, d16, bar);
             if (x16) bulk_load(slot + x_at, xr, x16, bar);
         }
-        if (d16 + words < dy_bytes) word_load(slot + d16 + words, d + d16 + words);
-        if (x16 + words < x_bytes) word_load(slot + x_at + x16 + words, xr + x16 + words);
+        if (d16 + words < dy_bytes) word_load(slot + d16 + words, d + d16 + words, min(4u, dy_bytes - d16 - words));
+        if (x16 + words < x_bytes) word_load(slot + x_at + x16 + words, xr + x16 + words, min(4u, x_bytes - x16 - words));
         if (lane == 8) word_load(slot + more_at, mean + row);
         if (lane == 9) word_load(slot + more_at + 4, rstd + row);
         if (sizeof(XT) == 1 && lane < (cols + 4 * kBlock - 1) / (4 * kBlock))            // (at most 16 words: 8192 columns)

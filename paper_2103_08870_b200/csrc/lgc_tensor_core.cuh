@@ -151,10 +151,10 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
                  : "memory");
 }
-// Four bytes, asynchronously, by this thread
-__device__ __forceinline__ void word_load(uint32_t dst, const void *src)
+// Four bytes, asynchronously, by this thread; with `bytes` below four only those are read and the rest becomes zero.
+__device__ __forceinline__ void word_load(uint32_t dst, const void *src, uint32_t bytes = 4)
 {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, uint32_t bar, int c0, int c1)
 {

@@ -37,7 +37,7 @@ _TYPES = {torch.float32: TYPE_FP32, torch.bfloat16: TYPE_BF16}
 
 class Packed:
     """An 8-bit matrix: e4m3 `codes` (uint8 [rows][ld], unit column stride, 16-byte aligned rows) and the blocks' scale
-    bytes (uint8 [ceil(rows / block_rows)][..]); `cols` of the codes' columns belong to it."""
+    bytes (uint8 [ceil(rows / block_rows)][..], read four at a time); `cols` of the codes' columns belong to it."""
 
     __slots__ = ("codes", "scales", "rows", "cols", "block_rows", "device_index", "_c")
 
