@@ -298,6 +298,40 @@ def backward_within_bounds(ds, xs, gs, m, rs, start, bf16, dx, dg, db):
         assert ((db[k] - t).abs() <= tol * a + 1e-30).all()
 
 
+# Chunks of more rows than the ring of shared-memory slots has slots (9 rows and 5 slots; 17 and 8; 16 and 8; 28 and 8; 21 and 3; ...),
+# for every thread layout, rows whose last bytes fill no 16, and (contiguous) results whose rows start anywhere.
+@pytest.mark.parametrize("rows,cols", [(1200, 4100), (40000, 33), (16384, 1001), (4099, 4096), (3000, 8192), (2500, 500), (16000, 2047), (2000, 2050)])
+@pytest.mark.parametrize("kind,xkind", [(torch.float32, torch.float32), (torch.bfloat16, torch.bfloat16), (torch.bfloat16, "kept"),
+                                        (torch.float32, "kept"), (torch.float32, torch.bfloat16)])
+@pytest.mark.parametrize("contiguous", [False, True])
+def test_layer_norm_backward_of_many_rows(rows, cols, kind, xkind, contiguous):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(rows + cols)
+    normal = lambda *s: torch.randn(*s, generator=g, device="cuda")                                  # noqa: E731
+    x = normal(rows, cols) * normal(rows, 1).exp() + 3 * normal(rows, 1)
+    dy = view((1e-2 * normal(rows, cols) * normal(rows, 1).exp()).to(kind), -(-cols // 8) * 8)
+    gamma = 1 + 0.3 * normal(cols)
+    mean, rstd = x.mean(1), (x.var(1, correction=0) + 1e-5).rsqrt()
+    if xkind == "kept":
+        arg, xs = layers.packed_empty(rows, cols), torch.empty_like(x)
+        layers.pack(x, arg)
+        layers.unpack(arg, xs)
+    else:
+        arg = xs = view(x.to(xkind), -(-cols // 8) * 8)
+    start = [0, rows // 3, rows // 3, rows // 3 + 5, rows]
+    dx = torch.empty(rows, cols, dtype=kind, device="cuda") if contiguous else torch.empty_like(dy)
+    grads = torch.full((4, 2 * cols + 3), 3.0, device="cuda")
+    at = torch.tensor(start, device="cuda")
+    layers.layer_norm_backward(dy, arg, gamma, mean, rstd, dx, grads[:, :cols], grads[:, cols:2 * cols], node_start=at)
+    backward_within_bounds(dy.double(), xs.double(), gamma.double(), mean.double(), rstd.double(), start, kind == torch.bfloat16, dx.double(),
+                           grads[:, :cols].double(), grads[:, cols:2 * cols].double())
+    assert (grads[:, 2 * cols:] == 3).all()
+    before = grads.clone()
+    layers.layer_norm_backward(dy, arg, gamma, mean, rstd, dy, grads[:, :cols], grads[:, cols:2 * cols], node_start=at)      # in place
+    assert torch.equal(dy, dx) and torch.equal(grads, before)
+    layers.check()
+
+
 @pytest.mark.parametrize("rows,cols", [(50, 127), (33, 2048), (700, 257), (20, 9001)])
 @pytest.mark.parametrize("start", [[7, 20], [0, 5, 9], [30, 30, 30], [3, 3, 12, 12, 33]])
 @pytest.mark.parametrize("aligned", [True, False])
@@ -434,6 +468,69 @@ def test_weight_gradient_of_every_code_and_scale():
     assert (np.abs(host(grads) - want)[~big] <= np.abs(want)[~big]).all()
 
 
+# ---- more tiles than CTAs --------------------------------------------------------------------------------------------------
+
+def operands(rows, inner, cols, across, seed):
+    """8-bit operands and their product in 64 bits, on the GPU."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    a, b = layers.packed_empty(rows, inner), layers.packed_empty(*((inner, cols) if across else (cols, inner)), 128)
+    for p in (a, b):
+        layers.pack(torch.randn(p.rows, p.cols, generator=g, device="cuda") * torch.randn(p.rows, 1, generator=g, device="cuda").exp(), p)
+    A, B = (torch.empty(p.rows, p.cols, device="cuda") for p in (a, b))
+    layers.unpack(a, A)
+    layers.unpack(b, B)
+    A, B = A.double(), B.double() if across else B.double().t()
+    return a, b, A @ B, A.abs() @ B.abs()
+
+
+# (17, 20000) and (100, 40000): single CTAs, more than 148 tiles of 128 columns; (5000, 4200): pairs, 340 tiles for 74
+@pytest.mark.parametrize("rows,cols,inner", [(17, 20000, 300), (100, 40000, 1200), (5000, 4200, 4200), (5000, 4200, 130), (1, 700, 8000)])
+@pytest.mark.parametrize("across", [False, True])
+def test_product_of_several_tiles_per_cta(rows, cols, inner, across):
+    a, b, want, size = operands(rows, inner, cols, across, rows + inner)
+    y, p = torch.empty(rows, cols, device="cuda"), layers.packed_empty(rows, cols)
+    layers.product(a, b, y=y, packed=p, across=across)
+    # exact products; less than a unit in the last place per step of 32 of the magnitudes' sum, of 2048 terms at most, then a
+    # half per addition (and at most 64 additions where the fp32 pipes make the product of one row, 32 partial sums in a tree)
+    bound = (min(inner, 2048) / 32 + 1 + inner / 2048 + 1 + (inner / 64 + 5 if rows == 1 else 0)) * 2.0 ** -23 * size
+    assert ((y.double() - want).abs() <= bound).all()
+    again = torch.empty(rows, cols, dtype=torch.bfloat16, device="cuda")
+    layers.product(a, b, y=again, across=across)
+    assert torch.equal(again, y.bfloat16())
+    q = layers.packed_empty(rows, cols)
+    layers.pack(y, q)
+    n = -(-cols // 128)
+    assert torch.equal(p.codes[:, :cols], q.codes[:, :cols]) and torch.equal(p.scales[:, :n], q.scales[:, :n])
+    layers.check()
+
+
+# 180, 180 and 160 tiles of 256 x 256 for 74 pairs; runs that end inside a stage of 64 rows, on its edge, that are empty, and longer
+# than the ring of six stages
+@pytest.mark.parametrize("cols,inner,start", [(1100, 1300, [0, 1000, 1000, 1640, 1641, 4000, 4064]), (1288, 1300, [0, 640, 1333, 4000, 4096, 4100]),
+                                              (2000, 2560, [17, 5000, 5101])])
+def test_weight_gradient_of_several_tiles_per_pair(cols, inner, start):
+    rows = start[-1] + 9                                  # (the last rows are no node's)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(cols)
+    dy = view(torch.randn(rows, cols, generator=g, device="cuda").bfloat16(), -(-cols // 8) * 8)
+    x, X = layers.packed_empty(rows, inner), torch.empty(rows, inner, device="cuda")
+    layers.pack(torch.randn(rows, inner, generator=g, device="cuda"), x)
+    layers.unpack(x, X)
+    dy[start[-1]:] = float("nan")
+    K, n = len(start) - 1, cols * inner
+    grads = torch.full((K, n + 4), 3.0, device="cuda")
+    layers.weight_gradient(dy, x, grads[:, :n], node_start=torch.tensor(start, device="cuda"))
+    for k, (lo, hi) in enumerate(zip(start[:-1], start[1:])):
+        D, Xk = dy[lo:hi].double(), X[lo:hi].double()
+        want, size = D.t() @ Xk, D.abs().t() @ Xk.abs()
+        # less than a unit in the last place per step of 16 rows, of 512 at most, then a half per addition
+        bound = (min(hi - lo, 512) / 16 + 1 + (hi - lo) / 1024 + 1) * 2.0 ** -23 * size
+        assert ((grads[k, :n].view(cols, inner).double() - want).abs() <= bound).all()
+    assert (grads[:, n:] == 3).all()
+    layers.check()
+
+
 # ---- long sums ----------------------------------------------------------------------------------------------------------
 
 # The tensor cores' additions round towards zero: a step (32 terms of the product, 16 of the weight gradient) loses less than a
@@ -549,6 +646,51 @@ def test_scratch_of_calls_on_two_streams_at_a_time():
         torch.cuda.synchronize()
         for a, b in zip(want, got):
             assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    layers.check()
+
+
+def test_calls_in_a_cuda_graph_repeat_their_bits():
+    r = rng("graph")
+    rows, cols, K = 300, 520, 3
+    x, dy = dev(r.randn(rows, cols), torch.bfloat16), dev(r.randn(rows, cols), torch.bfloat16)
+    one = dev(r.randn(1, cols), torch.bfloat16)
+    gamma, beta = torch.ones(cols, device="cuda"), torch.zeros(cols, device="cuda")
+    w, w8 = dev(r.randn(cols, cols)), layers.packed_empty(cols, cols, 128)
+    h, d8, h1 = layers.packed_empty(rows, cols), layers.packed_empty(rows, cols), layers.packed_empty(1, cols)
+    mean, rstd, m1, r1 = (torch.empty(n, device="cuda") for n in (rows, rows, 1, 1))
+    y, dh, dx = (torch.zeros(rows, cols, dtype=torch.bfloat16, device="cuda") for _ in range(3))
+    y1 = torch.zeros(1, cols, device="cuda")
+    grads = torch.zeros(K, cols * cols + 2 * cols, device="cuda")
+    start = torch.tensor([0, 100, 100, rows], device="cuda")
+
+    def step():
+        layers.pack(w, w8)
+        layers.layer_norm(x, gamma, beta, 1e-5, mean, rstd, packed=h)
+        layers.product(h, w8, y=y)
+        layers.layer_norm(one, gamma, beta, 1e-5, m1, r1, packed=h1)
+        layers.product(h1, w8, y=y1)
+        layers.pack(dy, d8)
+        layers.product(d8, w8, y=dh, across=True)
+        layers.weight_gradient(dy, h, grads[:, :cols * cols], node_start=start)
+        layers.layer_norm_backward(dh, x, gamma, mean, rstd, dx, grads[:, cols * cols:-cols], grads[:, -cols:], node_start=start)
+
+    out = (y, y1, dh, dx, grads, mean, rstd)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for new in (False, True, True):
+        if new:
+            x.copy_(dev(r.randn(rows, cols), torch.bfloat16))
+            start[1:3] = 37
+            step()
+        want = [t.clone() for t in out]
+        for t in out:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, out))
     layers.check()
 
 
