@@ -266,12 +266,11 @@ __device__ __forceinline__ Chunk find_chunk(const int64_t *start, int nodes, int
     const int lane = threadIdx.x & 31;
     for (int k0 = 0; k0 < nodes + 2; k0 += 32) {
         const int k = k0 + lane;
-        int64_t lo = 0, hi = 0;
-        if (k < nodes + 2) {
-            if (k != nodes) lo = node_first_row(start, k < nodes ? k : nodes, rows);
-            hi = k <= nodes ? node_first_row(start, k < nodes ? k + 1 : 0, rows) : rows;
-            if (hi < lo) hi = lo;
-        }
+        // (both loads at once, whatever the lane: one latency in front of the CTA's work, not two)
+        int64_t lo = node_first_row(start, min(k, nodes), rows), hi = node_first_row(start, k < nodes ? k + 1 : 0, rows);
+        if (k == nodes) lo = 0;
+        if (k > nodes) hi = k == nodes + 1 ? rows : lo;
+        if (hi < lo) hi = lo;
         const int64_t mine = (hi - lo + chunk_rows - 1) / chunk_rows;
         int64_t upto = mine;
 #pragma unroll
@@ -354,7 +353,8 @@ layer_norm_backward_kernel(const T *__restrict__ dy, int64_t ld_dy, const XT *__
 {
     __shared__ float shared[2][2 * (TPR / 32)];
     const int t = threadIdx.x;
-    const Chunk ch = find_chunk(node_start, nodes, rows, chunk_rows, blockIdx.x);
+    const int number = gridDim.x - 1 - blockIdx.x;               // (the first CTAs are those that may find no chunk: see max_chunks_for)
+    const Chunk ch = find_chunk(node_start, nodes, rows, chunk_rows, number);
     if (ch.node < 0) return;
     float g[NV][8], dg[NV][8], db[NV][8];
 #pragma unroll
@@ -395,7 +395,7 @@ layer_norm_backward_kernel(const T *__restrict__ dy, int64_t ld_dy, const XT *__
             store8<T, false>(dx + row * ld_dx, (int64_t)(i * TPR + t) * 8, cols, d[i]);
         }
     }
-    float *out = partial + (int64_t)blockIdx.x * 2 * cols;
+    float *out = partial + (int64_t)number * 2 * cols;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         store8<float, false>(out, (int64_t)(i * TPR + t) * 8, cols, dg[i]);
@@ -424,7 +424,8 @@ layer_norm_backward_ring_kernel(const T *__restrict__ dy, int64_t ld_dy, const X
     __shared__ volatile int failed;
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
     grid_release_dependents();                                   // the kernel that adds up the chunks waits for this one's end
-    const Chunk ch = find_chunk(node_start, nodes, rows, chunk_rows, blockIdx.x);
+    const int number = gridDim.x - 1 - blockIdx.x;               // (the first CTAs are those that may find no chunk: see max_chunks_for)
+    const Chunk ch = find_chunk(node_start, nodes, rows, chunk_rows, number);
     if (ch.node < 0) return;
     if (t == 0) {
         failed = 0;
@@ -448,8 +449,11 @@ layer_norm_backward_ring_kernel(const T *__restrict__ dy, int64_t ld_dy, const X
             if (d16) bulk_load(slot, d, d16, bar);
             if (x16) bulk_load(slot + x_at, xr, x16, bar);
         }
-        if (d16 + words < dy_bytes) word_load(slot + d16 + words, d + d16 + words, min(4u, dy_bytes - d16 - words));
-        if (x16 + words < x_bytes) word_load(slot + x_at + x16 + words, xr + x16 + words, min(4u, x_bytes - x16 - words));
+        // at most four words; of the last one only what belongs to the row
+        if (d16 + words < dy_bytes) word_load(slot + d16 + words, d + d16 + words, sizeof(T) == 4 ? 4u : 2u + (d16 + words + 2 < dy_bytes) * 2u);
+        if (x16 + words < x_bytes)
+            word_load(slot + x_at + x16 + words, xr + x16 + words,
+                      sizeof(XT) == 4 ? 4u : sizeof(XT) == 2 ? 2u + (x16 + words + 2 < x_bytes) * 2u : min(4u, x_bytes - x16 - words));
         if (lane == 8) word_load(slot + more_at, mean + row);
         if (lane == 9) word_load(slot + more_at + 4, rstd + row);
         if (sizeof(XT) == 1 && lane < (cols + 4 * kBlock - 1) / (4 * kBlock))            // (at most 16 words: 8192 columns)
@@ -546,7 +550,7 @@ layer_norm_backward_ring_kernel(const T *__restrict__ dy, int64_t ld_dy, const X
                 }
             }
         }
-        float *out = partial + (int64_t)blockIdx.x * 2 * cols;
+        float *out = partial + (int64_t)number * 2 * cols;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (i * THREADS + t) * 8;
@@ -619,10 +623,11 @@ int64_t chunk_rows_for(int64_t rows, int64_t cols, int32_t nodes)
     const int64_t room = per_sm * 148 - nodes, r = (rows + (room < 148 ? 148 : room) - 1) / (room < 148 ? 148 : room);
     return r < 4 ? 4 : r;
 }
+// Every run of rows, the two of no node among them, may end in part of a chunk.  The CTAs that find no chunk come first and
+// make room at once: behind the others, one that found no room would hold up the launch of the kernel that adds up the chunks.
 int64_t max_chunks_for(int64_t rows, int64_t cols, int32_t nodes)
 {
-    const int64_t r = chunk_rows_for(rows, cols, nodes);
-    return rows / r + nodes + 2;                                 // (every run, the two of no node among them, may end in part of a chunk)
+    return rows / chunk_rows_for(rows, cols, nodes) + nodes + 2;
 }
 
 struct ForwardArgs {
