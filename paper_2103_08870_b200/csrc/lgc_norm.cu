@@ -479,7 +479,9 @@ layer_norm_backward_ring_kernel(const T *__restrict__ dy, int64_t ld_dy, const X
         int issuer = 0;                                          // the warp that loads into this row's slot
         T *to = dx + ch.begin * ld_dx;
         for (int k = 0; k < count; ++k, to += ld_dx, s = s + 1 == slots ? 0 : s + 1, phase ^= s == 0, set ^= 1) {
-            bar_wait(smem_addr(&full_bar[s]), phase, &failed);   // (a wait that runs out is recorded; the warps stay together)
+            // a wait that runs out is recorded; the warps stay together, and this one loads nothing more (a slot's barrier may still
+            // count the copies of the row that it waited for)
+            if (!bar_wait(smem_addr(&full_bar[s]), phase, &failed)) issuer = kWarps;
             __syncwarp();
             const uint8_t *slot = ring + s * slot_bytes;
             const float *more = reinterpret_cast<const float *>(slot + more_at);
