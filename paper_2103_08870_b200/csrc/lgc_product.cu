@@ -339,7 +339,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 }
 
 // ---- pairs of CTAs: tiles of 256 x 256 ------------------------------------------------------------------------------------
-// (16384 x 4096 x 8192 to 8 bits: 390 us in a burst, 2819 TFLOP/s; 421 us in a row, where the power cap holds the clock down.)
+// (16384 x 4096 x 8192 to 8 bits: 390 us in a burst, 2819 TFLOP/s; 415 to 445 us in a row, where the power cap holds the clock
+// down.)
 // Each CTA loads 128 rows of A and half of B's 256, and the pair's tensor cores share them: 32 KB per CTA and block of 128
 // along the contraction for twice the products of the single CTA's tile, half of what its loads cost (which bound it: at
 // 128 x 128 every SM takes 128 bytes a clock from L2).
@@ -355,8 +356,8 @@ constexpr int kStages = 6;
 constexpr int kScaleBytes = (kHalf + kTile) * 4;                 // A: this CTA's rows; B: all of the tile's
 constexpr int kStaged = 16;                                      // rows that a result warp stages at a time
 constexpr int kPieceWarp = kStaged * kPiecePitch;
-// At the start of a segment the tensor cores wait for the shared columns, about 0.55 us for the way there and back between the
-// CTAs: 16384 x 4096 x 8192 with 4, 8, 16 blocks a segment and without an end 505, 445, 421, 398 us in a row.  16: the error of
+// At the start of a segment the tensor cores wait for the shared columns, about 0.4 us for the way there and back between the
+// CTAs: 16384 x 4096 x 8192 with 8 and 16 blocks a segment and without an end 408, 390 and 378 us in a burst.  16: the error of
 // the sums no longer grows with their length and is that of fp32 products elsewhere (random signs: 1.1e-7 of the result at 4096
 // terms, where segments of 4 blocks have 6e-8 and a sum without an end 2.2e-7).
 constexpr int kFlushBlocks = 16;
@@ -497,33 +498,37 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                     const int q = quads & 1, buf = acc & 1;
                     const bool begin = kb % kFlushBlocks == 0, end = kb % kFlushBlocks == kFlushBlocks - 1 || kb == blocks - 1;
                     const uint32_t d = tmem + (buf ? kSecond : 0);
-                    if (begin) {                                      // the columns shared with the accumulator in front, and this one's last use
-                        if (acc >= 1 && !bar_wait_together(smem_addr(&shared_bar), (acc - 1) & 1, &failed)) { ok = false; break; }
-                        if (acc >= 2 && !bar_wait_together(smem_addr(&tempty_bar[buf]), ((acc >> 1) & 1) ^ 1, &failed)) { ok = false; break; }
-                    }
                     const uint32_t sa = tmem + kScaleCol + q * kScaleCols, sb = sa + kHalf / 32;
-                    // full means that the set's last user has finished: its shared memory and its columns are free
-                    if ((kb & 3) == 0 && !bar_wait_together(smem_addr(&sfull_bar[q]), (quads >> 1) & 1, &failed)) { ok = false; break; }
+                    if ((kb & 3) == 0) {
+                        // full means that the set's last user has finished: its shared memory and its columns are free
+                        if (!bar_wait_together(smem_addr(&sfull_bar[q]), (quads >> 1) & 1, &failed)) { ok = false; break; }
+                        tc_fence_after();
+                        if (issuer) {
+                            const uint32_t at = scales + q * kScaleBytes;
+                            copy_scales(sa, at);
+                            copy_scales(sb, at + kHalf * 4);
+                            copy_scales(sb + 4, at + kHalf * 8);
+                        }
+                        __syncwarp();
+                    }
                     if (!bar_wait_together(smem_addr(&full_bar[s]), phase, &failed)) { ok = false; break; }
+                    if (begin) {                                      // this accumulator's last use and, what is waited for longest, the shared columns
+                        if (acc >= 2 && !bar_wait_together(smem_addr(&tempty_bar[buf]), ((acc >> 1) & 1) ^ 1, &failed)) { ok = false; break; }
+                        if (acc >= 1 && !bar_wait_together(smem_addr(&shared_bar), (acc - 1) & 1, &failed)) { ok = false; break; }
+                    }
                     tc_fence_after();
                     const uint32_t st = tiles + s * kStageBytes;
                     const uint32_t id = idesc | (uint32_t)(kb & 3) << 4 | (uint32_t)(kb & 3) << 29;    // which byte of the scale words
                     const uint64_t a = tc_desc_k(st), b = ACROSS ? tc_desc(st + kHalf * kBlock, kHalf * kBlock) : tc_desc_k(st + kHalf * kBlock);
                     const bool last = (kb & 3) == 3 || kb == blocks - 1;
                     if (issuer) {
-                        if ((kb & 3) == 0) {
-                            const uint32_t at = scales + q * kScaleBytes;
-                            copy_scales(sa, at);
-                            copy_scales(sb, at + kHalf * 4);
-                            copy_scales(sb + 4, at + kHalf * 8);
-                        }
-    #pragma unroll
+#pragma unroll
                         for (int ks = 0; ks < 4; ++ks)                 // 32 along the contraction: 32 bytes, or 32 rows of 128 bytes
                             mma_block_scaled(d, a + (uint64_t)(ks * 32 >> 4), b + (uint64_t)((ACROSS ? ks * 4096 : ks * 32) >> 4), id, sa, sb,
                                              !begin || ks > 0);
+                        if (end) tc_commit_pair(smem_addr(&tfull_bar[buf]));
                         tc_commit_pair(smem_addr(&empty_bar[s]));
                         if (last) tc_commit_pair(smem_addr(&sempty_bar[q]));
-                        if (end) tc_commit_pair(smem_addr(&tfull_bar[buf]));
                     }
                     __syncwarp();
                     if (++s == kStages) s = 0, phase ^= 1;
@@ -541,18 +546,18 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                 for (int kb = 0; kb < blocks; kb += 4, ++quads) {
                     const int q = quads & 1;
                     uint32_t wa[4], wb[2] = {0, 0};
-    #pragma unroll
+#pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         int64_t r = (int64_t)m * kTile + rank * kHalf + 32 * j + lane;
                         if (r >= p.rows) r = p.rows - 1;               // (its codes arrive as zeros and its result is not written)
                         wa[j] = __ldg(reinterpret_cast<const uint32_t *>(p.a_scales + r * p.ld_as + kb));
                     }
-    #pragma unroll
+#pragma unroll
                     for (int g = 0; g < 2; ++g) {
                         const int64_t group = (int64_t)n * 2 + g;
                         if (group * kBlock >= p.cols) continue;        // (columns that are not written)
                         if (ACROSS) {
-    #pragma unroll
+#pragma unroll
                             for (int j = 0; j < 4; ++j)
                                 if (kb + j < blocks) wb[g] |= (uint32_t)__ldg(p.b_scales + (int64_t)(kb + j) * p.ld_bs + group) << (8 * j);
                         } else {
