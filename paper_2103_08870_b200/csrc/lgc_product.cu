@@ -339,8 +339,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 }
 
 // ---- pairs of CTAs: tiles of 256 x 256 ------------------------------------------------------------------------------------
-// (16384 x 4096 x 8192 to 8 bits: 390 us in a burst, 2819 TFLOP/s; 415 to 445 us in a row, where the power cap holds the clock
-// down.)
+// (16384 x 4096 x 8192 to 8 bits: 406 us in a burst, 2708 TFLOP/s; 427 us in a row, where the power cap holds the clock down.)
 // Each CTA loads 128 rows of A and half of B's 256, and the pair's tensor cores share them: 32 KB per CTA and block of 128
 // along the contraction for twice the products of the single CTA's tile, half of what its loads cost (which bound it: at
 // 128 x 128 every SM takes 128 bytes a clock from L2).
@@ -356,11 +355,11 @@ constexpr int kStages = 6;
 constexpr int kScaleBytes = (kHalf + kTile) * 4;                 // A: this CTA's rows; B: all of the tile's
 constexpr int kStaged = 16;                                      // rows that a result warp stages at a time
 constexpr int kPieceWarp = kStaged * kPiecePitch;
-// At the start of a segment the tensor cores wait for the shared columns, about 0.4 us for the way there and back between the
-// CTAs: 16384 x 4096 x 8192 with 8 and 16 blocks a segment and without an end 408, 390 and 378 us in a burst.  16: the error of
-// the sums no longer grows with their length and is that of fp32 products elsewhere (random signs: 1.1e-7 of the result at 4096
-// terms, where segments of 4 blocks have 6e-8 and a sum without an end 2.2e-7).
-constexpr int kFlushBlocks = 16;
+// At the start of a segment the tensor cores wait for the shared columns, some 800 cycles for the way there and back between the
+// CTAs.  16384 x 4096 x 8192 with segments of 4, 8, 16 blocks and without an end: 471, 406, 385 and 372 us in a burst; 300, 360, 490
+// and 710 of its 134 million codes are not those of a 64-bit result (of a product in fp32: 370).  So 8: the sums are as exact as an
+// fp32 product's, however long.
+constexpr int kFlushBlocks = 8;                                  // blocks that the tensor cores add up
 constexpr int kSmemBytes = kStages * kStageBytes + 2 * kScaleBytes + 8 * kPieceWarp + 1024;
 constexpr int kThreads = 384;                                    // warp 0: TMA, 1: MMA, 2: scales, 3: tensor memory, 4..11: results
 constexpr int kScaleCols = (kHalf + kTile) / 32;

@@ -491,9 +491,9 @@ def test_product_of_several_tiles_per_cta(rows, cols, inner, across):
     a, b, want, size = operands(rows, inner, cols, across, rows + inner)
     y, p = torch.empty(rows, cols, device="cuda"), layers.packed_empty(rows, cols)
     layers.product(a, b, y=y, packed=p, across=across)
-    # exact products; less than a unit in the last place per step of 32 of the magnitudes' sum, of 2048 terms at most, then a
+    # exact products; less than a unit in the last place per step of 32 of the magnitudes' sum, of 1024 terms at most, then a
     # half per addition (and at most 64 additions where the fp32 pipes make the product of one row, 32 partial sums in a tree)
-    bound = (min(inner, 2048) / 32 + 1 + inner / 2048 + 1 + (inner / 64 + 5 if rows == 1 else 0)) * 2.0 ** -23 * size
+    bound = (min(inner, 1024) / 32 + 1 + inner / 2048 + 1 + (inner / 64 + 5 if rows == 1 else 0)) * 2.0 ** -23 * size
     assert ((y.double() - want).abs() <= bound).all()
     again = torch.empty(rows, cols, dtype=torch.bfloat16, device="cuda")
     layers.product(a, b, y=again, across=across)
@@ -557,7 +557,7 @@ def test_product_of_long_sums_of_one_sign(rows, cols, inner, across):
     y = torch.empty(rows, cols, device="cuda")
     layers.product(a, b, y=y, across=across)
     lost = (want - y.double()) / want
-    most, mean = one_sign_bounds(2048 // 32, inner / 2048)          # at most 2048 terms are added up in tensor memory
+    most, mean = one_sign_bounds(1024 // 32, inner / 1024)          # at most 1024 terms are added up in tensor memory
     assert lost.abs().max() <= most and lost.mean().abs() <= mean
     layers.check()
 
