@@ -360,7 +360,7 @@ lgc_status lgc_layer_norm_backward(const void *dy, int32_t dy_type, int64_t ld_d
  *     across = 0:  Y[t][n] = act(sum_i A[t][i] B[n][i])     (a linear layer: A activations, B weights)
  *     across = 1:  Y[t][n] = act(sum_i A[t][i] B[i][n])     (the gradient at its input: the same weights, A the
  *                                                            gradient at its output)
- * for t < num_rows, n < num_cols, i < inner.  A has block_rows = 1, B block_rows = 128.  The tensor cores add up at most 2048
+ * for t < num_rows, n < num_cols, i < inner.  A has block_rows = 1, B block_rows = 128.  The tensor cores add up at most 1024
  * terms of a sum (their additions round towards zero), the rest is fp32 additions to nearest in a fixed order.
  * act is the leaky ReLU with `slope` (1 = none).  y: NULL, or fp32 / bf16 (type); packed: NULL, or Y in 8 bits
  * (block_rows = 1), rounded from the fp32 sums.  At least one of the two. */
@@ -381,7 +381,8 @@ lgc_status lgc_weight_gradient(const void *dy, int64_t ld_dy, const lgc_packed *
                                void *scratch, size_t scratch_bytes, void *stream);
 
 /* What the kernels of lgc_layer_norm_backward, lgc_product and lgc_weight_gradient recorded on the current device (a
- * wait inside a kernel that ran out): waits for `stream`, returns LGC_OK or LGC_ERR_DEVICE_CHECK and clears the record. */
+ * wait inside a kernel that ran out): waits for `stream`, returns LGC_OK or LGC_ERR_DEVICE_CHECK and clears the record.
+ * There is one record per device and process: a failure is reported to whoever checks first, whichever call it was of. */
 lgc_status lgc_layers_check(void *stream);
 
 /* ---- inspection --------------------------------------------------------------------------- */

@@ -60,7 +60,8 @@ class ResidualBlock:
         layers.pack(self.w2, self.w2_8)
 
     def forward(self, x: torch.Tensor) -> torch.Tensor:
-        """x: bf16 [rows][width].  Keeps x, norm(x) and the hidden layer in 8 bits."""
+        """x: bf16 [rows][width].  Keeps x, norm(x) and the hidden layer in 8 bits.  Returns the block's own buffer, which the
+        next call writes."""
         layers.pack(x, self.x8)
         layers.layer_norm(x, self.gamma, self.beta, EPS, self.mean, self.rstd, packed=self.h8)
         layers.product(self.h8, self.w1_8, packed=self.a8, slope=SLOPE)
@@ -68,7 +69,8 @@ class ResidualBlock:
         return self.y.add_(x)
 
     def backward(self, dy: torch.Tensor, node_start: Optional[torch.Tensor] = None) -> torch.Tensor:
-        """dy: bf16 [rows][width], the gradient at y.  Every node's gradients go to its row of `grads`; returns the gradient at x."""
+        """dy: bf16 [rows][width], the gradient at y.  Every node's gradients go to its row of `grads`; returns the gradient at
+        x, in the block's own buffer, which the next call writes."""
         at, g = self.at, self.grads
         layers.pack(dy, self.dy8)
         layers.weight_gradient(dy, self.a8, g[:, at[3]:at[4]], node_start=node_start)

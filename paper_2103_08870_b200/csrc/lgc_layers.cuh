@@ -146,7 +146,7 @@ __device__ __forceinline__ uint32_t most_of_block(const float (&v)[8])
 }
 
 // ---- sixteen neighbouring entries of a row, as pairs ---------------------------------------------------------------------
-// The streaming kernels are close to the issue rate, so they work on pairs of fp32 numbers in one instruction (add, mul,
+// The streaming kernels fill half to two thirds of the issue slots, so they work on pairs of fp32 numbers in one instruction (add, mul,
 // fma .f32x2), take the magnitude's maximum of two entries at a time, and give a lane 16 neighbours: eight lanes hold a
 // block, three shuffles find its maximum, and a lane's codes are one 16-byte store.
 typedef unsigned long long f2;          // (lower entry, upper entry)

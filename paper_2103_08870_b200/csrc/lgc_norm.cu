@@ -1,7 +1,7 @@
 // Layer norm over the rows of a matrix, and its backward pass with the weight's and bias's gradients per node.
 //
 // Forward: a row stays in registers between its three uses (sum, sum of squared deviations, result), so x is read once
-// and y (and / or its 8-bit form) written once: DRAM bounds it.  The variance is the mean of the squared deviations from
+// and y (and / or its 8-bit form) written once.  The variance is the mean of the squared deviations from
 // the mean that was found, not a difference of squares.
 // Backward: dx needs two sums per row, the weight's gradient a sum over rows per column.  A CTA walks down a chunk of
 // consecutive rows of one node; a thread keeps its columns' gradients in registers on the way, so dy and x are read once;
@@ -43,7 +43,7 @@ __device__ __forceinline__ void row_sums(float (&v)[COUNT], float *shared)
     }
 }
 
-// Few rows (less than four per SM), wide rows, rows that start anywhere: a CTA of TPR threads per row, NV vectors of eight
+// Few rows (less than four per SM), or rows that start anywhere: a CTA of TPR threads per row, NV vectors of eight
 // entries each.  Lanes hold neighbouring vectors, so that 16 lanes hold a block of the 8-bit form.  One row of 4096: 8 us
 // from cold caches.
 template <typename T, bool VEC, int TPR, int NV>
@@ -136,9 +136,11 @@ __device__ __forceinline__ void keep_raw(Raw16<T> (&raw)[UNITS])
 
 // Many rows: WPR warps per row, walking from row to row.  The row stays as it was loaded (bf16: half the registers of fp32
 // numbers), UNITS times 16 neighbouring entries per lane; gamma and beta lie in shared memory in the order in which lanes
-// read them, one 16-byte piece per lane without bank conflicts.  16384 x 4096 bf16 to 8 bits: 58 us, 3.5 TB/s; the issue
-// rate bounds it (17 instructions an entry), so four warps a row (32 per SM) beat one warp a row (76 us), and the next
-// row's loads, ahead in registers or in shared memory, gained nothing (61 and 73 us).
+// read them, one 16-byte piece per lane without bank conflicts.  16384 x 4096 bf16 to 8 bits: 59 us, 3.4 TB/s.  Nothing is full
+// (issue slots 63 %, DRAM 35 %): a row's chain of load, two exchanges among its warps and store is long, and 32 warps per SM
+// do not cover it; of the time between two instructions of a warp a quarter is waiting for the row's loads and a fifth for shuffles and
+// shared memory.  One warp a row is slower (76 us), and the next row's loads, ahead in registers or in shared memory, gained
+// nothing (61 and 73 us).
 constexpr int kRowThreads = 256;
 
 // A sum over the WPR warps of a row; the groups of a CTA have a named barrier each.
@@ -405,7 +407,8 @@ layer_norm_backward_kernel(const T *__restrict__ dy, int64_t ld_dy, const XT *__
 
 // The same for rows that start on 16-byte boundaries: whole rows of dy and x (and the 8-bit form's scales) come into a ring
 // of shared-memory slots by bulk copies, so that the loads of the rows to come are always under way, whatever the registers
-// hold (16384 x 4096 bf16, x in 8 bits: 98 us against 196 with plain loads).  The barrier in the middle of a row's work says that every warp has read its slot, which a warp (another one each
+// hold (16384 x 4096 bf16, x in 8 bits: 100 us against 196 with plain loads; issue slots 44 %, DRAM 37 %: the 16 warps of an SM
+// wait for one another at a barrier per row, and for the shuffles and shared-memory reads around it).  The barrier in the middle of a row's work says that every warp has read its slot, which a warp (another one each
 // row) then gives to a row to come.  A thread owns NV vectors of 8 neighbouring columns.  A row's last bytes that do not
 // fill 16 come in words of four, the last of them perhaps in part.
 template <typename T, typename XT, int THREADS, int NV>
@@ -616,9 +619,10 @@ layer_norm_gradient_kernel(const float *__restrict__ partial, int64_t rows, int6
     }
 }
 
-// Rows per chunk, at least four: as many chunks as there is room for CTAs at a time (two per SM for rows of 4096 and more,
-// up to sixteen for narrow ones), the nodes' rounding included, since a chunk too many costs a second round of CTAs.  The
-// chunks' 2 * cols partial sums stay small beside their rows.
+// Rows per chunk, at least four: as many chunks as there is room for CTAs at a time (one per SM for rows of more than 4096, two
+// from 2049 on, up to sixteen for narrow ones), the nodes' rounding included, since a chunk too many costs a second round of CTAs.
+// (The ring's slots leave no room for the last of them at about 470 to 510 columns, and of fp32 at about 990 to 1020: there 16384
+// rows do take a second round.)  The chunks' 2 * cols partial sums stay small beside their rows.
 int64_t chunk_rows_for(int64_t rows, int64_t cols, int32_t nodes)
 {
     const int64_t per_sm = cols > 4096 ? 1 : cols > 2048 ? 2 : cols > 1024 ? 4 : cols > 512 ? 8 : 16;
@@ -713,7 +717,8 @@ struct BackwardArgs {
     cudaStream_t s;
 };
 
-// Rows that start anywhere, or wider than the ring kernel's threads can own.
+// Rows that start anywhere, or wider than the ring kernel's threads can own (beyond 8192 columns 1024 threads of 64 registers
+// spill up to 256 bytes each).
 template <typename T, typename XT>
 void backward_any(const BackwardArgs &a)
 {

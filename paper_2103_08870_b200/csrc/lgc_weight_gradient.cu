@@ -14,6 +14,10 @@
 // grows with the rows), so their accumulator takes only 8 * 64 rows at a time; eight warps add those sums up in registers
 // while the other accumulator fills.  Where there are few tiles a node's rows are cut into parts, whose sums a last kernel
 // adds in order.
+//
+// What bounds it (16384 x 4096 x 4096, eight nodes: 470 us, tensor pipe 59 %): of its 740,000 cycles the issuing warp waits 46 %
+// for loads (boxes of 64 rows of 128 bytes that lie 8 KB apart; 32 KB per CTA and 512 cycles of products), 2 % for cleared
+// rows and 10 % for an accumulator to be read.
 #include "lgc_layers.cuh"
 #include "lgc_tensor_core.cuh"
 

@@ -261,7 +261,8 @@ def weight_gradient(dy: torch.Tensor, x: Packed, dw: torch.Tensor, node_start: O
 
 
 def check(stream: Optional[torch.cuda.Stream] = None) -> None:
-    """Waits for the stream and raises if a kernel recorded a failure (a wait that ran out)."""
+    """Waits for the stream and raises if a kernel recorded a failure (a wait that ran out).  One record per device and
+    process: whoever checks first hears of it, and clears it."""
     s = stream if stream is not None else torch.cuda.current_stream()
     _device(s.device_index, None)
     _done(lgc.lib().lgc_layers_check(s.cuda_stream), "lgc_layers_check")
