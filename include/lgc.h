@@ -380,8 +380,77 @@ lgc_status lgc_weight_gradient(const void *dy, int64_t ld_dy, const lgc_packed *
                                int64_t inner, const int64_t *node_start, int32_t num_nodes, float *dw, int64_t node_stride,
                                void *scratch, size_t scratch_bytes, void *stream);
 
-/* What the kernels of lgc_layer_norm_backward, lgc_product and lgc_weight_gradient recorded on the current device (a
- * wait inside a kernel that ran out): waits for `stream`, returns LGC_OK or LGC_ERR_DEVICE_CHECK and clears the record.
+/* ---- the attention layer's operators ----
+ * Operands of heads are [rows][heads][dim] with any distance between rows and between heads: views of the result of one
+ * linear layer, for instance.  (`ld` of a single row and `head_stride` of a single head are not looked at.)  Rows and heads
+ * of an operand may not overlap. */
+typedef struct {
+    void *p;              /* device */
+    int64_t ld;           /* elements from row to row */
+    int64_t head_stride;  /* elements from head to head */
+} lgc_heads;
+
+/* Rotary positions: for i < num_pairs the pair (a, b) of every head's entries becomes
+ *     (A (a cos t - b sin t), A (a sin t + b cos t)),   t = positions[row] * frequencies[i],   A = amplitude;
+ * a, b are the entries 2 i and 2 i + 1 (interleaved = 1) or i and i + num_pairs (interleaved = 0).  Entries from
+ * 2 * num_pairs on pass through.  backward = 1: t has the opposite sign, which makes the call the gradient's way back (x: the
+ * gradient at y, y: the gradient at x).
+ *   x, y        : fp32 or bf16 (type); y->p may be x->p (with the same strides), otherwise they may not overlap
+ *   positions   : device, int64 [num_rows], any sign
+ *   frequencies : device, fp64 [num_pairs], radians per position (scaled for long contexts as the caller likes)
+ * The angle is formed in 64 bits.  1 <= heads <= 65536, 2 <= dim <= 65536. */
+lgc_status lgc_rotary(const lgc_heads *x, int32_t type, int64_t num_rows, int32_t heads, int32_t dim, const int64_t *positions,
+                      const double *frequencies, int32_t num_pairs, int32_t interleaved, float amplitude, int32_t backward,
+                      const lgc_heads *y, void *stream);
+
+/* Attention over sequences.  The rows of q are the queries, the rows of k and v the keys of num_sequences sequences: sequence s
+ * has queries query_start[s] .. query_start[s + 1] - 1 and keys key_start[s] .. key_start[s + 1] - 1; runs may be empty, and
+ * rows in no run are neither read nor written.  With i and j counted from the sequence's first query and key, L its number of
+ * keys minus its number of queries, query i sees
+ *     every key                                   (causal = 0)
+ *     the keys j <= i + L                         (causal = 1: the last query sees all of them)
+ *     of those the keys j > i + L - window        (window > 0; only with causal = 1)
+ * and, for every head h of q and the head h / (heads / kv_heads) of k and v that it shares with its group,
+ *     s_ij = scale * sum_d q_id k_jd,   lse_i = log(sum over the keys that i sees of exp(s_ij)),
+ *     y_i = sum over the keys that i sees of exp(s_ij - lse_i) v_j.
+ * A query that sees no key has y = 0 and lse = -infinity.
+ *   q, k, v, y : bf16, 16-byte aligned, strides multiples of 8; dim a multiple of 8, at most 128 (LGC_ERR_UNSUPPORTED above)
+ *   heads      : a multiple of kv_heads, at most 128 per head of k and v
+ *   query_start, key_start : device, int64 [num_sequences + 1], ascending.  Both NULL: one sequence with every row.
+ *                key_start NULL: the same as query_start (then query_rows = key_rows).  What lies outside the matrix is cut off.
+ *   scale      : positive, 2^-100 to 2^100
+ *   lse        : device, fp32 [query_rows][heads]
+ * Logits, the softmax's statistics and the sums are fp32; the probabilities are rounded to bf16 in front of their product
+ * with v, and dy's with the logits' gradients likewise.  A NaN or an infinity in a row of a sequence may reach every result of
+ * that sequence and kv head (also of queries that do not see the row), never another sequence's.
+ * scratch: lgc_attention_scratch bytes, 16-byte aligned. */
+typedef struct {
+    int64_t query_rows, key_rows;        /* 0 to 2^30 */
+    int32_t heads, kv_heads, dim;
+    int32_t num_sequences;               /* 1 to 2^20 */
+    const int64_t *query_start, *key_start;
+    int32_t causal;
+    int64_t window;                      /* 0: none */
+    float scale;
+} lgc_attention_shape;
+
+lgc_status lgc_attention_scratch(const lgc_attention_shape *shape, size_t *bytes);
+lgc_status lgc_attention(const lgc_attention_shape *shape, const lgc_heads *q, const lgc_heads *k, const lgc_heads *v, const lgc_heads *y,
+                         float *lse, void *scratch, size_t scratch_bytes, void *stream);
+
+/* Its backward pass: from dy, the gradient at y, and the forward pass' q, k, v, y and lse, with p_ij = exp(s_ij - lse_i),
+ *     delta_i = sum_d dy_id y_id,   ds_ij = p_ij (sum_d dy_id v_jd - delta_i),
+ *     dv_j = sum_i p_ij dy_i,   dq_i = scale sum_j ds_ij k_j,   dk_j = scale sum_i ds_ij q_i,
+ * dk and dv also summed over the heads that share a head of k and v.  dq, dk, dv: bf16, like q, k, v; each sum is fp32 in a
+ * fixed order (the same call gives the same bits).  No output may overlap an input or another output.
+ * scratch: lgc_attention_backward_scratch bytes, 16-byte aligned. */
+lgc_status lgc_attention_backward_scratch(const lgc_attention_shape *shape, size_t *bytes);
+lgc_status lgc_attention_backward(const lgc_attention_shape *shape, const lgc_heads *dy, const lgc_heads *q, const lgc_heads *k,
+                                  const lgc_heads *v, const lgc_heads *y, const float *lse, const lgc_heads *dq, const lgc_heads *dk,
+                                  const lgc_heads *dv, void *scratch, size_t scratch_bytes, void *stream);
+
+/* What the kernels of lgc_layer_norm_backward, lgc_product, lgc_weight_gradient, lgc_attention and lgc_attention_backward
+ * recorded on the current device (a wait inside a kernel that ran out): waits for `stream`, returns LGC_OK or LGC_ERR_DEVICE_CHECK and clears the record.
  * There is one record per device and process: a failure is reported to whoever checks first, whichever call it was of. */
 lgc_status lgc_layers_check(void *stream);
 

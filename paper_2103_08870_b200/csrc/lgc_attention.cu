@@ -1,0 +1,585 @@
+// Attention over sequences, forward: y = softmax(scale q k^T) v and the logarithm of the softmax's denominator.
+//
+// One pass over the keys with a running maximum and sum per row.  A CTA has two tiles of 128 rows (queries x the heads that
+// share a head of k and v) and takes the keys 128 at a time: S = Q K^T on the tensor cores into tensor memory; a thread per row
+// reads its 128 logits, takes the maximum, the exponentials and their sum, and writes P in bf16 over S; the tensor cores add
+// P V to O, which stays in tensor memory.  While one tile's threads are at their exponentials the tensor cores work for the
+// other tile.  The maximum that the exponents refer to is raised (and O multiplied) only when it has grown by more than
+// kSlack in powers of two: P then is 2^kSlack at most, and the quotient O / sum is the same.
+//
+// Precision: logits, maximum, sum and O are fp32 (the tensor cores' additions round towards zero: 2^-24 of a term, a few
+// thousand times at most, far below y's bf16); P is rounded to bf16 for the product, as every operand is; the sum takes P unrounded.
+#include "lgc_attention.cuh"
+
+namespace lgc {
+
+using namespace attention;
+
+namespace {
+
+constexpr float kSlack = 8.0f;
+constexpr int kThreads = 384;           // warps 0..3: rows of tile 0, 4..7: of tile 1, 8: MMA, 9: TMA, 10 and 11 only give registers
+// Registers per thread: 168 at the launch, then 208 for the rows' threads (128 logits each), 88 for the others: 2 * 208 + 88 = 3 * 168.
+constexpr int kRowRegisters = 208, kOtherRegisters = 88;
+
+struct ForwardArgs {
+    Runs runs;
+    Plan plan;
+    Mask mask;
+    int heads, kv_heads, group, dim;
+    int queries;                        // of a tile
+    float scale_log2;                   // scale * log2(e)
+    __nv_bfloat16 *y;
+    int64_t ld_y, head_stride_y;
+    float *lse;
+    int chunk, splits;                  // tiles of keys of a split, at least
+    float *part_y, *part_lse;           // splits > 1: [splits][query rows][heads][dim], [splits][query rows][heads]
+    int32_t *errword;
+};
+
+template <int DP>
+constexpr int kStages = DP == 128 ? 4 : 8;
+template <int DP>
+constexpr int kTileBytes = DP / 64 * kPiece;
+template <int DP>
+constexpr int kSmem = (2 + kStages<DP>) * kTileBytes<DP> + 1024;
+
+// The keys of a unit: tiles of 128 from `base` on; tile t is of slot s if first[s] <= t < end[s].
+struct Range {
+    int base, begin, end;
+    int first[2], last[2];
+};
+__device__ __forceinline__ Range range_of(const ForwardArgs &p, const Unit &u)
+{
+    Range r;
+    int lo[2], hi[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+        keys_seen(p.mask, u.pos + s * p.queries, min(p.queries, u.rows - s * p.queries), u.shift, u.other_len, lo[s], hi[s]);
+    r.base = hi[0] == 0 ? lo[1] : hi[1] == 0 ? lo[0] : min(lo[0], lo[1]);
+    int from = 0, to = 0x7fffffff;                         // tiles of this split
+    if (p.splits > 1) {
+        const int tiles = (max(hi[0], hi[1]) - r.base + kRows - 1) >> 7;
+        const int chunk = max(p.chunk, (tiles + p.splits - 1) / p.splits);
+        from = blockIdx.z * chunk;
+        to = from + chunk;
+    }
+    r.begin = 0x7fffffff;
+    r.end = 0;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        r.first[s] = max(from, (lo[s] - r.base) >> 7);
+        r.last[s] = min(to, (hi[s] - r.base + kRows - 1) >> 7);
+        if (hi[s] == 0 || r.last[s] <= r.first[s]) {
+            r.first[s] = r.last[s] = 0;
+        } else {
+            r.begin = min(r.begin, r.first[s]);
+            r.end = max(r.end, r.last[s]);
+        }
+    }
+    if (r.end == 0) r.begin = 0;
+    return r;
+}
+
+template <int DP>
+__global__ void __launch_bounds__(kThreads, 1)
+attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                 const __grid_constant__ ForwardArgs p)
+{
+    constexpr int kStage = kStages<DP>, kTile = kTileBytes<DP>;
+    extern __shared__ uint8_t dyn_smem[];
+    __shared__ __align__(8) uint64_t q_full[2], full_bar[kStage], empty_bar[kStage], s_full[2], p_full[2], o_full;
+    __shared__ uint32_t tmem_base;
+    __shared__ volatile int failed;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t base = (smem_addr(dyn_smem) + 1023u) & ~1023u;
+    const uint32_t q_tile = base, ring = base + 2 * kTile;
+
+    if (threadIdx.x == 0) {
+        failed = 0;
+        for (int s = 0; s < 2; ++s) {
+            bar_init(smem_addr(&q_full[s]), 1);
+            bar_init(smem_addr(&s_full[s]), 1);
+            bar_init(smem_addr(&p_full[s]), 4);
+        }
+        bar_init(smem_addr(&o_full), 1);
+        for (int s = 0; s < kStage; ++s) {
+            bar_init(smem_addr(&full_bar[s]), 1);
+            bar_init(smem_addr(&empty_bar[s]), 1);
+        }
+        bar_init_fence();
+    }
+    if (warp == 8) tc_alloc(&tmem_base, 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_base;
+    grid_wait();
+    const int kv_head = (int)(blockIdx.x % p.kv_heads), head0 = kv_head * p.group;
+    Unit u;
+    const bool any = unit_of(p.runs, p.plan, false, blockIdx.x / p.kv_heads, u);
+    Range r;
+    if (any) r = range_of(p, u);
+
+    if (!any) {
+    } else if (warp >= 8) {
+        give_registers<kOtherRegisters>();
+        if (warp == 9) {
+            if (lane == 0 && r.end > 0) {
+                const uint32_t q_bytes = (uint32_t)p.queries * p.group * (DP * 2);
+    #pragma unroll
+                for (int s = 0; s < 2; ++s)
+                    if (r.last[s] > 0) {
+                        bar_expect(smem_addr(&q_full[s]), q_bytes);
+                        load_tile<DP>(q_tile + s * kTile, &map_q, smem_addr(&q_full[s]), head0, u.row + s * p.queries);
+                    }
+                int st = 0;
+                uint32_t phase = 1;
+                bool ok = true;
+                for (int t = r.begin; t < r.end && ok; ++t)
+    #pragma unroll
+                    for (int kv = 0; kv < 2; ++kv) {
+                        if (!bar_wait(smem_addr(&empty_bar[st]), phase, &failed)) { ok = false; break; }
+                        bar_expect(smem_addr(&full_bar[st]), kTile);
+                        load_tile<DP>(ring + st * kTile, kv ? &map_v : &map_k, smem_addr(&full_bar[st]), kv_head, u.other_row + r.base + t * kRows);
+                        if (++st == kStage) st = 0, phase ^= 1;
+                    }
+            }
+        } else if (warp == 8) {
+            const bool issuer = elect_one();
+            int st_k = 0, st_v = 1;                              // stages of K(t + 1) and V(t)
+            uint32_t ph_k = 0, ph_v = 0, ph_p[2] = {0, 0};
+            bool ok = r.end > 0;
+            for (int t = r.begin - 1; t < r.end && ok; ++t) {
+                const bool has_v = t >= r.begin, has_k = t + 1 < r.end;
+                const uint32_t tile_v = ring + st_v * kTile, tile_k = ring + st_k * kTile;
+                if (has_v) {
+                    if (!bar_wait_together(smem_addr(&full_bar[st_v]), ph_v, &failed)) break;
+                    const int live = u.other_len - (r.base + t * kRows);
+                    if (live < kRows) clear_rows<DP>(tile_v, live);
+                }
+                if (has_k && !bar_wait_together(smem_addr(&full_bar[st_k]), ph_k, &failed)) break;
+    #pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    if (has_v && t >= r.first[s] && t < r.last[s]) {
+                        if (!bar_wait_together(smem_addr(&p_full[s]), ph_p[s], &failed)) { ok = false; break; }
+                        ph_p[s] ^= 1;
+                        tc_fence_after();
+                        if (issuer) {
+    #pragma unroll
+                            for (int ks = 0; ks < kRows / 16; ++ks)
+                                product_step<DP>(tmem + 256 + s * DP, tmem + s * kRows + ks * 8, tile_v, ks, t > r.first[s] || ks > 0);
+                        }
+                        __syncwarp();
+                    }
+                    if (has_k && t + 1 >= r.first[s] && t + 1 < r.last[s]) {
+                        if (t + 1 == r.first[s] && !bar_wait_together(smem_addr(&q_full[s]), 0, &failed)) { ok = false; break; }
+                        tc_fence_after();
+                        if (issuer) {
+                            // (after the product that reads P in the same columns: the tensor cores work in order)
+                            product_of_tiles<DP>(tmem + s * kRows, q_tile + s * kTile, tile_k);
+                            tc_commit(smem_addr(&s_full[s]));
+                        }
+                        __syncwarp();
+                    }
+                }
+                if (!ok) break;
+                if (issuer) {
+                    if (has_v) tc_commit(smem_addr(&empty_bar[st_v]));
+                    if (has_k) tc_commit(smem_addr(&empty_bar[st_k]));
+                    if (t == r.end - 1) tc_commit(smem_addr(&o_full));
+                }
+                __syncwarp();
+                if (has_v && (st_v += 2) >= kStage) st_v -= kStage, ph_v ^= 1;
+                if (has_k && (st_k += 2) >= kStage) st_k -= kStage, ph_k ^= 1;
+            }
+        }
+    } else {
+        take_registers<kRowRegisters>();
+        const int slot = warp >> 2;
+        const int row = (warp & 3) * 32 + lane;                                  // of the tile
+        const int query = row / p.group;
+        const int i = slot * p.queries + query;                                  // of the unit
+        const bool live = query < p.queries && i < u.rows;
+        int lo = 0, hi = 0x7fffffff;                                             // (rows that nobody reads need no mask)
+        if (live) keys_seen(p.mask, u.pos + i, 1, u.shift, u.other_len, lo, hi);
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t s_at = tmem + lanes + slot * kRows, o_at = tmem + lanes + 256 + slot * DP;
+        const float c = p.scale_log2;
+        float most = -INFINITY, sum = 0.0f;                                      // the exponents' reference, and sum of exponentials
+        bool ok = true;
+        const int first = slot ? r.first[1] : r.first[0], last = slot ? r.last[1] : r.last[0];
+        for (int t = first; t < last; ++t) {
+            if (!bar_wait_together(smem_addr(&s_full[slot]), (t - first) & 1, &failed)) { ok = false; break; }
+            tc_fence_after();
+            float v[kRows];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) tc_read32(s_at + 32 * j, reinterpret_cast<uint32_t(&)[32]>(v[32 * j]));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) tc_read_wait(reinterpret_cast<uint32_t(&)[32]>(v[32 * j]));
+            const int key0 = r.base + t * kRows, from = lo - key0, to = hi - key0;
+            if (__any_sync(0xffffffffu, from > 0 || to < kRows)) {
+#pragma unroll
+                for (int j = 0; j < kRows; ++j) v[j] = j >= from && j < to ? v[j] : -INFINITY;
+            }
+            float m4[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+            for (int j = 4; j < kRows; j += 8) {
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+                    const float b = j + 4 + n < kRows ? v[(j + 4 + n) % kRows] : v[j + n];
+                    m4[n] = fmaxf(fmaxf(m4[n], v[j + n]), b);
+                }
+            }
+            const float top = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+            const bool raise = top > most && (most == -INFINITY || (top - most) * c > kSlack);
+            const float now = raise ? top : most;
+            const float zero = now == -INFINITY ? 0.0f : now;                    // a row that has seen nothing: exponentials of -inf
+            if (__any_sync(0xffffffffu, raise)) {
+                const float by = raise ? exp2_of(__fmul_rn(most == -INFINITY ? -INFINITY : __fsub_rn(most, now), c)) : 1.0f;
+                sum = __fmul_rn(sum, by);
+                if (t > first) {
+                    // the product in front of this tile's S has ended with it: O is complete
+#pragma unroll
+                    for (int j = 0; j < DP; j += 32) {
+                        uint32_t o[32];
+                        tc_read32(o_at + j, o);
+                        tc_read_wait(o);
+#pragma unroll
+                        for (int n = 0; n < 32; ++n) o[n] = __float_as_uint(__fmul_rn(__uint_as_float(o[n]), by));
+                        tc_write32(o_at + j, o);
+                    }
+                }
+                most = now;
+            }
+            const float minus = -__fmul_rn(zero, c);
+            const f2 cc = f2_of(c, c), mm = f2_of(minus, minus);
+            f2 sums[2] = {0, 0};
+#pragma unroll
+            for (int j = 0; j < kRows; j += 64) {
+                uint32_t w[32];
+#pragma unroll
+                for (int n = 0; n < 64; n += 2) {
+                    const f2 x = f2_fma(f2_of(v[j + n], v[j + n + 1]), cc, mm);
+                    const float a = exp2_of(f2_lo(x)), b = exp2_of(f2_hi(x));
+                    sums[(n >> 1) & 1] = f2_add(sums[(n >> 1) & 1], f2_of(a, b));
+                    w[n >> 1] = bf16_pair(a, b);
+                }
+                tc_write32(s_at + (j >> 1), w);
+            }
+            tc_write_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(smem_addr(&p_full[slot]));
+            const f2 both = f2_add(sums[0], sums[1]);
+            sum = __fadd_rn(sum, __fadd_rn(f2_lo(both), f2_hi(both)));
+        }
+        if (ok && r.end > 0 && !bar_wait_together(smem_addr(&o_full), 0, &failed)) ok = false;
+        if (ok) {
+            tc_fence_after();
+            const float inverse = sum > 0.0f ? __fdiv_rn(1.0f, sum) : sum == 0.0f ? 0.0f : sum;      // (a NaN stays one)
+            const int head = head0 + row - query * p.group;
+            const int64_t q = (int64_t)u.row + i;
+            const int64_t at = q * p.heads + head;
+            const float lse = sum == 0.0f ? -INFINITY : __fmul_rn(__fadd_rn(__fmul_rn(most, c), log2f(sum)), kLn2);
+            if (p.splits > 1) {
+                const int64_t all = p.runs.query_rows * p.heads;
+                if (live) p.part_lse[blockIdx.z * all + at] = lse;
+                float *out = p.part_y + (blockIdx.z * all + at) * p.dim;
+#pragma unroll
+                for (int j = 0; j < DP; j += 32) {
+                    uint32_t o[32];
+                    tc_read32(o_at + j, o);
+                    tc_read_wait(o);
+#pragma unroll
+                    for (int n = 0; n < 32; n += 4)
+                        if (live && j + n < p.dim) {
+                            float4 f = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                            if (last > 0) f = make_float4(__fmul_rn(__uint_as_float(o[n]), inverse), __fmul_rn(__uint_as_float(o[n + 1]), inverse),
+                                                          __fmul_rn(__uint_as_float(o[n + 2]), inverse), __fmul_rn(__uint_as_float(o[n + 3]), inverse));
+                            *reinterpret_cast<float4 *>(out + j + n) = f;
+                        }
+                }
+            } else {
+                if (live) p.lse[at] = lse;
+                __nv_bfloat16 *out = p.y + q * p.ld_y + head * p.head_stride_y;
+#pragma unroll
+                for (int j = 0; j < DP; j += 32) {
+                    uint32_t o[32];
+                    tc_read32(o_at + j, o);
+                    tc_read_wait(o);
+#pragma unroll
+                    for (int n = 0; n < 32; n += 8)
+                        if (live && j + n < p.dim) {
+                            float f[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) f[e] = last > 0 ? __fmul_rn(__uint_as_float(o[n + e]), inverse) : 0.0f;
+                            store_bf16x8(out + j + n, f);
+                        }
+                }
+            }
+        }
+    }
+    let_copies_land(&failed);
+    tc_fence_before();
+    __syncthreads();
+    if (threadIdx.x == 0 && failed) atomicExch(p.errword, 2);
+    if (warp == 8) tc_free(tmem, 512);
+}
+
+// The splits of a row and head joined: y = sum_z w_z y_z, w_z = exp(lse_z - lse).  A warp per row and head.
+__global__ void __launch_bounds__(256)
+join_kernel(const __grid_constant__ ForwardArgs p)
+{
+    grid_wait();
+    const int64_t all = p.runs.query_rows * p.heads, at = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 5;
+    const int lane = threadIdx.x & 31;
+    if (at >= all) return;
+    const int64_t q = at / p.heads;
+    const int head = (int)(at - q * p.heads);
+    if (p.runs.query_start) {                                 // rows in no sequence stay as they are
+        // (starts ascend: the row lies in a run if it lies between the first and the last)
+        if (q < max((int64_t)0, p.runs.query_start[0]) || q >= p.runs.query_start[p.runs.sequences]) return;
+    }
+    float most = -INFINITY;
+    for (int z = lane; z < p.splits; z += 32) most = fmaxf(most, p.part_lse[z * all + at]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+    const float zero = most == -INFINITY ? 0.0f : most;
+    float total = 0.0f, y[4] = {};
+    for (int z = 0; z < p.splits; ++z) {
+        const float lse = p.part_lse[z * all + at];
+        const float w = exp2_of(__fmul_rn(__fsub_rn(lse, zero), kLog2e));
+        total = __fadd_rn(total, w);
+        if (w != 0.0f && lane * 4 < p.dim) {
+            const float4 v = *reinterpret_cast<const float4 *>(p.part_y + (z * all + at) * p.dim + lane * 4);
+            y[0] = __fmaf_rn(w, v.x, y[0]);
+            y[1] = __fmaf_rn(w, v.y, y[1]);
+            y[2] = __fmaf_rn(w, v.z, y[2]);
+            y[3] = __fmaf_rn(w, v.w, y[3]);
+        }
+    }
+    const float inverse = total == 0.0f ? 0.0f : __fdiv_rn(1.0f, total);
+    if (lane * 4 < p.dim)
+        *reinterpret_cast<uint2 *>(p.y + q * p.ld_y + head * p.head_stride_y + lane * 4) =
+            make_uint2(bf16_pair(__fmul_rn(y[0], inverse), __fmul_rn(y[1], inverse)), bf16_pair(__fmul_rn(y[2], inverse), __fmul_rn(y[3], inverse)));
+    if (lane == 0) p.lse[at] = total == 0.0f ? -INFINITY : __fmaf_rn(log2f(total), kLn2, most);
+}
+
+// The table of units.  One CTA per table: units in front of every sequence's, then the units in the order of their work (the
+// order among equals varies from call to call; every unit is computed by itself, so results do not).
+struct PlanArgs {
+    Runs runs;
+    Mask mask;
+    Plan plan[2];
+    int by_key[2];
+};
+constexpr int kPlanThreads = 1024, kBins = 256;
+
+__device__ __forceinline__ int64_t start_of(const int64_t *start, int s, int64_t rows)
+{
+    const int64_t r = start[s];
+    return r < 0 ? 0 : r > rows ? rows : r;
+}
+__device__ __forceinline__ Unit unit_number(const PlanArgs &a, const Plan &plan, bool by_key, int e)
+{
+    int lo = 0, hi = a.runs.sequences;                        // prefix[lo] <= e < prefix[hi]
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (plan.prefix[mid] <= e) lo = mid;
+        else hi = mid;
+    }
+    const Runs &r = a.runs;
+    const int q0 = (int)start_of(r.query_start, lo, r.query_rows), q1 = (int)start_of(r.query_start, lo + 1, r.query_rows);
+    const int k0 = (int)start_of(r.key_start, lo, r.key_rows), k1 = (int)start_of(r.key_start, lo + 1, r.key_rows);
+    const int queries = max(0, q1 - q0), keys = max(0, k1 - k0);
+    Unit u;
+    u.pos = (e - plan.prefix[lo]) * plan.per;
+    u.row = (by_key ? k0 : q0) + u.pos;
+    u.rows = min(plan.per, (by_key ? keys : queries) - u.pos);
+    u.other_row = by_key ? q0 : k0;
+    u.other_len = by_key ? queries : keys;
+    u.shift = keys - queries;
+    return u;
+}
+__device__ __forceinline__ int work_of(const PlanArgs &a, bool by_key, const Unit &u)
+{
+    int lo, hi;
+    if (by_key) queries_seeing(a.mask, u.pos, u.rows, u.shift, u.other_len, lo, hi);
+    else keys_seen(a.mask, u.pos, u.rows, u.shift, u.other_len, lo, hi);
+    return (hi - lo + kRows - 1) / kRows;
+}
+
+__global__ void __launch_bounds__(kPlanThreads)
+plan_kernel(const __grid_constant__ PlanArgs a)
+{
+    __shared__ long long of_warp[32];
+    __shared__ int bins[kBins], most_work;
+    const bool by_key = a.by_key[blockIdx.x] != 0;
+    const Plan &plan = a.plan[blockIdx.x];
+    const int S = a.runs.sequences, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t *start = by_key ? a.runs.key_start : a.runs.query_start;
+    const int64_t rows = by_key ? a.runs.key_rows : a.runs.query_rows;
+    const int each = (S + kPlanThreads - 1) / kPlanThreads, from = min(S, (int)threadIdx.x * each), to = min(S, from + each);
+    long long mine = 0;
+    for (int s = from; s < to; ++s) mine += (max((int64_t)0, start_of(start, s + 1, rows) - start_of(start, s, rows)) + plan.per - 1) / plan.per;
+    long long before = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long v = __shfl_up_sync(0xffffffffu, before, o);
+        if (lane >= o) before += v;
+    }
+    if (lane == 31) of_warp[warp] = before;
+    if (threadIdx.x < kBins) bins[threadIdx.x] = 0;
+    if (threadIdx.x == 0) most_work = 0;
+    __syncthreads();
+    long long total = 0;
+    before -= mine;
+    for (int w = 0; w < kPlanThreads / 32; ++w) {
+        if (w < warp) before += of_warp[w];
+        total += of_warp[w];
+    }
+    // (starts that do not ascend could ask for more units than there is room for: those are left out)
+    const long long cap = plan.most;
+    for (int s = from; s < to; ++s) {
+        plan.prefix[s] = (int)min(before, cap);
+        before += (max((int64_t)0, start_of(start, s + 1, rows) - start_of(start, s, rows)) + plan.per - 1) / plan.per;
+    }
+    const int n = (int)min(total, cap);
+    if (threadIdx.x == 0) plan.prefix[S] = n, *plan.count = n;
+    __syncthreads();
+    int top = 0;
+    for (int e = threadIdx.x; e < n; e += kPlanThreads) top = max(top, work_of(a, by_key, unit_number(a, plan, by_key, e)));
+    atomicMax(&most_work, top);
+    __syncthreads();
+    const int shift = max(0, 24 - __clz(most_work | 1));      // most_work >> shift is below kBins
+    for (int e = threadIdx.x; e < n; e += kPlanThreads)
+        atomicAdd(&bins[kBins - 1 - (work_of(a, by_key, unit_number(a, plan, by_key, e)) >> shift)], 1);
+    __syncthreads();
+    if (warp == 0) {                                          // units in front of every bin
+        int sum = 0, of[kBins / 32];
+#pragma unroll
+        for (int i = 0; i < kBins / 32; ++i) {
+            of[i] = sum;
+            sum += bins[lane * (kBins / 32) + i];
+        }
+        int up = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, up, o);
+            if (lane >= o) up += v;
+        }
+#pragma unroll
+        for (int i = 0; i < kBins / 32; ++i) bins[lane * (kBins / 32) + i] = up - sum + of[i];
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < n; e += kPlanThreads) {
+        const Unit u = unit_number(a, plan, by_key, e);
+        plan.units[atomicAdd(&bins[kBins - 1 - (work_of(a, by_key, u) >> shift)], 1)] = u;
+    }
+}
+
+// How the keys are cut: only where the tiles of queries leave half of the SMs without work.  A split has at least `chunk` tiles of
+// keys: as many as give every SM a CTA if all sequences were of average length, two at least (a split's partial result is written
+// and read once more).  Longer sequences have more splits, up to four times the average's.
+struct Splits {
+    int chunk, splits;
+};
+Splits splits_of(const AttentionShape &a, int64_t units)
+{
+    const int64_t tiles = (a.key_rows + kRows - 1) / kRows, ctas = units * a.kv_heads, sms = 148;
+    if (ctas == 0 || ctas * 2 > sms || tiles < 4) return Splits{0, 1};
+    const int64_t average = (tiles + a.sequences - 1) / a.sequences;
+    int64_t chunk = (average * ctas + sms - 1) / sms;
+    if (chunk < 2) chunk = 2;
+    int64_t splits = (tiles + chunk - 1) / chunk;
+    const int64_t most = (a.query_start ? 4 : 1) * ((sms + ctas - 1) / ctas);
+    if (splits > most) splits = most;
+    return splits > 1 ? Splits{(int)chunk, (int)splits} : Splits{0, 1};
+}
+int queries_of_tile(const AttentionShape &a) { return kRows / (a.heads / a.kv_heads); }
+
+template <int DP>
+cudaError_t launch_forward(const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v, const ForwardArgs &p, bool dependent, cudaStream_t s)
+{
+    static OncePerDevice configured;
+    cudaError_t e = configured.run([&] { return cudaFuncSetAttribute(attention_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem<DP>); });
+    if (e != cudaSuccess) return e;
+    const dim3 grid((unsigned)(p.plan.most * p.kv_heads), 1, (unsigned)p.splits);
+    if (dependent) {
+        e = launch_dependent_smem(attention_kernel<DP>, grid, dim3(kThreads), kSmem<DP>, s, q, k, v, p);
+    } else {
+        attention_kernel<DP><<<grid, kThreads, kSmem<DP>, s>>>(q, k, v, p);
+        e = cudaGetLastError();
+    }
+    if (e == cudaSuccess) ++g_kernel_launches;
+    return e;
+}
+
+}  // namespace
+
+namespace attention {
+
+cudaError_t launch_plan(const Runs &runs, const Mask &mask, const Plan *queries, const Plan *keys, cudaStream_t s)
+{
+    PlanArgs a{};
+    a.runs = runs;
+    a.mask = mask;
+    int n = 0;
+    if (queries) a.plan[n] = *queries, a.by_key[n++] = 0;
+    if (keys) a.plan[n] = *keys, a.by_key[n++] = 1;
+    plan_kernel<<<n, kPlanThreads, 0, s>>>(a);
+    ++g_kernel_launches;
+    return cudaGetLastError();
+}
+
+}  // namespace attention
+
+// CTAs of a launch: one per unit and head of k and v
+bool attention_grid_fits(const AttentionShape &a)
+{
+    const int per = queries_of_tile(a);
+    return most_units(a.query_start, a.query_rows, per, a.sequences) <= 0x7fffffff / a.kv_heads &&
+           most_units(a.key_start, a.key_rows, kRows, a.sequences) <= 0x7fffffff / a.kv_heads;
+}
+
+size_t attention_scratch(const AttentionShape &a)
+{
+    const int per = 2 * queries_of_tile(a);
+    const Splits z = splits_of(a, most_units(a.query_start, a.query_rows, per, a.sequences));
+    size_t bytes = plan_bytes(a.query_start, a.query_rows, per, a.sequences);
+    if (z.splits > 1) bytes += (size_t)z.splits * a.query_rows * a.heads * ((size_t)a.dim + 1) * 4;
+    return bytes < 16 ? 16 : bytes;
+}
+
+cudaError_t launch_attention(const AttentionShape &a, const Heads &q, const Heads &k, const Heads &v, const Heads &y, float *lse, void *scratch,
+                             int32_t *errword, cudaStream_t s)
+{
+    const int group = a.heads / a.kv_heads, queries = queries_of_tile(a), per = 2 * queries;
+    char *at = static_cast<char *>(scratch);
+    ForwardArgs p{};
+    p.runs = Runs{a.query_start, a.key_start, a.sequences, a.query_rows, a.key_rows};
+    p.plan = plan_at(at, a.query_start, a.query_rows, per, a.sequences);
+    p.mask = Mask{a.causal, a.window};
+    p.heads = a.heads, p.kv_heads = a.kv_heads, p.group = group, p.dim = a.dim, p.queries = queries;
+    p.scale_log2 = (float)((double)a.scale * 1.4426950408889634);
+    p.y = static_cast<__nv_bfloat16 *>(y.p), p.ld_y = y.ld, p.head_stride_y = y.head_stride;
+    p.lse = lse, p.errword = errword;
+    const Splits z = splits_of(a, p.plan.most);
+    p.chunk = z.chunk, p.splits = z.splits;
+    p.part_y = reinterpret_cast<float *>(at + plan_bytes(a.query_start, a.query_rows, per, a.sequences));
+    p.part_lse = p.part_y + (size_t)z.splits * a.query_rows * a.heads * a.dim;
+    CUtensorMap mq, mk, mv;
+    cudaError_t e = make_heads_map(&mq, q.p, a.dim, a.heads, a.query_rows, q.head_stride, q.ld, group, queries);
+    if (e == cudaSuccess && a.key_rows > 0) e = make_heads_map(&mk, k.p, a.dim, a.kv_heads, a.key_rows, k.head_stride, k.ld, 1, kRows);
+    if (e == cudaSuccess && a.key_rows > 0) e = make_heads_map(&mv, v.p, a.dim, a.kv_heads, a.key_rows, v.head_stride, v.ld, 1, kRows);
+    if (e == cudaSuccess && a.query_start) e = launch_plan(p.runs, p.mask, &p.plan, nullptr, s);
+    if (e != cudaSuccess) return e;
+    e = a.dim <= 64 ? launch_forward<64>(mq, mk, mv, p, a.query_start != nullptr, s) : launch_forward<128>(mq, mk, mv, p, a.query_start != nullptr, s);
+    if (e != cudaSuccess || z.splits == 1) return e;
+    e = launch_dependent(join_kernel, dim3((unsigned)((a.query_rows * a.heads + 7) / 8)), dim3(256), s, p);
+    if (e == cudaSuccess) ++g_kernel_launches;
+    return e;
+}
+
+}  // namespace lgc

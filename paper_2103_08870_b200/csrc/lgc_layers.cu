@@ -3,8 +3,7 @@
 #include <cmath>
 #include <mutex>
 
-#include "lgc_layers.cuh"
-#include "lgc_tensor_core.cuh"
+#include "lgc_attention.cuh"
 
 namespace lgc {
 
@@ -93,6 +92,55 @@ const char *bad_nodes(const int64_t *node_start, int32_t num_nodes, int64_t per_
     return nullptr;
 }
 
+
+// The strides that a single row or head leaves open are filled in.
+const char *heads_of(const lgc_heads *h, int64_t rows, int32_t heads, int32_t dim, int elem_bytes, Heads &out)
+{
+    if (!h || !h->p) return "NULL operand of heads";
+    if (reinterpret_cast<uintptr_t>(h->p) % elem_bytes != 0) return "misaligned operand of heads";
+    const int64_t tight = ((int64_t)dim + 7) / 8 * 8;
+    out = Heads{h->p, rows > 1 ? h->ld : tight, heads > 1 ? h->head_stride : tight};
+    if (out.ld < dim || out.head_stride < dim || out.ld > ((int64_t)1 << 38) || out.head_stride > ((int64_t)1 << 38))
+        return "rows or heads overlap, or lie more than 2^38 elements apart";
+    if (rows > 1 && heads > 1) {
+        const bool by_row = out.ld >= out.head_stride;                   // rows are the outer dimension
+        const int64_t inner = by_row ? out.head_stride : out.ld, outer = by_row ? out.ld : out.head_stride, n = by_row ? heads : rows;
+        if ((outer - dim) / (n - 1) < inner) return "rows and heads overlap";
+    }
+    return nullptr;
+}
+// ... of bf16 that the TMA reads, or that is written 16 bytes at a time
+const char *tensor_heads_of(const lgc_heads *h, int64_t rows, int32_t heads, int32_t dim, Heads &out)
+{
+    const char *why = heads_of(h, rows, heads, dim, 2, out);
+    if (!why && ((reinterpret_cast<uintptr_t>(out.p) & 15) != 0 || out.ld % 8 != 0 || out.head_stride % 8 != 0))
+        why = "operands of attention must be 16-byte aligned, their strides multiples of 8";
+    return why;
+}
+lgc_status attention_shape_of(const char *where, const lgc_attention_shape *s, AttentionShape &a)
+{
+    if (!s) return refuse(where, "NULL shape");
+    if (s->query_rows < 0 || s->query_rows > kMaxRows || s->key_rows < 0 || s->key_rows > kMaxRows)
+        return refuse(where, "query_rows and key_rows must be in [0, 2^30]");
+    if (s->heads < 1 || s->kv_heads < 1 || s->heads % s->kv_heads != 0) return refuse(where, "heads must be a multiple of kv_heads");
+    if (s->dim < 8 || s->dim % 8 != 0) return refuse(where, "dim must be a multiple of 8");
+    if (s->dim > attention::kMostDim) return refuse(where, "dim above 128", LGC_ERR_UNSUPPORTED);
+    if (s->heads / s->kv_heads > attention::kRows) return refuse(where, "more than 128 heads share a head of k and v", LGC_ERR_UNSUPPORTED);
+    if (s->heads > 65536) return refuse(where, "more than 65536 heads", LGC_ERR_UNSUPPORTED);
+    if (s->num_sequences < 1 || s->num_sequences > (1 << 20)) return refuse(where, "num_sequences must be in [1, 2^20]");
+    if (!s->query_start && (s->num_sequences != 1 || s->key_start)) return refuse(where, "query_start is NULL with several sequences or a key_start");
+    if (s->query_start && !s->key_start && s->query_rows != s->key_rows) return refuse(where, "key_start is NULL and query_rows is not key_rows");
+    if (((reinterpret_cast<uintptr_t>(s->query_start) | reinterpret_cast<uintptr_t>(s->key_start)) & 7) != 0) return refuse(where, "misaligned starts");
+    if (s->causal != 0 && s->causal != 1) return refuse(where, "causal must be 0 or 1");
+    if (s->window < 0 || (s->window > 0 && !s->causal)) return refuse(where, "window must not be negative, and goes with causal");
+    if (!(s->scale >= 0x1p-100f && s->scale <= 0x1p100f)) return refuse(where, "scale must be in [2^-100, 2^100]");
+    a = AttentionShape{s->query_rows, s->key_rows, s->heads, s->kv_heads, s->dim, s->query_start, s->key_start ? s->key_start : s->query_start,
+                       s->num_sequences, s->causal, s->window > kMaxRows ? 0 : (int)s->window, s->scale};
+    if (!attention_grid_fits(a)) return refuse(where, "more than 2^31 - 1 tiles", LGC_ERR_UNSUPPORTED);
+    return LGC_OK;
+}
+const char *bad_scratch(const void *scratch) { return !scratch || (reinterpret_cast<uintptr_t>(scratch) & 15) != 0 ? "scratch is NULL or not 16-byte aligned" : nullptr; }
+
 }  // namespace
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
@@ -129,6 +177,22 @@ cudaError_t make_matrix_map(CUtensorMap *m, CUtensorMapDataType type, int elem_b
     const cuuint32_t es[2] = {1, 1};
     return enc(m, type, 2, const_cast<void *>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+               ? cudaSuccess
+               : cudaErrorInvalidValue;
+}
+
+cudaError_t make_heads_map(CUtensorMap *m, const void *base, int64_t dim, int64_t heads, int64_t rows, int64_t head_stride, int64_t ld,
+                           int box_heads, int box_rows)
+{
+    EncodeTiledFn enc;
+    const cudaError_t e = encode_fn(&enc);
+    if (e != cudaSuccess) return e;
+    const cuuint64_t dims[3] = {(cuuint64_t)dim, (cuuint64_t)heads, (cuuint64_t)rows};
+    const cuuint64_t strides[2] = {(cuuint64_t)head_stride * 2, (cuuint64_t)ld * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_rows};
+    const cuuint32_t es[3] = {1, 1, 1};
+    return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
                ? cudaSuccess
                : cudaErrorInvalidValue;
 }
@@ -272,6 +336,96 @@ lgc_status lgc_weight_gradient(const void *dy, int64_t ld_dy, const lgc_packed *
     if (e == cudaSuccess)
         e = launch_weight_gradient(dy, ld_dy, *x, num_rows, num_cols, inner, node_start, num_nodes, dw, node_stride, scratch, record,
                                    static_cast<cudaStream_t>(stream));
+    return done(where, e);
+}
+
+lgc_status lgc_rotary(const lgc_heads *x, int32_t type, int64_t num_rows, int32_t heads, int32_t dim, const int64_t *positions,
+                      const double *frequencies, int32_t num_pairs, int32_t interleaved, float amplitude, int32_t backward, const lgc_heads *y,
+                      void *stream)
+{
+    const char *where = "lgc_rotary", *why = nullptr;
+    if (num_rows < 0 || num_rows > kMaxRows) return refuse(where, "num_rows must be in [0, 2^30]");
+    if (heads < 1 || heads > 65536 || dim < 2 || dim > 65536) return refuse(where, "heads must be in [1, 65536], dim in [2, 65536]");
+    if (num_pairs < 1 || num_pairs > dim / 2) return refuse(where, "num_pairs must be in [1, dim / 2]");
+    if (type != LGC_TYPE_FP32 && type != LGC_TYPE_BF16) return refuse(where, "heads are fp32 or bf16");
+    if ((interleaved != 0 && interleaved != 1) || (backward != 0 && backward != 1)) return refuse(where, "interleaved and backward must be 0 or 1");
+    if (num_rows == 0) return LGC_OK;
+    Heads hx, hy;
+    const int size = type == LGC_TYPE_FP32 ? 4 : 2;
+    if ((why = heads_of(x, num_rows, heads, dim, size, hx)) || (why = heads_of(y, num_rows, heads, dim, size, hy))) return refuse(where, why);
+    if (hx.p == hy.p && (hx.ld != hy.ld || hx.head_stride != hy.head_stride)) return refuse(where, "y lies in x with other strides");
+    if (!positions || !frequencies || ((reinterpret_cast<uintptr_t>(positions) | reinterpret_cast<uintptr_t>(frequencies)) & 7) != 0)
+        return refuse(where, "NULL or misaligned positions or frequencies");
+    return done(where, launch_rotary(hx.p, type, num_rows, heads, dim, hx.ld, hx.head_stride, positions, frequencies, num_pairs, interleaved != 0,
+                                     amplitude, backward != 0, hy.p, hy.ld, hy.head_stride, static_cast<cudaStream_t>(stream)));
+}
+
+lgc_status lgc_attention_scratch(const lgc_attention_shape *shape, size_t *bytes)
+{
+    const char *where = "lgc_attention_scratch";
+    AttentionShape a;
+    const lgc_status st = attention_shape_of(where, shape, a);
+    if (st != LGC_OK) return st;
+    if (!bytes) return refuse(where, "NULL result");
+    *bytes = attention_scratch(a);
+    return LGC_OK;
+}
+
+lgc_status lgc_attention(const lgc_attention_shape *shape, const lgc_heads *q, const lgc_heads *k, const lgc_heads *v, const lgc_heads *y,
+                         float *lse, void *scratch, size_t scratch_bytes, void *stream)
+{
+    const char *where = "lgc_attention", *why = nullptr;
+    AttentionShape a;
+    const lgc_status st = attention_shape_of(where, shape, a);
+    if (st != LGC_OK) return st;
+    if (a.query_rows == 0) return LGC_OK;
+    Heads hq, hk{}, hv{}, hy;
+    if ((why = tensor_heads_of(q, a.query_rows, a.heads, a.dim, hq)) || (why = tensor_heads_of(y, a.query_rows, a.heads, a.dim, hy)) ||
+        (a.key_rows > 0 && ((why = tensor_heads_of(k, a.key_rows, a.kv_heads, a.dim, hk)) || (why = tensor_heads_of(v, a.key_rows, a.kv_heads, a.dim, hv)))))
+        return refuse(where, why);
+    if (!aligned4(lse)) return refuse(where, "NULL or misaligned lse");
+    if ((why = bad_scratch(scratch))) return refuse(where, why);
+    if (scratch_bytes < attention_scratch(a)) return refuse(where, "scratch is smaller than lgc_attention_scratch says", LGC_ERR_WORKSPACE);
+    int32_t *record = nullptr;
+    cudaError_t e = record_address(&record);
+    if (e == cudaSuccess) e = launch_attention(a, hq, hk, hv, hy, lse, scratch, record, static_cast<cudaStream_t>(stream));
+    return done(where, e);
+}
+
+lgc_status lgc_attention_backward_scratch(const lgc_attention_shape *shape, size_t *bytes)
+{
+    const char *where = "lgc_attention_backward_scratch";
+    AttentionShape a;
+    const lgc_status st = attention_shape_of(where, shape, a);
+    if (st != LGC_OK) return st;
+    if (!bytes) return refuse(where, "NULL result");
+    *bytes = attention_backward_scratch(a);
+    return LGC_OK;
+}
+
+lgc_status lgc_attention_backward(const lgc_attention_shape *shape, const lgc_heads *dy, const lgc_heads *q, const lgc_heads *k, const lgc_heads *v,
+                                  const lgc_heads *y, const float *lse, const lgc_heads *dq, const lgc_heads *dk, const lgc_heads *dv, void *scratch,
+                                  size_t scratch_bytes, void *stream)
+{
+    const char *where = "lgc_attention_backward", *why = nullptr;
+    AttentionShape a;
+    const lgc_status st = attention_shape_of(where, shape, a);
+    if (st != LGC_OK) return st;
+    if (a.query_rows == 0 && a.key_rows == 0) return LGC_OK;
+    Heads h[8] = {};                      // dy, q, y, dq; k, v, dk, dv
+    const lgc_heads *by_query[4] = {dy, q, y, dq}, *by_key[4] = {k, v, dk, dv};
+    for (int i = 0; i < 4; ++i)
+        if ((a.query_rows > 0 && (why = tensor_heads_of(by_query[i], a.query_rows, a.heads, a.dim, h[i]))) ||
+            (a.key_rows > 0 && (why = tensor_heads_of(by_key[i], a.key_rows, a.kv_heads, a.dim, h[4 + i]))))
+            return refuse(where, why);
+    if (a.query_rows > 0 && !aligned4(lse)) return refuse(where, "NULL or misaligned lse");
+    if ((why = bad_scratch(scratch))) return refuse(where, why);
+    if (scratch_bytes < attention_backward_scratch(a))
+        return refuse(where, "scratch is smaller than lgc_attention_backward_scratch says", LGC_ERR_WORKSPACE);
+    int32_t *record = nullptr;
+    cudaError_t e = record_address(&record);
+    if (e == cudaSuccess)
+        e = launch_attention_backward(a, h[0], h[1], h[4], h[5], h[2], lse, h[3], h[6], h[7], scratch, record, static_cast<cudaStream_t>(stream));
     return done(where, e);
 }
 

@@ -1,5 +1,5 @@
-"""Layer operators in front of the gradient compression: layer norm, 8-bit checkpoints, block-scaled 8-bit products and
-per-node weight gradients (binding of the section "layer operators" of include/lgc.h: argument checks and marshalling
+"""Layer operators in front of the gradient compression: layer norm, 8-bit checkpoints, block-scaled 8-bit products,
+per-node weight gradients, rotary positions and attention over sequences (binding of the section "layer operators" of include/lgc.h: argument checks and marshalling
 only).
 
 The K nodes' tokens are K runs of rows of one activation matrix; node k has rows ``node_start[k] .. node_start[k+1]-1``.
@@ -14,6 +14,15 @@ Gradients of weights come out per node, in views of the ``[K][N]`` gradients tha
     layers.weight_gradient(dz, h8, grads[:, at:at + n], node_start=starts)   # dW of every node into its row
     layers.layer_norm_backward(dh, x, gamma, mean, rstd, dx, grads[:, g0:g1], grads[:, b0:b1], node_start=starts)
 
+Attention reads its heads where the linear layer in front left them; sequences are runs of rows, like the nodes'::
+
+    q, k, v = (qkv[:, a:b].unflatten(1, (-1, dim)) for a, b in ...)          # views, [rows][heads][dim]
+    layers.rotary(qk, positions, layers.rotary_frequencies(dim), qk)         # the heads of q and k, in place
+    layers.attention(q, k, v, y, lse, query_start=starts)
+    ...
+    layers.attention_backward(dy, q, k, v, y, lse, dq, dk, dv, query_start=starts)
+    layers.rotary(dqk, positions, frequencies, dqk, backward=True)
+
 Outputs are the caller's tensors; a call enqueues on ``stream`` (default: the current stream) and returns.  With a ``stream``
 of the caller's, the order against other streams and the tensors' lifetime until the stream is done (``record_stream``) are
 the caller's too; scratch that a call allocates belongs to that stream.  A call runs on the current device and refuses
@@ -23,6 +32,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes as C
+import math
 from typing import Optional, Union
 
 import torch
@@ -258,6 +268,150 @@ def weight_gradient(dy: torch.Tensor, x: Packed, dw: torch.Tensor, node_start: O
     scratch, size = _scratch(weight_gradient_scratch(rows, cols, inner, K), scratch, stream, dy)
     _done(lgc.lib().lgc_weight_gradient(dy.data_ptr(), ld_dy, xp, rows, cols, inner, start, K, dw.data_ptr(), stride, scratch.data_ptr(), size,
                                         _stream(stream, device)), "lgc_weight_gradient")
+
+
+def rotary_frequencies(rotary_dim: int, base: float = 10000.0, interpolation: float = 1.0, context: int = 0, slow_turns: float = 1.0,
+                       fast_turns: float = 32.0, device: Optional[torch.device] = None) -> torch.Tensor:
+    """Radians per position of the `rotary_dim / 2` pairs (fp64): base ^ (-2 i / rotary_dim).  For contexts `interpolation` times as
+    long as the trained ones: with context = 0 every frequency is divided by it; with `context`, the trained length, pairs that turn
+    at least `fast_turns` times in it keep their frequency, those that turn at most `slow_turns` times are divided, and a ramp lies
+    in between."""
+    if rotary_dim < 2 or rotary_dim % 2:
+        raise ValueError("rotary_dim: an even number of entries")
+    if not (base > 0 and interpolation >= 1 and context >= 0 and fast_turns > slow_turns):
+        raise ValueError("need base > 0, interpolation >= 1, context >= 0, fast_turns > slow_turns")
+    f = float(base) ** (-torch.arange(0, rotary_dim, 2, dtype=torch.float64) / rotary_dim)
+    if context:
+        keep = ((context * f / (2 * math.pi) - slow_turns) / (fast_turns - slow_turns)).clamp(0, 1)
+    else:
+        keep = torch.zeros_like(f)
+    return (f * (keep + (1 - keep) / interpolation)).to(device if device is not None else torch.device("cuda"))
+
+
+def _heads(t: torch.Tensor, name: str, device: int, want: Optional[tuple] = None, kinds=(TYPE_BF16,)):
+    """A [rows][heads][dim] argument for the library, after the checks that need the tensor: (struct, shape, type)."""
+    shape, kind = t.shape, _TYPES.get(t.dtype)
+    if kind not in kinds or len(shape) != 3 or t.get_device() != device:
+        raise ValueError(f"{name}: need a [rows][heads][dim] {'bf16' if len(kinds) == 1 else 'fp32 or bf16'} tensor on cuda:{device}")
+    ld, head, unit = t.stride()
+    if unit != 1 and shape[2] > 1:
+        raise ValueError(f"{name}: need unit stride along a head")
+    if want is not None and tuple(shape) != want:
+        raise ValueError(f"{name}: need {want[0]} x {want[1]} x {want[2]} elements, got {tuple(shape)}")
+    return lgc.lgc_heads(t.data_ptr(), ld, head), shape, kind
+
+
+def rotary(x: torch.Tensor, positions: torch.Tensor, frequencies: torch.Tensor, y: torch.Tensor, interleaved: bool = False, amplitude: float = 1.0,
+           backward: bool = False, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Turns the pairs of the first 2 * len(frequencies) entries of every head of `x` ([rows][heads][dim], fp32 or bf16) by
+    positions[row] (int64) * frequencies[pair] (fp64), times `amplitude`, into `y` (x's type; `x` itself for in place); the
+    rest of a head passes through.  Pairs: neighbours (`interleaved`), or entry i and entry i + len(frequencies).  `backward`: the
+    gradient's way back."""
+    device = _device(x.get_device(), stream)
+    hx, shape, kind = _heads(x, "x", device, None, (TYPE_FP32, TYPE_BF16))
+    hy, _, ykind = _heads(y, "y", device, tuple(shape), (TYPE_FP32, TYPE_BF16))
+    if ykind != kind:
+        raise ValueError("y: need x's type")
+    rows, heads, dim = shape
+    if not (positions.get_device() == device and positions.dtype is torch.int64 and positions.is_contiguous() and positions.numel() == rows):
+        raise ValueError(f"positions: need a contiguous int64 tensor of {rows} elements on cuda:{device}")
+    if not (frequencies.get_device() == device and frequencies.dtype is torch.float64 and frequencies.is_contiguous() and frequencies.dim() == 1):
+        raise ValueError(f"frequencies: need a contiguous 1-D fp64 tensor on cuda:{device}")
+    _done(lgc.lib().lgc_rotary(C.byref(hx), kind, rows, heads, dim, positions.data_ptr(), frequencies.data_ptr(), frequencies.numel(),
+                               1 if interleaved else 0, amplitude, 1 if backward else 0, C.byref(hy), _stream(stream, device)), "lgc_rotary")
+
+
+def _starts(t: Optional[torch.Tensor], name: str, device: int, n: Optional[int] = None):
+    if not (t.get_device() == device and t.dtype is torch.int64 and t.is_contiguous() and t.dim() == 1 and (t.numel() == n if n is not None else t.numel() > 1)):
+        raise ValueError(f"{name}: need a contiguous int64 tensor of {n if n is not None else 'sequences + 1'} elements on cuda:{device}")
+    return t.data_ptr()
+
+
+def _attention_shape(q_shape, k_shape, query_start, key_start, causal: bool, window: int, scale: Optional[float], device: int):
+    rows, heads, dim = q_shape
+    keys, kv_heads, _ = k_shape
+    if query_start is None and key_start is not None:
+        raise ValueError("key_start: goes with query_start")
+    qs = ks = None
+    sequences = 1
+    if query_start is not None:
+        qs, sequences = _starts(query_start, "query_start", device), query_start.numel() - 1
+        if key_start is not None:
+            ks = _starts(key_start, "key_start", device, sequences + 1)
+    return lgc.lgc_attention_shape(rows, keys, heads, kv_heads, dim, sequences, qs, ks, 1 if causal else 0, window,
+                                   scale if scale is not None else 1.0 / math.sqrt(dim) if dim else 1.0)
+
+
+def _attention_room(name: str, shape, scratch, stream, like):
+    n = C.c_size_t()
+    _done(getattr(lgc.lib(), name)(C.byref(shape), C.byref(n)), name)
+    return _scratch(n.value, scratch, stream, like)
+
+
+def _sizes_only(query_rows, key_rows, heads, kv_heads, dim, num_sequences):
+    # (the sizes need to know that there are starts, not where)
+    at = 8 if num_sequences else None
+    return lgc.lgc_attention_shape(query_rows, key_rows, heads, kv_heads, dim, num_sequences or 1, at, at, 0, 0, 1.0)
+
+
+def attention_scratch(query_rows: int, key_rows: int, heads: int, kv_heads: int, dim: int, num_sequences: int = 0) -> int:
+    """Bytes of scratch that attention needs.  num_sequences: 0 without query_start."""
+    n, shape = C.c_size_t(), _sizes_only(query_rows, key_rows, heads, kv_heads, dim, num_sequences)
+    _done(lgc.lib().lgc_attention_scratch(C.byref(shape), C.byref(n)), "lgc_attention_scratch")
+    return n.value
+
+
+def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, y: torch.Tensor, lse: torch.Tensor, query_start: Optional[torch.Tensor] = None,
+              key_start: Optional[torch.Tensor] = None, causal: bool = True, window: int = 0, scale: Optional[float] = None,
+              scratch: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """y = softmax(scale q k^T) v within every sequence, and `lse` (fp32 [rows][heads]), the logarithm of the softmax's denominator,
+    for the backward pass.  q, y: bf16 [query rows][heads][dim]; k, v: bf16 [key rows][kv_heads][dim], kv_heads dividing heads.
+    `query_start`, `key_start` (int64 [sequences + 1]): where the sequences' rows start; None: one sequence; key_start
+    None: as the queries.  `causal`: the last query of a sequence sees all of its keys, the one before one less, ...;
+    `window` (0: none): of those only the last ones.  `scale`: 1 / sqrt(dim) by default.  A query that sees no key has y = 0,
+    lse = -inf.  `scratch`: a uint8 tensor of attention_scratch bytes; without one it comes from PyTorch's allocator."""
+    device = _device(q.get_device(), stream)
+    hq, qshape, _ = _heads(q, "q", device)
+    hk, kshape, _ = _heads(k, "k", device)
+    if kshape[2] != qshape[2]:
+        raise ValueError(f"k: need heads of {qshape[2]} elements")
+    hv, _, _ = _heads(v, "v", device, tuple(kshape))
+    hy, _, _ = _heads(y, "y", device, tuple(qshape))
+    shape = _attention_shape(qshape, kshape, query_start, key_start, causal, window, scale, device)
+    lp = _vector(lse, qshape[0] * qshape[1], "lse", device)
+    scratch, size = _attention_room("lgc_attention_scratch", shape, scratch, stream, q)
+    _done(lgc.lib().lgc_attention(C.byref(shape), C.byref(hq), C.byref(hk), C.byref(hv), C.byref(hy), lp, scratch.data_ptr(), size,
+                                  _stream(stream, device)), "lgc_attention")
+
+
+def attention_backward_scratch(query_rows: int, key_rows: int, heads: int, kv_heads: int, dim: int, num_sequences: int = 0) -> int:
+    """Bytes of scratch that attention_backward needs.  num_sequences: 0 without query_start."""
+    n, shape = C.c_size_t(), _sizes_only(query_rows, key_rows, heads, kv_heads, dim, num_sequences)
+    _done(lgc.lib().lgc_attention_backward_scratch(C.byref(shape), C.byref(n)), "lgc_attention_backward_scratch")
+    return n.value
+
+
+def attention_backward(dy: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, y: torch.Tensor, lse: torch.Tensor, dq: torch.Tensor,
+                       dk: torch.Tensor, dv: torch.Tensor, query_start: Optional[torch.Tensor] = None, key_start: Optional[torch.Tensor] = None,
+                       causal: bool = True, window: int = 0, scale: Optional[float] = None, scratch: Optional[torch.Tensor] = None,
+                       stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Backward pass of attention: from dy and the forward pass' operands and results (and its other arguments) the gradients dq,
+    dk, dv (bf16, like q, k, v); dk and dv are summed over the heads that share a head of k and v.  The same call gives the
+    same bits.  `scratch`: a uint8 tensor of attention_backward_scratch bytes; without one it comes from PyTorch's allocator."""
+    device = _device(dy.get_device(), stream)
+    hdy, qshape, _ = _heads(dy, "dy", device)
+    qshape = tuple(qshape)
+    hk, kshape, _ = _heads(k, "k", device)
+    kshape = tuple(kshape)
+    if kshape[2] != qshape[2]:
+        raise ValueError(f"k: need heads of {qshape[2]} elements")
+    hq, hy, hdq = (_heads(t, name, device, qshape)[0] for t, name in ((q, "q"), (y, "y"), (dq, "dq")))
+    hv, hdk, hdv = (_heads(t, name, device, kshape)[0] for t, name in ((v, "v"), (dk, "dk"), (dv, "dv")))
+    shape = _attention_shape(qshape, kshape, query_start, key_start, causal, window, scale, device)
+    lp = _vector(lse, qshape[0] * qshape[1], "lse", device)
+    scratch, size = _attention_room("lgc_attention_backward_scratch", shape, scratch, stream, dy)
+    _done(lgc.lib().lgc_attention_backward(C.byref(shape), C.byref(hdy), C.byref(hq), C.byref(hk), C.byref(hv), C.byref(hy), lp, C.byref(hdq),
+                                           C.byref(hdk), C.byref(hdv), scratch.data_ptr(), size, _stream(stream, device)), "lgc_attention_backward")
 
 
 def check(stream: Optional[torch.cuda.Stream] = None) -> None:

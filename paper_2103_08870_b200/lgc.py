@@ -30,6 +30,7 @@ EXPORTS = (
     "lgc_selection_stats",
     "lgc_pack", "lgc_unpack", "lgc_layer_norm", "lgc_layer_norm_backward_scratch", "lgc_layer_norm_backward", "lgc_product",
     "lgc_weight_gradient_scratch", "lgc_weight_gradient", "lgc_layers_check",
+    "lgc_rotary", "lgc_attention_scratch", "lgc_attention", "lgc_attention_backward_scratch", "lgc_attention_backward",
 )
 NOALLOC_MAX_N = 16777216
 
@@ -46,6 +47,18 @@ class lgc_config(C.Structure):
 
 class lgc_packed(C.Structure):
     _fields_ = [("codes", C.c_void_p), ("ld", C.c_int64), ("scales", C.c_void_p), ("ld_scales", C.c_int64)]
+
+
+class lgc_heads(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("ld", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class lgc_attention_shape(C.Structure):
+    _fields_ = [
+        ("query_rows", C.c_int64), ("key_rows", C.c_int64), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("dim", C.c_int32),
+        ("num_sequences", C.c_int32), ("query_start", C.c_void_p), ("key_start", C.c_void_p), ("causal", C.c_int32), ("window", C.c_int64),
+        ("scale", C.c_float),
+    ]
 
 
 _lib = None
@@ -102,6 +115,12 @@ def lib() -> C.CDLL:
         l.lgc_weight_gradient_scratch.argtypes = [i64, i64, i64, i32, C.POINTER(sz)]
         l.lgc_weight_gradient.argtypes = [vp, i64, pk, i64, i64, i64, vp, i32, vp, i64, vp, sz, vp]
         l.lgc_layers_check.argtypes = [vp]
+        hd, sh = C.POINTER(lgc_heads), C.POINTER(lgc_attention_shape)
+        l.lgc_rotary.argtypes = [hd, i32, i64, i32, i32, vp, vp, i32, i32, f32, i32, hd, vp]
+        l.lgc_attention_scratch.argtypes = [sh, C.POINTER(sz)]
+        l.lgc_attention.argtypes = [sh, hd, hd, hd, hd, vp, vp, sz, vp]
+        l.lgc_attention_backward_scratch.argtypes = [sh, C.POINTER(sz)]
+        l.lgc_attention_backward.argtypes = [sh, hd, hd, hd, hd, hd, vp, hd, hd, hd, vp, sz, vp]
         for name in EXPORTS:            # every declared entry point must be exported
             getattr(l, name)
         _lib = l

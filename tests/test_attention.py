@@ -1,0 +1,119 @@
+"""The attention layer's operators without a GPU: the plain 64-bit forms that the kernels are tested against, and what the library
+refuses on the host before it enqueues anything."""
+import ctypes as C
+import math
+
+import pytest
+import torch
+
+import attention_reference as R
+from paper_2103_08870_b200 import build as B
+from paper_2103_08870_b200 import lgc
+
+OK, INVALID, WORKSPACE, UNSUPPORTED = 0, 1, 3, 4
+
+
+@pytest.fixture(scope="module")
+def lib():
+    B.build()
+    return lgc.lib()
+
+
+def test_reference_attention_and_its_gradient():
+    g = torch.Generator().manual_seed(0)
+    r = lambda *s: torch.randn(*s, generator=g, dtype=torch.float64)  # noqa: E731
+    q, k, v, dy = r(30, 4, 8).requires_grad_(), r(41, 2, 8).requires_grad_(), r(41, 2, 8).requires_grad_(), r(30, 4, 8)
+    starts = dict(query_start=[0, 10, 10, 30], key_start=[0, 13, 20, 41])
+    for causal, window in ((False, 0), (True, 0), (True, 5)):
+        y, lse, _, _ = R.attention(q, k, v, causal=causal, window=window, **starts)
+        for q0, q1, k0, k1 in ((0, 10, 0, 13), (10, 30, 20, 41)):
+            seen = ~R.hidden(q1 - q0, k1 - k0, causal, window, "cpu")
+            want = torch.nn.functional.scaled_dot_product_attention(
+                q[q0:q1].transpose(0, 1), k[k0:k1].transpose(0, 1).repeat_interleave(2, 0), v[k0:k1].transpose(0, 1).repeat_interleave(2, 0), attn_mask=seen)
+            assert torch.allclose(y[q0:q1], want.transpose(0, 1), atol=1e-12)
+        grads = torch.autograd.grad((y * dy).sum(), [q, k, v], allow_unused=True)
+        got, _ = R.attention_backward(dy, q.detach(), k.detach(), v.detach(), y.detach(), lse.detach(), causal=causal, window=window, **starts)
+        for a, b in zip(got, grads):
+            assert torch.allclose(a, b, atol=1e-11)
+
+
+def test_reference_rotary():
+    x, f = torch.randn(5, 2, 10, dtype=torch.float64), torch.tensor([0.5, 0.01, 2.0], dtype=torch.float64)
+    p = torch.tensor([0, 1, 7, -3, 1000])
+    for interleaved in (False, True):
+        y = R.rotary(x, p, f, interleaved)
+        assert torch.equal(y[0], x[0]) and torch.equal(y[..., 6:], x[..., 6:])
+        assert torch.allclose(R.rotary(y, p, f, interleaved, backward=True), x, atol=1e-12)
+        i, j = (2, 3) if interleaved else (1, 4)
+        z = torch.complex(x[2, 1, i], x[2, 1, j]) * torch.exp(torch.tensor(7 * 0.01j, dtype=torch.complex128))
+        assert abs(y[2, 1, i] - z.real) < 1e-12 and abs(y[2, 1, j] - z.imag) < 1e-12
+
+
+def heads(p=4096, ld=512, head_stride=64):
+    return C.byref(lgc.lgc_heads(p, ld, head_stride))
+
+
+def shape(**kw):
+    d = dict(query_rows=40, key_rows=40, heads=8, kv_heads=8, dim=64, num_sequences=1, query_start=None, key_start=None, causal=1, window=0, scale=0.125)
+    d.update(kw)
+    return C.byref(lgc.lgc_attention_shape(*[d[n] for n, _ in lgc.lgc_attention_shape._fields_]))
+
+
+BAD_SHAPES = [
+    (dict(query_rows=-1), INVALID), (dict(key_rows=(1 << 30) + 1), INVALID), (dict(heads=0), INVALID), (dict(kv_heads=3), INVALID), (dict(kv_heads=0), INVALID),
+    (dict(dim=0), INVALID), (dict(dim=60), INVALID), (dict(dim=136), UNSUPPORTED), (dict(heads=129, kv_heads=1), UNSUPPORTED), (dict(heads=1 << 17, kv_heads=1 << 17), UNSUPPORTED),
+    (dict(num_sequences=0), INVALID), (dict(num_sequences=2), INVALID), (dict(key_start=4096), INVALID), (dict(query_start=4096, key_rows=41), INVALID),
+    (dict(query_start=4100), INVALID), (dict(query_start=4096, num_sequences=(1 << 20) + 1), INVALID), (dict(causal=2), INVALID), (dict(window=-1), INVALID),
+    (dict(window=3, causal=0), INVALID), (dict(scale=0.0), INVALID), (dict(scale=-1.0), INVALID), (dict(scale=math.nan), INVALID), (dict(scale=math.inf), INVALID),
+    (dict(query_rows=1 << 30, heads=8192, kv_heads=64, key_rows=1), UNSUPPORTED),
+]
+
+
+def test_refused_on_the_host(lib):
+    """Made-up device addresses: a call that is refused never uses them."""
+    n = C.c_size_t()
+    P, much = 4096, 1 << 40
+    fwd = lambda s=shape(), q=heads(), k=heads(), v=heads(), y=heads(), lse=P, scratch=P, size=much: lib.lgc_attention(s, q, k, v, y, lse, scratch, size, None)  # noqa: E731
+    def bwd(s=shape(), h=None, lse=P, scratch=P, size=much, at=-1):
+        ops = [heads() for _ in range(8)]
+        if at >= 0:
+            ops[at] = h
+        return lib.lgc_attention_backward(s, *ops[:5], lse, *ops[5:], scratch, size, None)
+    for kw, status in BAD_SHAPES:
+        for call in (lib.lgc_attention_scratch, lib.lgc_attention_backward_scratch):
+            assert call(shape(**kw), C.byref(n)) == status, kw
+        assert fwd(shape(**kw)) == status and bwd(shape(**kw)) == status, kw
+    assert lib.lgc_attention_scratch(None, C.byref(n)) == INVALID and lib.lgc_attention_scratch(shape(), None) == INVALID
+    assert lib.lgc_attention_backward_scratch(shape(), None) == INVALID
+    bad_heads = [None, heads(p=None), heads(p=4104), heads(ld=500), heads(head_stride=60), heads(ld=0), heads(head_stride=0), heads(ld=504), heads(ld=64, head_stride=64),
+                 heads(ld=1 << 39), heads(ld=64, head_stride=40 * 64 - 8)]
+    for h in bad_heads:
+        assert fwd(q=h) == INVALID and fwd(k=h) == INVALID and fwd(v=h) == INVALID and fwd(y=h) == INVALID
+        assert all(bwd(h=h, at=i) == INVALID for i in range(8))
+    assert fwd(lse=None) == INVALID and fwd(lse=P + 2) == INVALID and fwd(scratch=None) == INVALID and fwd(scratch=P + 8) == INVALID
+    assert bwd(lse=None) == INVALID and bwd(scratch=None) == INVALID and bwd(scratch=P + 8) == INVALID
+    assert lib.lgc_attention_scratch(shape(), C.byref(n)) == OK and fwd(size=n.value - 1) == WORKSPACE
+    assert lib.lgc_attention_backward_scratch(shape(), C.byref(n)) == OK and n.value >= 2 * 40 * 8 * 4 and bwd(size=n.value - 1) == WORKSPACE
+    assert b"scratch" in lib.lgc_last_error(None)
+    assert fwd(shape(query_rows=0, key_rows=7), q=None, y=None) == OK and bwd(shape(query_rows=0, key_rows=0)) == OK
+    # a table of units for sequences, partial results where there are few queries
+    assert lib.lgc_attention_scratch(shape(query_rows=1, key_rows=8192, query_start=P, key_start=P, num_sequences=4), C.byref(n)) == OK and n.value > 4 * 8 * 65 * 4
+
+
+def test_rotary_refused_on_the_host(lib):
+    P = 4096
+    call = lambda x=heads(), t=0, rows=9, h=8, d=64, p=P, f=P, n=32, il=0, back=0, y=heads(p=8192): lib.lgc_rotary(x, t, rows, h, d, p, f, n, il, 1.0, back, y, None)  # noqa: E731
+    for kw in (dict(x=None), dict(y=None), dict(x=heads(p=4098)), dict(t=2), dict(rows=-1), dict(rows=(1 << 30) + 1), dict(h=0), dict(h=65537), dict(d=1), dict(d=65537),
+               dict(n=0), dict(n=33), dict(p=None), dict(f=None), dict(p=4100), dict(f=4100), dict(il=2), dict(back=-1), dict(x=heads(ld=60)), dict(x=heads(ld=500)),
+               dict(x=heads(), y=heads(ld=576)), dict(t=1, x=heads(p=4097))):
+        assert call(**kw) == INVALID, kw
+    assert call(rows=0, x=None) == OK
+
+
+def test_scratch_does_not_grow_with_the_square_of_anything(lib):
+    n = C.c_size_t()
+    for sequences in (1, 3, 40, 1000):
+        for rows in (1, 100, 5000):
+            for keys in (1, 5000, 1 << 20):
+                assert lib.lgc_attention_scratch(shape(query_rows=rows, key_rows=keys, query_start=4096, key_start=4096, num_sequences=sequences), C.byref(n)) == OK
+                assert n.value < 200 << 20

@@ -1,0 +1,502 @@
+"""The attention layer's operators on the GPU against plain 64-bit forms: rotary positions, attention over sequences, its backward
+pass; the sizes, masks and strides where they can go wrong, and what the binding refuses."""
+import math
+import zlib
+
+import pytest
+import torch
+
+import attention_reference as R
+from paper_2103_08870_b200 import layers, lgc
+
+pytestmark = pytest.mark.gpu
+
+BF = torch.bfloat16
+
+
+def generator(*key):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(zlib.crc32(repr(key).encode()))
+    return g
+
+
+def randn(g, *shape):
+    return torch.randn(*shape, generator=g, device="cuda")
+
+
+def starts(*lengths, first=0):
+    at = [first]
+    for n in lengths:
+        at.append(at[-1] + n)
+    return torch.tensor(at, device="cuda")
+
+
+def laid_out(t, how):
+    """The [rows][heads][dim] tensor in another layout, with NaN where it is not."""
+    rows, heads, dim = t.shape
+    if how == "rows":
+        return t.contiguous()
+    if how == "heads":                                   # a head's rows behind each other
+        room = torch.full((heads, rows + 3, dim + 8), math.nan, dtype=t.dtype, device="cuda")
+        v = room[:, 1:rows + 1, :dim].transpose(0, 1)
+    else:                                                # among other heads of the same rows
+        room = torch.full((rows, heads + 3, dim), math.nan, dtype=t.dtype, device="cuda")
+        v = room[:, 2:heads + 2]
+    v.copy_(t)
+    return v
+
+
+# ---- rotary positions ----------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("kind", [torch.float32, BF])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("rows,heads,dim,pairs,how", [
+    (1, 1, 2, 1, "rows"), (1, 40, 128, 64, "rows"), (5, 3, 64, 32, "among"), (7, 2, 80, 20, "rows"), (33, 5, 96, 8, "heads"), (130, 3, 7, 2, "rows"),
+    (3, 2, 2000, 900, "among"), (2400, 2, 16, 4, "heads"), (2371, 3, 128, 64, "among"), (2369, 1, 1200, 600, "rows")])
+def test_rotary(rows, heads, dim, pairs, how, interleaved, kind):
+    g = generator("rotary", rows, heads, dim, pairs)
+    x = laid_out(randn(g, rows, heads, dim).to(kind), how)
+    positions = torch.randint(-(1 << 21), 1 << 21, (rows,), generator=g, device="cuda")
+    positions[0] = 0
+    frequencies = layers.rotary_frequencies(2 * pairs, interpolation=4.0, context=4096)
+    for backward, amplitude in ((False, 1.0), (True, 1.25)):
+        want = R.rotary(x, positions, frequencies, interleaved, amplitude, backward)
+        # cosine and sine with the rounding of the angle (pi units of half a turn) and CUDA's 2 ulp, the two products, the sum
+        a = torch.arange(pairs, device="cuda")
+        i, j = (2 * a, 2 * a + 1) if interleaved else (a, a + pairs)
+        size = x.double().abs().clone()
+        both = amplitude * (x.double()[..., i].abs() + x.double()[..., j].abs())
+        size[..., i] = size[..., j] = both
+        tol = (12 * R.U32 + 2.0 ** -30) * size + (R.UBF * want.abs() if kind is BF else 0)
+        y = laid_out(torch.zeros(rows, heads, dim, dtype=kind, device="cuda"), how)
+        layers.rotary(x, positions, frequencies, y, interleaved, amplitude, backward)
+        assert ((y.double() - want).abs() <= tol).all()
+        assert torch.equal(y[..., 2 * pairs:], x[..., 2 * pairs:])
+        z = laid_out(x, how)
+        layers.rotary(z, positions, frequencies, z, interleaved, amplitude, backward)
+        assert torch.equal(z, y)
+
+
+def test_rotary_backward_is_the_gradient():
+    g = generator("rotary gradient")
+    x, dy = randn(g, 9, 2, 24).double().requires_grad_(), randn(g, 9, 2, 24)
+    positions, frequencies = torch.arange(9, device="cuda") * 1000, layers.rotary_frequencies(16)
+    for interleaved in (False, True):
+        (want,) = torch.autograd.grad((R.rotary(x, positions, frequencies, interleaved, 0.7) * dy).sum(), [x])
+        dx = torch.empty_like(dy)
+        layers.rotary(dy, positions, frequencies, dx, interleaved, 0.7, backward=True)
+        assert ((dx - want).abs() <= 16 * R.U32 * 2 * dy.abs().max()).all()
+
+
+def test_rotary_frequencies():
+    f = layers.rotary_frequencies(8, base=100.0)
+    assert torch.allclose(f.cpu(), 100.0 ** (-torch.arange(4).double() / 4), rtol=1e-14)
+    assert torch.allclose(layers.rotary_frequencies(8, base=100.0, interpolation=2.0), f / 2, rtol=1e-14)
+    # 1000 positions: 159, 50, 16 and 5 turns
+    g = layers.rotary_frequencies(8, base=100.0, interpolation=2.0, context=1000, slow_turns=5.5, fast_turns=50.0)
+    assert g[0] == f[0] and g[1] == f[1] and f[2] / 2 < g[2] < f[2] and g[3] == f[3] / 2
+
+
+# ---- attention -------------------------------------------------------------------------------------------------------------
+
+# lengths of queries, of keys (None: the same, and the same starts), heads, kv_heads, dim, causal, window
+CASES = [
+    ([1], None, 1, 1, 64, True, 0),
+    ([1], None, 8, 1, 8, False, 0),
+    ([127, 1, 0, 128, 129], None, 2, 2, 64, True, 0),
+    ([255, 256, 257], None, 4, 2, 128, True, 0),
+    ([700], None, 3, 1, 72, True, 0),                       # 42 queries to a tile, two rows of it left over
+    ([513], None, 10, 2, 128, False, 0),
+    ([300, 17], None, 6, 6, 40, True, 33),
+    ([1000], None, 4, 1, 64, True, 1),                      # every query sees itself
+    ([900, 200], None, 2, 1, 128, True, 500),
+    ([640], None, 2, 2, 128, True, 10000),
+    ([5, 0, 40, 300], [700, 9, 0, 301], 4, 2, 128, True, 0),    # keys without queries, queries without keys
+    ([200, 300], [60, 300], 8, 2, 64, True, 0),             # queries that see nothing
+    ([200, 300], [60, 1000], 2, 2, 64, True, 90),
+    ([130, 1], [517, 129], 5, 5, 104, False, 0),
+    ([70], [1500], 128, 1, 16, True, 0),                    # a query to a tile
+    ([3, 2], [400, 300], 12, 12, 128, False, 0),
+    ([1], [5000], 32, 8, 128, True, 0),                     # keys cut into parts
+    ([1, 1, 1, 0, 2], [3000, 1, 129, 700, 8000], 16, 4, 64, True, 0),
+    ([9], [4100], 2, 1, 128, False, 0),
+    ([40, 3], [100, 5000], 4, 4, 120, True, 0),             # parts that see nothing
+    ([33], [6000], 4, 2, 64, True, 700),
+]
+
+
+def operands(case, how="rows", sharp=1.0):
+    lq, lk, heads, kv_heads, dim, causal, window = case
+    g = generator(case)
+    same = lk is None
+    lk = lq if same else lk
+    T, S = sum(lq), sum(lk)
+    q = laid_out((sharp * randn(g, T, heads, dim)).to(BF), how)
+    k, v = laid_out(randn(g, S, kv_heads, dim).to(BF), how), laid_out((randn(g, S, kv_heads, dim) + 0.3).to(BF), how)
+    runs = {}
+    if len(lq) > 1:
+        runs = {"query_start": starts(*lq)}
+        if not same:
+            runs["key_start"] = starts(*lk)
+    return g, q, k, v, dict(runs, causal=causal, window=window)
+
+
+def forward(q, k, v, how="rows", **named):
+    y = laid_out(torch.full(q.shape, 7.0, dtype=BF, device="cuda"), how)
+    lse = torch.full(q.shape[:2], 7.0, device="cuda")
+    layers.attention(q, k, v, y, lse, **named)
+    return y, lse
+
+
+def check_forward(q, k, v, y, lse, **named):
+    want, want_lse, off, off_lse = R.attention(q, k, v, **named)
+    ours = ~want_lse.isnan()
+    assert ((y.double() - want).abs() <= off)[ours].all()
+    empty = want_lse == -math.inf
+    assert (y[empty] == 0).all() and (lse[empty] == -math.inf).all()
+    full = ours & ~empty
+    assert ((lse.double() - want_lse).abs() <= off_lse)[full].all()
+    assert (y[~ours] == 7).all() and (lse[~ours] == 7).all()
+
+
+def backward(dy, q, k, v, y, lse, how="rows", **named):
+    out = [laid_out(torch.full(t.shape, 7.0, dtype=BF, device="cuda"), how) for t in (q, k, v)]
+    layers.attention_backward(dy, q, k, v, y, lse, *out, **named)
+    return out
+
+
+def check_backward(dy, q, k, v, y, lse, got, **named):
+    want, off = R.attention_backward(dy, q, k, v, y, lse, **named)
+    for a, w, o in zip(got, want, off):
+        ours = ~w.isnan()
+        assert ((a.double() - w).abs() <= o)[ours].all()
+        assert (a[~ours] == 7).all()
+
+
+@pytest.mark.parametrize("case", CASES, ids=str)
+def test_attention(case):
+    _, q, k, v, named = operands(case, sharp=2.0)
+    y, lse = forward(q, k, v, **named)
+    layers.check()
+    check_forward(q, k, v, y, lse, **named)
+
+
+@pytest.mark.parametrize("case", CASES, ids=str)
+def test_attention_backward(case):
+    g, q, k, v, named = operands(case, sharp=2.0)
+    y, lse = forward(q, k, v, **named)
+    dy = randn(g, *q.shape).to(BF)
+    got = backward(dy, q, k, v, y, lse, **named)
+    layers.check()
+    check_backward(dy, q, k, v, y, lse, got, **named)
+
+
+@pytest.mark.parametrize("how", ["heads", "among"])
+@pytest.mark.parametrize("case", [CASES[3], CASES[4], CASES[10], CASES[17]], ids=str)
+def test_strides(case, how):
+    g, q, k, v, named = operands(case, how)
+    y, lse = forward(q, k, v, how, **named)
+    check_forward(q, k, v, y, lse, **named)
+    dy = laid_out(randn(g, *q.shape).to(BF), how)
+    check_backward(dy, q, k, v, y, lse, backward(dy, q, k, v, y, lse, how, **named), **named)
+    layers.check()
+
+
+def test_rows_of_no_sequence_and_of_other_sequences():
+    """What lies in front of the first run, behind the last and in another sequence must not matter, whatever it holds."""
+    g = generator("no sequence")
+    heads, kv_heads, dim = 6, 2, 72
+    query_start, key_start = starts(40, 130, 1, 60, first=9), starts(200, 77, 130, 0, first=3)
+    T, S = 9 + 231 + 50, 3 + 407 + 90
+    q, k, v, dy = randn(g, T, heads, dim).to(BF), randn(g, S, kv_heads, dim).to(BF), randn(g, S, kv_heads, dim).to(BF), randn(g, T, heads, dim).to(BF)
+    named = dict(query_start=query_start, key_start=key_start, causal=True)
+    for bad in (math.nan, math.inf):
+        for t, at in ((q, query_start), (dy, query_start), (k, key_start), (v, key_start)):
+            t[:int(at[0])] = bad
+            t[int(at[-1]):] = -bad
+        y, lse = forward(q, k, v, **named)
+        check_forward(q, k, v, y, lse, **named)
+        check_backward(dy, q, k, v, y, lse, backward(dy, q, k, v, y, lse, **named), **named)
+    # the second sequence has nothing but NaN: the others keep their bits
+    grads = backward(dy, q, k, v, y, lse, **named)
+    q1, k1, v1, dy1 = (t.clone() for t in (q, k, v, dy))
+    for t, at in ((q1, query_start), (dy1, query_start), (k1, key_start), (v1, key_start)):
+        t[int(at[1]):int(at[2])] = math.nan
+    y1, lse1 = forward(q1, k1, v1, **named)
+    grads1 = backward(dy1, q1, k1, v1, y1, lse1, **named)
+    for a, b, at in [(y, y1, query_start), (lse, lse1, query_start), (grads[0], grads1[0], query_start), (grads[1], grads1[1], key_start), (grads[2], grads1[2], key_start)]:
+        other = torch.ones(a.shape[0], dtype=torch.bool, device="cuda")
+        other[int(at[1]):int(at[2])] = False
+        assert torch.equal(a[other], b[other])
+    layers.check()
+
+
+def test_gradients_agree_with_differences():
+    g = generator("differences")
+    q, k, v = randn(g, 150, 4, 16).to(BF), randn(g, 150, 2, 16).to(BF), randn(g, 150, 2, 16).to(BF)
+    dy = randn(g, 150, 4, 16).to(BF)
+    named = dict(query_start=starts(60, 90), causal=True, window=40)
+    y, lse = forward(q, k, v, **named)
+    got = backward(dy, q, k, v, y, lse, **named)
+    _, off = R.attention_backward(dy, q, k, v, y, lse, **named)
+    f = lambda *a: (R.attention(*a, **named)[0] * dy.double()).sum()     # noqa: E731
+    for i, (x, dx, o) in enumerate(zip((q, k, v), got, off)):
+        for _ in range(3):
+            u = randn(g, *x.shape).double()
+            h = 1e-5
+            args = [t.double() for t in (q, k, v)]
+            args[i] = x.double() + h * u
+            up = f(*args)
+            args[i] = x.double() - h * u
+            slope = (up - f(*args)) / (2 * h)
+            # the entries' bounds along u; the rounding of y enters delta, and with it dq and dk: |y| 2^-8 |dy| per entry again
+            room = (o * u.abs()).sum() + (0 if i == 2 else 2 ** -8 * (y.double() * dy.double()).abs().sum() * 2 * u.abs().max())
+            assert abs((dx.double() * u).sum() - slope) <= room
+
+
+@pytest.mark.parametrize("group", [1, 4])
+def test_large_logits_and_equal_ones(group):
+    """Maxima that rise from tile to tile by more than the exponents' slack, logits of hundreds, all logits equal."""
+    g = generator("large", group)
+    T, D = 700, 64
+    q, k, v = randn(g, T, 2 * group, D).to(BF), randn(g, T, 2, D).to(BF), randn(g, T, 2, D).to(BF)
+    ramp = torch.linspace(0.1, 12, T, device="cuda")[:, None, None]
+    for kk in (k.float() * ramp, k.float() * ramp.flip(0), torch.ones_like(k), torch.zeros_like(k), 40 * k.float()):
+        kk = kk.to(BF)
+        for causal in (False, True):
+            y, lse = forward(q, kk, v, causal=causal)
+            check_forward(q, kk, v, y, lse, causal=causal)
+            dy = randn(g, T, 2 * group, D).to(BF)
+            check_backward(dy, q, kk, v, y, lse, backward(dy, q, kk, v, y, lse, causal=causal), causal=causal)
+
+
+def test_scales_and_masks_together():
+    g = generator("scales")
+    q, k, v = randn(g, 200, 2, 32).to(BF), randn(g, 333, 2, 32).to(BF), randn(g, 333, 2, 32).to(BF)
+    for scale in (1e-6, 0.03, 1.0):
+        named = dict(causal=True, scale=scale, window=100)
+        y, lse = forward(q, k, v, **named)
+        check_forward(q, k, v, y, lse, **named)
+        dy = randn(g, 200, 2, 32).to(BF)
+        check_backward(dy, q, k, v, y, lse, backward(dy, q, k, v, y, lse, **named), **named)
+
+
+def test_starts_that_do_not_ascend_stay_inside():
+    """Their results mean nothing; what is read and written does not leave the matrices (the plan cuts every run off)."""
+    g = generator("starts")
+    q, k, v = (randn(g, 300, 2, 64).to(BF) for _ in range(3))
+    around = torch.full((500, 2, 64), 7.0, dtype=BF, device="cuda")
+    y, lse = around[100:400], torch.zeros(300, 2, device="cuda")
+    at = torch.tensor([-5, 300, 0, 300, 10, 1 << 40, -(1 << 40), 200], device="cuda")
+    layers.attention(q, k, v, y, lse, query_start=at)
+    layers.attention_backward(q, q, k, v, y, lse, torch.empty_like(q), torch.empty_like(k), torch.empty_like(v), query_start=at)
+    layers.check()
+    assert (around[:100] == 7).all() and (around[400:] == 7).all()
+
+
+def test_no_rows():
+    none, some = torch.empty(0, 4, 64, dtype=BF, device="cuda"), torch.ones(5, 4, 64, dtype=BF, device="cuda")
+    y, lse = forward(none, some, some)
+    y, lse = forward(some, none, none)
+    assert (y == 0).all() and (lse == -math.inf).all()
+    dq, dk, dv = backward(some, some, none, none, y, lse)
+    assert (dq == 0).all()
+    dq, dk, dv = backward(none, none, some, some, none, torch.empty(0, 4, device="cuda"))
+    assert (dk == 0).all() and (dv == 0).all()
+    backward(none, none, none, none, none, torch.empty(0, 4, device="cuda"))
+    layers.rotary(none, torch.empty(0, dtype=torch.int64, device="cuda"), layers.rotary_frequencies(64), none)
+    layers.check()
+
+
+def test_many_sequences():
+    g = generator("many")
+    lengths = torch.randint(0, 12, (3000,), generator=g, device="cuda")
+    at = torch.cat([torch.zeros(1, dtype=torch.int64, device="cuda"), lengths.cumsum(0)])
+    T = int(at[-1])
+    q, k, v = randn(g, T, 2, 64).to(BF), randn(g, T, 1, 64).to(BF), randn(g, T, 1, 64).to(BF)
+    y, lse = forward(q, k, v, query_start=at)
+    check_forward(q, k, v, y, lse, query_start=at)
+    dy = randn(g, T, 2, 64).to(BF)
+    check_backward(dy, q, k, v, y, lse, backward(dy, q, k, v, y, lse, query_start=at), query_start=at)
+
+
+@pytest.mark.parametrize("dim,heads,kv_heads", [(128, 4, 2), (64, 2, 2)])
+def test_long_sequences(dim, heads, kv_heads):
+    """Many tiles on both sides: every ring of buffers goes round several times, the load is uneven."""
+    case = ([4500, 300, 2048], None, heads, kv_heads, dim, True, 0)
+    g, q, k, v, named = operands(case)
+    y, lse = forward(q, k, v, **named)
+    check_forward(q, k, v, y, lse, **named)
+    dy = randn(g, *q.shape).to(BF)
+    first = backward(dy, q, k, v, y, lse, **named)
+    check_backward(dy, q, k, v, y, lse, first, **named)
+    for _ in range(5):
+        y2, lse2 = forward(q, k, v, **named)
+        assert torch.equal(y, y2) and torch.equal(lse, lse2)
+        for a, b in zip(first, backward(dy, q, k, v, y, lse, **named)):
+            assert torch.equal(a, b)
+    layers.check()
+
+
+def test_rows_beyond_32_bits_of_bytes():
+    """Offsets of rows and heads above 2^31 elements."""
+    g = generator("far")
+    T, D = 300, 64
+    room = torch.zeros((1 << 31) + (1 << 24), dtype=BF, device="cuda")
+    stride = ((1 << 31) // T // 8) * 8
+    q = room.as_strided((T, 2, D), (stride, D, 1))
+    k, v = room.as_strided((T, 1, D), (stride, D, 1), 2 * D), room.as_strided((T, 1, D), (stride, D, 1), 3 * D)
+    y, dq = room.as_strided((T, 2, D), (stride, D, 1), 4 * D), room.as_strided((T, 2, D), (stride, D, 1), 6 * D)
+    dk, dv = room.as_strided((T, 1, D), (stride, D, 1), 8 * D), room.as_strided((T, 1, D), (stride, D, 1), 9 * D)
+    for t in (q, k, v):
+        t.copy_(randn(g, *t.shape))
+    lse = torch.zeros(T, 2, device="cuda")
+    layers.attention(q, k, v, y, lse)
+    check_forward(q, k, v, y, lse)
+    dy = randn(g, T, 2, D).to(BF)
+    layers.attention_backward(dy, q, k, v, y, lse, dq, dk, dv)
+    check_backward(dy, q, k, v, y, lse, (dq, dk, dv))
+    x = room.as_strided((T, 2, D), (stride, D, 1), 4 * D)
+    before = x.clone()
+    positions, frequencies = torch.arange(T, device="cuda"), layers.rotary_frequencies(D)
+    layers.rotary(x, positions, frequencies, x)
+    assert ((x.double() - R.rotary(before, positions, frequencies)).abs() <= (R.UBF + 2.0 ** -18) * 2 * before.double().abs().max()).all()
+
+
+# ---- streams, graphs, refusals --------------------------------------------------------------------------------------------------
+
+def test_streams_and_graphs_repeat_the_bits():
+    g = generator("graphs")
+    heads, kv_heads, dim = 6, 2, 64
+    T = 700
+    qkv, dy = randn(g, T, heads + 2 * kv_heads, dim).to(BF), randn(g, T, heads, dim).to(BF)
+    one, keys = randn(g, 1, heads, dim).to(BF), randn(g, 5000, 2 * kv_heads, dim).to(BF)
+    at, positions, frequencies = starts(100, 0, 400, 200), torch.arange(T, device="cuda"), layers.rotary_frequencies(dim)
+    turned, grads = torch.empty_like(qkv), torch.empty_like(qkv)
+    y, lse = torch.empty_like(dy), torch.empty(T, heads, device="cuda")
+    y1, lse1 = torch.empty_like(one), torch.empty(1, heads, device="cuda")
+    parts = lambda t: (t[:, :heads], t[:, heads:heads + kv_heads], t[:, heads + kv_heads:])     # noqa: E731
+
+    def step(stream=None):
+        layers.rotary(qkv, positions, frequencies, turned, stream=stream)
+        layers.attention(*parts(turned), y, lse, query_start=at, stream=stream)
+        layers.attention_backward(dy, *parts(turned), y, lse, *parts(grads), query_start=at, stream=stream)
+        layers.rotary(grads, positions, frequencies, grads, backward=True, stream=stream)
+        layers.attention(one, keys[:, :kv_heads], keys[:, kv_heads:], y1, lse1, stream=stream)
+
+    out = (y, lse, grads, y1, lse1)
+    step()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in out]
+    side = torch.cuda.Stream()
+    for t in out:
+        t.zero_()
+    torch.cuda.synchronize()
+    step(side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, out))
+    graph, other = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    with torch.cuda.graph(other):
+        step()
+    for new in (False, True, True):
+        if new:
+            qkv.copy_(randn(g, *qkv.shape))
+            at[1:3] = 300
+            step()
+        torch.cuda.synchronize()
+        want = [t.clone() for t in out]
+        for replayed in (graph, other):
+            for t in out:
+                t.zero_()
+            replayed.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(want, out))
+    layers.check()
+
+
+def test_calls_on_two_streams_at_a_time():
+    side = torch.cuda.Stream()
+    cases = [operands(([900, 100], None, 4, 2, 128, True, 0)), operands(([1], [6000], 8, 2, 64, True, 0))]
+    want = []
+    for g, q, k, v, named in cases:
+        y, lse = forward(q, k, v, **named)
+        want.append((y, lse, *backward(y, q, k, v, y, lse, **named)))
+    torch.cuda.synchronize()
+    for _ in range(10):
+        got = []
+        for (g, q, k, v, named), stream in zip(cases, (None, side)):
+            out = [torch.zeros_like(t) for t in (q, q, k, v)]
+            lse = torch.zeros(q.shape[:2], device="cuda")
+            got.append((out[0], lse, *out[1:]))
+        torch.cuda.synchronize()
+        for (g, q, k, v, named), o, stream in zip(cases, got, (None, side)):
+            layers.attention(q, k, v, o[0], o[1], stream=stream, **named)
+            layers.attention_backward(o[0], q, k, v, o[0], o[1], *o[2:], stream=stream, **named)
+        torch.cuda.synchronize()
+        for a, b in zip(want, got):
+            assert all(torch.equal(x, z) for x, z in zip(a, b))
+    layers.check()
+
+
+def test_scratch_of_the_callers():
+    g, q, k, v, named = operands(([1, 2], [3000, 500], 8, 2, 64, True, 0))
+    y, lse = forward(q, k, v, **named)
+    dy = randn(g, *q.shape).to(BF)
+    grads = backward(dy, q, k, v, y, lse, **named)
+    size = layers.attention_scratch(3, 3500, 8, 2, 64, 2)
+    room = torch.full((size + 64,), 0x55, dtype=torch.uint8, device="cuda")
+    y2, lse2 = forward(q, k, v, scratch=room[:size], **named)
+    assert torch.equal(y, y2) and torch.equal(lse, lse2) and (room[size:] == 0x55).all()
+    size = layers.attention_backward_scratch(3, 3500, 8, 2, 64, 2)
+    room = torch.full((size + 64,), 0x55, dtype=torch.uint8, device="cuda")
+    for a, b in zip(grads, backward(dy, q, k, v, y, lse, scratch=room[:size], **named)):
+        assert torch.equal(a, b)
+    assert (room[size:] == 0x55).all()
+    with pytest.raises(lgc.LGCError) as e:
+        layers.attention(q, k, v, y, lse, scratch=room[:16], **named)
+    assert e.value.status == 3
+    with pytest.raises(lgc.LGCError) as e:
+        layers.attention_backward(dy, q, k, v, y, lse, *grads, scratch=room[:16], **named)
+    assert e.value.status == 3
+
+
+def test_refusals():
+    z = lambda *s, dtype=BF: torch.zeros(*s, dtype=dtype, device="cuda")                        # noqa: E731
+    q, k, lse = z(6, 4, 64), z(6, 2, 64), z(6, 4, dtype=torch.float32)
+    at = starts(2, 4)
+    pos, f = torch.arange(6, device="cuda"), layers.rotary_frequencies(64)
+    call = lambda q=q, k=k, v=k, y=q, lse=lse, **n: layers.attention(q, k, v, y, lse, **n)      # noqa: E731
+    back = lambda dy=q, q=q, k=k, v=k, y=q, lse=lse, dq=q, dk=k, dv=k, **n: layers.attention_backward(dy, q, k, v, y, lse, dq, dk, dv, **n)    # noqa: E731
+    turn = lambda x=q, p=pos, f=f, y=q, **n: layers.rotary(x, p, f, y, **n)                     # noqa: E731
+    bad = [
+        lambda: call(q=q.float()), lambda: call(q=q.cpu()), lambda: call(q=q[0]), lambda: call(k=z(6, 2, 32)), lambda: call(v=z(5, 2, 64)),
+        lambda: call(y=z(6, 3, 64)), lambda: call(lse=z(6, 4)), lambda: call(lse=lse[:5]), lambda: call(q=q.transpose(1, 2)),
+        lambda: call(query_start=at.int()), lambda: call(query_start=at[:1]), lambda: call(key_start=at), lambda: call(query_start=at, key_start=starts(1, 2, 3)),
+        lambda: call(scratch=z(1 << 20)), lambda: call(query_start=at.cpu()),
+        lambda: back(dy=z(5, 4, 64)), lambda: back(dq=z(6, 4, 32)), lambda: back(dk=z(6, 4, 64)), lambda: back(dv=k.float()), lambda: back(y=q.float()),
+        lambda: back(dy=q.cpu()), lambda: back(lse=lse.double()),
+        lambda: turn(p=pos.int()), lambda: turn(p=pos[:5]), lambda: turn(f=f.float()), lambda: turn(y=q.float()), lambda: turn(y=k), lambda: turn(x=q.half(), y=q.half()),
+        lambda: layers.rotary_frequencies(7), lambda: layers.rotary_frequencies(8, interpolation=0.5), lambda: layers.rotary_frequencies(8, context=10, fast_turns=1.0),
+    ]
+    for c in bad:
+        with pytest.raises(ValueError):
+            c()
+    wide, odd = z(6, 4, 136), z(6, 4, 68)
+    calls = [       # what the library itself refuses
+        (lambda: call(q=wide, y=wide, k=z(6, 2, 136), v=z(6, 2, 136)), 4), (lambda: call(q=odd, y=odd, k=z(6, 2, 68), v=z(6, 2, 68)), 1),
+        (lambda: call(k=z(6, 3, 64), v=z(6, 3, 64)), 1), (lambda: call(q=z(6, 256, 8), y=z(6, 256, 8), k=z(6, 1, 8), v=z(6, 1, 8), lse=z(6, 256, dtype=torch.float32)), 4),
+        (lambda: call(window=-1), 1), (lambda: call(window=5, causal=False), 1), (lambda: call(scale=0.0), 1), (lambda: call(scale=-1.0), 1),
+        (lambda: call(scale=math.nan), 1), (lambda: call(scale=math.inf), 1),
+        (lambda: call(query_start=at, k=z(5, 2, 64), v=z(5, 2, 64)), 1),
+        (lambda: call(q=z(6, 4, 72)[:, :, 4:68]), 1), (lambda: call(k=z(1, 2, 64).expand(6, 2, 64)), 1), (lambda: call(k=z(6, 1, 64).expand(6, 2, 64)), 1),
+        (lambda: back(dk=z(6, 1, 64).expand(6, 2, 64)), 1), (lambda: back(scale=0.0), 1),
+        (lambda: turn(f=layers.rotary_frequencies(66)), 1), (lambda: turn(x=q, y=q.view(-1).as_strided((6, 4, 64), (64, 384, 1))), 1),
+        (lambda: turn(x=z(6, 1, 64).expand(6, 4, 64)), 1),
+    ]
+    for c, status in calls:
+        with pytest.raises(lgc.LGCError) as e:
+            c()
+        assert e.value.status == status
+    layers.check()
