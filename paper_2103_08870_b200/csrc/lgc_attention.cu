@@ -18,9 +18,9 @@ using namespace attention;
 namespace {
 
 constexpr float kSlack = 8.0f;
-constexpr int kThreads = 384;           // warps 0..3: rows of tile 0, 4..7: of tile 1, 8: MMA, 9: TMA, 10 and 11 only give registers
-// Registers per thread: 168 at the launch, then 208 for the rows' threads (128 logits each), 88 for the others: 2 * 208 + 88 = 3 * 168.
-constexpr int kRowRegisters = 208, kOtherRegisters = 88;
+constexpr int kThreads = 384;           // warps 0..3: rows of tile 0, 4..7: of tile 1, 8: products, 9: TMA, 10 and 11 only give registers
+// Registers per thread: 168 at the launch, then 216 for the rows' threads (128 logits each), 72 for the others: 2 * 216 + 72 = 3 * 168.
+constexpr int kRowRegisters = 224, kOtherRegisters = 56;
 
 struct ForwardArgs {
     Runs runs;
@@ -49,7 +49,7 @@ struct Range {
     int base, begin, end;
     int first[2], last[2];
 };
-__device__ __forceinline__ Range range_of(const ForwardArgs &p, const Unit &u)
+__device__ __forceinline__ Range range_of(const ForwardArgs &p, const Unit &u, int split)
 {
     Range r;
     int lo[2], hi[2];
@@ -61,7 +61,7 @@ __device__ __forceinline__ Range range_of(const ForwardArgs &p, const Unit &u)
     if (p.splits > 1) {
         const int tiles = (max(hi[0], hi[1]) - r.base + kRows - 1) >> 7;
         const int chunk = max(p.chunk, (tiles + p.splits - 1) / p.splits);
-        from = blockIdx.z * chunk;
+        from = split * chunk;
         to = from + chunk;
     }
     r.begin = 0x7fffffff;
@@ -81,6 +81,9 @@ __device__ __forceinline__ Range range_of(const ForwardArgs &p, const Unit &u)
     return r;
 }
 
+// One warp issues the products of both tiles, in turn: issuing takes as long as the product, and so one tile's threads are at their
+// exponentials while the other's have their products made (a warp for each tile lets them fall into step: 1100 against 850 us for 16384
+// tokens, 16 heads).
 template <int DP>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
@@ -88,7 +91,9 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
 {
     constexpr int kStage = kStages<DP>, kTile = kTileBytes<DP>;
     extern __shared__ uint8_t dyn_smem[];
-    __shared__ __align__(8) uint64_t q_full[2], full_bar[kStage], empty_bar[kStage], s_full[2], p_full[2], o_full;
+    // q_full, full: loaded; q_empty, empty: read by the tensor cores; s_full: S is there, p_full: P is; o_full: a unit's O is complete,
+    // o_empty: read
+    __shared__ __align__(8) uint64_t q_full[2], q_empty[2], full_bar[kStage], empty_bar[kStage], s_full[2], p_full[2], o_full, o_empty[2];
     __shared__ uint32_t tmem_base;
     __shared__ volatile int failed;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -99,14 +104,16 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         failed = 0;
         for (int s = 0; s < 2; ++s) {
             bar_init(smem_addr(&q_full[s]), 1);
+            bar_init(smem_addr(&q_empty[s]), 1);
             bar_init(smem_addr(&s_full[s]), 1);
             bar_init(smem_addr(&p_full[s]), 4);
+            bar_init(smem_addr(&o_empty[s]), 4);
         }
-        bar_init(smem_addr(&o_full), 1);
         for (int s = 0; s < kStage; ++s) {
             bar_init(smem_addr(&full_bar[s]), 1);
             bar_init(smem_addr(&empty_bar[s]), 1);
         }
+        bar_init(smem_addr(&o_full), 1);
         bar_init_fence();
     }
     if (warp == 8) tc_alloc(&tmem_base, 512);
@@ -115,208 +122,226 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     tc_fence_after();
     const uint32_t tmem = tmem_base;
     grid_wait();
-    const int kv_head = (int)(blockIdx.x % p.kv_heads), head0 = kv_head * p.group;
-    Unit u;
-    const bool any = unit_of(p.runs, p.plan, false, blockIdx.x / p.kv_heads, u);
-    Range r;
-    if (any) r = range_of(p, u);
 
-    if (!any) {
-    } else if (warp >= 8) {
+    if (warp >= 8) {
         give_registers<kOtherRegisters>();
-        if (warp == 9) {
-            if (lane == 0 && r.end > 0) {
-                const uint32_t q_bytes = (uint32_t)p.queries * p.group * (DP * 2);
-    #pragma unroll
+        if (warp == 9 && lane == 0) {
+            const uint32_t q_bytes = (uint32_t)p.queries * p.group * (DP * 2);
+            int st = 0;
+            uint32_t phase = 1, q_phase[2] = {1, 1};
+            bool ok = true;
+            for (Walk w(p.runs, p.plan, false, p.kv_heads, p.splits); ok && w.next();) {
+                const Unit u = w.unit;
+                const Range r = range_of(p, u, w.split);
+                if (r.end == 0) continue;
+#pragma unroll
                 for (int s = 0; s < 2; ++s)
-                    if (r.last[s] > 0) {
+                    if (r.last[s] > 0 && ok) {
+                        if (!bar_wait(smem_addr(&q_empty[s]), q_phase[s], &failed)) { ok = false; break; }
+                        q_phase[s] ^= 1;
                         bar_expect(smem_addr(&q_full[s]), q_bytes);
-                        load_tile<DP>(q_tile + s * kTile, &map_q, smem_addr(&q_full[s]), head0, u.row + s * p.queries);
+                        load_tile<DP>(q_tile + s * kTile, &map_q, smem_addr(&q_full[s]), w.head * p.group, u.row + s * p.queries);
                     }
-                int st = 0;
-                uint32_t phase = 1;
-                bool ok = true;
                 for (int t = r.begin; t < r.end && ok; ++t)
-    #pragma unroll
+#pragma unroll
                     for (int kv = 0; kv < 2; ++kv) {
                         if (!bar_wait(smem_addr(&empty_bar[st]), phase, &failed)) { ok = false; break; }
                         bar_expect(smem_addr(&full_bar[st]), kTile);
-                        load_tile<DP>(ring + st * kTile, kv ? &map_v : &map_k, smem_addr(&full_bar[st]), kv_head, u.other_row + r.base + t * kRows);
+                        load_tile<DP>(ring + st * kTile, kv ? &map_v : &map_k, smem_addr(&full_bar[st]), w.head, u.other_row + r.base + t * kRows);
                         if (++st == kStage) st = 0, phase ^= 1;
                     }
             }
         } else if (warp == 8) {
             const bool issuer = elect_one();
-            int st_k = 0, st_v = 1;                              // stages of K(t + 1) and V(t)
-            uint32_t ph_k = 0, ph_v = 0, ph_p[2] = {0, 0};
-            bool ok = r.end > 0;
-            for (int t = r.begin - 1; t < r.end && ok; ++t) {
-                const bool has_v = t >= r.begin, has_k = t + 1 < r.end;
-                const uint32_t tile_v = ring + st_v * kTile, tile_k = ring + st_k * kTile;
-                if (has_v) {
-                    if (!bar_wait_together(smem_addr(&full_bar[st_v]), ph_v, &failed)) break;
-                    const int live = u.other_len - (r.base + t * kRows);
-                    if (live < kRows) clear_rows<DP>(tile_v, live);
-                }
-                if (has_k && !bar_wait_together(smem_addr(&full_bar[st_k]), ph_k, &failed)) break;
-    #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    if (has_v && t >= r.first[s] && t < r.last[s]) {
-                        if (!bar_wait_together(smem_addr(&p_full[s]), ph_p[s], &failed)) { ok = false; break; }
-                        ph_p[s] ^= 1;
-                        tc_fence_after();
-                        if (issuer) {
-    #pragma unroll
-                            for (int ks = 0; ks < kRows / 16; ++ks)
-                                product_step<DP>(tmem + 256 + s * DP, tmem + s * kRows + ks * 8, tile_v, ks, t > r.first[s] || ks > 0);
+            int st_k = 0, st_v = 1;                          // stages of K(t + 1) and V(t)
+            uint32_t ph_k = 0, ph_v = 0, ph_q[2] = {0, 0}, ph_p[2] = {0, 0}, ph_o = 1;
+            bool ok = true;
+            for (Walk w(p.runs, p.plan, false, p.kv_heads, p.splits); ok && w.next();) {
+                const Unit u = w.unit;
+                const Range r = range_of(p, u, w.split);
+                if (r.end == 0) continue;
+                for (int t = r.begin - 1; t < r.end && ok; ++t) {
+                    const bool has_v = t >= r.begin, has_k = t + 1 < r.end;
+                    const uint32_t tile_v = ring + st_v * kTile, tile_k = ring + st_k * kTile;
+                    // what has long been there is waited for first
+                    if (has_v) {
+                        if (!bar_wait_together(smem_addr(&full_bar[st_v]), ph_v, &failed)) { ok = false; break; }
+                        const int live = u.other_len - (r.base + t * kRows);
+                        if (live < kRows) clear_rows<DP>(tile_v, live);
+                        if (t == r.begin) {                  // the last unit's O has been read
+                            if (!bar_wait_together(smem_addr(&o_empty[0]), ph_o, &failed) || !bar_wait_together(smem_addr(&o_empty[1]), ph_o, &failed)) {
+                                ok = false;
+                                break;
+                            }
+                            ph_o ^= 1;
                         }
-                        __syncwarp();
                     }
-                    if (has_k && t + 1 >= r.first[s] && t + 1 < r.last[s]) {
-                        if (t + 1 == r.first[s] && !bar_wait_together(smem_addr(&q_full[s]), 0, &failed)) { ok = false; break; }
-                        tc_fence_after();
-                        if (issuer) {
-                            // (after the product that reads P in the same columns: the tensor cores work in order)
-                            product_of_tiles<DP>(tmem + s * kRows, q_tile + s * kTile, tile_k);
-                            tc_commit(smem_addr(&s_full[s]));
+                    if (has_k && !bar_wait_together(smem_addr(&full_bar[st_k]), ph_k, &failed)) { ok = false; break; }
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        if (has_v && t >= r.first[s] && t < r.last[s]) {
+                            if (!bar_wait_together(smem_addr(&p_full[s]), ph_p[s], &failed)) { ok = false; break; }
+                            ph_p[s] ^= 1;
+                            tc_fence_after();
+                            if (issuer) {
+#pragma unroll
+                                for (int ks = 0; ks < kRows / 16; ++ks)
+                                    product_step<DP>(tmem + 256 + s * DP, tmem + s * kRows + ks * 8, tile_v, ks, t > r.first[s] || ks > 0);
+                            }
+                            __syncwarp();
                         }
-                        __syncwarp();
+                        if (has_k && t + 1 >= r.first[s] && t + 1 < r.last[s]) {
+                            if (t + 1 == r.first[s]) {
+                                if (!bar_wait_together(smem_addr(&q_full[s]), ph_q[s], &failed)) { ok = false; break; }
+                                ph_q[s] ^= 1;
+                            }
+                            tc_fence_after();
+                            if (issuer) {
+                                // (after the product that reads P in the same columns: the tensor cores work in order)
+                                product_of_tiles<DP>(tmem + s * kRows, q_tile + s * kTile, tile_k);
+                                tc_commit(smem_addr(&s_full[s]));
+                                if (t + 2 == r.last[s]) tc_commit(smem_addr(&q_empty[s]));
+                            }
+                            __syncwarp();
+                        }
                     }
+                    if (!ok) break;
+                    if (issuer) {
+                        if (has_v) tc_commit(smem_addr(&empty_bar[st_v]));
+                        if (has_k) tc_commit(smem_addr(&empty_bar[st_k]));
+                        if (t == r.end - 1) tc_commit(smem_addr(&o_full));
+                    }
+                    __syncwarp();
+                    if (has_v && (st_v += 2) >= kStage) st_v -= kStage, ph_v ^= 1;
+                    if (has_k && (st_k += 2) >= kStage) st_k -= kStage, ph_k ^= 1;
                 }
-                if (!ok) break;
-                if (issuer) {
-                    if (has_v) tc_commit(smem_addr(&empty_bar[st_v]));
-                    if (has_k) tc_commit(smem_addr(&empty_bar[st_k]));
-                    if (t == r.end - 1) tc_commit(smem_addr(&o_full));
-                }
-                __syncwarp();
-                if (has_v && (st_v += 2) >= kStage) st_v -= kStage, ph_v ^= 1;
-                if (has_k && (st_k += 2) >= kStage) st_k -= kStage, ph_k ^= 1;
             }
         }
     } else {
         take_registers<kRowRegisters>();
         const int slot = warp >> 2;
         const int row = (warp & 3) * 32 + lane;                                  // of the tile
-        const int query = row / p.group;
-        const int i = slot * p.queries + query;                                  // of the unit
-        const bool live = query < p.queries && i < u.rows;
-        int lo = 0, hi = 0x7fffffff;                                             // (rows that nobody reads need no mask)
-        if (live) keys_seen(p.mask, u.pos + i, 1, u.shift, u.other_len, lo, hi);
+        const int query = row / p.group, of_group = row - query * p.group;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t s_at = tmem + lanes + slot * kRows, o_at = tmem + lanes + 256 + slot * DP;
         const float c = p.scale_log2;
-        float most = -INFINITY, sum = 0.0f;                                      // the exponents' reference, and sum of exponentials
+        uint32_t ph_s = 0, ph_o = 0;
         bool ok = true;
-        const int first = slot ? r.first[1] : r.first[0], last = slot ? r.last[1] : r.last[0];
-        for (int t = first; t < last; ++t) {
-            if (!bar_wait_together(smem_addr(&s_full[slot]), (t - first) & 1, &failed)) { ok = false; break; }
-            tc_fence_after();
-            float v[kRows];
+        for (Walk walk(p.runs, p.plan, false, p.kv_heads, p.splits); ok && walk.next();) {
+            const Unit u = walk.unit;
+            const Range r = range_of(p, u, walk.split);
+            const int i = slot * p.queries + query;                              // of the unit
+            const bool live = query < p.queries && i < u.rows;
+            int lo = 0, hi = 0x7fffffff;                                         // (rows that nobody reads need no mask)
+            if (live) keys_seen(p.mask, u.pos + i, 1, u.shift, u.other_len, lo, hi);
+            float most = -INFINITY, sum = 0.0f;                                  // the exponents' reference, and sum of exponentials
+            const int first = slot ? r.first[1] : r.first[0], last = slot ? r.last[1] : r.last[0];
+            for (int t = first; t < last; ++t) {
+                if (!bar_wait_together(smem_addr(&s_full[slot]), ph_s, &failed)) { ok = false; break; }
+                ph_s ^= 1;
+                tc_fence_after();
+                float v[kRows];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) tc_read32(s_at + 32 * j, reinterpret_cast<uint32_t(&)[32]>(v[32 * j]));
+                for (int j = 0; j < 4; ++j) tc_read32(s_at + 32 * j, reinterpret_cast<uint32_t(&)[32]>(v[32 * j]));
 #pragma unroll
-            for (int j = 0; j < 4; ++j) tc_read_wait(reinterpret_cast<uint32_t(&)[32]>(v[32 * j]));
-            const int key0 = r.base + t * kRows, from = lo - key0, to = hi - key0;
-            if (__any_sync(0xffffffffu, from > 0 || to < kRows)) {
+                for (int j = 0; j < 4; ++j) tc_read_wait(reinterpret_cast<uint32_t(&)[32]>(v[32 * j]));
+                const int key0 = r.base + t * kRows, from = lo - key0, to = hi - key0;
+                if (__any_sync(0xffffffffu, to < kRows)) {
 #pragma unroll
-                for (int j = 0; j < kRows; ++j) v[j] = j >= from && j < to ? v[j] : -INFINITY;
-            }
-            float m4[4] = {v[0], v[1], v[2], v[3]};
-#pragma unroll
-            for (int j = 4; j < kRows; j += 8) {
-#pragma unroll
-                for (int n = 0; n < 4; ++n) {
-                    const float b = j + 4 + n < kRows ? v[(j + 4 + n) % kRows] : v[j + n];
-                    m4[n] = fmaxf(fmaxf(m4[n], v[j + n]), b);
+                    for (int j = 0; j < kRows; ++j) v[j] = j < to ? v[j] : -INFINITY;
                 }
+                if (__any_sync(0xffffffffu, from > 0)) {
+#pragma unroll
+                    for (int j = 0; j < kRows; ++j) v[j] = j >= from ? v[j] : -INFINITY;
+                }
+                float m4[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+                for (int j = 4; j < kRows; j += 8) {
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) {
+                        const float b = j + 4 + n < kRows ? v[(j + 4 + n) % kRows] : v[j + n];
+                        m4[n] = fmaxf(fmaxf(m4[n], v[j + n]), b);
+                    }
+                }
+                const float top = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+                const bool raise = top > most && (most == -INFINITY || (top - most) * c > kSlack);
+                const float now = raise ? top : most;
+                const float zero = now == -INFINITY ? 0.0f : now;                // a row that has seen nothing: exponentials of -inf
+                if (__any_sync(0xffffffffu, raise)) {
+                    const float by = raise ? exp2_of(__fmul_rn(most == -INFINITY ? -INFINITY : __fsub_rn(most, now), c)) : 1.0f;
+                    sum = __fmul_rn(sum, by);
+                    if (t > first) {
+                        // the product in front of this tile's S has ended with it: O is complete
+#pragma unroll
+                        for (int j = 0; j < DP; j += 16) {
+                            uint32_t o[16];
+                            tc_read16(o_at + j, o);
+#pragma unroll
+                            for (int n = 0; n < 16; ++n) o[n] = __float_as_uint(__fmul_rn(__uint_as_float(o[n]), by));
+                            tc_write16(o_at + j, o);
+                        }
+                    }
+                    most = now;
+                }
+                const float minus = -__fmul_rn(zero, c);
+                const f2 cc = f2_of(c, c), mm = f2_of(minus, minus);
+                f2 sums[2] = {0, 0};
+#pragma unroll
+                for (int j = 0; j < kRows; j += 64) {
+                    uint32_t w[32];
+#pragma unroll
+                    for (int n = 0; n < 64; n += 2) {
+                        const f2 x = f2_fma(f2_of(v[j + n], v[j + n + 1]), cc, mm);
+                        const float a = exp2_of(f2_lo(x)), b = exp2_of(f2_hi(x));
+                        sums[(n >> 1) & 1] = f2_add(sums[(n >> 1) & 1], f2_of(a, b));
+                        w[n >> 1] = bf16_pair(a, b);
+                    }
+                    tc_write32(s_at + (j >> 1), w);
+                }
+                tc_write_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(smem_addr(&p_full[slot]));
+                const f2 both = f2_add(sums[0], sums[1]);
+                sum = __fadd_rn(sum, __fadd_rn(f2_lo(both), f2_hi(both)));
             }
-            const float top = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
-            const bool raise = top > most && (most == -INFINITY || (top - most) * c > kSlack);
-            const float now = raise ? top : most;
-            const float zero = now == -INFINITY ? 0.0f : now;                    // a row that has seen nothing: exponentials of -inf
-            if (__any_sync(0xffffffffu, raise)) {
-                const float by = raise ? exp2_of(__fmul_rn(most == -INFINITY ? -INFINITY : __fsub_rn(most, now), c)) : 1.0f;
-                sum = __fmul_rn(sum, by);
-                if (t > first) {
-                    // the product in front of this tile's S has ended with it: O is complete
+            if (!ok) break;
+            if (r.end > 0) {
+                if (!bar_wait_together(smem_addr(&o_full), ph_o, &failed)) break;
+                ph_o ^= 1;
+                tc_fence_after();
+            }
+            const float inverse = last == 0 ? 0.0f : sum > 0.0f ? __fdiv_rn(1.0f, sum) : sum == 0.0f ? 0.0f : sum;      // (a NaN stays one)
+            const int head = walk.head * p.group + of_group;
+            const int64_t q = (int64_t)u.row + i;
+            const int64_t at = q * p.heads + head;
+            const float lse = sum == 0.0f ? -INFINITY : __fmul_rn(__fadd_rn(__fmul_rn(most, c), log2f(sum)), kLn2);
+            if (p.splits > 1) {
+                const int64_t all = p.runs.query_rows * p.heads;
+                if (live) p.part_lse[walk.split * all + at] = lse;
+                if (last > 0) {                              // (the part of a split without keys is not read)
+                    float *out = p.part_y + (walk.split * all + at) * p.dim;
 #pragma unroll
                     for (int j = 0; j < DP; j += 32) {
                         uint32_t o[32];
                         tc_read32(o_at + j, o);
                         tc_read_wait(o);
 #pragma unroll
-                        for (int n = 0; n < 32; ++n) o[n] = __float_as_uint(__fmul_rn(__uint_as_float(o[n]), by));
-                        tc_write32(o_at + j, o);
+                        for (int n = 0; n < 32; n += 4)
+                            if (live && j + n < p.dim)
+                                *reinterpret_cast<float4 *>(out + j + n) =
+                                    make_float4(__fmul_rn(__uint_as_float(o[n]), inverse), __fmul_rn(__uint_as_float(o[n + 1]), inverse),
+                                                __fmul_rn(__uint_as_float(o[n + 2]), inverse), __fmul_rn(__uint_as_float(o[n + 3]), inverse));
                     }
-                }
-                most = now;
-            }
-            const float minus = -__fmul_rn(zero, c);
-            const f2 cc = f2_of(c, c), mm = f2_of(minus, minus);
-            f2 sums[2] = {0, 0};
-#pragma unroll
-            for (int j = 0; j < kRows; j += 64) {
-                uint32_t w[32];
-#pragma unroll
-                for (int n = 0; n < 64; n += 2) {
-                    const f2 x = f2_fma(f2_of(v[j + n], v[j + n + 1]), cc, mm);
-                    const float a = exp2_of(f2_lo(x)), b = exp2_of(f2_hi(x));
-                    sums[(n >> 1) & 1] = f2_add(sums[(n >> 1) & 1], f2_of(a, b));
-                    w[n >> 1] = bf16_pair(a, b);
-                }
-                tc_write32(s_at + (j >> 1), w);
-            }
-            tc_write_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(smem_addr(&p_full[slot]));
-            const f2 both = f2_add(sums[0], sums[1]);
-            sum = __fadd_rn(sum, __fadd_rn(f2_lo(both), f2_hi(both)));
-        }
-        if (ok && r.end > 0 && !bar_wait_together(smem_addr(&o_full), 0, &failed)) ok = false;
-        if (ok) {
-            tc_fence_after();
-            const float inverse = sum > 0.0f ? __fdiv_rn(1.0f, sum) : sum == 0.0f ? 0.0f : sum;      // (a NaN stays one)
-            const int head = head0 + row - query * p.group;
-            const int64_t q = (int64_t)u.row + i;
-            const int64_t at = q * p.heads + head;
-            const float lse = sum == 0.0f ? -INFINITY : __fmul_rn(__fadd_rn(__fmul_rn(most, c), log2f(sum)), kLn2);
-            if (p.splits > 1) {
-                const int64_t all = p.runs.query_rows * p.heads;
-                if (live) p.part_lse[blockIdx.z * all + at] = lse;
-                float *out = p.part_y + (blockIdx.z * all + at) * p.dim;
-#pragma unroll
-                for (int j = 0; j < DP; j += 32) {
-                    uint32_t o[32];
-                    tc_read32(o_at + j, o);
-                    tc_read_wait(o);
-#pragma unroll
-                    for (int n = 0; n < 32; n += 4)
-                        if (live && j + n < p.dim) {
-                            float4 f = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                            if (last > 0) f = make_float4(__fmul_rn(__uint_as_float(o[n]), inverse), __fmul_rn(__uint_as_float(o[n + 1]), inverse),
-                                                          __fmul_rn(__uint_as_float(o[n + 2]), inverse), __fmul_rn(__uint_as_float(o[n + 3]), inverse));
-                            *reinterpret_cast<float4 *>(out + j + n) = f;
-                        }
                 }
             } else {
                 if (live) p.lse[at] = lse;
-                __nv_bfloat16 *out = p.y + q * p.ld_y + head * p.head_stride_y;
-#pragma unroll
-                for (int j = 0; j < DP; j += 32) {
-                    uint32_t o[32];
-                    tc_read32(o_at + j, o);
-                    tc_read_wait(o);
-#pragma unroll
-                    for (int n = 0; n < 32; n += 8)
-                        if (live && j + n < p.dim) {
-                            float f[8];
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) f[e] = last > 0 ? __fmul_rn(__uint_as_float(o[n + e]), inverse) : 0.0f;
-                            store_bf16x8(out + j + n, f);
-                        }
-                }
+                store_rows<DP>(live ? p.y + q * p.ld_y + head * p.head_stride_y : nullptr, p.dim, o_at, inverse, last > 0);
+            }
+            if (r.end > 0) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(smem_addr(&o_empty[slot]));
             }
         }
     }
@@ -351,7 +376,7 @@ join_kernel(const __grid_constant__ ForwardArgs p)
         const float lse = p.part_lse[z * all + at];
         const float w = exp2_of(__fmul_rn(__fsub_rn(lse, zero), kLog2e));
         total = __fadd_rn(total, w);
-        if (w != 0.0f && lane * 4 < p.dim) {
+        if (lse > -INFINITY && lane * 4 < p.dim) {
             const float4 v = *reinterpret_cast<const float4 *>(p.part_y + (z * all + at) * p.dim + lane * 4);
             y[0] = __fmaf_rn(w, v.x, y[0]);
             y[1] = __fmaf_rn(w, v.y, y[1]);
@@ -505,7 +530,8 @@ cudaError_t launch_forward(const CUtensorMap &q, const CUtensorMap &k, const CUt
     static OncePerDevice configured;
     cudaError_t e = configured.run([&] { return cudaFuncSetAttribute(attention_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem<DP>); });
     if (e != cudaSuccess) return e;
-    const dim3 grid((unsigned)(p.plan.most * p.kv_heads), 1, (unsigned)p.splits);
+    const int64_t work = p.plan.most * p.kv_heads * p.splits, sms = sm_count();
+    const dim3 grid((unsigned)(work < sms ? work : sms));
     if (dependent) {
         e = launch_dependent_smem(attention_kernel<DP>, grid, dim3(kThreads), kSmem<DP>, s, q, k, v, p);
     } else {
@@ -535,7 +561,7 @@ cudaError_t launch_plan(const Runs &runs, const Mask &mask, const Plan *queries,
 
 }  // namespace attention
 
-// CTAs of a launch: one per unit and head of k and v
+// Units times heads of k and v are counted in 32 bits.
 bool attention_grid_fits(const AttentionShape &a)
 {
     const int per = queries_of_tile(a);

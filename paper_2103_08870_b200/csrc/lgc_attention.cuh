@@ -62,24 +62,53 @@ inline Plan plan_at(char *p, const int64_t *start, int64_t rows, int per, int se
 // Writes the table of the queries' units and / or the keys' (nullptr: not wanted).
 cudaError_t launch_plan(const Runs &runs, const Mask &mask, const Plan *queries, const Plan *keys, cudaStream_t s);
 
-// The unit of a CTA; units with more to do come first (causal: the last queries, the first keys).  False: there is none.
-__device__ __forceinline__ bool unit_of(const Runs &r, const Plan &plan, bool by_key, int64_t index, Unit &u)
+// The units' number and the units themselves; those with more to do come first (causal: the last queries, the first keys).
+__device__ __forceinline__ uint32_t units_of(const Runs &r, const Plan &plan) { return r.query_start ? (uint32_t)*plan.count : (uint32_t)plan.most; }
+__device__ __forceinline__ Unit unit_at(const Runs &r, const Plan &plan, bool by_key, uint32_t index)
 {
+    Unit u;
     if (r.query_start) {
-        if (index >= *plan.count) return false;
-        u = plan.units[index];
-        return true;
+        const int4 a = *reinterpret_cast<const int4 *>(plan.units + index), b = *(reinterpret_cast<const int4 *>(plan.units + index) + 1);
+        u.row = a.x, u.rows = a.y, u.pos = a.z, u.other_row = a.w, u.other_len = b.x, u.shift = b.y;
+        return u;
     }
-    const int64_t rows = by_key ? r.key_rows : r.query_rows;
-    if (index >= plan.most) return false;
-    if (!by_key) index = plan.most - 1 - index;
-    u.row = u.pos = (int)(index * plan.per);
-    u.rows = (int)min((int64_t)plan.per, rows - index * plan.per);
+    const int rows = (int)(by_key ? r.key_rows : r.query_rows);
+    if (!by_key) index = (uint32_t)plan.most - 1 - index;
+    u.row = u.pos = (int)index * plan.per;
+    u.rows = min(plan.per, rows - u.row);
     u.other_row = 0;
     u.other_len = (int)(by_key ? r.query_rows : r.key_rows);
     u.shift = (int)(r.key_rows - r.query_rows);
-    return true;
+    return u;
 }
+
+// A CTA's share of the work, (unit, split, head of k and v) with the head fastest: one of every round of gridDim.x, every other round from
+// the other end, so that the sums of what the CTAs get are nearly equal.  Every warp works it out for itself, from what is the same in all
+// lanes: then the loops and the products' descriptors are uniform values.  (Handed over in shared memory behind a barrier they are
+// not, for the compiler, and issuing a product takes a third longer: 967 against 847 us for 16384 tokens, 16 heads.)
+struct Walk {
+    const Runs &runs;
+    const Plan &plan;
+    bool by_key;
+    uint32_t kv_heads, splits, total, round = 0;
+    Unit unit;
+    int head, split;
+
+    __device__ __forceinline__ Walk(const Runs &r, const Plan &p, bool keys, int heads, int cuts) : runs(r), plan(p), by_key(keys), kv_heads(heads), splits(cuts)
+    {
+        total = units_of(r, p) * kv_heads * splits;
+    }
+    __device__ __forceinline__ bool next()
+    {
+        const uint32_t i = round * gridDim.x + (round & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+        if (i >= total) return false;
+        unit = unit_at(runs, plan, by_key, i / (kv_heads * splits));
+        head = (int)(i % kv_heads);
+        split = (int)(i / kv_heads % splits);
+        ++round;
+        return true;
+    }
+};
 
 // Keys [lo, hi) of the sequence that some of the queries pos .. pos + rows - 1 see.
 __device__ __forceinline__ void keys_seen(const Mask &m, int pos, int rows, int shift, int keys, int &lo, int &hi)
@@ -158,10 +187,77 @@ __device__ __forceinline__ float exp2_of(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// Eight neighbours of a row as bf16; rows start 16-byte aligned.
-__device__ __forceinline__ void store_bf16x8(__nv_bfloat16 *at, const float *v)
+// Two powers of two at a time without the exponential unit, which gives 4 a cycle and quarter of an SM where the others are
+// idle half of the time: x = n + f, |f| <= 1/2 (Cody and Waite), 2^f by the polynomial of degree 4 of least relative error (2.7e-6,
+// far below the bf16 that a probability is rounded to), n into the exponent.  x from 2^-120 up; below it the result is 2^-120.
+__device__ __forceinline__ f2 exp2_by_polynomial(f2 x)
 {
-    *reinterpret_cast<uint4 *>(at) = make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
+    x = f2_of(fmaxf(f2_lo(x), -120.0f), fmaxf(f2_hi(x), -120.0f));
+    const float big = 12582912.0f;                                      // 1.5 * 2^23: the sum's last bits are the nearest whole number
+    const f2 t = f2_add(x, f2_of(big, big)), f = f2_add(x, f2_mul(f2_add(t, f2_of(-big, -big)), f2_of(-1.0f, -1.0f)));
+    f2 y = f2_fma(f, f2_of(0.009570102207362652f, 0.009570102207362652f), f2_of(0.05591785907745361f, 0.05591785907745361f));
+    y = f2_fma(f, y, f2_of(0.240247443318367f, 0.240247443318367f));
+    y = f2_fma(f, y, f2_of(0.6931217908859253f, 0.6931217908859253f));
+    y = f2_fma(f, y, f2_of(0.9999992847442627f, 0.9999992847442627f));
+    return f2_of(__uint_as_float(((uint32_t)t << 23) + (uint32_t)y), __uint_as_float(((uint32_t)(t >> 32) << 23) + (uint32_t)(y >> 32)));
+}
+// exp2(v * c + m) in place of v; every kPolynomial-th pair by the polynomial where every entry is seen (-inf would not become zero).
+constexpr int kPolynomial = 4;
+template <int N, bool POLYNOMIAL>
+__device__ __forceinline__ void exponentials(float *v, f2 c, f2 m)
+{
+#pragma unroll
+    for (int n = 0; n < N; n += 2) {
+        f2 x = f2_fma(f2_of(v[n], v[n + 1]), c, m);
+        if (POLYNOMIAL && n / 2 % kPolynomial == kPolynomial - 1) {
+            x = exp2_by_polynomial(x);
+            v[n] = f2_lo(x);
+            v[n + 1] = f2_hi(x);
+        } else {
+            v[n] = exp2_of(f2_lo(x));
+            v[n + 1] = exp2_of(f2_hi(x));
+        }
+    }
+}
+// A warp's 32 rows of tensor memory (a lane per row, DP columns from taddr on) times `by` to rows of bf16; row: where the lane's row goes,
+// nullptr: nowhere.  Eight lanes exchange what they hold in steps of eight columns, so that they write 128 bytes of a row
+// together: a lane per row would make every 16 bytes a write of their own (32 lines an instruction, 2 us a tile of 128 x 128).
+template <int DP>
+__device__ __forceinline__ void store_rows(__nv_bfloat16 *row, int dim, uint32_t taddr, float by, bool any)
+{
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int j = 0; j < DP; j += 64) {
+        uint32_t x[8][4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint32_t o[32];
+            tc_read32(taddr + j + 32 * h, o);
+            tc_read_wait(o);
+#pragma unroll
+            for (int n = 0; n < 16; ++n)
+                x[4 * h + n / 4][n % 4] = any ? bf16_pair(__fmul_rn(__uint_as_float(o[2 * n]), by), __fmul_rn(__uint_as_float(o[2 * n + 1]), by)) : 0u;
+        }
+#pragma unroll
+        for (int s = 1; s < 8; s *= 2)                       // lane l, step i  <->  lane i, step l of every group of eight
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (!(i & s)) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const bool up = lane & s;
+                        const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? x[i][e] : x[i | s][e], s);
+                        if (up) x[i][e] = got;
+                        else x[i | s][e] = got;
+                    }
+                }
+        const int column = j + (lane & 7) * 8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            __nv_bfloat16 *out = reinterpret_cast<__nv_bfloat16 *>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(row), (lane & 24) + i));
+            if (out && column < dim) *reinterpret_cast<uint4 *>(out + column) = make_uint4(x[i][0], x[i][1], x[i][2], x[i][3]);
+        }
+    }
 }
 
 }  // namespace attention

@@ -20,7 +20,7 @@ using namespace attention;
 
 namespace {
 
-constexpr int kThreads = 384;           // warps 0..7: P and dS, 8: MMA, 9: TMA, 10 and 11 only give registers
+constexpr int kThreads = 384;           // warps 0..7: P and dS, the others issue products, loads
 constexpr int kRowRegisters = 208, kOtherRegisters = 88;      // 2 * 208 + 88 = 3 * 168 at the launch
 
 struct BackwardArgs {
@@ -35,35 +35,29 @@ struct BackwardArgs {
     const float *lse;
     __nv_bfloat16 *dq, *dk, *dv;
     int64_t ld_dq, head_stride_dq, ld_dk, head_stride_dk, ld_dv, head_stride_dv;
-    float *minus_lse2, *delta;          // [kv_heads][query rows][group]: -lse * log2(e), delta
+    float *minus_lse2, *minus_delta;    // [kv_heads][query rows][group]: -lse * log2(e), -delta
+    float heavy;                        // see attention_dkv_kernel
     int32_t *errword;
 };
 
 template <int DP>
 constexpr int kTileBytes = DP / 64 * kPiece;
 
-// 32 columns times `by` to a row of bf16.
-__device__ __forceinline__ void store_columns(__nv_bfloat16 *out, int column, int dim, uint32_t taddr, float by, bool live, bool any)
-{
-    uint32_t o[32];
-    tc_read32(taddr, o);
-    tc_read_wait(o);
-#pragma unroll
-    for (int n = 0; n < 32; n += 8)
-        if (live && column + n < dim) {
-            float f[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = any ? __fmul_rn(__uint_as_float(o[n + e]), by) : 0.0f;
-            store_bf16x8(out + column + n, f);
-        }
-}
-
 // ---- dq: a tile of queries goes over its keys --------------------------------------------------------------------------------
 // Tensor memory: S of two tiles of keys in turn (columns 0 and 128; dS takes its place), dP (256), dQ (384).
-// The tensor cores' order: dP(t + 1) once dP(t) has been read, dQ += dS(t) K(t), S(t + 2): the threads find the next S ready.
+// One warp issues S and dP, another dQ: issuing takes as long as the product, and while one waits for its next operands the other
+// issues.  S and dP of the next tile are made while the threads are at one.  delta is made by the rows' threads: the loads for a unit are
+// under way while the last unit's results are written.
 constexpr int kKeyStages = 3, kValueStages = 2;
+struct QueryBars {
+    uint64_t q_full, q_empty, k_full[kKeyStages], k_empty[kKeyStages], v_full[kValueStages], v_empty[kValueStages], s_full[2], s_empty[2], dp_full,
+        dp_taken, ds_full, dq_full, dq_empty;
+    float minus_lse2[2][kRows], minus_delta[2][kRows];
+    uint32_t tmem_base;
+    int failed;
+};
 template <int DP>
-constexpr int kQuerySmem = (2 + kKeyStages + kValueStages) * kTileBytes<DP> + 1024;
+constexpr int kQuerySmem = (2 + kKeyStages + kValueStages) * kTileBytes<DP> + (int)sizeof(QueryBars);
 
 template <int DP>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -71,203 +65,262 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
                     const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ BackwardArgs p)
 {
     constexpr int kTile = kTileBytes<DP>;
-    extern __shared__ uint8_t dyn_smem[];
-    __shared__ __align__(8) uint64_t q_full, k_full[kKeyStages], k_empty[kKeyStages], v_full[kValueStages], v_empty[kValueStages], s_full[2], dp_full,
-        dp_taken, ds_full, done;
-    __shared__ float delta_half[2][kRows];
-    __shared__ uint32_t tmem_base;
-    __shared__ volatile int failed;
+    extern __shared__ __align__(1024) uint8_t dyn_smem[];
+    QueryBars &b = *reinterpret_cast<QueryBars *>(dyn_smem + (2 + kKeyStages + kValueStages) * kTile);
+    volatile int &failed = *const_cast<volatile int *>(&b.failed);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t base = (smem_addr(dyn_smem) + 1023u) & ~1023u;
+    const uint32_t base = smem_addr(dyn_smem);
     const uint32_t q_tile = base, dy_tile = base + kTile, k_ring = base + 2 * kTile, v_ring = k_ring + kKeyStages * kTile;
 
     if (threadIdx.x == 0) {
-        failed = 0;
-        bar_init(smem_addr(&q_full), 1);
-        for (int s = 0; s < kKeyStages; ++s) bar_init(smem_addr(&k_full[s]), 1), bar_init(smem_addr(&k_empty[s]), 1);
-        for (int s = 0; s < kValueStages; ++s) bar_init(smem_addr(&v_full[s]), 1), bar_init(smem_addr(&v_empty[s]), 1);
-        for (int s = 0; s < 2; ++s) bar_init(smem_addr(&s_full[s]), 1);
-        bar_init(smem_addr(&dp_full), 1);
-        bar_init(smem_addr(&dp_taken), 8);
-        bar_init(smem_addr(&ds_full), 8);
-        bar_init(smem_addr(&done), 1);
+        failed = base & 1023u ? 1 : 0;                            // (the swizzle goes by addresses: nothing runs on another alignment)
+        bar_init(smem_addr(&b.q_full), 1);
+        bar_init(smem_addr(&b.q_empty), 1);
+        for (int s = 0; s < kKeyStages; ++s) bar_init(smem_addr(&b.k_full[s]), 1), bar_init(smem_addr(&b.k_empty[s]), 1);
+        for (int s = 0; s < kValueStages; ++s) bar_init(smem_addr(&b.v_full[s]), 1), bar_init(smem_addr(&b.v_empty[s]), 1);
+        for (int s = 0; s < 2; ++s) bar_init(smem_addr(&b.s_full[s]), 1), bar_init(smem_addr(&b.s_empty[s]), 1);
+        bar_init(smem_addr(&b.dp_full), 1);
+        bar_init(smem_addr(&b.dp_taken), 8);
+        bar_init(smem_addr(&b.ds_full), 8);
+        bar_init(smem_addr(&b.dq_full), 1);
+        bar_init(smem_addr(&b.dq_empty), 8);
         bar_init_fence();
     }
-    if (warp == 8) tc_alloc(&tmem_base, 512);
+    if (warp == 8) tc_alloc(&b.tmem_base, 512);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = tmem_base;
+    const uint32_t tmem = b.tmem_base;
     grid_wait();
-    const int kv_head = (int)(blockIdx.x % p.kv_heads), head0 = kv_head * p.group;
-    Unit u;
-    const bool any = unit_of(p.runs, p.plan, false, blockIdx.x / p.kv_heads, u);
-    int key_lo = 0, key_hi = 0;
-    if (any) keys_seen(p.mask, u.pos, u.rows, u.shift, u.other_len, key_lo, key_hi);
-    const int tiles = (key_hi - key_lo + kRows - 1) / kRows;
 
-    if (!any) {
-    } else if (warp >= 8) {
+    const auto keys_of = [&](const Unit &u, int &lo) {
+        int hi;
+        keys_seen(p.mask, u.pos, u.rows, u.shift, u.other_len, lo, hi);
+        return (hi - lo + kRows - 1) / kRows;
+    };
+    if (warp >= 8) {
         give_registers<kOtherRegisters>();
-        if (warp == 9) {
-            if (lane == 0 && tiles > 0) {
-                const uint32_t q_bytes = (uint32_t)p.queries * p.group * (DP * 2);
-                bar_expect(smem_addr(&q_full), 2 * q_bytes);
-                load_tile<DP>(q_tile, &map_q, smem_addr(&q_full), head0, u.row);
-                load_tile<DP>(dy_tile, &map_dy, smem_addr(&q_full), head0, u.row);
-                int sk = 0, sv = 0;
-                uint32_t ph_k = 1, ph_v = 1;
+        if (warp == 10 && lane == 0 && !failed) {
+            const uint32_t q_bytes = (uint32_t)p.queries * p.group * (DP * 2);
+            int sk = 0, sv = 0;
+            uint32_t ph_q = 1, ph_k = 1, ph_v = 1;
+            bool ok = true;
+            for (Walk w(p.runs, p.plan, false, p.kv_heads, 1); ok && w.next();) {
+                const Unit u = w.unit;
+                int key_lo;
+                const int tiles = keys_of(u, key_lo);
+                if (tiles == 0) continue;
+                if (!bar_wait(smem_addr(&b.q_empty), ph_q, &failed)) break;
+                ph_q ^= 1;
+                bar_expect(smem_addr(&b.q_full), 2 * q_bytes);
+                load_tile<DP>(q_tile, &map_q, smem_addr(&b.q_full), w.head * p.group, u.row);
+                load_tile<DP>(dy_tile, &map_dy, smem_addr(&b.q_full), w.head * p.group, u.row);
                 for (int t = 0; t < tiles; ++t) {
                     const int row = u.other_row + key_lo + t * kRows;
-                    if (!bar_wait(smem_addr(&k_empty[sk]), ph_k, &failed)) break;
-                    bar_expect(smem_addr(&k_full[sk]), kTile);
-                    load_tile<DP>(k_ring + sk * kTile, &map_k, smem_addr(&k_full[sk]), kv_head, row);
-                    if (!bar_wait(smem_addr(&v_empty[sv]), ph_v, &failed)) break;
-                    bar_expect(smem_addr(&v_full[sv]), kTile);
-                    load_tile<DP>(v_ring + sv * kTile, &map_v, smem_addr(&v_full[sv]), kv_head, row);
+                    if (!bar_wait(smem_addr(&b.k_empty[sk]), ph_k, &failed)) { ok = false; break; }
+                    bar_expect(smem_addr(&b.k_full[sk]), kTile);
+                    load_tile<DP>(k_ring + sk * kTile, &map_k, smem_addr(&b.k_full[sk]), w.head, row);
+                    if (!bar_wait(smem_addr(&b.v_empty[sv]), ph_v, &failed)) { ok = false; break; }
+                    bar_expect(smem_addr(&b.v_full[sv]), kTile);
+                    load_tile<DP>(v_ring + sv * kTile, &map_v, smem_addr(&b.v_full[sv]), w.head, row);
                     if (++sk == kKeyStages) sk = 0, ph_k ^= 1;
                     if (++sv == kValueStages) sv = 0, ph_v ^= 1;
                 }
             }
-        } else if (warp == 8 && tiles > 0) {
+        } else if (warp == 8) {
             const bool issuer = elect_one();
-            int sk = 0, sd = 0, sv = 0;                       // stages of S's K, of dQ's K, of V
-            uint32_t ph_k = 0, ph_v = 0;
-            // S(t): waits for K(t); its rows behind the sequence become zero, since dQ sums over them
-            const auto make_s = [&](int t) {
-                if (!bar_wait_together(smem_addr(&k_full[sk]), ph_k, &failed)) return false;
-                const uint32_t tile = k_ring + sk * kTile;
-                const int live = u.other_len - (key_lo + t * kRows);
-                if (live < kRows) clear_rows<DP>(tile, live);
-                tc_fence_after();
-                if (issuer) {
-                    product_of_tiles<DP>(tmem + (t & 1) * kRows, q_tile, tile);
-                    tc_commit(smem_addr(&s_full[t & 1]));
+            int sk = 0, sv = 0, g = 0;                        // stages, tiles so far
+            uint32_t ph_q = 0, ph_k = 0, ph_v = 0;
+            bool ok = true;
+            for (Walk w(p.runs, p.plan, false, p.kv_heads, 1); ok && w.next();) {
+                const Unit u = w.unit;
+                int key_lo;
+                const int tiles = keys_of(u, key_lo);
+                if (tiles == 0) continue;
+                if (!bar_wait_together(smem_addr(&b.q_full), ph_q, &failed)) break;
+                ph_q ^= 1;
+                for (int t = 0; t < tiles; ++t, ++g) {
+                    const int buf = g & 1;
+                    // S: its place is free once dQ has read dS of two tiles ago; K's rows behind the sequence become zero, since dQ sums over them
+                    if (!bar_wait_together(smem_addr(&b.k_full[sk]), ph_k, &failed) ||
+                        !bar_wait_together(smem_addr(&b.s_empty[buf]), ((g >> 1) & 1) ^ 1, &failed)) { ok = false; break; }
+                    const uint32_t tile = k_ring + sk * kTile;
+                    const int live = u.other_len - (key_lo + t * kRows);
+                    if (live < kRows) clear_rows<DP>(tile, live);
+                    tc_fence_after();
+                    if (issuer) {
+                        product_of_tiles<DP>(tmem + buf * kRows, q_tile, tile);
+                        tc_commit(smem_addr(&b.s_full[buf]));
+                    }
+                    __syncwarp();
+                    if (++sk == kKeyStages) sk = 0, ph_k ^= 1;
+                    // dP: once the threads have the last one
+                    if (!bar_wait_together(smem_addr(&b.v_full[sv]), ph_v, &failed) ||
+                        !bar_wait_together(smem_addr(&b.dp_taken), (g & 1) ^ 1, &failed)) { ok = false; break; }
+                    tc_fence_after();
+                    if (issuer) {
+                        product_of_tiles<DP>(tmem + 256, dy_tile, v_ring + sv * kTile);
+                        tc_commit(smem_addr(&b.dp_full));
+                        tc_commit(smem_addr(&b.v_empty[sv]));
+                        if (t == tiles - 1) tc_commit(smem_addr(&b.q_empty));
+                    }
+                    __syncwarp();
+                    if (++sv == kValueStages) sv = 0, ph_v ^= 1;
                 }
-                __syncwarp();
-                if (++sk == kKeyStages) sk = 0, ph_k ^= 1;
-                return true;
-            };
-            const auto make_dp = [&]() {
-                if (!bar_wait_together(smem_addr(&v_full[sv]), ph_v, &failed)) return false;
-                tc_fence_after();
-                if (issuer) {
-                    product_of_tiles<DP>(tmem + 256, dy_tile, v_ring + sv * kTile);
-                    tc_commit(smem_addr(&dp_full));
-                    tc_commit(smem_addr(&v_empty[sv]));
-                }
-                __syncwarp();
-                if (++sv == kValueStages) sv = 0, ph_v ^= 1;
-                return true;
-            };
-            bool ok = bar_wait_together(smem_addr(&q_full), 0, &failed) && make_s(0) && make_dp() && (tiles < 2 || make_s(1));
-            for (int t = 0; t < tiles && ok; ++t) {
-                if (t + 1 < tiles && !(bar_wait_together(smem_addr(&dp_taken), t & 1, &failed) && make_dp())) break;
-                if (!bar_wait_together(smem_addr(&ds_full), t & 1, &failed)) break;
-                tc_fence_after();
-                if (issuer) {
+            }
+        } else if (warp == 9) {
+            const bool issuer = elect_one();
+            int sd = 0, g = 0;
+            uint32_t ph_o = 1;
+            bool ok = true;
+            for (Walk w(p.runs, p.plan, false, p.kv_heads, 1); ok && w.next();) {
+                const Unit u = w.unit;
+                int key_lo;
+                const int tiles = keys_of(u, key_lo);
+                if (tiles == 0) continue;
+                if (!bar_wait_together(smem_addr(&b.dq_empty), ph_o, &failed)) break;          // the last unit's dQ has been read
+                ph_o ^= 1;
+                for (int t = 0; t < tiles; ++t, ++g) {
+                    const int buf = g & 1;
+                    if (!bar_wait_together(smem_addr(&b.ds_full), g & 1, &failed)) { ok = false; break; }
+                    tc_fence_after();
+                    if (issuer) {
 #pragma unroll
-                    for (int ks = 0; ks < kRows / 16; ++ks)
-                        product_step<DP>(tmem + 384, tmem + (t & 1) * kRows + ks / 4 * 64 + ks % 4 * 8, k_ring + sd * kTile, ks, t > 0 || ks > 0);
-                    tc_commit(smem_addr(&k_empty[sd]));
-                    if (t == tiles - 1) tc_commit(smem_addr(&done));
+                        for (int ks = 0; ks < kRows / 16; ++ks)
+                            product_step<DP>(tmem + 384, tmem + buf * kRows + ks / 4 * 64 + ks % 4 * 8, k_ring + sd * kTile, ks, t > 0 || ks > 0);
+                        tc_commit(smem_addr(&b.s_empty[buf]));
+                        tc_commit(smem_addr(&b.k_empty[sd]));
+                        if (t == tiles - 1) tc_commit(smem_addr(&b.dq_full));
+                    }
+                    __syncwarp();
+                    if (++sd == kKeyStages) sd = 0;
                 }
-                __syncwarp();
-                if (++sd == kKeyStages) sd = 0;
-                if (t + 2 < tiles && !make_s(t + 2)) break;      // (after the product that reads dS in the same columns)
             }
         }
     } else {
         take_registers<kRowRegisters>();
         const int half = warp >> 2;                              // of the columns
         const int row = (warp & 3) * 32 + lane;                  // of the tile
-        const int query = row / p.group, head = head0 + row - query * p.group;
-        const bool live = query < p.queries && query < u.rows;
-        const int64_t q = (int64_t)u.row + query;
-        int lo = 0, hi = 0x7fffffff;                             // (rows that nobody reads need no mask)
-        if (live) keys_seen(p.mask, u.pos + query, 1, u.shift, u.other_len, lo, hi);
-        // delta, half of the columns to each group of warps
-        float part = 0.0f, minus_lse2 = 0.0f;
-        if (live) {
-            const __nv_bfloat16 *a = p.dy + q * p.ld_dy + head * p.head_stride_dy, *b = p.y + q * p.ld_y + head * p.head_stride_y;
-            float sums[4] = {};
-#pragma unroll 4
-            for (int j = half * (DP / 2); j < (half + 1) * (DP / 2); j += 8)
-                if (j < p.dim) {
-                    float x[8], z[8];
-                    load8<__nv_bfloat16, true>(a, j, p.dim, x);
-                    load8<__nv_bfloat16, true>(b, j, p.dim, z);
-#pragma unroll
-                    for (int n = 0; n < 8; ++n) sums[n & 3] = __fmaf_rn(x[n], z[n], sums[n & 3]);
-                }
-            part = __fadd_rn(__fadd_rn(sums[0], sums[1]), __fadd_rn(sums[2], sums[3]));
-            const float lse = p.lse[q * p.heads + head];
-            minus_lse2 = lse == -INFINITY ? 0.0f : -__fmul_rn(lse, kLog2e);
-        }
-        delta_half[half][row] = part;
-        asm volatile("bar.sync 1, 256;" ::: "memory");
-        const float delta = __fadd_rn(delta_half[0][row], delta_half[1][row]);
-        if (live && half == 0) {
-            const int64_t at = ((int64_t)kv_head * p.runs.query_rows + u.row) * p.group + row;
-            p.minus_lse2[at] = minus_lse2;
-            p.delta[at] = delta;
-        }
+        const int query = row / p.group, of_group = row - query * p.group;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const f2 cc = f2_of(p.scale_log2, p.scale_log2), mm = f2_of(minus_lse2, minus_lse2), dd = f2_of(-delta, -delta);
+        const f2 cc = f2_of(p.scale_log2, p.scale_log2);
+        int g = 0, number = 0;
+        uint32_t ph_o = 0;
         bool ok = true;
-        for (int t = 0; t < tiles; ++t) {
-            const uint32_t s_at = tmem + lanes + (t & 1) * kRows + half * 64;
-            if (!bar_wait_together(smem_addr(&s_full[t & 1]), (t >> 1) & 1, &failed)) { ok = false; break; }
-            tc_fence_after();
-            float v[64];
+        // delta: a warp has sixteen of the tile's rows, eight or sixteen lanes to a row
+        constexpr int kLanes = DP / 8, kPass = 32 / kLanes, kPasses = 16 / kPass;
+        const int part = lane % kLanes;
+        uint4 dy8[kPasses], y8[kPasses];
+        float lse = 0.0f;
+        const auto load_ahead = [&](const Unit &u, int kv_head) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) tc_read32(s_at + 32 * j, reinterpret_cast<uint32_t(&)[32]>(v[32 * j]));
-#pragma unroll
-            for (int j = 0; j < 2; ++j) tc_read_wait(reinterpret_cast<uint32_t(&)[32]>(v[32 * j]));
-#pragma unroll
-            for (int n = 0; n < 64; n += 2) {
-                const f2 x = f2_fma(f2_of(v[n], v[n + 1]), cc, mm);
-                v[n] = exp2_of(f2_lo(x));
-                v[n + 1] = exp2_of(f2_hi(x));
+            for (int n = 0; n < kPasses; ++n) {
+                const int r = warp * 16 + n * kPass + lane / kLanes, i = r / p.group, head = kv_head * p.group + r - i * p.group;
+                dy8[n] = y8[n] = make_uint4(0, 0, 0, 0);
+                if (i < min(p.queries, u.rows) && part * 8 < p.dim) {
+                    const int64_t q = (int64_t)u.row + i;
+                    dy8[n] = __ldg(reinterpret_cast<const uint4 *>(p.dy + q * p.ld_dy + head * p.head_stride_dy) + part);
+                    y8[n] = __ldg(reinterpret_cast<const uint4 *>(p.y + q * p.ld_y + head * p.head_stride_y) + part);
+                }
             }
-            if (!bar_wait_together(smem_addr(&dp_full), t & 1, &failed)) { ok = false; break; }
-            tc_fence_after();
-            float d[64];
+            if (half == 0 && query < min(p.queries, u.rows)) lse = p.lse[((int64_t)u.row + query) * p.heads + kv_head * p.group + of_group];
+        };
+        Walk walk(p.runs, p.plan, false, p.kv_heads, 1);
+        bool more = walk.next();
+        if (more) load_ahead(walk.unit, walk.head);
+        while (more) {
+            const Unit u = walk.unit;
+            const int kv_head = walk.head;
+            int key_lo;
+            const int tiles = keys_of(u, key_lo);
+            const bool live = query < p.queries && query < u.rows;
+            int lo = 0, hi = 0x7fffffff;                         // (rows that nobody reads need no mask)
+            if (live) keys_seen(p.mask, u.pos + query, 1, u.shift, u.other_len, lo, hi);
+            const int64_t at = ((int64_t)kv_head * p.runs.query_rows + u.row) * p.group;
+            float *rows_lse = b.minus_lse2[number & 1], *rows_delta = b.minus_delta[number & 1];
+            ++number;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) tc_read32(tmem + lanes + 256 + half * 64 + 32 * j, reinterpret_cast<uint32_t(&)[32]>(d[32 * j]));
+            for (int n = 0; n < kPasses; ++n) {
+                const uint32_t a[4] = {dy8[n].x, dy8[n].y, dy8[n].z, dy8[n].w}, z[4] = {y8[n].x, y8[n].y, y8[n].z, y8[n].w};
+                float sum = 0.0f;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) tc_read_wait(reinterpret_cast<uint32_t(&)[32]>(d[32 * j]));
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(smem_addr(&dp_taken));
+                for (int e = 0; e < 4; ++e) {
+                    sum = __fmaf_rn(__uint_as_float(a[e] << 16), __uint_as_float(z[e] << 16), sum);
+                    sum = __fmaf_rn(__uint_as_float(a[e] & 0xffff0000u), __uint_as_float(z[e] & 0xffff0000u), sum);
+                }
 #pragma unroll
-            for (int n = 0; n < 64; n += 2) {
-                const f2 x = f2_mul(f2_of(v[n], v[n + 1]), f2_add(f2_of(d[n], d[n + 1]), dd));
-                v[n] = f2_lo(x);
-                v[n + 1] = f2_hi(x);
+                for (int o = kLanes / 2; o > 0; o >>= 1) sum = __fadd_rn(sum, __shfl_xor_sync(0xffffffffu, sum, o));
+                const int r = warp * 16 + n * kPass + lane / kLanes;
+                if (part == 0) {
+                    rows_delta[r] = -sum;
+                    if (r < min(p.queries, u.rows) * p.group) p.minus_delta[at + r] = -sum;
+                }
             }
-            const int key0 = key_lo + t * kRows + half * 64, from = lo - key0, to = hi - key0;
-            if (__any_sync(0xffffffffu, from > 0 || to < 64)) {
-#pragma unroll
-                for (int n = 0; n < 64; ++n) v[n] = n >= from && n < to ? v[n] : 0.0f;
+            if (half == 0) {
+                const float m = !live || lse == -INFINITY ? 0.0f : -__fmul_rn(lse, kLog2e);
+                rows_lse[row] = m;
+                if (live) p.minus_lse2[at + row] = m;
             }
-            uint32_t w[32];
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+            const float m0 = rows_lse[row], d0 = rows_delta[row];
+            const f2 mm = f2_of(m0, m0), dd = f2_of(d0, d0);
+            for (int t = 0; t < tiles; ++t, ++g) {
+                const uint32_t s_at = tmem + lanes + (g & 1) * kRows + half * 64;
+                if (!bar_wait_together(smem_addr(&b.s_full[g & 1]), (g >> 1) & 1, &failed)) { ok = false; break; }
+                tc_fence_after();
+                float v[64];
 #pragma unroll
-            for (int n = 0; n < 64; n += 2) w[n >> 1] = bf16_pair(v[n], v[n + 1]);
-            tc_write32(s_at, w);
-            tc_write_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(smem_addr(&ds_full));
-        }
-        if (ok && tiles > 0 && !bar_wait_together(smem_addr(&done), 0, &failed)) ok = false;
-        if (ok) {
-            tc_fence_after();
-            __nv_bfloat16 *out = p.dq + q * p.ld_dq + head * p.head_stride_dq;
+                for (int j = 0; j < 2; ++j) tc_read32(s_at + 32 * j, reinterpret_cast<uint32_t(&)[32]>(v[32 * j]));
 #pragma unroll
-            for (int j = 0; j < DP / 2; j += 32) {
-                const int column = half * (DP / 2) + j;
-                store_columns(out, column, p.dim, tmem + lanes + 384 + column, p.scale, live, tiles > 0);
+                for (int j = 0; j < 2; ++j) tc_read_wait(reinterpret_cast<uint32_t(&)[32]>(v[32 * j]));
+                const int key0 = key_lo + t * kRows + half * 64, from = lo - key0, to = hi - key0;
+                const bool masked = __any_sync(0xffffffffu, from > 0 || to < 64);
+                if (masked) exponentials<64, false>(v, cc, mm);
+                else exponentials<64, true>(v, cc, mm);
+                if (!bar_wait_together(smem_addr(&b.dp_full), g & 1, &failed)) { ok = false; break; }
+                tc_fence_after();
+                float d[64];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) tc_read32(tmem + lanes + 256 + half * 64 + 32 * j, reinterpret_cast<uint32_t(&)[32]>(d[32 * j]));
+#pragma unroll
+                for (int j = 0; j < 2; ++j) tc_read_wait(reinterpret_cast<uint32_t(&)[32]>(d[32 * j]));
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(smem_addr(&b.dp_taken));
+                uint32_t w[32];
+#pragma unroll
+                for (int n = 0; n < 64; n += 2) {
+                    const f2 x = f2_mul(f2_of(v[n], v[n + 1]), f2_add(f2_of(d[n], d[n + 1]), dd));
+                    w[n >> 1] = bf16_pair(f2_lo(x), f2_hi(x));
+                }
+                if (masked) {                                    // whatever an unseen entry holds, also a NaN
+#pragma unroll
+                    for (int n = 0; n < 64; n += 2)
+                        w[n >> 1] = (n >= from && n < to ? w[n >> 1] & 0xffffu : 0u) | (n + 1 >= from && n + 1 < to ? w[n >> 1] & 0xffff0000u : 0u);
+                }
+                tc_write32(s_at, w);
+                tc_write_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(smem_addr(&b.ds_full));
+            }
+            if (!ok) break;
+            const int head = kv_head * p.group + of_group, column = half * (DP / 2);
+            more = walk.next();
+            if (more) load_ahead(walk.unit, walk.head);
+            if (tiles > 0) {
+                if (!bar_wait_together(smem_addr(&b.dq_full), ph_o, &failed)) break;
+                ph_o ^= 1;
+                tc_fence_after();
+            }
+            const int64_t q = (int64_t)u.row + query;
+            __nv_bfloat16 *out = live ? p.dq + q * p.ld_dq + head * p.head_stride_dq : nullptr;
+            if (DP == 128) store_rows<64>(out ? out + column : nullptr, p.dim - column, tmem + lanes + 384 + column, p.scale, tiles > 0);
+            else if (half == 0) store_rows<64>(out, p.dim, tmem + lanes + 384, p.scale, tiles > 0);
+            if (tiles > 0) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(smem_addr(&b.dq_empty));
             }
         }
     }
@@ -280,221 +333,368 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
 
 // ---- dk and dv: a tile of keys goes over the queries that see it -----------------------------------------------------------------
 // Tensor memory: S^T (columns 0; P^T takes its place), dP^T (128; dS^T takes its place), dV (256), dK (256 + DP).
-// The tensor cores' order: dV += P(t) dY(t), S(t + 1), dK += dS(t) Q(t), dP(t + 1): while the threads are at P they have dK and dP
-// to do, while they are at dS, dV and the next S.
-constexpr int kPairStages = 2;          // of Q and dY
+// The tensor cores' order: dV += P(t) dY(t) as the halves of P come, S(t + 1), dK += dS(t) Q(t), dP(t + 1): while the threads are at P
+// they have dK and dP to do, while they are at dS, dV and the next S.  One warp issues them all: two warps' products would share the
+// tensor cores, and the next S, for which the threads wait, would come later (3640 against 3200 us for the whole backward pass of
+// 16384 tokens, 16 heads).
+//
+// Keys that most queries look at (the first of a sequence, often) have gradients hundreds of times the others', and P's rounding to
+// bf16 would be off by as much as the others' gradients.  So the threads keep a sample of a key's probabilities' sum, and
+// once it is sixteen times what a key has on average, the tiles that follow take P and dS as two bf16 numbers each (the second: what the
+// first has lost) in two more products.  The decision goes by sums of earlier tiles in the unit, the same in every call.
+constexpr int kQueryStages = 3, kDyStages = 2, kRowStages = 2;
+struct KeyBars {
+    uint64_t kv_full, kv_empty, q_full[kQueryStages], q_empty[kQueryStages], dy_full[kDyStages], dy_empty[kDyStages], row_full[kRowStages],
+        row_empty[kRowStages], s_full, p_full[2], dp_full, ds_full, sums_full, sums_empty;
+    uint32_t tmem_base;
+    int failed, heavy_unit, two_terms[2];
+};
 template <int DP>
-constexpr int kKeySmem = (2 + 2 * kPairStages) * kTileBytes<DP> + kPairStages * kRows * 8 + 1024;
+constexpr int kKeySmem = (2 + kQueryStages + kDyStages) * kTileBytes<DP> + kRowStages * kRows * 8 + (int)sizeof(KeyBars);
+
+// What a pair of numbers loses when it becomes the bf16 pair w.
+__device__ __forceinline__ uint32_t bf16_lost(float lo, float hi, uint32_t w)
+{
+    return bf16_pair(__fsub_rn(lo, __uint_as_float(w << 16)), __fsub_rn(hi, __uint_as_float(w & 0xffff0000u)));
+}
+// A place in a ring of buffers.
+template <int STAGES>
+struct Ring {
+    int at = 0;
+    uint32_t phase;
+    __device__ __forceinline__ explicit Ring(uint32_t first) : phase(first) {}
+    __device__ __forceinline__ void next()
+    {
+        if (++at == STAGES) at = 0, phase ^= 1;
+    }
+};
 
 template <int DP>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                      const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ BackwardArgs p)
 {
-    constexpr int kTile = kTileBytes<DP>;
-    extern __shared__ uint8_t dyn_smem[];
-    __shared__ __align__(8) uint64_t kv_full, q_full[kPairStages], q_empty[kPairStages], dy_full[kPairStages], dy_empty[kPairStages],
-        row_full[kPairStages], s_full, p_full, dp_full, ds_full, done;
-    __shared__ uint32_t tmem_base;
-    __shared__ volatile int failed;
+    constexpr int kTile = kTileBytes<DP>, kTiles = (2 + kQueryStages + kDyStages) * kTile;
+    extern __shared__ __align__(1024) uint8_t dyn_smem[];
+    KeyBars &b = *reinterpret_cast<KeyBars *>(dyn_smem + kTiles + kRowStages * kRows * 8);
+    volatile int &failed = *const_cast<volatile int *>(&b.failed), &heavy_unit = *const_cast<volatile int *>(&b.heavy_unit);
+    volatile int *two_terms = b.two_terms;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t base = (smem_addr(dyn_smem) + 1023u) & ~1023u;
-    const uint32_t k_tile = base, v_tile = base + kTile, q_ring = base + 2 * kTile, dy_ring = q_ring + kPairStages * kTile,
-                   rows_at = dy_ring + kPairStages * kTile;       // [stage][-lse2 of 128 rows, delta of 128 rows]
+    const uint32_t base = smem_addr(dyn_smem);
+    const uint32_t k_tile = base, v_tile = base + kTile, q_ring = base + 2 * kTile, dy_ring = q_ring + kQueryStages * kTile,
+                   rows_at = base + kTiles;                       // [stage][-lse2 of 128 rows, -delta of 128 rows]
 
     if (threadIdx.x == 0) {
-        failed = 0;
-        bar_init(smem_addr(&kv_full), 1);
-        for (int s = 0; s < kPairStages; ++s) {
-            bar_init(smem_addr(&q_full[s]), 1), bar_init(smem_addr(&q_empty[s]), 1);
-            bar_init(smem_addr(&dy_full[s]), 1), bar_init(smem_addr(&dy_empty[s]), 1);
-            bar_init(smem_addr(&row_full[s]), 1);
-        }
-        bar_init(smem_addr(&s_full), 1);
-        bar_init(smem_addr(&p_full), 8);
-        bar_init(smem_addr(&dp_full), 1);
-        bar_init(smem_addr(&ds_full), 8);
-        bar_init(smem_addr(&done), 1);
+        failed = base & 1023u ? 1 : 0;                            // (the swizzle goes by addresses: nothing runs on another alignment)
+        heavy_unit = 0;
+        bar_init(smem_addr(&b.kv_full), 1);
+        bar_init(smem_addr(&b.kv_empty), 1);
+        for (int s = 0; s < kQueryStages; ++s) bar_init(smem_addr(&b.q_full[s]), 1), bar_init(smem_addr(&b.q_empty[s]), 1);
+        for (int s = 0; s < kDyStages; ++s) bar_init(smem_addr(&b.dy_full[s]), 1), bar_init(smem_addr(&b.dy_empty[s]), 1);
+        for (int s = 0; s < kRowStages; ++s) bar_init(smem_addr(&b.row_full[s]), 1), bar_init(smem_addr(&b.row_empty[s]), 8);
+        bar_init(smem_addr(&b.s_full), 2);                        // the product, and the word that says how P is wanted
+        bar_init(smem_addr(&b.p_full[0]), 8);
+        bar_init(smem_addr(&b.p_full[1]), 8);
+        bar_init(smem_addr(&b.dp_full), 1);
+        bar_init(smem_addr(&b.ds_full), 8);
+        bar_init(smem_addr(&b.sums_full), 1);
+        bar_init(smem_addr(&b.sums_empty), 8);
         bar_init_fence();
     }
-    if (warp == 8) tc_alloc(&tmem_base, 512);
+    if (warp == 8) tc_alloc(&b.tmem_base, 512);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = tmem_base;
+    const uint32_t tmem = b.tmem_base;
     grid_wait();
-    const int kv_head = (int)(blockIdx.x % p.kv_heads), head0 = kv_head * p.group;
-    Unit u;
-    const bool any = unit_of(p.runs, p.plan, true, blockIdx.x / p.kv_heads, u);
-    int query_lo = 0, query_hi = 0;
-    if (any) queries_seeing(p.mask, u.pos, u.rows, u.shift, u.other_len, query_lo, query_hi);
-    const int tiles = (query_hi - query_lo + p.queries - 1) / p.queries;
 
-    if (!any) {
-    } else if (warp >= 8) {
+    const auto queries_of = [&](const Unit &u, int &lo) {
+        int hi;
+        queries_seeing(p.mask, u.pos, u.rows, u.shift, u.other_len, lo, hi);
+        return (hi - lo + p.queries - 1) / p.queries;
+    };
+    if (warp >= 8) {
         give_registers<kOtherRegisters>();
-        if (warp == 9) {
+        if (warp == 9 && lane == 0 && !failed) {
             const uint32_t q_bytes = (uint32_t)p.queries * p.group * (DP * 2);
-            if (lane == 0 && tiles > 0) {
-                bar_expect(smem_addr(&kv_full), 2 * kTile);
-                load_tile<DP>(k_tile, &map_k, smem_addr(&kv_full), kv_head, u.row);
-                load_tile<DP>(v_tile, &map_v, smem_addr(&kv_full), kv_head, u.row);
+            Ring<kQueryStages> rq(1);
+            Ring<kDyStages> rd(1);
+            uint32_t ph_kv = 1;
+            bool ok = true;
+            for (Walk w(p.runs, p.plan, true, p.kv_heads, 1); ok && w.next();) {
+                const Unit u = w.unit;
+                int query_lo;
+                const int tiles = queries_of(u, query_lo);
+                if (tiles == 0) continue;
+                if (!bar_wait(smem_addr(&b.kv_empty), ph_kv, &failed)) break;
+                ph_kv ^= 1;
+                bar_expect(smem_addr(&b.kv_full), 2 * kTile);
+                load_tile<DP>(k_tile, &map_k, smem_addr(&b.kv_full), w.head, u.row);
+                load_tile<DP>(v_tile, &map_v, smem_addr(&b.kv_full), w.head, u.row);
+                for (int t = 0; t < tiles; ++t) {
+                    const int row = u.other_row + query_lo + t * p.queries;
+                    if (!bar_wait(smem_addr(&b.q_empty[rq.at]), rq.phase, &failed)) { ok = false; break; }
+                    bar_expect(smem_addr(&b.q_full[rq.at]), q_bytes);
+                    load_tile<DP>(q_ring + rq.at * kTile, &map_q, smem_addr(&b.q_full[rq.at]), w.head * p.group, row);
+                    if (!bar_wait(smem_addr(&b.dy_empty[rd.at]), rd.phase, &failed)) { ok = false; break; }
+                    bar_expect(smem_addr(&b.dy_full[rd.at]), q_bytes);
+                    load_tile<DP>(dy_ring + rd.at * kTile, &map_dy, smem_addr(&b.dy_full[rd.at]), w.head * p.group, row);
+                    rq.next();
+                    rd.next();
+                }
             }
-            int s = 0;
-            uint32_t phase = 1;
-            for (int t = 0; t < tiles; ++t) {
-                const int first = query_lo + t * p.queries;
-                if (!bar_wait_together(smem_addr(&q_empty[s]), phase, &failed)) break;
-                if (lane == 0) {
-                    bar_expect(smem_addr(&q_full[s]), q_bytes);
-                    load_tile<DP>(q_ring + s * kTile, &map_q, smem_addr(&q_full[s]), head0, u.other_row + first);
-                }
-                if (!bar_wait_together(smem_addr(&dy_empty[s]), phase, &failed)) break;
-                if (lane == 0) {
-                    bar_expect(smem_addr(&dy_full[s]), q_bytes);
-                    load_tile<DP>(dy_ring + s * kTile, &map_dy, smem_addr(&dy_full[s]), head0, u.other_row + first);
-                }
-                // (dK(t - 2), which q_empty told of, came after the threads had read these rows)
-                const int live = min(p.queries, u.other_len - first) * p.group;
-                const int64_t at = ((int64_t)kv_head * p.runs.query_rows + u.other_row + first) * p.group;
-                float a[4], b[4];
+        } else if (warp == 10) {
+            Ring<kRowStages> rr(1);
+            bool ok = true;
+            for (Walk w(p.runs, p.plan, true, p.kv_heads, 1); ok && w.next();) {
+                const Unit u = w.unit;
+                int query_lo;
+                const int tiles = queries_of(u, query_lo);
+                for (int t = 0; t < tiles; ++t) {
+                    const int first = query_lo + t * p.queries;
+                    const int rows = min(p.queries, u.other_len - first) * p.group;
+                    const int64_t at = ((int64_t)w.head * p.runs.query_rows + u.other_row + first) * p.group;
+                    float l[4], d[4];
 #pragma unroll
-                for (int n = 0; n < 4; ++n) {
-                    const int r = n * 32 + lane;
-                    a[n] = r < live ? p.minus_lse2[at + r] : 0.0f;
-                    b[n] = r < live ? p.delta[at + r] : 0.0f;
-                }
+                    for (int n = 0; n < 4; ++n) {
+                        const int r = n * 32 + lane;
+                        l[n] = r < rows ? p.minus_lse2[at + r] : 0.0f;
+                        d[n] = r < rows ? p.minus_delta[at + r] : 0.0f;
+                    }
+                    if (!bar_wait_together(smem_addr(&b.row_empty[rr.at]), rr.phase, &failed)) { ok = false; break; }
 #pragma unroll
-                for (int n = 0; n < 4; ++n) {
-                    const uint32_t to = rows_at + s * (kRows * 8) + (n * 32 + lane) * 4;
-                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(to), "f"(a[n]) : "memory");
-                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + kRows * 4), "f"(-b[n]) : "memory");
+                    for (int n = 0; n < 4; ++n) {
+                        const uint32_t to = rows_at + rr.at * (kRows * 8) + (n * 32 + lane) * 4;
+                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(to), "f"(l[n]) : "memory");
+                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + kRows * 4), "f"(d[n]) : "memory");
+                    }
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(smem_addr(&b.row_full[rr.at]));
+                    rr.next();
                 }
-                __syncwarp();
-                if (lane == 0) bar_arrive(smem_addr(&row_full[s]));
-                if (++s == kPairStages) s = 0, phase ^= 1;
             }
-        } else if (warp == 8 && tiles > 0) {
+        } else if (warp == 8) {
             const bool issuer = elect_one();
-            // Rows that are not the sequence's, or that the group leaves over, become zero: dV and dK sum over them.
-            const auto make = [&](int t, uint64_t *full, uint32_t a, uint32_t ring, uint32_t d, uint64_t *ready) {
-                const int s = t % kPairStages;
-                if (!bar_wait_together(smem_addr(&full[s]), (t / kPairStages) & 1, &failed)) return false;
-                const int live = min(p.queries, u.other_len - (query_lo + t * p.queries)) * p.group;
-                if (live < kRows) clear_rows<DP>(ring + s * kTile, live);
-                tc_fence_after();
-                if (issuer) {
-                    product_of_tiles<DP>(d, a, ring + s * kTile);
-                    tc_commit(smem_addr(ready));
-                }
-                __syncwarp();
-                return true;
-            };
-            const auto add = [&](int t, uint32_t d, uint32_t operand, uint32_t ring, uint64_t *empty) {
-                const int s = t % kPairStages;
-                tc_fence_after();
-                if (issuer) {
+            int g = 0, number = 0;                               // tiles so far, units so far
+            Ring<kQueryStages> made_q(0), used_q(0);             // of the next S, of the next dK
+            Ring<kDyStages> made_dy(0), used_dy(0);              // of the next dP, of the next dV
+            uint32_t ph_kv = 0, ph_o = 1;
+            bool ok = true;
+            for (Walk w(p.runs, p.plan, true, p.kv_heads, 1); ok && w.next();) {
+                const Unit u = w.unit;
+                int query_lo;
+                const int tiles = queries_of(u, query_lo);
+                ++number;
+                if (tiles == 0) continue;
+                // A tile is there.  Rows that are not the sequence's, or that the group leaves over, become zero: dV and dK sum over them.
+                const auto loaded = [&](uint64_t &full, uint32_t phase, uint32_t tile, int t) {
+                    if (!bar_wait_together(smem_addr(&full), phase, &failed)) return false;
+                    const int live = min(p.queries, u.other_len - (query_lo + t * p.queries)) * p.group;
+                    if (live < kRows) clear_rows<DP>(tile, live);
+                    return true;
+                };
+                const auto make_s = [&](int t) {
+                    tc_fence_after();
+                    if (issuer) {
+                        product_of_tiles<DP>(tmem, k_tile, q_ring + made_q.at * kTile);
+                        tc_commit(smem_addr(&b.s_full));
+                        two_terms[(g + (t > 0)) & 1] = t > 0 && heavy_unit == number;
+                        bar_arrive(smem_addr(&b.s_full));
+                    }
+                    __syncwarp();
+                    made_q.next();
+                };
+                const auto make_dp = [&](int t) {
+                    tc_fence_after();
+                    if (issuer) {
+                        product_of_tiles<DP>(tmem + 128, v_tile, dy_ring + made_dy.at * kTile);
+                        tc_commit(smem_addr(&b.dp_full));
+                        if (t == tiles - 1) tc_commit(smem_addr(&b.kv_empty));            // (the last S has been issued too)
+                    }
+                    __syncwarp();
+                    made_dy.next();
+                };
+                // steps of 16 rows of a sum, those of the threads' first halves and then of the second
+                const auto add = [&](uint32_t d, uint32_t operand, uint32_t tile, int half, bool more) {
 #pragma unroll
-                    for (int ks = 0; ks < kRows / 16; ++ks) product_step<DP>(d, operand + ks / 4 * 64 + ks % 4 * 8, ring + s * kTile, ks, t > 0 || ks > 0);
-                    tc_commit(smem_addr(&empty[s]));
+                    for (int n = 0; n < 4; ++n) {
+                        const int ks = (n >> 1) * 4 + half * 2 + (n & 1);
+                        product_step<DP>(d, operand + ks / 4 * 64 + ks % 4 * 8, tile, ks, more || n > 0);
+                    }
+                };
+                if (!bar_wait_together(smem_addr(&b.kv_full), ph_kv, &failed) || !loaded(b.q_full[made_q.at], made_q.phase, q_ring + made_q.at * kTile, 0)) break;
+                ph_kv ^= 1;
+                make_s(0);
+                if (!loaded(b.dy_full[made_dy.at], made_dy.phase, dy_ring + made_dy.at * kTile, 0)) break;
+                make_dp(0);
+                if (!bar_wait_together(smem_addr(&b.sums_empty), ph_o, &failed)) break;          // the last unit's sums have been read
+                ph_o ^= 1;
+                for (int t = 0; t < tiles; ++t, ++g) {
+                    const uint32_t q_tile = q_ring + used_q.at * kTile, dy_tile = dy_ring + used_dy.at * kTile;
+                    // what may have been there for long is waited for first
+                    if (t + 1 < tiles && !loaded(b.q_full[made_q.at], made_q.phase, q_ring + made_q.at * kTile, t + 1)) { ok = false; break; }
+                    if (!bar_wait_together(smem_addr(&b.p_full[0]), g & 1, &failed)) { ok = false; break; }
+                    const int two = __shfl_sync(0xffffffffu, two_terms[g & 1], 0);
+                    tc_fence_after();
+                    if (issuer) {
+                        add(tmem + 256, tmem, dy_tile, 0, t > 0);
+                        if (two) add(tmem + 256, tmem + 32, dy_tile, 0, true);
+                    }
+                    __syncwarp();
+                    if (!bar_wait_together(smem_addr(&b.p_full[1]), g & 1, &failed)) { ok = false; break; }
+                    tc_fence_after();
+                    if (issuer) {
+                        add(tmem + 256, tmem, dy_tile, 1, true);
+                        if (two) add(tmem + 256, tmem + 32, dy_tile, 1, true);
+                        tc_commit(smem_addr(&b.dy_empty[used_dy.at]));
+                    }
+                    __syncwarp();
+                    used_dy.next();
+                    // (the next S takes the columns of P, the next dP those of dS: the tensor cores work in order)
+                    if (t + 1 < tiles) {
+                        make_s(t + 1);
+                        if (!loaded(b.dy_full[made_dy.at], made_dy.phase, dy_ring + made_dy.at * kTile, t + 1)) { ok = false; break; }
+                    }
+                    if (!bar_wait_together(smem_addr(&b.ds_full), g & 1, &failed)) { ok = false; break; }
+                    tc_fence_after();
+                    if (issuer) {
+                        add(tmem + 256 + DP, tmem + 128, q_tile, 0, t > 0);
+                        add(tmem + 256 + DP, tmem + 128, q_tile, 1, true);
+                        if (two) {
+                            add(tmem + 256 + DP, tmem + 160, q_tile, 0, true);
+                            add(tmem + 256 + DP, tmem + 160, q_tile, 1, true);
+                        }
+                        tc_commit(smem_addr(&b.q_empty[used_q.at]));
+                        if (t == tiles - 1) tc_commit(smem_addr(&b.sums_full));
+                    }
+                    __syncwarp();
+                    used_q.next();
+                    if (t + 1 < tiles) make_dp(t + 1);
                 }
-                __syncwarp();
-            };
-            bool ok = bar_wait_together(smem_addr(&kv_full), 0, &failed) && make(0, q_full, k_tile, q_ring, tmem, &s_full) &&
-                      make(0, dy_full, v_tile, dy_ring, tmem + 128, &dp_full);
-            for (int t = 0; t < tiles && ok; ++t) {
-                if (!bar_wait_together(smem_addr(&p_full), t & 1, &failed)) break;
-                add(t, tmem + 256, tmem, dy_ring, dy_empty);
-                // (the next S takes the columns of P, the next dP those of dS: the tensor cores work in order)
-                if (t + 1 < tiles && !make(t + 1, q_full, k_tile, q_ring, tmem, &s_full)) break;
-                if (!bar_wait_together(smem_addr(&ds_full), t & 1, &failed)) break;
-                add(t, tmem + 256 + DP, tmem + 128, q_ring, q_empty);
-                if (t + 1 < tiles && !make(t + 1, dy_full, v_tile, dy_ring, tmem + 128, &dp_full)) break;
-                if (t == tiles - 1 && issuer) tc_commit(smem_addr(&done));
-                __syncwarp();
             }
         }
     } else {
         take_registers<kRowRegisters>();
         const int half = warp >> 2;                              // of the columns
         const int row = (warp & 3) * 32 + lane;                  // the key
-        const bool live = row < u.rows;
-        int seen_lo = 0, seen_hi = u.other_len;                  // by these queries of the sequence (keys that nobody reads: by all)
-        if (live) queries_seeing(p.mask, u.pos + row, 1, u.shift, u.other_len, seen_lo, seen_hi);
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t s_at = tmem + lanes + half * 64, d_at = s_at + 128;
         const f2 cc = f2_of(p.scale_log2, p.scale_log2);
+        int g = 0, number = 0;
+        Ring<kRowStages> rr(0);
+        uint32_t ph_o = 0;
         bool ok = true;
-        for (int t = 0; t < tiles; ++t) {
-            const int s = t % kPairStages;
-            const uint32_t rows = rows_at + s * (kRows * 8) + half * 256;
-            if (!bar_wait_together(smem_addr(&row_full[s]), (t / kPairStages) & 1, &failed) || !bar_wait_together(smem_addr(&s_full), t & 1, &failed)) {
-                ok = false;
-                break;
-            }
-            tc_fence_after();
-            float v[64];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) tc_read32(s_at + 32 * j, reinterpret_cast<uint32_t(&)[32]>(v[32 * j]));
-#pragma unroll
-            for (int j = 0; j < 2; ++j) tc_read_wait(reinterpret_cast<uint32_t(&)[32]>(v[32 * j]));
-#pragma unroll
-            for (int n = 0; n < 64; n += 4) {
-                f2 m[2];
-                asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(m[0]), "=l"(m[1]) : "r"(rows + n * 4));
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const f2 x = f2_fma(f2_of(v[n + 2 * e], v[n + 2 * e + 1]), cc, m[e]);
-                    v[n + 2 * e] = exp2_of(f2_lo(x));
-                    v[n + 2 * e + 1] = exp2_of(f2_hi(x));
+        for (Walk walk(p.runs, p.plan, true, p.kv_heads, 1); ok && walk.next();) {
+            const Unit u = walk.unit;
+            int query_lo;
+            const int tiles = queries_of(u, query_lo);
+            ++number;
+            const bool live = row < u.rows;
+            int seen_lo = 0, seen_hi = u.other_len;              // by these queries of the sequence (keys that nobody reads: by all)
+            if (live) queries_seeing(p.mask, u.pos + row, 1, u.shift, u.other_len, seen_lo, seen_hi);
+            f2 mass = 0;                                         // of every eighth column's probabilities
+            for (int t = 0; t < tiles; ++t, ++g) {
+                const uint32_t rows = rows_at + rr.at * (kRows * 8) + half * 256;
+                if (!bar_wait_together(smem_addr(&b.row_full[rr.at]), rr.phase, &failed) || !bar_wait_together(smem_addr(&b.s_full), g & 1, &failed)) {
+                    ok = false;
+                    break;
                 }
-            }
-            // of the tile's rows, those of the queries that see the key
-            const int first = query_lo + t * p.queries;
-            const int from = max(0, min(p.queries, seen_lo - first)) * p.group - half * 64, to = max(0, min(p.queries, seen_hi - first)) * p.group - half * 64;
-            if (__any_sync(0xffffffffu, from > 0 || to < 64)) {
+                tc_fence_after();
+                const int two = two_terms[g & 1];
+                // (after this tile's S, before its P: read in between the P and the next S, by tiles in front of this one)
+                if (live && __fadd_rn(f2_lo(mass), f2_hi(mass)) > p.heavy) heavy_unit = number;
+                float v[64];
 #pragma unroll
-                for (int n = 0; n < 64; ++n) v[n] = n >= from && n < to ? v[n] : 0.0f;
-            }
-            uint32_t w[32];
+                for (int j = 0; j < 2; ++j) tc_read32(s_at + 32 * j, reinterpret_cast<uint32_t(&)[32]>(v[32 * j]));
 #pragma unroll
-            for (int n = 0; n < 64; n += 2) w[n >> 1] = bf16_pair(v[n], v[n + 1]);
-            tc_write32(s_at, w);
-            tc_write_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(smem_addr(&p_full));
-            if (!bar_wait_together(smem_addr(&dp_full), t & 1, &failed)) { ok = false; break; }
-            tc_fence_after();
-            float d[64];
+                for (int j = 0; j < 2; ++j) tc_read_wait(reinterpret_cast<uint32_t(&)[32]>(v[32 * j]));
+                // of the tile's rows, those of the queries that see the key
+                const int first = query_lo + t * p.queries;
+                const int from = max(0, min(p.queries, seen_lo - first)) * p.group - half * 64, to = max(0, min(p.queries, seen_hi - first)) * p.group - half * 64;
+                const bool masked = __any_sync(0xffffffffu, from > 0 || to < 64);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) tc_read32(d_at + 32 * j, reinterpret_cast<uint32_t(&)[32]>(d[32 * j]));
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t w[16];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) tc_read_wait(reinterpret_cast<uint32_t(&)[32]>(d[32 * j]));
+                    for (int n = 32 * h; n < 32 * h + 32; n += 4) {
+                        f2 m[2];
+                        asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(m[0]), "=l"(m[1]) : "r"(rows + n * 4));
 #pragma unroll
-            for (int n = 0; n < 64; n += 4) {
-                f2 m[2];
-                asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(m[0]), "=l"(m[1]) : "r"(rows + kRows * 4 + n * 4));
+                        for (int e = 0; e < 4; e += 2) {
+                            const f2 x = f2_fma(f2_of(v[n + e], v[n + e + 1]), cc, m[e / 2]);
+                            v[n + e] = exp2_of(f2_lo(x));
+                            v[n + e + 1] = exp2_of(f2_hi(x));
+                        }
+                    }
+                    if (masked) {
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const f2 x = f2_mul(f2_of(v[n + 2 * e], v[n + 2 * e + 1]), f2_add(f2_of(d[n + 2 * e], d[n + 2 * e + 1]), m[e]));
-                    w[(n >> 1) + e] = bf16_pair(f2_lo(x), f2_hi(x));
+                        for (int n = 32 * h; n < 32 * h + 32; ++n) v[n] = n >= from && n < to ? v[n] : 0.0f;
+                    }
+#pragma unroll
+                    for (int n = 0; n < 32; n += 2) w[n >> 1] = bf16_pair(v[32 * h + n], v[32 * h + n + 1]);
+                    tc_write16(s_at + 16 * h, w);
+                    if (two) {
+#pragma unroll
+                        for (int n = 0; n < 32; n += 2) w[n >> 1] = bf16_lost(v[32 * h + n], v[32 * h + n + 1], w[n >> 1]);
+                        tc_write16(s_at + 32 + 16 * h, w);
+                    }
+                    tc_write_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(smem_addr(&b.p_full[h]));
                 }
+#pragma unroll
+                for (int n = 0; n < 64; n += 16) mass = f2_add(mass, f2_of(v[n], v[n + 1]));
+                if (!bar_wait_together(smem_addr(&b.dp_full), g & 1, &failed)) { ok = false; break; }
+                tc_fence_after();
+                float d[64];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) tc_read32(d_at + 32 * j, reinterpret_cast<uint32_t(&)[32]>(d[32 * j]));
+#pragma unroll
+                for (int j = 0; j < 2; ++j) tc_read_wait(reinterpret_cast<uint32_t(&)[32]>(d[32 * j]));
+                uint32_t w[32];
+#pragma unroll
+                for (int n = 0; n < 64; n += 4) {
+                    f2 m[2];
+                    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(m[0]), "=l"(m[1]) : "r"(rows + kRows * 4 + n * 4));
+#pragma unroll
+                    for (int e = 0; e < 4; e += 2) {
+                        const f2 x = f2_mul(f2_of(v[n + e], v[n + e + 1]), f2_add(f2_of(d[n + e], d[n + e + 1]), m[e / 2]));
+                        d[n + e] = f2_lo(x);
+                        d[n + e + 1] = f2_hi(x);
+                        w[(n + e) >> 1] = bf16_pair(d[n + e], d[n + e + 1]);
+                    }
+                }
+                tc_write32(d_at, w);
+                if (two) {
+#pragma unroll
+                    for (int n = 0; n < 64; n += 2) w[n >> 1] = bf16_lost(d[n], d[n + 1], w[n >> 1]);
+                    tc_write32(d_at + 32, w);
+                }
+                tc_write_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    bar_arrive(smem_addr(&b.ds_full));
+                    bar_arrive(smem_addr(&b.row_empty[rr.at]));
+                }
+                rr.next();
             }
-            tc_write32(d_at, w);
-            tc_write_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(smem_addr(&ds_full));
-        }
-        if (ok && tiles > 0 && !bar_wait_together(smem_addr(&done), 0, &failed)) ok = false;
-        if (ok) {
-            tc_fence_after();
+            if (!ok) break;
+            if (tiles > 0) {
+                if (!bar_wait_together(smem_addr(&b.sums_full), ph_o, &failed)) break;
+                ph_o ^= 1;
+                tc_fence_after();
+            }
             // one group of warps writes dv, the other dk
             const int64_t key = (int64_t)u.row + row;
-            __nv_bfloat16 *out = half ? p.dk + key * p.ld_dk + kv_head * p.head_stride_dk : p.dv + key * p.ld_dv + kv_head * p.head_stride_dv;
-#pragma unroll
-            for (int j = 0; j < DP; j += 32) store_columns(out, j, p.dim, tmem + lanes + 256 + half * DP + j, half ? p.scale : 1.0f, live, tiles > 0);
+            __nv_bfloat16 *out = half ? p.dk + key * p.ld_dk + walk.head * p.head_stride_dk : p.dv + key * p.ld_dv + walk.head * p.head_stride_dv;
+            store_rows<DP>(live ? out : nullptr, p.dim, tmem + lanes + 256 + half * DP, half ? p.scale : 1.0f, tiles > 0);
+            if (tiles > 0) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(smem_addr(&b.sums_empty));
+            }
         }
     }
     let_copies_land(&failed);
@@ -516,7 +716,8 @@ cudaError_t launch_both(const Maps &m, const BackwardArgs &by_query, const Backw
         return f != cudaSuccess ? f : cudaFuncSetAttribute(attention_dkv_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, kKeySmem<DP>);
     });
     if (e != cudaSuccess) return e;
-    const dim3 grid_q((unsigned)(by_query.plan.most * by_query.kv_heads)), grid_k((unsigned)(by_key.plan.most * by_key.kv_heads));
+    const int64_t work_q = by_query.plan.most * by_query.kv_heads, work_k = by_key.plan.most * by_key.kv_heads, sms = sm_count();
+    const dim3 grid_q((unsigned)(work_q < sms ? work_q : sms)), grid_k((unsigned)work_k);
     if (grid_q.x > 0) {
         if (dependent) {
             e = launch_dependent_smem(attention_dq_kernel<DP>, grid_q, dim3(kThreads), kQuerySmem<DP>, s, m.q, m.k, m.v, m.dy, by_query);
@@ -562,7 +763,9 @@ cudaError_t launch_attention_backward(const AttentionShape &a, const Heads &dy, 
     p.dq = static_cast<__nv_bfloat16 *>(dq.p), p.ld_dq = dq.ld, p.head_stride_dq = dq.head_stride;
     p.dk = static_cast<__nv_bfloat16 *>(dk.p), p.ld_dk = dk.ld, p.head_stride_dk = dk.head_stride;
     p.dv = static_cast<__nv_bfloat16 *>(dv.p), p.ld_dv = dv.ld, p.head_stride_dv = dv.head_stride;
-    p.minus_lse2 = reinterpret_cast<float *>(at), p.delta = reinterpret_cast<float *>(at + row_bytes(a));
+    p.minus_lse2 = reinterpret_cast<float *>(at), p.minus_delta = reinterpret_cast<float *>(at + row_bytes(a));
+    const double mean = a.key_rows > 0 ? (double)a.query_rows * group / a.key_rows : 0.0;     // of a key's sum of probabilities
+    p.heavy = (float)(mean > 1.0 ? mean : 1.0);                // half of the columns, one in eight of them, sixteen times the mean
     at += 2 * row_bytes(a);
     BackwardArgs by_key = p;
     p.plan = plan_at(at, a.query_start, a.query_rows, queries, a.sequences);
