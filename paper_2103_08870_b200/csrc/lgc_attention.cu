@@ -32,8 +32,8 @@ struct ForwardArgs {
     __nv_bfloat16 *y;
     int64_t ld_y, head_stride_y;
     float *lse;
-    int chunk, splits;                  // tiles of keys of a split, at least
-    float *part_y, *part_lse;           // splits > 1: [splits][query rows][heads][dim], [splits][query rows][heads]
+    float *part_y, *part_lse;           // plan.splits > 1: [splits][query rows][heads][dim], [splits][query rows][heads]
+    int *parts;                         // ... and how many there are, [query rows][heads]
     int32_t *errword;
 };
 
@@ -49,7 +49,7 @@ struct Range {
     int base, begin, end;
     int first[2], last[2];
 };
-__device__ __forceinline__ Range range_of(const ForwardArgs &p, const Unit &u, int split)
+__device__ __forceinline__ Range range_of(const ForwardArgs &p, const Unit &u)
 {
     Range r;
     int lo[2], hi[2];
@@ -58,10 +58,9 @@ __device__ __forceinline__ Range range_of(const ForwardArgs &p, const Unit &u, i
         keys_seen(p.mask, u.pos + s * p.queries, min(p.queries, u.rows - s * p.queries), u.shift, u.other_len, lo[s], hi[s]);
     r.base = hi[0] == 0 ? lo[1] : hi[1] == 0 ? lo[0] : min(lo[0], lo[1]);
     int from = 0, to = 0x7fffffff;                         // tiles of this split
-    if (p.splits > 1) {
-        const int tiles = (max(hi[0], hi[1]) - r.base + kRows - 1) >> 7;
-        const int chunk = max(p.chunk, (tiles + p.splits - 1) / p.splits);
-        from = split * chunk;
+    if (u.splits > 1) {
+        const int tiles = (max(hi[0], hi[1]) - r.base + kRows - 1) >> 7, chunk = (tiles + u.splits - 1) / u.splits;
+        from = u.split * chunk;
         to = from + chunk;
     }
     r.begin = 0x7fffffff;
@@ -130,9 +129,9 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             int st = 0;
             uint32_t phase = 1, q_phase[2] = {1, 1};
             bool ok = true;
-            for (Walk w(p.runs, p.plan, false, p.kv_heads, p.splits); ok && w.next();) {
+            for (Walk w(p.runs, p.plan, false, p.kv_heads); ok && w.next();) {
                 const Unit u = w.unit;
-                const Range r = range_of(p, u, w.split);
+                const Range r = range_of(p, u);
                 if (r.end == 0) continue;
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
@@ -156,9 +155,9 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             int st_k = 0, st_v = 1;                          // stages of K(t + 1) and V(t)
             uint32_t ph_k = 0, ph_v = 0, ph_q[2] = {0, 0}, ph_p[2] = {0, 0}, ph_o = 1;
             bool ok = true;
-            for (Walk w(p.runs, p.plan, false, p.kv_heads, p.splits); ok && w.next();) {
+            for (Walk w(p.runs, p.plan, false, p.kv_heads); ok && w.next();) {
                 const Unit u = w.unit;
-                const Range r = range_of(p, u, w.split);
+                const Range r = range_of(p, u);
                 if (r.end == 0) continue;
                 for (int t = r.begin - 1; t < r.end && ok; ++t) {
                     const bool has_v = t >= r.begin, has_k = t + 1 < r.end;
@@ -227,9 +226,9 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         const float c = p.scale_log2;
         uint32_t ph_s = 0, ph_o = 0;
         bool ok = true;
-        for (Walk walk(p.runs, p.plan, false, p.kv_heads, p.splits); ok && walk.next();) {
+        for (Walk walk(p.runs, p.plan, false, p.kv_heads); ok && walk.next();) {
             const Unit u = walk.unit;
-            const Range r = range_of(p, u, walk.split);
+            const Range r = range_of(p, u);
             const int i = slot * p.queries + query;                              // of the unit
             const bool live = query < p.queries && i < u.rows;
             int lo = 0, hi = 0x7fffffff;                                         // (rows that nobody reads need no mask)
@@ -316,11 +315,12 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             const int64_t q = (int64_t)u.row + i;
             const int64_t at = q * p.heads + head;
             const float lse = sum == 0.0f ? -INFINITY : __fmul_rn(__fadd_rn(__fmul_rn(most, c), log2f(sum)), kLn2);
-            if (p.splits > 1) {
+            if (p.plan.splits > 1) {
                 const int64_t all = p.runs.query_rows * p.heads;
-                if (live) p.part_lse[walk.split * all + at] = lse;
+                if (live) p.part_lse[u.split * all + at] = lse;
+                if (live && u.split == 0) p.parts[at] = u.splits;
                 if (last > 0) {                              // (the part of a split without keys is not read)
-                    float *out = p.part_y + (walk.split * all + at) * p.dim;
+                    float *out = p.part_y + (u.split * all + at) * p.dim;
 #pragma unroll
                     for (int j = 0; j < DP; j += 32) {
                         uint32_t o[32];
@@ -366,13 +366,14 @@ join_kernel(const __grid_constant__ ForwardArgs p)
         // (starts ascend: the row lies in a run if it lies between the first and the last)
         if (q < max((int64_t)0, p.runs.query_start[0]) || q >= p.runs.query_start[p.runs.sequences]) return;
     }
+    const int splits = p.parts[at];
     float most = -INFINITY;
-    for (int z = lane; z < p.splits; z += 32) most = fmaxf(most, p.part_lse[z * all + at]);
+    for (int z = lane; z < splits; z += 32) most = fmaxf(most, p.part_lse[z * all + at]);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
     const float zero = most == -INFINITY ? 0.0f : most;
     float total = 0.0f, y[4] = {};
-    for (int z = 0; z < p.splits; ++z) {
+    for (int z = 0; z < splits; ++z) {
         const float lse = p.part_lse[z * all + at];
         const float w = exp2_of(__fmul_rn(__fsub_rn(lse, zero), kLog2e));
         total = __fadd_rn(total, w);
@@ -392,34 +393,41 @@ join_kernel(const __grid_constant__ ForwardArgs p)
 }
 
 // The table of units.  One CTA per table: units in front of every sequence's, then the units in the order of their work (the
-// order among equals varies from call to call; every unit is computed by itself, so results do not).
+// order among equals varies from call to call; every unit is computed by itself, so results do not).  Up to kPlanThreads sequences
+// stay in shared memory; more go through the table's own prefix in memory.
 struct PlanArgs {
     Runs runs;
     Mask mask;
     Plan plan[2];
     int by_key[2];
 };
-constexpr int kPlanThreads = 1024, kBins = 256;
+constexpr int kPlanThreads = 512, kBins = 256;
 
-__device__ __forceinline__ int64_t start_of(const int64_t *start, int s, int64_t rows)
+__device__ __forceinline__ int start_of(const int64_t *start, int s, int64_t rows)
 {
     const int64_t r = start[s];
-    return r < 0 ? 0 : r > rows ? rows : r;
+    return (int)(r < 0 ? 0 : r > rows ? rows : r);
 }
-__device__ __forceinline__ Unit unit_number(const PlanArgs &a, const Plan &plan, bool by_key, int e)
+struct Starts {
+    const int *prefix, *query, *key;      // of every sequence, and behind the last; query, key: nullptr: from the call's arrays
+};
+__device__ __forceinline__ Unit unit_number(const PlanArgs &a, const Starts &st, const Plan &plan, bool by_key, int e)
 {
     int lo = 0, hi = a.runs.sequences;                        // prefix[lo] <= e < prefix[hi]
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (plan.prefix[mid] <= e) lo = mid;
+        if (st.prefix[mid] <= e) lo = mid;
         else hi = mid;
     }
     const Runs &r = a.runs;
-    const int q0 = (int)start_of(r.query_start, lo, r.query_rows), q1 = (int)start_of(r.query_start, lo + 1, r.query_rows);
-    const int k0 = (int)start_of(r.key_start, lo, r.key_rows), k1 = (int)start_of(r.key_start, lo + 1, r.key_rows);
+    const int q0 = st.query ? st.query[lo] : start_of(r.query_start, lo, r.query_rows), q1 = st.query ? st.query[lo + 1] : start_of(r.query_start, lo + 1, r.query_rows);
+    const int k0 = st.key ? st.key[lo] : start_of(r.key_start, lo, r.key_rows), k1 = st.key ? st.key[lo + 1] : start_of(r.key_start, lo + 1, r.key_rows);
     const int queries = max(0, q1 - q0), keys = max(0, k1 - k0);
     Unit u;
-    u.pos = (e - plan.prefix[lo]) * plan.per;
+    u.splits = by_key ? 1 : parts_of(plan, keys);
+    const int number = e - st.prefix[lo];
+    u.split = number % u.splits;
+    u.pos = number / u.splits * plan.per;
     u.row = (by_key ? k0 : q0) + u.pos;
     u.rows = min(plan.per, (by_key ? keys : queries) - u.pos);
     u.other_row = by_key ? q0 : k0;
@@ -432,22 +440,40 @@ __device__ __forceinline__ int work_of(const PlanArgs &a, bool by_key, const Uni
     int lo, hi;
     if (by_key) queries_seeing(a.mask, u.pos, u.rows, u.shift, u.other_len, lo, hi);
     else keys_seen(a.mask, u.pos, u.rows, u.shift, u.other_len, lo, hi);
-    return (hi - lo + kRows - 1) / kRows;
+    return ((hi - lo + kRows - 1) / kRows + u.splits - 1) / u.splits;
 }
 
 __global__ void __launch_bounds__(kPlanThreads)
 plan_kernel(const __grid_constant__ PlanArgs a)
 {
-    __shared__ long long of_warp[32];
-    __shared__ int bins[kBins], most_work;
+    __shared__ long long of_warp[kPlanThreads / 32];
+    __shared__ int bins[kBins], most_work, prefix[kPlanThreads + 1], starts[2][kPlanThreads + 1];
     const bool by_key = a.by_key[blockIdx.x] != 0;
     const Plan &plan = a.plan[blockIdx.x];
-    const int S = a.runs.sequences, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int S = a.runs.sequences, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tid = (int)threadIdx.x;
     const int64_t *start = by_key ? a.runs.key_start : a.runs.query_start;
     const int64_t rows = by_key ? a.runs.key_rows : a.runs.query_rows;
-    const int each = (S + kPlanThreads - 1) / kPlanThreads, from = min(S, (int)threadIdx.x * each), to = min(S, from + each);
+    const bool few = S <= kPlanThreads;
+    const int each = (S + kPlanThreads - 1) / kPlanThreads, from = min(S, tid * each), to = min(S, from + each);
+    if (few)
+        for (int s = tid; s <= S; s += kPlanThreads) {
+            starts[0][s] = start_of(a.runs.query_start, s, a.runs.query_rows);
+            starts[1][s] = start_of(a.runs.key_start, s, a.runs.key_rows);
+        }
+    if (tid < kBins) bins[tid] = 0;
+    if (tid == 0) most_work = 0;
+    __syncthreads();
+    const Starts st{few ? prefix : plan.prefix, few ? starts[0] : nullptr, few ? starts[1] : nullptr};
+    int *to_prefix = few ? prefix : plan.prefix;
+    const auto units = [&](int s) {
+        const int b = few ? starts[by_key][s] : start_of(start, s, rows), e = few ? starts[by_key][s + 1] : start_of(start, s + 1, rows);
+        const int n = (max(0, e - b) + plan.per - 1) / plan.per;
+        if (plan.splits == 1) return n;
+        const int k0 = few ? starts[1][s] : start_of(a.runs.key_start, s, a.runs.key_rows), k1 = few ? starts[1][s + 1] : start_of(a.runs.key_start, s + 1, a.runs.key_rows);
+        return n * parts_of(plan, max(0, k1 - k0));
+    };
     long long mine = 0;
-    for (int s = from; s < to; ++s) mine += (max((int64_t)0, start_of(start, s + 1, rows) - start_of(start, s, rows)) + plan.per - 1) / plan.per;
+    for (int s = from; s < to; ++s) mine += units(s);
     long long before = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -455,11 +481,10 @@ plan_kernel(const __grid_constant__ PlanArgs a)
         if (lane >= o) before += v;
     }
     if (lane == 31) of_warp[warp] = before;
-    if (threadIdx.x < kBins) bins[threadIdx.x] = 0;
-    if (threadIdx.x == 0) most_work = 0;
     __syncthreads();
     long long total = 0;
     before -= mine;
+#pragma unroll
     for (int w = 0; w < kPlanThreads / 32; ++w) {
         if (w < warp) before += of_warp[w];
         total += of_warp[w];
@@ -467,19 +492,25 @@ plan_kernel(const __grid_constant__ PlanArgs a)
     // (starts that do not ascend could ask for more units than there is room for: those are left out)
     const long long cap = plan.most;
     for (int s = from; s < to; ++s) {
-        plan.prefix[s] = (int)min(before, cap);
-        before += (max((int64_t)0, start_of(start, s + 1, rows) - start_of(start, s, rows)) + plan.per - 1) / plan.per;
+        to_prefix[s] = (int)min(before, cap);
+        before += units(s);
     }
     const int n = (int)min(total, cap);
-    if (threadIdx.x == 0) plan.prefix[S] = n, *plan.count = n;
+    if (tid == 0) to_prefix[S] = n, *plan.count = n;
     __syncthreads();
-    int top = 0;
-    for (int e = threadIdx.x; e < n; e += kPlanThreads) top = max(top, work_of(a, by_key, unit_number(a, plan, by_key, e)));
-    atomicMax(&most_work, top);
+    // the first kPlanThreads units stay in registers through the three steps
+    Unit first{};
+    int first_work = 0;
+    if (tid < n) first = unit_number(a, st, plan, by_key, tid), first_work = work_of(a, by_key, first);
+    int top = first_work;
+    for (int e = tid + kPlanThreads; e < n; e += kPlanThreads) top = max(top, work_of(a, by_key, unit_number(a, st, plan, by_key, e)));
+    top = __reduce_max_sync(0xffffffffu, top);
+    if (lane == 0) atomicMax(&most_work, top);
     __syncthreads();
     const int shift = max(0, 24 - __clz(most_work | 1));      // most_work >> shift is below kBins
-    for (int e = threadIdx.x; e < n; e += kPlanThreads)
-        atomicAdd(&bins[kBins - 1 - (work_of(a, by_key, unit_number(a, plan, by_key, e)) >> shift)], 1);
+    const auto bin = [&](int work) { return &bins[kBins - 1 - (work >> shift)]; };
+    if (tid < n) atomicAdd(bin(first_work), 1);
+    for (int e = tid + kPlanThreads; e < n; e += kPlanThreads) atomicAdd(bin(work_of(a, by_key, unit_number(a, st, plan, by_key, e))), 1);
     __syncthreads();
     if (warp == 0) {                                          // units in front of every bin
         int sum = 0, of[kBins / 32];
@@ -498,29 +529,29 @@ plan_kernel(const __grid_constant__ PlanArgs a)
         for (int i = 0; i < kBins / 32; ++i) bins[lane * (kBins / 32) + i] = up - sum + of[i];
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < n; e += kPlanThreads) {
-        const Unit u = unit_number(a, plan, by_key, e);
-        plan.units[atomicAdd(&bins[kBins - 1 - (work_of(a, by_key, u) >> shift)], 1)] = u;
+    if (tid < n) plan.units[atomicAdd(bin(first_work), 1)] = first;
+    for (int e = tid + kPlanThreads; e < n; e += kPlanThreads) {
+        const Unit u = unit_number(a, st, plan, by_key, e);
+        plan.units[atomicAdd(bin(work_of(a, by_key, u)), 1)] = u;
     }
 }
 
-// How the keys are cut: only where the tiles of queries leave half of the SMs without work.  A split has at least `chunk` tiles of
-// keys: as many as give every SM a CTA if all sequences were of average length, two at least (a split's partial result is written
-// and read once more).  Longer sequences have more splits, up to four times the average's.
+// How the keys are cut: only where there are fewer units than would fill two rounds of CTAs, and so few rows that the parts' results,
+// which are written and read once more, are much less than the keys.  A part has at least `chunk` tiles of keys: as many as make
+// the work one round (ragged sequences: three rounds of shorter ones), two at least.  `splits` bounds their number.
 struct Splits {
     int chunk, splits;
 };
 Splits splits_of(const AttentionShape &a, int64_t units)
 {
     const int64_t tiles = (a.key_rows + kRows - 1) / kRows, ctas = units * a.kv_heads, sms = 148;
-    if (ctas == 0 || ctas * 2 > sms || tiles < 4) return Splits{0, 1};
-    const int64_t average = (tiles + a.sequences - 1) / a.sequences;
-    int64_t chunk = (average * ctas + sms - 1) / sms;
+    if (ctas == 0 || ctas >= 2 * sms || tiles < 8 || a.query_rows * (a.heads / a.kv_heads) * 8 > a.key_rows) return Splits{1, 1};
+    const int64_t average = (tiles + a.sequences - 1) / a.sequences, rounds = a.query_start ? 3 : 1;      // tiles of a sequence
+    int64_t chunk = (average * ctas + rounds * sms - 1) / (rounds * sms);
     if (chunk < 2) chunk = 2;
     int64_t splits = (tiles + chunk - 1) / chunk;
-    const int64_t most = (a.query_start ? 4 : 1) * ((sms + ctas - 1) / ctas);
-    if (splits > most) splits = most;
-    return splits > 1 ? Splits{(int)chunk, (int)splits} : Splits{0, 1};
+    if (splits > 64) splits = 64;
+    return splits > 1 ? Splits{(int)chunk, (int)splits} : Splits{1, 1};
 }
 int queries_of_tile(const AttentionShape &a) { return kRows / (a.heads / a.kv_heads); }
 
@@ -530,7 +561,7 @@ cudaError_t launch_forward(const CUtensorMap &q, const CUtensorMap &k, const CUt
     static OncePerDevice configured;
     cudaError_t e = configured.run([&] { return cudaFuncSetAttribute(attention_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem<DP>); });
     if (e != cudaSuccess) return e;
-    const int64_t work = p.plan.most * p.kv_heads * p.splits, sms = sm_count();
+    const int64_t work = p.plan.most * p.kv_heads, sms = sm_count();
     const dim3 grid((unsigned)(work < sms ? work : sms));
     if (dependent) {
         e = launch_dependent_smem(attention_kernel<DP>, grid, dim3(kThreads), kSmem<DP>, s, q, k, v, p);
@@ -573,9 +604,9 @@ size_t attention_scratch(const AttentionShape &a)
 {
     const int per = 2 * queries_of_tile(a);
     const Splits z = splits_of(a, most_units(a.query_start, a.query_rows, per, a.sequences));
-    size_t bytes = plan_bytes(a.query_start, a.query_rows, per, a.sequences);
-    if (z.splits > 1) bytes += (size_t)z.splits * a.query_rows * a.heads * ((size_t)a.dim + 1) * 4;
-    return bytes < 16 ? 16 : bytes;
+    size_t bytes = plan_bytes(a.query_start, a.query_rows, per, a.sequences, z.splits);
+    if (z.splits > 1) bytes += (size_t)a.query_rows * a.heads * ((size_t)z.splits * ((size_t)a.dim + 1) + 1) * 4;
+    return bytes;
 }
 
 cudaError_t launch_attention(const AttentionShape &a, const Heads &q, const Heads &k, const Heads &v, const Heads &y, float *lse, void *scratch,
@@ -585,16 +616,19 @@ cudaError_t launch_attention(const AttentionShape &a, const Heads &q, const Head
     char *at = static_cast<char *>(scratch);
     ForwardArgs p{};
     p.runs = Runs{a.query_start, a.key_start, a.sequences, a.query_rows, a.key_rows};
-    p.plan = plan_at(at, a.query_start, a.query_rows, per, a.sequences);
+    const Splits z = splits_of(a, most_units(a.query_start, a.query_rows, per, a.sequences));
+    p.plan = plan_at(at, a.query_start, a.query_rows, per, a.sequences, z.chunk, z.splits);
     p.mask = Mask{a.causal, a.window};
     p.heads = a.heads, p.kv_heads = a.kv_heads, p.group = group, p.dim = a.dim, p.queries = queries;
     p.scale_log2 = (float)((double)a.scale * 1.4426950408889634);
     p.y = static_cast<__nv_bfloat16 *>(y.p), p.ld_y = y.ld, p.head_stride_y = y.head_stride;
     p.lse = lse, p.errword = errword;
-    const Splits z = splits_of(a, p.plan.most);
-    p.chunk = z.chunk, p.splits = z.splits;
-    p.part_y = reinterpret_cast<float *>(at + plan_bytes(a.query_start, a.query_rows, per, a.sequences));
-    p.part_lse = p.part_y + (size_t)z.splits * a.query_rows * a.heads * a.dim;
+    if (z.splits > 1) {
+        const size_t all = (size_t)a.query_rows * a.heads;
+        p.part_y = reinterpret_cast<float *>(at + plan_bytes(a.query_start, a.query_rows, per, a.sequences, z.splits));
+        p.part_lse = p.part_y + (size_t)z.splits * all * a.dim;
+        p.parts = reinterpret_cast<int *>(p.part_lse + (size_t)z.splits * all);
+    }
     CUtensorMap mq, mk, mv;
     cudaError_t e = make_heads_map(&mq, q.p, a.dim, a.heads, a.query_rows, q.head_stride, q.ld, group, queries);
     if (e == cudaSuccess && a.key_rows > 0) e = make_heads_map(&mk, k.p, a.dim, a.kv_heads, a.key_rows, k.head_stride, k.ld, 1, kRows);

@@ -30,7 +30,7 @@ struct __align__(16) Unit {
     int pos;                   // of the first row in its sequence
     int other_row, other_len;  // the sequence's keys, or queries
     int shift;                 // number of keys - number of queries: causal: query i sees keys up to i + shift
-    int pad[2];
+    int split, splits;         // the unit takes part `split` of `splits` of the other side (1 but for few queries and many keys)
 };
 
 struct Mask {
@@ -44,19 +44,26 @@ struct Plan {
     Unit *units;
     int *prefix;               // [sequences + 1] units in front of a sequence's
     int per;                   // rows of a unit
-    int64_t most;              // units that there is room for, and CTAs per head
+    int64_t most;              // units that there is room for
+    int chunk, splits;         // tiles of the other side that a part has at least, parts at most
 };
 
 inline int64_t most_units(const int64_t *start, int64_t rows, int per, int sequences) { return start ? rows / per + sequences : (rows + per - 1) / per; }
-inline size_t plan_bytes(const int64_t *start, int64_t rows, int per, int sequences)
+inline size_t plan_bytes(const int64_t *start, int64_t rows, int per, int sequences, int splits = 1)
 {
-    return start ? 16 + (size_t)most_units(start, rows, per, sequences) * sizeof(Unit) + ((size_t)sequences + 1 + 3) / 4 * 16 : 0;
+    return start ? 16 + (size_t)most_units(start, rows, per, sequences) * splits * sizeof(Unit) + ((size_t)sequences + 1 + 3) / 4 * 16 : 0;
 }
-inline Plan plan_at(char *p, const int64_t *start, int64_t rows, int per, int sequences)
+inline Plan plan_at(char *p, const int64_t *start, int64_t rows, int per, int sequences, int chunk = 1, int splits = 1)
 {
-    const int64_t most = most_units(start, rows, per, sequences);
+    const int64_t most = most_units(start, rows, per, sequences) * splits;
     Unit *units = reinterpret_cast<Unit *>(p + 16);
-    return Plan{reinterpret_cast<int *>(p), units, reinterpret_cast<int *>(units + most), per, most};
+    return Plan{reinterpret_cast<int *>(p), units, reinterpret_cast<int *>(units + most), per, most, chunk, splits};
+}
+// Parts of a sequence's keys.
+__host__ __device__ __forceinline__ int parts_of(const Plan &plan, int keys)
+{
+    const int tiles = (keys + kRows - 1) / kRows, parts = (tiles + plan.chunk - 1) / plan.chunk;
+    return plan.splits == 1 || parts < 1 ? 1 : parts < plan.splits ? parts : plan.splits;
 }
 
 // Writes the table of the queries' units and / or the keys' (nullptr: not wanted).
@@ -69,12 +76,14 @@ __device__ __forceinline__ Unit unit_at(const Runs &r, const Plan &plan, bool by
     Unit u;
     if (r.query_start) {
         const int4 a = *reinterpret_cast<const int4 *>(plan.units + index), b = *(reinterpret_cast<const int4 *>(plan.units + index) + 1);
-        u.row = a.x, u.rows = a.y, u.pos = a.z, u.other_row = a.w, u.other_len = b.x, u.shift = b.y;
+        u.row = a.x, u.rows = a.y, u.pos = a.z, u.other_row = a.w, u.other_len = b.x, u.shift = b.y, u.split = b.z, u.splits = b.w;
         return u;
     }
     const int rows = (int)(by_key ? r.key_rows : r.query_rows);
     if (!by_key) index = (uint32_t)plan.most - 1 - index;
-    u.row = u.pos = (int)index * plan.per;
+    u.splits = by_key ? 1 : parts_of(plan, (int)r.key_rows);      // (one sequence: every unit has plan.splits)
+    u.split = plan.splits == 1 ? 0 : (int)(index % (uint32_t)plan.splits);
+    u.row = u.pos = (int)(plan.splits == 1 ? index : index / (uint32_t)plan.splits) * plan.per;
     u.rows = min(plan.per, rows - u.row);
     u.other_row = 0;
     u.other_len = (int)(by_key ? r.query_rows : r.key_rows);
@@ -82,7 +91,7 @@ __device__ __forceinline__ Unit unit_at(const Runs &r, const Plan &plan, bool by
     return u;
 }
 
-// A CTA's share of the work, (unit, split, head of k and v) with the head fastest: one of every round of gridDim.x, every other round from
+// A CTA's share of the work, (unit, head of k and v) with the head fastest: one of every round of gridDim.x, every other round from
 // the other end, so that the sums of what the CTAs get are nearly equal.  Every warp works it out for itself, from what is the same in all
 // lanes: then the loops and the products' descriptors are uniform values.  (Handed over in shared memory behind a barrier they are
 // not, for the compiler, and issuing a product takes a third longer: 967 against 847 us for 16384 tokens, 16 heads.)
@@ -90,21 +99,20 @@ struct Walk {
     const Runs &runs;
     const Plan &plan;
     bool by_key;
-    uint32_t kv_heads, splits, total, round = 0;
+    uint32_t kv_heads, total, round = 0;
     Unit unit;
-    int head, split;
+    int head;
 
-    __device__ __forceinline__ Walk(const Runs &r, const Plan &p, bool keys, int heads, int cuts) : runs(r), plan(p), by_key(keys), kv_heads(heads), splits(cuts)
+    __device__ __forceinline__ Walk(const Runs &r, const Plan &p, bool keys, int heads) : runs(r), plan(p), by_key(keys), kv_heads(heads)
     {
-        total = units_of(r, p) * kv_heads * splits;
+        total = units_of(r, p) * kv_heads;
     }
     __device__ __forceinline__ bool next()
     {
         const uint32_t i = round * gridDim.x + (round & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
         if (i >= total) return false;
-        unit = unit_at(runs, plan, by_key, i / (kv_heads * splits));
+        unit = unit_at(runs, plan, by_key, i / kv_heads);
         head = (int)(i % kv_heads);
-        split = (int)(i / kv_heads % splits);
         ++round;
         return true;
     }

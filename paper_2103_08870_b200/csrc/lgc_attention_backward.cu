@@ -43,14 +43,25 @@ struct BackwardArgs {
 template <int DP>
 constexpr int kTileBytes = DP / 64 * kPiece;
 
+// A place in a ring of buffers.
+template <int STAGES>
+struct Ring {
+    int at = 0;
+    uint32_t phase;
+    __device__ __forceinline__ explicit Ring(uint32_t first) : phase(first) {}
+    __device__ __forceinline__ void next()
+    {
+        if (++at == STAGES) at = 0, phase ^= 1;
+    }
+};
+
 // ---- dq: a tile of queries goes over its keys --------------------------------------------------------------------------------
 // Tensor memory: S of two tiles of keys in turn (columns 0 and 128; dS takes its place), dP (256), dQ (384).
-// One warp issues S and dP, another dQ: issuing takes as long as the product, and while one waits for its next operands the other
-// issues.  S and dP of the next tile are made while the threads are at one.  delta is made by the rows' threads: the loads for a unit are
-// under way while the last unit's results are written.
+// The tensor cores' order: dP(t + 1) once dP(t) has been read, dQ += dS(t) K(t), S(t + 2): the threads find the next S ready.
+// delta is made by the rows' threads: the loads for a unit are under way while the last unit's results are written.
 constexpr int kKeyStages = 3, kValueStages = 2;
 struct QueryBars {
-    uint64_t q_full, q_empty, k_full[kKeyStages], k_empty[kKeyStages], v_full[kValueStages], v_empty[kValueStages], s_full[2], s_empty[2], dp_full,
+    uint64_t q_full, q_empty, k_full[kKeyStages], k_empty[kKeyStages], v_full[kValueStages], v_empty[kValueStages], s_full[2], dp_full,
         dp_taken, ds_full, dq_full, dq_empty;
     float minus_lse2[2][kRows], minus_delta[2][kRows];
     uint32_t tmem_base;
@@ -78,7 +89,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
         bar_init(smem_addr(&b.q_empty), 1);
         for (int s = 0; s < kKeyStages; ++s) bar_init(smem_addr(&b.k_full[s]), 1), bar_init(smem_addr(&b.k_empty[s]), 1);
         for (int s = 0; s < kValueStages; ++s) bar_init(smem_addr(&b.v_full[s]), 1), bar_init(smem_addr(&b.v_empty[s]), 1);
-        for (int s = 0; s < 2; ++s) bar_init(smem_addr(&b.s_full[s]), 1), bar_init(smem_addr(&b.s_empty[s]), 1);
+        for (int s = 0; s < 2; ++s) bar_init(smem_addr(&b.s_full[s]), 1);
         bar_init(smem_addr(&b.dp_full), 1);
         bar_init(smem_addr(&b.dp_taken), 8);
         bar_init(smem_addr(&b.ds_full), 8);
@@ -100,12 +111,12 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     };
     if (warp >= 8) {
         give_registers<kOtherRegisters>();
-        if (warp == 10 && lane == 0 && !failed) {
+        if (warp == 9 && lane == 0 && !failed) {
             const uint32_t q_bytes = (uint32_t)p.queries * p.group * (DP * 2);
             int sk = 0, sv = 0;
             uint32_t ph_q = 1, ph_k = 1, ph_v = 1;
             bool ok = true;
-            for (Walk w(p.runs, p.plan, false, p.kv_heads, 1); ok && w.next();) {
+            for (Walk w(p.runs, p.plan, false, p.kv_heads); ok && w.next();) {
                 const Unit u = w.unit;
                 int key_lo;
                 const int tiles = keys_of(u, key_lo);
@@ -129,72 +140,64 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
             }
         } else if (warp == 8) {
             const bool issuer = elect_one();
-            int sk = 0, sv = 0, g = 0;                        // stages, tiles so far
-            uint32_t ph_q = 0, ph_k = 0, ph_v = 0;
+            int sk = 0, sv = 0, sd = 0, g = 0;                // stages of S's K, of V, of dQ's K; tiles so far
+            uint32_t ph_q = 0, ph_k = 0, ph_v = 0, ph_o = 1;
             bool ok = true;
-            for (Walk w(p.runs, p.plan, false, p.kv_heads, 1); ok && w.next();) {
+            for (Walk w(p.runs, p.plan, false, p.kv_heads); ok && w.next();) {
                 const Unit u = w.unit;
                 int key_lo;
                 const int tiles = keys_of(u, key_lo);
                 if (tiles == 0) continue;
-                if (!bar_wait_together(smem_addr(&b.q_full), ph_q, &failed)) break;
-                ph_q ^= 1;
-                for (int t = 0; t < tiles; ++t, ++g) {
-                    const int buf = g & 1;
-                    // S: its place is free once dQ has read dS of two tiles ago; K's rows behind the sequence become zero, since dQ sums over them
-                    if (!bar_wait_together(smem_addr(&b.k_full[sk]), ph_k, &failed) ||
-                        !bar_wait_together(smem_addr(&b.s_empty[buf]), ((g >> 1) & 1) ^ 1, &failed)) { ok = false; break; }
+                // S(t): K's rows behind the sequence become zero, since dQ sums over them
+                const auto make_s = [&](int t) {
+                    if (!bar_wait_together(smem_addr(&b.k_full[sk]), ph_k, &failed)) return false;
                     const uint32_t tile = k_ring + sk * kTile;
                     const int live = u.other_len - (key_lo + t * kRows);
                     if (live < kRows) clear_rows<DP>(tile, live);
                     tc_fence_after();
                     if (issuer) {
-                        product_of_tiles<DP>(tmem + buf * kRows, q_tile, tile);
-                        tc_commit(smem_addr(&b.s_full[buf]));
+                        product_of_tiles<DP>(tmem + ((g + t) & 1) * kRows, q_tile, tile);
+                        tc_commit(smem_addr(&b.s_full[(g + t) & 1]));
                     }
                     __syncwarp();
                     if (++sk == kKeyStages) sk = 0, ph_k ^= 1;
-                    // dP: once the threads have the last one
-                    if (!bar_wait_together(smem_addr(&b.v_full[sv]), ph_v, &failed) ||
-                        !bar_wait_together(smem_addr(&b.dp_taken), (g & 1) ^ 1, &failed)) { ok = false; break; }
+                    return true;
+                };
+                const auto make_dp = [&](bool last) {
+                    if (!bar_wait_together(smem_addr(&b.v_full[sv]), ph_v, &failed)) return false;
                     tc_fence_after();
                     if (issuer) {
                         product_of_tiles<DP>(tmem + 256, dy_tile, v_ring + sv * kTile);
                         tc_commit(smem_addr(&b.dp_full));
                         tc_commit(smem_addr(&b.v_empty[sv]));
-                        if (t == tiles - 1) tc_commit(smem_addr(&b.q_empty));
+                        if (last) tc_commit(smem_addr(&b.q_empty));           // (the last S has been issued too)
                     }
                     __syncwarp();
                     if (++sv == kValueStages) sv = 0, ph_v ^= 1;
-                }
-            }
-        } else if (warp == 9) {
-            const bool issuer = elect_one();
-            int sd = 0, g = 0;
-            uint32_t ph_o = 1;
-            bool ok = true;
-            for (Walk w(p.runs, p.plan, false, p.kv_heads, 1); ok && w.next();) {
-                const Unit u = w.unit;
-                int key_lo;
-                const int tiles = keys_of(u, key_lo);
-                if (tiles == 0) continue;
+                    return true;
+                };
+                if (!bar_wait_together(smem_addr(&b.q_full), ph_q, &failed)) break;
+                ph_q ^= 1;
+                if (!make_s(0) || (tiles > 1 && !make_s(1)) || !make_dp(tiles == 1)) break;
                 if (!bar_wait_together(smem_addr(&b.dq_empty), ph_o, &failed)) break;          // the last unit's dQ has been read
                 ph_o ^= 1;
-                for (int t = 0; t < tiles; ++t, ++g) {
-                    const int buf = g & 1;
-                    if (!bar_wait_together(smem_addr(&b.ds_full), g & 1, &failed)) { ok = false; break; }
+                for (int t = 0; t < tiles; ++t) {
+                    if (!bar_wait_together(smem_addr(&b.dp_taken), (g + t) & 1, &failed)) { ok = false; break; }
+                    if (t + 1 < tiles && !make_dp(t + 2 == tiles)) { ok = false; break; }
+                    if (!bar_wait_together(smem_addr(&b.ds_full), (g + t) & 1, &failed)) { ok = false; break; }
                     tc_fence_after();
                     if (issuer) {
 #pragma unroll
                         for (int ks = 0; ks < kRows / 16; ++ks)
-                            product_step<DP>(tmem + 384, tmem + buf * kRows + ks / 4 * 64 + ks % 4 * 8, k_ring + sd * kTile, ks, t > 0 || ks > 0);
-                        tc_commit(smem_addr(&b.s_empty[buf]));
+                            product_step<DP>(tmem + 384, tmem + ((g + t) & 1) * kRows + ks / 4 * 64 + ks % 4 * 8, k_ring + sd * kTile, ks, t > 0 || ks > 0);
                         tc_commit(smem_addr(&b.k_empty[sd]));
                         if (t == tiles - 1) tc_commit(smem_addr(&b.dq_full));
                     }
                     __syncwarp();
                     if (++sd == kKeyStages) sd = 0;
+                    if (t + 2 < tiles && !make_s(t + 2)) { ok = false; break; }      // (after the product that reads dS in the same columns)
                 }
+                g += tiles;
             }
         }
     } else {
@@ -225,7 +228,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
             }
             if (half == 0 && query < min(p.queries, u.rows)) lse = p.lse[((int64_t)u.row + query) * p.heads + kv_head * p.group + of_group];
         };
-        Walk walk(p.runs, p.plan, false, p.kv_heads, 1);
+        Walk walk(p.runs, p.plan, false, p.kv_heads);
         bool more = walk.next();
         if (more) load_ahead(walk.unit, walk.head);
         while (more) {
@@ -276,7 +279,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
                 const int key0 = key_lo + t * kRows + half * 64, from = lo - key0, to = hi - key0;
                 const bool masked = __any_sync(0xffffffffu, from > 0 || to < 64);
                 if (masked) exponentials<64, false>(v, cc, mm);
-                else exponentials<64, true>(v, cc, mm);
+                else exponentials<64, DP == 64>(v, cc, mm);
                 if (!bar_wait_together(smem_addr(&b.dp_full), g & 1, &failed)) { ok = false; break; }
                 tc_fence_after();
                 float d[64];
@@ -333,19 +336,19 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
 
 // ---- dk and dv: a tile of keys goes over the queries that see it -----------------------------------------------------------------
 // Tensor memory: S^T (columns 0; P^T takes its place), dP^T (128; dS^T takes its place), dV (256), dK (256 + DP).
-// The tensor cores' order: dV += P(t) dY(t) as the halves of P come, S(t + 1), dK += dS(t) Q(t), dP(t + 1): while the threads are at P
+// The tensor cores' order: dV += P(t) dY(t), S(t + 1), dK += dS(t) Q(t), dP(t + 1): while the threads are at P
 // they have dK and dP to do, while they are at dS, dV and the next S.  One warp issues them all: two warps' products would share the
 // tensor cores, and the next S, for which the threads wait, would come later (3640 against 3200 us for the whole backward pass of
 // 16384 tokens, 16 heads).
 //
 // Keys that most queries look at (the first of a sequence, often) have gradients hundreds of times the others', and P's rounding to
 // bf16 would be off by as much as the others' gradients.  So the threads keep a sample of a key's probabilities' sum, and
-// once it is sixteen times what a key has on average, the tiles that follow take P and dS as two bf16 numbers each (the second: what the
+// once it is 256 times what a key has on average, the tiles that follow take P and dS as two bf16 numbers each (the second: what the
 // first has lost) in two more products.  The decision goes by sums of earlier tiles in the unit, the same in every call.
 constexpr int kQueryStages = 3, kDyStages = 2, kRowStages = 2;
 struct KeyBars {
     uint64_t kv_full, kv_empty, q_full[kQueryStages], q_empty[kQueryStages], dy_full[kDyStages], dy_empty[kDyStages], row_full[kRowStages],
-        row_empty[kRowStages], s_full, p_full[2], dp_full, ds_full, sums_full, sums_empty;
+        row_empty[kRowStages], s_full, p_full, dp_full, ds_full, sums_full, sums_empty;
     uint32_t tmem_base;
     int failed, heavy_unit, two_terms[2];
 };
@@ -357,18 +360,6 @@ __device__ __forceinline__ uint32_t bf16_lost(float lo, float hi, uint32_t w)
 {
     return bf16_pair(__fsub_rn(lo, __uint_as_float(w << 16)), __fsub_rn(hi, __uint_as_float(w & 0xffff0000u)));
 }
-// A place in a ring of buffers.
-template <int STAGES>
-struct Ring {
-    int at = 0;
-    uint32_t phase;
-    __device__ __forceinline__ explicit Ring(uint32_t first) : phase(first) {}
-    __device__ __forceinline__ void next()
-    {
-        if (++at == STAGES) at = 0, phase ^= 1;
-    }
-};
-
 template <int DP>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
@@ -393,8 +384,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         for (int s = 0; s < kDyStages; ++s) bar_init(smem_addr(&b.dy_full[s]), 1), bar_init(smem_addr(&b.dy_empty[s]), 1);
         for (int s = 0; s < kRowStages; ++s) bar_init(smem_addr(&b.row_full[s]), 1), bar_init(smem_addr(&b.row_empty[s]), 8);
         bar_init(smem_addr(&b.s_full), 2);                        // the product, and the word that says how P is wanted
-        bar_init(smem_addr(&b.p_full[0]), 8);
-        bar_init(smem_addr(&b.p_full[1]), 8);
+        bar_init(smem_addr(&b.p_full), 8);
         bar_init(smem_addr(&b.dp_full), 1);
         bar_init(smem_addr(&b.ds_full), 8);
         bar_init(smem_addr(&b.sums_full), 1);
@@ -421,7 +411,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             Ring<kDyStages> rd(1);
             uint32_t ph_kv = 1;
             bool ok = true;
-            for (Walk w(p.runs, p.plan, true, p.kv_heads, 1); ok && w.next();) {
+            for (Walk w(p.runs, p.plan, true, p.kv_heads); ok && w.next();) {
                 const Unit u = w.unit;
                 int query_lo;
                 const int tiles = queries_of(u, query_lo);
@@ -446,7 +436,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         } else if (warp == 10) {
             Ring<kRowStages> rr(1);
             bool ok = true;
-            for (Walk w(p.runs, p.plan, true, p.kv_heads, 1); ok && w.next();) {
+            for (Walk w(p.runs, p.plan, true, p.kv_heads); ok && w.next();) {
                 const Unit u = w.unit;
                 int query_lo;
                 const int tiles = queries_of(u, query_lo);
@@ -480,7 +470,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             Ring<kDyStages> made_dy(0), used_dy(0);              // of the next dP, of the next dV
             uint32_t ph_kv = 0, ph_o = 1;
             bool ok = true;
-            for (Walk w(p.runs, p.plan, true, p.kv_heads, 1); ok && w.next();) {
+            for (Walk w(p.runs, p.plan, true, p.kv_heads); ok && w.next();) {
                 const Unit u = w.unit;
                 int query_lo;
                 const int tiles = queries_of(u, query_lo);
@@ -496,10 +486,10 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 const auto make_s = [&](int t) {
                     tc_fence_after();
                     if (issuer) {
-                        product_of_tiles<DP>(tmem, k_tile, q_ring + made_q.at * kTile);
-                        tc_commit(smem_addr(&b.s_full));
                         two_terms[(g + (t > 0)) & 1] = t > 0 && heavy_unit == number;
                         bar_arrive(smem_addr(&b.s_full));
+                        product_of_tiles<DP>(tmem, k_tile, q_ring + made_q.at * kTile);
+                        tc_commit(smem_addr(&b.s_full));
                     }
                     __syncwarp();
                     made_q.next();
@@ -514,13 +504,9 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     __syncwarp();
                     made_dy.next();
                 };
-                // steps of 16 rows of a sum, those of the threads' first halves and then of the second
-                const auto add = [&](uint32_t d, uint32_t operand, uint32_t tile, int half, bool more) {
+                const auto add = [&](uint32_t d, uint32_t operand, uint32_t tile, bool more) {
 #pragma unroll
-                    for (int n = 0; n < 4; ++n) {
-                        const int ks = (n >> 1) * 4 + half * 2 + (n & 1);
-                        product_step<DP>(d, operand + ks / 4 * 64 + ks % 4 * 8, tile, ks, more || n > 0);
-                    }
+                    for (int ks = 0; ks < kRows / 16; ++ks) product_step<DP>(d, operand + ks / 4 * 64 + ks % 4 * 8, tile, ks, more || ks > 0);
                 };
                 if (!bar_wait_together(smem_addr(&b.kv_full), ph_kv, &failed) || !loaded(b.q_full[made_q.at], made_q.phase, q_ring + made_q.at * kTile, 0)) break;
                 ph_kv ^= 1;
@@ -531,45 +517,36 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 ph_o ^= 1;
                 for (int t = 0; t < tiles; ++t, ++g) {
                     const uint32_t q_tile = q_ring + used_q.at * kTile, dy_tile = dy_ring + used_dy.at * kTile;
-                    // what may have been there for long is waited for first
-                    if (t + 1 < tiles && !loaded(b.q_full[made_q.at], made_q.phase, q_ring + made_q.at * kTile, t + 1)) { ok = false; break; }
-                    if (!bar_wait_together(smem_addr(&b.p_full[0]), g & 1, &failed)) { ok = false; break; }
+                    if (!bar_wait_together(smem_addr(&b.p_full), g & 1, &failed)) { ok = false; break; }
                     const int two = __shfl_sync(0xffffffffu, two_terms[g & 1], 0);
                     tc_fence_after();
                     if (issuer) {
-                        add(tmem + 256, tmem, dy_tile, 0, t > 0);
-                        if (two) add(tmem + 256, tmem + 32, dy_tile, 0, true);
-                    }
-                    __syncwarp();
-                    if (!bar_wait_together(smem_addr(&b.p_full[1]), g & 1, &failed)) { ok = false; break; }
-                    tc_fence_after();
-                    if (issuer) {
-                        add(tmem + 256, tmem, dy_tile, 1, true);
-                        if (two) add(tmem + 256, tmem + 32, dy_tile, 1, true);
+                        add(tmem + 256, tmem, dy_tile, t > 0);
+                        if (two) add(tmem + 256, tmem + 32, dy_tile, true);
                         tc_commit(smem_addr(&b.dy_empty[used_dy.at]));
                     }
                     __syncwarp();
                     used_dy.next();
                     // (the next S takes the columns of P, the next dP those of dS: the tensor cores work in order)
+                    // (each load is waited for behind the product in front of it, while that runs)
                     if (t + 1 < tiles) {
+                        if (!loaded(b.q_full[made_q.at], made_q.phase, q_ring + made_q.at * kTile, t + 1)) { ok = false; break; }
                         make_s(t + 1);
-                        if (!loaded(b.dy_full[made_dy.at], made_dy.phase, dy_ring + made_dy.at * kTile, t + 1)) { ok = false; break; }
                     }
                     if (!bar_wait_together(smem_addr(&b.ds_full), g & 1, &failed)) { ok = false; break; }
                     tc_fence_after();
                     if (issuer) {
-                        add(tmem + 256 + DP, tmem + 128, q_tile, 0, t > 0);
-                        add(tmem + 256 + DP, tmem + 128, q_tile, 1, true);
-                        if (two) {
-                            add(tmem + 256 + DP, tmem + 160, q_tile, 0, true);
-                            add(tmem + 256 + DP, tmem + 160, q_tile, 1, true);
-                        }
+                        add(tmem + 256 + DP, tmem + 128, q_tile, t > 0);
+                        if (two) add(tmem + 256 + DP, tmem + 160, q_tile, true);
                         tc_commit(smem_addr(&b.q_empty[used_q.at]));
                         if (t == tiles - 1) tc_commit(smem_addr(&b.sums_full));
                     }
                     __syncwarp();
                     used_q.next();
-                    if (t + 1 < tiles) make_dp(t + 1);
+                    if (t + 1 < tiles) {
+                        if (!loaded(b.dy_full[made_dy.at], made_dy.phase, dy_ring + made_dy.at * kTile, t + 1)) { ok = false; break; }
+                        make_dp(t + 1);
+                    }
                 }
             }
         }
@@ -584,7 +561,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         Ring<kRowStages> rr(0);
         uint32_t ph_o = 0;
         bool ok = true;
-        for (Walk walk(p.runs, p.plan, true, p.kv_heads, 1); ok && walk.next();) {
+        for (Walk walk(p.runs, p.plan, true, p.kv_heads); ok && walk.next();) {
             const Unit u = walk.unit;
             int query_lo;
             const int tiles = queries_of(u, query_lo);
@@ -612,37 +589,35 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 const int first = query_lo + t * p.queries;
                 const int from = max(0, min(p.queries, seen_lo - first)) * p.group - half * 64, to = max(0, min(p.queries, seen_hi - first)) * p.group - half * 64;
                 const bool masked = __any_sync(0xffffffffu, from > 0 || to < 64);
+                uint32_t w[32];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t w[16];
+                for (int n = 0; n < 64; n += 4) {
+                    f2 m[2];
+                    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(m[0]), "=l"(m[1]) : "r"(rows + n * 4));
 #pragma unroll
-                    for (int n = 32 * h; n < 32 * h + 32; n += 4) {
-                        f2 m[2];
-                        asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(m[0]), "=l"(m[1]) : "r"(rows + n * 4));
-#pragma unroll
-                        for (int e = 0; e < 4; e += 2) {
-                            const f2 x = f2_fma(f2_of(v[n + e], v[n + e + 1]), cc, m[e / 2]);
-                            v[n + e] = exp2_of(f2_lo(x));
-                            v[n + e + 1] = exp2_of(f2_hi(x));
-                        }
+                    for (int e = 0; e < 4; e += 2) {
+                        const f2 x = f2_fma(f2_of(v[n + e], v[n + e + 1]), cc, m[e / 2]);
+                        v[n + e] = exp2_of(f2_lo(x));
+                        v[n + e + 1] = exp2_of(f2_hi(x));
+                        w[(n + e) >> 1] = bf16_pair(v[n + e], v[n + e + 1]);
                     }
-                    if (masked) {
-#pragma unroll
-                        for (int n = 32 * h; n < 32 * h + 32; ++n) v[n] = n >= from && n < to ? v[n] : 0.0f;
-                    }
-#pragma unroll
-                    for (int n = 0; n < 32; n += 2) w[n >> 1] = bf16_pair(v[32 * h + n], v[32 * h + n + 1]);
-                    tc_write16(s_at + 16 * h, w);
-                    if (two) {
-#pragma unroll
-                        for (int n = 0; n < 32; n += 2) w[n >> 1] = bf16_lost(v[32 * h + n], v[32 * h + n + 1], w[n >> 1]);
-                        tc_write16(s_at + 32 + 16 * h, w);
-                    }
-                    tc_write_wait();
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) bar_arrive(smem_addr(&b.p_full[h]));
                 }
+                if (masked) {
+#pragma unroll
+                    for (int n = 0; n < 64; ++n) v[n] = n >= from && n < to ? v[n] : 0.0f;
+#pragma unroll
+                    for (int n = 0; n < 64; n += 2) w[n >> 1] = bf16_pair(v[n], v[n + 1]);
+                }
+                tc_write32(s_at, w);
+                if (two) {
+#pragma unroll
+                    for (int n = 0; n < 64; n += 2) w[n >> 1] = bf16_lost(v[n], v[n + 1], w[n >> 1]);
+                    tc_write32(s_at + 32, w);
+                }
+                tc_write_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(smem_addr(&b.p_full));
 #pragma unroll
                 for (int n = 0; n < 64; n += 16) mass = f2_add(mass, f2_of(v[n], v[n + 1]));
                 if (!bar_wait_together(smem_addr(&b.dp_full), g & 1, &failed)) { ok = false; break; }
@@ -652,7 +627,6 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 for (int j = 0; j < 2; ++j) tc_read32(d_at + 32 * j, reinterpret_cast<uint32_t(&)[32]>(d[32 * j]));
 #pragma unroll
                 for (int j = 0; j < 2; ++j) tc_read_wait(reinterpret_cast<uint32_t(&)[32]>(d[32 * j]));
-                uint32_t w[32];
 #pragma unroll
                 for (int n = 0; n < 64; n += 4) {
                     f2 m[2];
@@ -765,7 +739,7 @@ cudaError_t launch_attention_backward(const AttentionShape &a, const Heads &dy, 
     p.dv = static_cast<__nv_bfloat16 *>(dv.p), p.ld_dv = dv.ld, p.head_stride_dv = dv.head_stride;
     p.minus_lse2 = reinterpret_cast<float *>(at), p.minus_delta = reinterpret_cast<float *>(at + row_bytes(a));
     const double mean = a.key_rows > 0 ? (double)a.query_rows * group / a.key_rows : 0.0;     // of a key's sum of probabilities
-    p.heavy = (float)(mean > 1.0 ? mean : 1.0);                // half of the columns, one in eight of them, sixteen times the mean
+    p.heavy = (float)(16.0 * (mean > 1.0 ? mean : 1.0));       // half of the columns, one in eight of them, 256 times the mean
     at += 2 * row_bytes(a);
     BackwardArgs by_key = p;
     p.plan = plan_at(at, a.query_start, a.query_rows, queries, a.sequences);

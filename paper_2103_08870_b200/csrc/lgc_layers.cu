@@ -384,8 +384,10 @@ lgc_status lgc_attention(const lgc_attention_shape *shape, const lgc_heads *q, c
         (a.key_rows > 0 && ((why = tensor_heads_of(k, a.key_rows, a.kv_heads, a.dim, hk)) || (why = tensor_heads_of(v, a.key_rows, a.kv_heads, a.dim, hv)))))
         return refuse(where, why);
     if (!aligned4(lse)) return refuse(where, "NULL or misaligned lse");
-    if ((why = bad_scratch(scratch))) return refuse(where, why);
-    if (scratch_bytes < attention_scratch(a)) return refuse(where, "scratch is smaller than lgc_attention_scratch says", LGC_ERR_WORKSPACE);
+    if (const size_t need = attention_scratch(a)) {
+        if ((why = bad_scratch(scratch))) return refuse(where, why);
+        if (scratch_bytes < need) return refuse(where, "scratch is smaller than lgc_attention_scratch says", LGC_ERR_WORKSPACE);
+    }
     int32_t *record = nullptr;
     cudaError_t e = record_address(&record);
     if (e == cudaSuccess) e = launch_attention(a, hq, hk, hv, hy, lse, scratch, record, static_cast<cudaStream_t>(stream));

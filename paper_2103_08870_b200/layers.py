@@ -32,6 +32,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes as C
+import functools
 import math
 from typing import Optional, Union
 
@@ -296,7 +297,7 @@ def _heads(t: torch.Tensor, name: str, device: int, want: Optional[tuple] = None
     ld, head, unit = t.stride()
     if unit != 1 and shape[2] > 1:
         raise ValueError(f"{name}: need unit stride along a head")
-    if want is not None and tuple(shape) != want:
+    if want is not None and shape != want:
         raise ValueError(f"{name}: need {want[0]} x {want[1]} x {want[2]} elements, got {tuple(shape)}")
     return lgc.lgc_heads(t.data_ptr(), ld, head), shape, kind
 
@@ -309,7 +310,7 @@ def rotary(x: torch.Tensor, positions: torch.Tensor, frequencies: torch.Tensor, 
     gradient's way back."""
     device = _device(x.get_device(), stream)
     hx, shape, kind = _heads(x, "x", device, None, (TYPE_FP32, TYPE_BF16))
-    hy, _, ykind = _heads(y, "y", device, tuple(shape), (TYPE_FP32, TYPE_BF16))
+    hy, _, ykind = _heads(y, "y", device, shape, (TYPE_FP32, TYPE_BF16))
     if ykind != kind:
         raise ValueError("y: need x's type")
     rows, heads, dim = shape
@@ -342,23 +343,28 @@ def _attention_shape(q_shape, k_shape, query_start, key_start, causal: bool, win
                                    scale if scale is not None else 1.0 / math.sqrt(dim) if dim else 1.0)
 
 
-def _attention_room(name: str, shape, scratch, stream, like):
-    n = C.c_size_t()
-    _done(getattr(lgc.lib(), name)(C.byref(shape), C.byref(n)), name)
-    return _scratch(n.value, scratch, stream, like)
-
-
-def _sizes_only(query_rows, key_rows, heads, kv_heads, dim, num_sequences):
+@functools.lru_cache(maxsize=256)
+def _attention_size(name: str, query_rows: int, key_rows: int, heads: int, kv_heads: int, dim: int, num_sequences: int) -> int:
     # (the sizes need to know that there are starts, not where)
     at = 8 if num_sequences else None
-    return lgc.lgc_attention_shape(query_rows, key_rows, heads, kv_heads, dim, num_sequences or 1, at, at, 0, 0, 1.0)
+    n, shape = C.c_size_t(), lgc.lgc_attention_shape(query_rows, key_rows, heads, kv_heads, dim, num_sequences or 1, at, at, 0, 0, 1.0)
+    _done(getattr(lgc.lib(), name)(C.byref(shape), C.byref(n)), name)
+    return n.value
+
+
+def _attention_room(name: str, q_shape, k_shape, query_start, scratch, stream, like):
+    """(tensor or None, address, bytes) of a call's scratch."""
+    rows, heads, dim = q_shape
+    need = _attention_size(name, rows, k_shape[0], heads, k_shape[1], dim, 0 if query_start is None else query_start.numel() - 1)
+    if scratch is None and need == 0:
+        return None, None, 0
+    scratch, size = _scratch(need, scratch, stream, like)
+    return scratch, scratch.data_ptr(), size
 
 
 def attention_scratch(query_rows: int, key_rows: int, heads: int, kv_heads: int, dim: int, num_sequences: int = 0) -> int:
     """Bytes of scratch that attention needs.  num_sequences: 0 without query_start."""
-    n, shape = C.c_size_t(), _sizes_only(query_rows, key_rows, heads, kv_heads, dim, num_sequences)
-    _done(lgc.lib().lgc_attention_scratch(C.byref(shape), C.byref(n)), "lgc_attention_scratch")
-    return n.value
+    return _attention_size("lgc_attention_scratch", query_rows, key_rows, heads, kv_heads, dim, num_sequences)
 
 
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, y: torch.Tensor, lse: torch.Tensor, query_start: Optional[torch.Tensor] = None,
@@ -375,20 +381,18 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, y: torch.Tensor
     hk, kshape, _ = _heads(k, "k", device)
     if kshape[2] != qshape[2]:
         raise ValueError(f"k: need heads of {qshape[2]} elements")
-    hv, _, _ = _heads(v, "v", device, tuple(kshape))
-    hy, _, _ = _heads(y, "y", device, tuple(qshape))
+    hv, _, _ = _heads(v, "v", device, kshape)
+    hy, _, _ = _heads(y, "y", device, qshape)
     shape = _attention_shape(qshape, kshape, query_start, key_start, causal, window, scale, device)
     lp = _vector(lse, qshape[0] * qshape[1], "lse", device)
-    scratch, size = _attention_room("lgc_attention_scratch", shape, scratch, stream, q)
-    _done(lgc.lib().lgc_attention(C.byref(shape), C.byref(hq), C.byref(hk), C.byref(hv), C.byref(hy), lp, scratch.data_ptr(), size,
+    scratch, at, size = _attention_room("lgc_attention_scratch", qshape, kshape, query_start, scratch, stream, q)
+    _done(lgc.lib().lgc_attention(C.byref(shape), C.byref(hq), C.byref(hk), C.byref(hv), C.byref(hy), lp, at, size,
                                   _stream(stream, device)), "lgc_attention")
 
 
 def attention_backward_scratch(query_rows: int, key_rows: int, heads: int, kv_heads: int, dim: int, num_sequences: int = 0) -> int:
     """Bytes of scratch that attention_backward needs.  num_sequences: 0 without query_start."""
-    n, shape = C.c_size_t(), _sizes_only(query_rows, key_rows, heads, kv_heads, dim, num_sequences)
-    _done(lgc.lib().lgc_attention_backward_scratch(C.byref(shape), C.byref(n)), "lgc_attention_backward_scratch")
-    return n.value
+    return _attention_size("lgc_attention_backward_scratch", query_rows, key_rows, heads, kv_heads, dim, num_sequences)
 
 
 def attention_backward(dy: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, y: torch.Tensor, lse: torch.Tensor, dq: torch.Tensor,
@@ -400,18 +404,16 @@ def attention_backward(dy: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: to
     same bits.  `scratch`: a uint8 tensor of attention_backward_scratch bytes; without one it comes from PyTorch's allocator."""
     device = _device(dy.get_device(), stream)
     hdy, qshape, _ = _heads(dy, "dy", device)
-    qshape = tuple(qshape)
     hk, kshape, _ = _heads(k, "k", device)
-    kshape = tuple(kshape)
     if kshape[2] != qshape[2]:
         raise ValueError(f"k: need heads of {qshape[2]} elements")
     hq, hy, hdq = (_heads(t, name, device, qshape)[0] for t, name in ((q, "q"), (y, "y"), (dq, "dq")))
     hv, hdk, hdv = (_heads(t, name, device, kshape)[0] for t, name in ((v, "v"), (dk, "dk"), (dv, "dv")))
     shape = _attention_shape(qshape, kshape, query_start, key_start, causal, window, scale, device)
     lp = _vector(lse, qshape[0] * qshape[1], "lse", device)
-    scratch, size = _attention_room("lgc_attention_backward_scratch", shape, scratch, stream, dy)
+    scratch, at, size = _attention_room("lgc_attention_backward_scratch", qshape, kshape, query_start, scratch, stream, dy)
     _done(lgc.lib().lgc_attention_backward(C.byref(shape), C.byref(hdy), C.byref(hq), C.byref(hk), C.byref(hv), C.byref(hy), lp, C.byref(hdq),
-                                           C.byref(hdk), C.byref(hdv), scratch.data_ptr(), size, _stream(stream, device)), "lgc_attention_backward")
+                                           C.byref(hdk), C.byref(hdv), at, size, _stream(stream, device)), "lgc_attention_backward")
 
 
 def check(stream: Optional[torch.cuda.Stream] = None) -> None:

@@ -90,9 +90,11 @@ def test_refused_on_the_host(lib):
     for h in bad_heads:
         assert fwd(q=h) == INVALID and fwd(k=h) == INVALID and fwd(v=h) == INVALID and fwd(y=h) == INVALID
         assert all(bwd(h=h, at=i) == INVALID for i in range(8))
-    assert fwd(lse=None) == INVALID and fwd(lse=P + 2) == INVALID and fwd(scratch=None) == INVALID and fwd(scratch=P + 8) == INVALID
+    some = shape(query_start=P)                   # a table of units
+    assert fwd(lse=None) == INVALID and fwd(lse=P + 2) == INVALID and fwd(some, scratch=None) == INVALID and fwd(some, scratch=P + 8) == INVALID
     assert bwd(lse=None) == INVALID and bwd(scratch=None) == INVALID and bwd(scratch=P + 8) == INVALID
-    assert lib.lgc_attention_scratch(shape(), C.byref(n)) == OK and fwd(size=n.value - 1) == WORKSPACE
+    assert lib.lgc_attention_scratch(shape(), C.byref(n)) == OK and n.value == 0
+    assert lib.lgc_attention_scratch(some, C.byref(n)) == OK and n.value > 0 and fwd(some, size=n.value - 1) == WORKSPACE
     assert lib.lgc_attention_backward_scratch(shape(), C.byref(n)) == OK and n.value >= 2 * 40 * 8 * 4 and bwd(size=n.value - 1) == WORKSPACE
     assert b"scratch" in lib.lgc_last_error(None)
     assert fwd(shape(query_rows=0, key_rows=7), q=None, y=None) == OK and bwd(shape(query_rows=0, key_rows=0)) == OK
