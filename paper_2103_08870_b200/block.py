@@ -1,18 +1,22 @@
-"""A residual block trained on K nodes through the compressed gradient path: the layer operators and the compression
+"""Residual blocks trained on K nodes through the compressed gradient path: the layer operators and the compression
 together, as a training program uses them.
 
-    y = x + W2 leaky(W1 norm(x))
+    ResidualBlock    y = x + W2 leaky(W1 norm(x))
+    AttentionBlock   y = x + Wo attention(rotary(Wqkv norm(x)))
 
-The nodes' tokens are K runs of rows of x.  What the backward pass needs is kept in 8 bits (x, norm(x), and the hidden
-layer, whose sign is also the leaky ReLU's derivative); the products run on 8-bit operands; the gradients of gamma, beta,
-W1 and W2 land per node in the rows of `grads`, which the compression context reads::
+The nodes' tokens are K runs of rows of x.  What the backward pass needs is kept in 8 bits (x, norm(x), the hidden
+layer, whose sign is also the leaky ReLU's derivative, and the heads' results), q, k and v in bf16; the products run on 8-bit
+operands; the gradients of gamma, beta and the two matrices land per node in the rows of `grads`, which the compression
+context reads::
 
     python -m paper_2103_08870_b200.block --nodes 4 --rows 4096 --width 1024 --hidden 4096 --steps 40
+    python -m paper_2103_08870_b200.block --nodes 4 --rows 4096 --width 1024 --heads 16 --kv-heads 4 --sequence 512 --steps 40
 """
 from __future__ import annotations
 
 import argparse
-from typing import Optional
+import itertools
+from typing import Optional, Sequence, Union
 
 import torch
 
@@ -83,7 +87,89 @@ class ResidualBlock:
         return self.dx.add_(dy)
 
 
-def train(block: ResidualBlock, steps: int, lr: float = 0.0, density_ppm: int = 20000, seed: int = 1, say=None):
+class AttentionBlock:
+    """The same around attention: the rows of x are sequences (`lengths`, in order; nodes are runs of rows as above), `heads` heads of
+    q and `kv_heads` of k and v of `dim` entries, rotary positions counted from each sequence's start, causal.  Parameters lie
+    flat in the order gamma, beta, Wqkv, Wo."""
+
+    def __init__(self, lengths: Sequence[int], width: int, heads: int, kv_heads: int, dim: int, num_nodes: int, window: int = 0,
+                 device: Optional[torch.device] = None, seed: int = 0):
+        if width % 8 or dim % 8:
+            raise ValueError("width and dim: multiples of 8 (rows of the activations start 16-byte aligned)")
+        dev = torch.device(device if device is not None else "cuda:0")
+        torch.cuda.set_device(dev)                                        # (the calls run on the current device)
+        rows, across, inner = sum(lengths), (heads + 2 * kv_heads) * dim, heads * dim
+        self.rows, self.width, self.hidden, self.K, self.window = rows, width, across, num_nodes, window
+        self.heads, self.kv_heads, self.dim = heads, kv_heads, dim
+        self.numel = [width, width, across * width, width * inner]        # the layer table of the compression context
+        at = [0]
+        for n in self.numel:
+            at.append(at[-1] + n)
+        self.N, self.at = at[-1], at
+        self.query_start = torch.tensor([0] + list(itertools.accumulate(lengths)), device=dev)
+        self.positions = torch.cat([torch.arange(n, device=dev) for n in lengths])
+        self.frequencies = layers.rotary_frequencies(dim, device=dev)
+        g = torch.Generator(device=dev)
+        g.manual_seed(seed)
+        self.theta = torch.zeros(self.N, device=dev)
+        self.gamma, self.beta, wqkv, wo = (self.theta[a:b] for a, b in zip(at[:-1], at[1:]))
+        self.wqkv, self.wo = wqkv.view(across, width), wo.view(width, inner)
+        self.gamma.fill_(1.0)
+        self.wqkv.uniform_(-1, 1, generator=g).mul_(width ** -0.5)
+        self.wo.uniform_(-1, 1, generator=g).mul_(inner ** -0.5)
+        self.wqkv_8, self.wo_8 = layers.packed_empty(across, width, 128, dev), layers.packed_empty(width, inner, 128, dev)
+        self.grads = torch.zeros(num_nodes, self.N, device=dev)
+        bf = dict(dtype=torch.bfloat16, device=dev)
+        self.mean, self.rstd, self.lse = torch.empty(rows, device=dev), torch.empty(rows, device=dev), torch.empty(rows, heads, device=dev)
+        self.x8, self.h8, self.a8 = (layers.packed_empty(rows, n, device=dev) for n in (width, width, inner))
+        self.dy8, self.dqkv8 = layers.packed_empty(rows, width, device=dev), layers.packed_empty(rows, across, device=dev)
+        self.y, self.dh, self.dx = (torch.empty(rows, width, **bf) for _ in range(3))
+        self.qkv, self.dqkv = torch.empty(rows, across, **bf), torch.empty(rows, across, **bf)
+        self.a, self.da = torch.empty(rows, inner, **bf), torch.empty(rows, inner, **bf)
+        self.refresh()
+
+    def refresh(self) -> None:
+        """Rounds the weights to 8 bits; after every update of `theta`."""
+        layers.pack(self.wqkv, self.wqkv_8)
+        layers.pack(self.wo, self.wo_8)
+
+    def _parts(self, t: torch.Tensor):
+        """Views [rows][heads][dim] of q, k, v, and of q and k together, in the columns of qkv or its gradient."""
+        h, k = self.heads, self.kv_heads
+        t = t.unflatten(1, (-1, self.dim))
+        return t[:, :h], t[:, h:h + k], t[:, h + k:], t[:, :h + k]
+
+    def forward(self, x: torch.Tensor) -> torch.Tensor:
+        """x: bf16 [rows][width].  Returns the block's own buffer, which the next call writes."""
+        layers.pack(x, self.x8)
+        layers.layer_norm(x, self.gamma, self.beta, EPS, self.mean, self.rstd, packed=self.h8)
+        layers.product(self.h8, self.wqkv_8, y=self.qkv)
+        q, k, v, qk = self._parts(self.qkv)
+        layers.rotary(qk, self.positions, self.frequencies, qk)
+        layers.attention(q, k, v, self.a.view_as(q), self.lse, query_start=self.query_start, window=self.window)
+        layers.pack(self.a, self.a8)
+        layers.product(self.a8, self.wo_8, y=self.y)
+        return self.y.add_(x)
+
+    def backward(self, dy: torch.Tensor, node_start: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """dy: bf16 [rows][width], the gradient at y.  Every node's gradients go to its row of `grads`; returns the gradient at
+        x, in the block's own buffer, which the next call writes."""
+        at, g = self.at, self.grads
+        layers.pack(dy, self.dy8)
+        layers.weight_gradient(dy, self.a8, g[:, at[3]:at[4]], node_start=node_start)
+        layers.product(self.dy8, self.wo_8, y=self.da, across=True)
+        (q, k, v, _), (dq, dk, dv, dqk) = self._parts(self.qkv), self._parts(self.dqkv)
+        layers.attention_backward(self.da.view_as(q), q, k, v, self.a.view_as(q), self.lse, dq, dk, dv, query_start=self.query_start, window=self.window)
+        layers.rotary(dqk, self.positions, self.frequencies, dqk, backward=True)
+        layers.pack(self.dqkv, self.dqkv8)
+        layers.weight_gradient(self.dqkv, self.h8, g[:, at[2]:at[3]], node_start=node_start)
+        layers.product(self.dqkv8, self.wqkv_8, y=self.dh, across=True)
+        layers.layer_norm_backward(self.dh, self.x8, self.gamma, self.mean, self.rstd, self.dx, g[:, at[0]:at[1]], g[:, at[1]:at[2]],
+                                   node_start=node_start)
+        return self.dx.add_(dy)
+
+
+def train(block: Union[ResidualBlock, AttentionBlock], steps: int, lr: float = 0.0, density_ppm: int = 20000, seed: int = 1, say=None):
     """Fits the block to a fixed random map, its gradients compressed at every step: the norm's parameters are sent as they
     are, of the weights' gradients the largest entries with error feedback.  lr: 0 selects 1 / hidden (the curvature grows
     with the number of hidden units).  Returns the losses."""
@@ -114,8 +200,15 @@ def main() -> None:
     ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
     for name, value in (("nodes", 4), ("rows", 4096), ("width", 1024), ("hidden", 4096), ("steps", 40)):
         ap.add_argument("--" + name, type=int, default=value)
+    ap.add_argument("--heads", type=int, default=0, help="an attention block with so many heads instead of the hidden layer")
+    ap.add_argument("--kv-heads", type=int, default=0, help="heads of k and v (as many as --heads)")
+    ap.add_argument("--sequence", type=int, default=512, help="rows of a sequence")
     a = ap.parse_args()
-    block = ResidualBlock(a.rows, a.width, a.hidden, a.nodes)
+    if a.heads:
+        lengths = [a.sequence] * (a.rows // a.sequence) + [a.rows % a.sequence] * (a.rows % a.sequence > 0)
+        block = AttentionBlock(lengths, a.width, a.heads, a.kv_heads or a.heads, a.width // a.heads, a.nodes)
+    else:
+        block = ResidualBlock(a.rows, a.width, a.hidden, a.nodes)
     losses = train(block, a.steps, say=print)
     print(f"{a.steps} steps: loss {losses[0].item():.4f} -> {losses[-1].item():.4f}")
     x = torch.randn(a.rows, a.width, device="cuda").bfloat16()

@@ -1,0 +1,96 @@
+"""The attention block on the layer operators: its gradients per node against autograd, a run of it through the compressed
+gradient path, and its steps in a captured graph."""
+import math
+
+import pytest
+import torch
+
+import attention_reference as R
+from paper_2103_08870_b200 import block as B
+from paper_2103_08870_b200 import layers
+
+pytestmark = pytest.mark.gpu
+
+
+def reference(b, x, lengths, gamma, beta, wqkv, wo):
+    """The block in 64 bits."""
+    h = torch.nn.functional.layer_norm(x, (b.width,), gamma, beta, B.EPS) @ wqkv.t()
+    qkv = h.unflatten(1, (-1, b.dim))
+    n, k = b.heads, b.kv_heads
+    i = torch.arange(b.dim // 2, device=x.device)
+    t = b.positions.double()[:, None, None] * b.frequencies
+    qk = qkv[:, :n + k]
+    one, two = qk[..., i], qk[..., i + b.dim // 2]
+    qk = torch.cat([one * t.cos() - two * t.sin(), one * t.sin() + two * t.cos()], 2)
+    y, at = [], 0
+    for length in lengths:
+        part = slice(at, at + length)
+        at += length
+        hide = R.hidden(length, length, True, b.window, x.device)
+        s = torch.einsum("ihd,jhd->hij", qk[part, :n], qk[part, n:].repeat_interleave(n // k, 1)) / math.sqrt(b.dim)
+        p = torch.softmax(s.masked_fill(hide, -math.inf), 2)
+        y.append(torch.einsum("hij,jhd->ihd", p, qkv[part, n + k:].repeat_interleave(n // k, 1)).flatten(1))
+    return x + torch.cat(y) @ wo.t()
+
+
+@pytest.mark.parametrize("window", [0, 50])
+def test_gradients_are_those_of_autograd_up_to_the_rounding_to_8_bits(window):
+    lengths, width, K = [130, 1, 170, 199], 264, 3
+    b = B.AttentionBlock(lengths, width, 6, 2, 40, K, window=window)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    x = torch.randn(b.rows, width, generator=g, device="cuda").bfloat16()
+    dy = torch.randn(b.rows, width, generator=g, device="cuda").bfloat16()
+    start = torch.tensor([0, 131, 131, b.rows], device="cuda")                     # nodes: whole sequences, none, the rest
+    y = b.forward(x).double()
+    dx = b.backward(dy, start).double()
+    layers.check()
+    leaves = [t.double().clone().requires_grad_() for t in (b.gamma, b.beta, b.wqkv, b.wo)]
+    xd = x.double().requires_grad_()
+    want = reference(b, xd, lengths, *leaves)
+    # e4m3 keeps four bits of an entry: a rounding errs by 2^-4 of it at most, 2^-5.3 in the mean square (uniform between the
+    # neighbours, over a binade).  On the way to a gradient: norm(x) and Wqkv, twice (in v, and in the logits, which are below one
+    # and so enter the probabilities with less than their own error), dy and Wo, the heads' results (in delta), dqkv, and norm(x)
+    # or the weights again: ten roundings.
+    tol = 2 ** -5.3 * 10 ** 0.5
+    assert (y - want).norm() <= tol * (want - xd).norm()
+    for k in range(K):
+        part = slice(int(start[k]), int(start[k + 1]))
+        grads = torch.autograd.grad((want[part] * dy[part].double()).sum(), leaves, retain_graph=True)
+        got = b.grads[k].double().split(b.numel)
+        for a, w in zip(got, grads):
+            if part.start == part.stop:
+                assert (a == 0).all()
+            else:
+                assert (a - w.reshape(-1)).norm() <= tol * w.norm()
+    (dxw,) = torch.autograd.grad((want * dy.double()).sum(), [xd])
+    assert (dx - dxw).norm() <= tol * dxw.norm()
+
+
+def test_it_runs_through_the_compressed_path():
+    b = B.AttentionBlock([100, 156, 256], 128, 4, 2, 32, 4)
+    losses = B.train(b, 5)
+    assert torch.isfinite(losses).all() and torch.isfinite(b.theta).all()
+
+
+def test_steps_in_a_captured_graph_repeat_their_bits():
+    b = B.AttentionBlock([100, 0, 156], 128, 4, 1, 32, 2)
+    x, dy = torch.randn(256, 128, device="cuda").bfloat16(), torch.randn(256, 128, device="cuda").bfloat16()
+    start = torch.tensor([0, 100, 256], device="cuda")
+
+    def step():
+        return b.forward(x), b.backward(dy, start)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for _ in range(3):
+        x.copy_(torch.randn(256, 128, device="cuda"))
+        want = [t.clone() for t in step()] + [b.grads.clone()]
+        b.grads.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, w) for a, w in zip([*out, b.grads], want))
+    layers.check()
