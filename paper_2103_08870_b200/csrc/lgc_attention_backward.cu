@@ -62,7 +62,7 @@ struct Ring {
 constexpr int kKeyStages = 3, kValueStages = 2;
 struct QueryBars {
     uint64_t q_full, q_empty, k_full[kKeyStages], k_empty[kKeyStages], v_full[kValueStages], v_empty[kValueStages], s_full[2], dp_full,
-        dp_taken, ds_full, dq_full, dq_empty;
+        dp_taken, ds_full[2], dq_full, dq_empty;      // ds_full: of every other tile, since the threads may be a tile ahead of the issuing warp
     float minus_lse2[2][kRows], minus_delta[2][kRows];
     uint32_t tmem_base;
     int failed;
@@ -92,7 +92,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
         for (int s = 0; s < 2; ++s) bar_init(smem_addr(&b.s_full[s]), 1);
         bar_init(smem_addr(&b.dp_full), 1);
         bar_init(smem_addr(&b.dp_taken), 8);
-        bar_init(smem_addr(&b.ds_full), 8);
+        for (int s = 0; s < 2; ++s) bar_init(smem_addr(&b.ds_full[s]), 8);
         bar_init(smem_addr(&b.dq_full), 1);
         bar_init(smem_addr(&b.dq_empty), 8);
         bar_init_fence();
@@ -184,7 +184,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
                 for (int t = 0; t < tiles; ++t) {
                     if (!bar_wait_together(smem_addr(&b.dp_taken), (g + t) & 1, &failed)) { ok = false; break; }
                     if (t + 1 < tiles && !make_dp(t + 2 == tiles)) { ok = false; break; }
-                    if (!bar_wait_together(smem_addr(&b.ds_full), (g + t) & 1, &failed)) { ok = false; break; }
+                    if (!bar_wait_together(smem_addr(&b.ds_full[(g + t) & 1]), ((g + t) >> 1) & 1, &failed)) { ok = false; break; }
                     tc_fence_after();
                     if (issuer) {
 #pragma unroll
@@ -305,7 +305,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
                 tc_write_wait();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) bar_arrive(smem_addr(&b.ds_full));
+                if (lane == 0) bar_arrive(smem_addr(&b.ds_full[g & 1]));
             }
             if (!ok) break;
             const int head = kv_head * p.group + of_group, column = half * (DP / 2);
@@ -483,13 +483,13 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     if (live < kRows) clear_rows<DP>(tile, live);
                     return true;
                 };
-                const auto make_s = [&](int t) {
+                const auto make_s = [&](int t, int heavy) {
                     tc_fence_after();
                     if (issuer) {
-                        two_terms[(g + (t > 0)) & 1] = t > 0 && heavy_unit == number;
-                        bar_arrive(smem_addr(&b.s_full));
                         product_of_tiles<DP>(tmem, k_tile, q_ring + made_q.at * kTile);
                         tc_commit(smem_addr(&b.s_full));
+                        two_terms[(g + (t > 0)) & 1] = heavy;
+                        bar_arrive(smem_addr(&b.s_full));
                     }
                     __syncwarp();
                     made_q.next();
@@ -510,39 +510,47 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 };
                 if (!bar_wait_together(smem_addr(&b.kv_full), ph_kv, &failed) || !loaded(b.q_full[made_q.at], made_q.phase, q_ring + made_q.at * kTile, 0)) break;
                 ph_kv ^= 1;
-                make_s(0);
+                make_s(0, 0);
                 if (!loaded(b.dy_full[made_dy.at], made_dy.phase, dy_ring + made_dy.at * kTile, 0)) break;
                 make_dp(0);
                 if (!bar_wait_together(smem_addr(&b.sums_empty), ph_o, &failed)) break;          // the last unit's sums have been read
                 ph_o ^= 1;
+                bool two = false;                                // P and dS of tile t are of two terms
                 for (int t = 0; t < tiles; ++t, ++g) {
                     const uint32_t q_tile = q_ring + used_q.at * kTile, dy_tile = dy_ring + used_dy.at * kTile;
                     if (!bar_wait_together(smem_addr(&b.p_full), g & 1, &failed)) { ok = false; break; }
-                    const int two = __shfl_sync(0xffffffffu, two_terms[g & 1], 0);
+                    const int heavy = heavy_unit;                // (on its way while dV is issued)
                     tc_fence_after();
-                    if (issuer) {
-                        add(tmem + 256, tmem, dy_tile, t > 0);
-                        if (two) add(tmem + 256, tmem + 32, dy_tile, true);
-                        tc_commit(smem_addr(&b.dy_empty[used_dy.at]));
+                    if (issuer) add(tmem + 256, tmem, dy_tile, t > 0);
+                    __syncwarp();
+                    if (two) {
+                        if (issuer) add(tmem + 256, tmem + 32, dy_tile, true);
+                        __syncwarp();
                     }
+                    if (issuer) tc_commit(smem_addr(&b.dy_empty[used_dy.at]));
                     __syncwarp();
                     used_dy.next();
                     // (the next S takes the columns of P, the next dP those of dS: the tensor cores work in order)
                     // (each load is waited for behind the product in front of it, while that runs)
                     if (t + 1 < tiles) {
                         if (!loaded(b.q_full[made_q.at], made_q.phase, q_ring + made_q.at * kTile, t + 1)) { ok = false; break; }
-                        make_s(t + 1);
+                        make_s(t + 1, heavy == number);
                     }
                     if (!bar_wait_together(smem_addr(&b.ds_full), g & 1, &failed)) { ok = false; break; }
                     tc_fence_after();
+                    if (issuer) add(tmem + 256 + DP, tmem + 128, q_tile, t > 0);
+                    __syncwarp();
+                    if (two) {
+                        if (issuer) add(tmem + 256 + DP, tmem + 160, q_tile, true);
+                        __syncwarp();
+                    }
                     if (issuer) {
-                        add(tmem + 256 + DP, tmem + 128, q_tile, t > 0);
-                        if (two) add(tmem + 256 + DP, tmem + 160, q_tile, true);
                         tc_commit(smem_addr(&b.q_empty[used_q.at]));
                         if (t == tiles - 1) tc_commit(smem_addr(&b.sums_full));
                     }
                     __syncwarp();
                     used_q.next();
+                    two = __any_sync(0xffffffffu, heavy == number);
                     if (t + 1 < tiles) {
                         if (!loaded(b.dy_full[made_dy.at], made_dy.phase, dy_ring + made_dy.at * kTile, t + 1)) { ok = false; break; }
                         make_dp(t + 1);
