@@ -34,6 +34,7 @@ import contextlib
 import ctypes as C
 import functools
 import math
+import struct
 from typing import Optional, Union
 
 import torch
@@ -289,17 +290,23 @@ def rotary_frequencies(rotary_dim: int, base: float = 10000.0, interpolation: fl
     return (f * (keep + (1 - keep) / interpolation)).to(device if device is not None else torch.device("cuda"))
 
 
-def _heads(t: torch.Tensor, name: str, device: int, want: Optional[tuple] = None, kinds=(TYPE_BF16,)):
-    """A [rows][heads][dim] argument for the library, after the checks that need the tensor: (struct, shape, type)."""
-    shape, kind = t.shape, _TYPES.get(t.dtype)
-    if kind not in kinds or len(shape) != 3 or t.get_device() != device:
+# lgc_heads and lgc_attention_shape as bytes: packing them takes a third of the time of filling in a ctypes structure.
+_heads_bytes = struct.Struct("@Pqq").pack
+_shape_bytes = struct.Struct("@qqiiiiPPiqf4x").pack
+_BF16_ONLY, _BOTH = (torch.bfloat16,), (torch.bfloat16, torch.float32)
+
+
+def _heads(t: torch.Tensor, name: str, device: int, want: Optional[torch.Size] = None, kinds=_BF16_ONLY):
+    """(lgc_heads, shape) of a [rows][heads][dim] argument, after the checks that need the tensor."""
+    shape = t.shape
+    if t.dtype not in kinds or t.get_device() != device or len(shape) != 3:
         raise ValueError(f"{name}: need a [rows][heads][dim] {'bf16' if len(kinds) == 1 else 'fp32 or bf16'} tensor on cuda:{device}")
     ld, head, unit = t.stride()
     if unit != 1 and shape[2] > 1:
         raise ValueError(f"{name}: need unit stride along a head")
     if want is not None and shape != want:
         raise ValueError(f"{name}: need {want[0]} x {want[1]} x {want[2]} elements, got {tuple(shape)}")
-    return lgc.lgc_heads(t.data_ptr(), ld, head), shape, kind
+    return _heads_bytes(t.data_ptr(), ld, head), shape
 
 
 def rotary(x: torch.Tensor, positions: torch.Tensor, frequencies: torch.Tensor, y: torch.Tensor, interleaved: bool = False, amplitude: float = 1.0,
@@ -309,38 +316,42 @@ def rotary(x: torch.Tensor, positions: torch.Tensor, frequencies: torch.Tensor, 
     rest of a head passes through.  Pairs: neighbours (`interleaved`), or entry i and entry i + len(frequencies).  `backward`: the
     gradient's way back."""
     device = _device(x.get_device(), stream)
-    hx, shape, kind = _heads(x, "x", device, None, (TYPE_FP32, TYPE_BF16))
-    hy, _, ykind = _heads(y, "y", device, shape, (TYPE_FP32, TYPE_BF16))
-    if ykind != kind:
+    hx, shape = _heads(x, "x", device, None, _BOTH)
+    hy, _ = _heads(y, "y", device, shape, _BOTH)
+    if y.dtype is not x.dtype:
         raise ValueError("y: need x's type")
     rows, heads, dim = shape
     if not (positions.get_device() == device and positions.dtype is torch.int64 and positions.is_contiguous() and positions.numel() == rows):
         raise ValueError(f"positions: need a contiguous int64 tensor of {rows} elements on cuda:{device}")
     if not (frequencies.get_device() == device and frequencies.dtype is torch.float64 and frequencies.is_contiguous() and frequencies.dim() == 1):
         raise ValueError(f"frequencies: need a contiguous 1-D fp64 tensor on cuda:{device}")
-    _done(lgc.lib().lgc_rotary(C.byref(hx), kind, rows, heads, dim, positions.data_ptr(), frequencies.data_ptr(), frequencies.numel(),
-                               1 if interleaved else 0, amplitude, 1 if backward else 0, C.byref(hy), _stream(stream, device)), "lgc_rotary")
+    _done(lgc.lib().lgc_rotary(hx, _TYPES[x.dtype], rows, heads, dim, positions.data_ptr(), frequencies.data_ptr(), frequencies.numel(),
+                               1 if interleaved else 0, amplitude, 1 if backward else 0, hy, _stream(stream, device)), "lgc_rotary")
 
 
-def _starts(t: Optional[torch.Tensor], name: str, device: int, n: Optional[int] = None):
-    if not (t.get_device() == device and t.dtype is torch.int64 and t.is_contiguous() and t.dim() == 1 and (t.numel() == n if n is not None else t.numel() > 1)):
+def _starts(t: torch.Tensor, name: str, device: int, n: Optional[int] = None):
+    """(address, elements) of the array of the sequences' starts."""
+    shape = t.shape
+    if not (t.dtype is torch.int64 and t.get_device() == device and len(shape) == 1 and (shape[0] == n if n is not None else shape[0] > 1) and t.is_contiguous()):
         raise ValueError(f"{name}: need a contiguous int64 tensor of {n if n is not None else 'sequences + 1'} elements on cuda:{device}")
-    return t.data_ptr()
+    return t.data_ptr(), shape[0]
 
 
 def _attention_shape(q_shape, k_shape, query_start, key_start, causal: bool, window: int, scale: Optional[float], device: int):
+    """(lgc_attention_shape, number of sequences, 0 without starts)."""
     rows, heads, dim = q_shape
-    keys, kv_heads, _ = k_shape
-    if query_start is None and key_start is not None:
-        raise ValueError("key_start: goes with query_start")
-    qs = ks = None
-    sequences = 1
-    if query_start is not None:
-        qs, sequences = _starts(query_start, "query_start", device), query_start.numel() - 1
+    keys, kv_heads, k_dim = k_shape
+    if k_dim != dim:
+        raise ValueError(f"k: need heads of {dim} elements")
+    if scale is None:
+        scale = dim ** -0.5 if dim else 1.0
+    if query_start is None:
         if key_start is not None:
-            ks = _starts(key_start, "key_start", device, sequences + 1)
-    return lgc.lgc_attention_shape(rows, keys, heads, kv_heads, dim, sequences, qs, ks, 1 if causal else 0, window,
-                                   scale if scale is not None else 1.0 / math.sqrt(dim) if dim else 1.0)
+            raise ValueError("key_start: goes with query_start")
+        return _shape_bytes(rows, keys, heads, kv_heads, dim, 1, 0, 0, 1 if causal else 0, window, scale), 0
+    qs, n = _starts(query_start, "query_start", device)
+    ks = 0 if key_start is None else _starts(key_start, "key_start", device, n)[0]
+    return _shape_bytes(rows, keys, heads, kv_heads, dim, n - 1, qs, ks, 1 if causal else 0, window, scale), n - 1
 
 
 @functools.lru_cache(maxsize=256)
@@ -352,12 +363,15 @@ def _attention_size(name: str, query_rows: int, key_rows: int, heads: int, kv_he
     return n.value
 
 
-def _attention_room(name: str, q_shape, k_shape, query_start, scratch, stream, like):
+def _attention_room(name: str, q_shape, k_shape, num_sequences: int, scratch, stream, like):
     """(tensor or None, address, bytes) of a call's scratch."""
-    rows, heads, dim = q_shape
-    need = _attention_size(name, rows, k_shape[0], heads, k_shape[1], dim, 0 if query_start is None else query_start.numel() - 1)
-    if scratch is None and need == 0:
-        return None, None, 0
+    need = _attention_size(name, q_shape[0], k_shape[0], q_shape[1], k_shape[1], q_shape[2], num_sequences)
+    if scratch is None:
+        if need == 0:
+            return None, None, 0
+        if stream is None:
+            scratch = torch.empty(need, dtype=torch.uint8, device=like.device)
+            return scratch, scratch.data_ptr(), need
     scratch, size = _scratch(need, scratch, stream, like)
     return scratch, scratch.data_ptr(), size
 
@@ -377,17 +391,14 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, y: torch.Tensor
     `window` (0: none): of those only the last ones.  `scale`: 1 / sqrt(dim) by default.  A query that sees no key has y = 0,
     lse = -inf.  `scratch`: a uint8 tensor of attention_scratch bytes; without one it comes from PyTorch's allocator."""
     device = _device(q.get_device(), stream)
-    hq, qshape, _ = _heads(q, "q", device)
-    hk, kshape, _ = _heads(k, "k", device)
-    if kshape[2] != qshape[2]:
-        raise ValueError(f"k: need heads of {qshape[2]} elements")
-    hv, _, _ = _heads(v, "v", device, kshape)
-    hy, _, _ = _heads(y, "y", device, qshape)
-    shape = _attention_shape(qshape, kshape, query_start, key_start, causal, window, scale, device)
+    hq, qshape = _heads(q, "q", device)
+    hk, kshape = _heads(k, "k", device)
+    hv, _ = _heads(v, "v", device, kshape)
+    hy, _ = _heads(y, "y", device, qshape)
+    shape, sequences = _attention_shape(qshape, kshape, query_start, key_start, causal, window, scale, device)
     lp = _vector(lse, qshape[0] * qshape[1], "lse", device)
-    scratch, at, size = _attention_room("lgc_attention_scratch", qshape, kshape, query_start, scratch, stream, q)
-    _done(lgc.lib().lgc_attention(C.byref(shape), C.byref(hq), C.byref(hk), C.byref(hv), C.byref(hy), lp, at, size,
-                                  _stream(stream, device)), "lgc_attention")
+    scratch, at, size = _attention_room("lgc_attention_scratch", qshape, kshape, sequences, scratch, stream, q)
+    _done(lgc.lib().lgc_attention(shape, hq, hk, hv, hy, lp, at, size, _stream(stream, device)), "lgc_attention")
 
 
 def attention_backward_scratch(query_rows: int, key_rows: int, heads: int, kv_heads: int, dim: int, num_sequences: int = 0) -> int:
@@ -403,17 +414,18 @@ def attention_backward(dy: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: to
     dk, dv (bf16, like q, k, v); dk and dv are summed over the heads that share a head of k and v.  The same call gives the
     same bits.  `scratch`: a uint8 tensor of attention_backward_scratch bytes; without one it comes from PyTorch's allocator."""
     device = _device(dy.get_device(), stream)
-    hdy, qshape, _ = _heads(dy, "dy", device)
-    hk, kshape, _ = _heads(k, "k", device)
-    if kshape[2] != qshape[2]:
-        raise ValueError(f"k: need heads of {qshape[2]} elements")
-    hq, hy, hdq = (_heads(t, name, device, qshape)[0] for t, name in ((q, "q"), (y, "y"), (dq, "dq")))
-    hv, hdk, hdv = (_heads(t, name, device, kshape)[0] for t, name in ((v, "v"), (dk, "dk"), (dv, "dv")))
-    shape = _attention_shape(qshape, kshape, query_start, key_start, causal, window, scale, device)
+    hdy, qshape = _heads(dy, "dy", device)
+    hk, kshape = _heads(k, "k", device)
+    hq, _ = _heads(q, "q", device, qshape)
+    hy, _ = _heads(y, "y", device, qshape)
+    hdq, _ = _heads(dq, "dq", device, qshape)
+    hv, _ = _heads(v, "v", device, kshape)
+    hdk, _ = _heads(dk, "dk", device, kshape)
+    hdv, _ = _heads(dv, "dv", device, kshape)
+    shape, sequences = _attention_shape(qshape, kshape, query_start, key_start, causal, window, scale, device)
     lp = _vector(lse, qshape[0] * qshape[1], "lse", device)
-    scratch, at, size = _attention_room("lgc_attention_backward_scratch", qshape, kshape, query_start, scratch, stream, dy)
-    _done(lgc.lib().lgc_attention_backward(C.byref(shape), C.byref(hdy), C.byref(hq), C.byref(hk), C.byref(hv), C.byref(hy), lp, C.byref(hdq),
-                                           C.byref(hdk), C.byref(hdv), at, size, _stream(stream, device)), "lgc_attention_backward")
+    scratch, at, size = _attention_room("lgc_attention_backward_scratch", qshape, kshape, sequences, scratch, stream, dy)
+    _done(lgc.lib().lgc_attention_backward(shape, hdy, hq, hk, hv, hy, lp, hdq, hdk, hdv, at, size, _stream(stream, device)), "lgc_attention_backward")
 
 
 def check(stream: Optional[torch.cuda.Stream] = None) -> None:

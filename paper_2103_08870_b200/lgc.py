@@ -115,7 +115,7 @@ def lib() -> C.CDLL:
         l.lgc_weight_gradient_scratch.argtypes = [i64, i64, i64, i32, C.POINTER(sz)]
         l.lgc_weight_gradient.argtypes = [vp, i64, pk, i64, i64, i64, vp, i32, vp, i64, vp, sz, vp]
         l.lgc_layers_check.argtypes = [vp]
-        hd, sh = C.POINTER(lgc_heads), C.POINTER(lgc_attention_shape)
+        hd = sh = vp                    # lgc_heads *, lgc_attention_shape *: a structure by reference, or its bytes
         l.lgc_rotary.argtypes = [hd, i32, i64, i32, i32, vp, vp, i32, i32, f32, i32, hd, vp]
         l.lgc_attention_scratch.argtypes = [sh, C.POINTER(sz)]
         l.lgc_attention.argtypes = [sh, hd, hd, hd, hd, vp, vp, sz, vp]
