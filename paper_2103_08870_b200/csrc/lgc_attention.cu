@@ -32,7 +32,7 @@ struct ForwardArgs {
     __nv_bfloat16 *y;
     int64_t ld_y, head_stride_y;
     float *lse;
-    float *part_y, *part_lse;           // plan.splits > 1: [splits][query rows][heads][dim], [splits][query rows][heads]
+    float *part_y, *part_lse;           // plan.splits > 1: [parts][query rows][heads][dim], [parts][query rows][heads]; parts: 2 * splits
     int *parts;                         // ... and how many there are, [query rows][heads]
     int32_t *errword;
 };
@@ -44,11 +44,14 @@ constexpr int kTileBytes = DP / 64 * kPiece;
 template <int DP>
 constexpr int kSmem = (2 + kStages<DP>) * kTileBytes<DP> + 1024;
 
-// The keys of a unit: tiles of 128 from `base` on; tile t is of slot s if first[s] <= t < end[s].
+// The keys of a unit: tiles of 128 from `base` on; tile t is of slot s if first[s] <= t < last[s].  PARTS: the call's keys are cut into
+// parts; where a part's rows leave slot 1 empty, both slots have the same rows and every other tile (`both`), a part each.
 struct Range {
     int base, begin, end;
     int first[2], last[2];
+    bool both;
 };
+template <bool PARTS>
 __device__ __forceinline__ Range range_of(const ForwardArgs &p, const Unit &u)
 {
     Range r;
@@ -56,9 +59,10 @@ __device__ __forceinline__ Range range_of(const ForwardArgs &p, const Unit &u)
 #pragma unroll
     for (int s = 0; s < 2; ++s)
         keys_seen(p.mask, u.pos + s * p.queries, min(p.queries, u.rows - s * p.queries), u.shift, u.other_len, lo[s], hi[s]);
+    r.both = PARTS && u.splits > 1 && u.rows <= p.queries;
     r.base = hi[0] == 0 ? lo[1] : hi[1] == 0 ? lo[0] : min(lo[0], lo[1]);
     int from = 0, to = 0x7fffffff;                         // tiles of this split
-    if (u.splits > 1) {
+    if (PARTS && u.splits > 1) {
         const int tiles = (max(hi[0], hi[1]) - r.base + kRows - 1) >> 7, chunk = (tiles + u.splits - 1) / u.splits;
         from = u.split * chunk;
         to = from + chunk;
@@ -77,13 +81,20 @@ __device__ __forceinline__ Range range_of(const ForwardArgs &p, const Unit &u)
         }
     }
     if (r.end == 0) r.begin = 0;
+    if (PARTS && r.both && r.end > r.begin + 1) r.first[1] = r.begin + 1, r.last[1] = r.end;
     return r;
+}
+// Whether tile t is of slot s.
+template <bool PARTS>
+__device__ __forceinline__ bool of_slot(const Range &r, int s, int t)
+{
+    return t >= r.first[s] && t < r.last[s] && !(PARTS && r.both && ((t - r.first[s]) & 1));
 }
 
 // One warp issues the products of both tiles, in turn: issuing takes as long as the product, and so one tile's threads are at their
 // exponentials while the other's have their products made (a warp for each tile lets them fall into step: 1100 against 850 us for 16384
 // tokens, 16 heads).
-template <int DP>
+template <int DP, bool PARTS>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                  const __grid_constant__ ForwardArgs p)
@@ -131,7 +142,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             bool ok = true;
             for (Walk w(p.runs, p.plan, false, p.kv_heads); ok && w.next();) {
                 const Unit u = w.unit;
-                const Range r = range_of(p, u);
+                const Range r = range_of<PARTS>(p, u);
                 if (r.end == 0) continue;
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
@@ -139,7 +150,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                         if (!bar_wait(smem_addr(&q_empty[s]), q_phase[s], &failed)) { ok = false; break; }
                         q_phase[s] ^= 1;
                         bar_expect(smem_addr(&q_full[s]), q_bytes);
-                        load_tile<DP>(q_tile + s * kTile, &map_q, smem_addr(&q_full[s]), w.head * p.group, u.row + s * p.queries);
+                        load_tile<DP>(q_tile + s * kTile, &map_q, smem_addr(&q_full[s]), w.head * p.group, u.row + (PARTS && r.both ? 0 : s * p.queries));
                     }
                 for (int t = r.begin; t < r.end && ok; ++t)
 #pragma unroll
@@ -157,7 +168,7 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             bool ok = true;
             for (Walk w(p.runs, p.plan, false, p.kv_heads); ok && w.next();) {
                 const Unit u = w.unit;
-                const Range r = range_of(p, u);
+                const Range r = range_of<PARTS>(p, u);
                 if (r.end == 0) continue;
                 for (int t = r.begin - 1; t < r.end && ok; ++t) {
                     const bool has_v = t >= r.begin, has_k = t + 1 < r.end;
@@ -176,32 +187,45 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
                         }
                     }
                     if (has_k && !bar_wait_together(smem_addr(&full_bar[st_k]), ph_k, &failed)) { ok = false; break; }
+                    const auto add = [&](int s) {
+                        if (!bar_wait_together(smem_addr(&p_full[s]), ph_p[s], &failed)) return false;
+                        ph_p[s] ^= 1;
+                        tc_fence_after();
+                        if (issuer) {
 #pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        if (has_v && t >= r.first[s] && t < r.last[s]) {
-                            if (!bar_wait_together(smem_addr(&p_full[s]), ph_p[s], &failed)) { ok = false; break; }
-                            ph_p[s] ^= 1;
-                            tc_fence_after();
-                            if (issuer) {
-#pragma unroll
-                                for (int ks = 0; ks < kRows / 16; ++ks)
-                                    product_step<DP>(tmem + 256 + s * DP, tmem + s * kRows + ks * 8, tile_v, ks, t > r.first[s] || ks > 0);
-                            }
-                            __syncwarp();
+                            for (int ks = 0; ks < kRows / 16; ++ks)
+                                product_step<DP>(tmem + 256 + s * DP, tmem + s * kRows + ks * 8, tile_v, ks, t > r.first[s] || ks > 0);
                         }
-                        if (has_k && t + 1 >= r.first[s] && t + 1 < r.last[s]) {
-                            if (t + 1 == r.first[s]) {
-                                if (!bar_wait_together(smem_addr(&q_full[s]), ph_q[s], &failed)) { ok = false; break; }
-                                ph_q[s] ^= 1;
-                            }
-                            tc_fence_after();
-                            if (issuer) {
-                                // (after the product that reads P in the same columns: the tensor cores work in order)
-                                product_of_tiles<DP>(tmem + s * kRows, q_tile + s * kTile, tile_k);
-                                tc_commit(smem_addr(&s_full[s]));
-                                if (t + 2 == r.last[s]) tc_commit(smem_addr(&q_empty[s]));
-                            }
-                            __syncwarp();
+                        __syncwarp();
+                        return true;
+                    };
+                    const auto make = [&](int s) {
+                        if (t + 1 == r.first[s]) {
+                            if (!bar_wait_together(smem_addr(&q_full[s]), ph_q[s], &failed)) return false;
+                            ph_q[s] ^= 1;
+                        }
+                        tc_fence_after();
+                        if (issuer) {
+                            // (after the product that reads P in the same columns: the tensor cores work in order)
+                            product_of_tiles<DP>(tmem + s * kRows, q_tile + s * kTile, tile_k);
+                            tc_commit(smem_addr(&s_full[s]));
+                            if (t + 2 + (PARTS && r.both) >= r.last[s]) tc_commit(smem_addr(&q_empty[s]));
+                        }
+                        __syncwarp();
+                        return true;
+                    };
+                    if (PARTS && r.both) {                   // the next S is the other slot's
+#pragma unroll
+                        for (int s = 0; s < 2; ++s)
+                            if (has_k && of_slot<PARTS>(r, s, t + 1) && !make(s)) { ok = false; break; }
+#pragma unroll
+                        for (int s = 0; s < 2; ++s)
+                            if (ok && has_v && of_slot<PARTS>(r, s, t) && !add(s)) { ok = false; break; }
+                    } else {
+#pragma unroll
+                        for (int s = 0; s < 2; ++s) {
+                            if (has_v && of_slot<false>(r, s, t) && !add(s)) { ok = false; break; }
+                            if (has_k && of_slot<false>(r, s, t + 1) && !make(s)) { ok = false; break; }
                         }
                     }
                     if (!ok) break;
@@ -228,14 +252,14 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
         bool ok = true;
         for (Walk walk(p.runs, p.plan, false, p.kv_heads); ok && walk.next();) {
             const Unit u = walk.unit;
-            const Range r = range_of(p, u);
-            const int i = slot * p.queries + query;                              // of the unit
+            const Range r = range_of<PARTS>(p, u);
+            const int i = (PARTS && r.both ? 0 : slot * p.queries) + query;      // of the unit
             const bool live = query < p.queries && i < u.rows;
             int lo = 0, hi = 0x7fffffff;                                         // (rows that nobody reads need no mask)
             if (live) keys_seen(p.mask, u.pos + i, 1, u.shift, u.other_len, lo, hi);
             float most = -INFINITY, sum = 0.0f;                                  // the exponents' reference, and sum of exponentials
             const int first = slot ? r.first[1] : r.first[0], last = slot ? r.last[1] : r.last[0];
-            for (int t = first; t < last; ++t) {
+            for (int t = first; t < last; t += PARTS && r.both ? 2 : 1) {
                 if (!bar_wait_together(smem_addr(&s_full[slot]), ph_s, &failed)) { ok = false; break; }
                 ph_s ^= 1;
                 tc_fence_after();
@@ -315,12 +339,13 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
             const int64_t q = (int64_t)u.row + i;
             const int64_t at = q * p.heads + head;
             const float lse = sum == 0.0f ? -INFINITY : __fmul_rn(__fadd_rn(__fmul_rn(most, c), log2f(sum)), kLn2);
-            if (p.plan.splits > 1) {
+            if (PARTS) {
                 const int64_t all = p.runs.query_rows * p.heads;
-                if (live) p.part_lse[u.split * all + at] = lse;
-                if (live && u.split == 0) p.parts[at] = u.splits;
+                const int part = r.both ? 2 * u.split + slot : u.split;
+                if (live) p.part_lse[part * all + at] = lse;
+                if (live && part == 0) p.parts[at] = r.both ? 2 * u.splits : u.splits;
                 if (last > 0) {                              // (the part of a split without keys is not read)
-                    float *out = p.part_y + (u.split * all + at) * p.dim;
+                    float *out = p.part_y + (part * all + at) * p.dim;
 #pragma unroll
                     for (int j = 0; j < DP; j += 32) {
                         uint32_t o[32];
@@ -352,44 +377,73 @@ attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constan
     if (warp == 8) tc_free(tmem, 512);
 }
 
-// The splits of a row and head joined: y = sum_z w_z y_z, w_z = exp(lse_z - lse).  A warp per row and head.
-__global__ void __launch_bounds__(256)
+// The parts of a row and head joined: y = sum_z w_z y_z, w_z = exp(lse_z - lse).  A CTA per row and head: each of its four warps
+// takes every fourth part, four at a time under way.
+constexpr int kMostParts = 128, kJoinThreads = 128;
+__global__ void __launch_bounds__(kJoinThreads)
 join_kernel(const __grid_constant__ ForwardArgs p)
 {
+    __shared__ float sums[kJoinThreads / 32][kMostDim];
     grid_wait();
-    const int64_t all = p.runs.query_rows * p.heads, at = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 5;
-    const int lane = threadIdx.x & 31;
-    if (at >= all) return;
+    const int64_t all = p.runs.query_rows * p.heads, at = blockIdx.x;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t q = at / p.heads;
     const int head = (int)(at - q * p.heads);
     if (p.runs.query_start) {                                 // rows in no sequence stay as they are
         // (starts ascend: the row lies in a run if it lies between the first and the last)
         if (q < max((int64_t)0, p.runs.query_start[0]) || q >= p.runs.query_start[p.runs.sequences]) return;
     }
-    const int splits = p.parts[at];
-    float most = -INFINITY;
-    for (int z = lane; z < splits; z += 32) most = fmaxf(most, p.part_lse[z * all + at]);
+    // a lane's weights are those of the parts lane, lane + 32, ...
+    const int parts = min(p.parts[at], kMostParts);
+    float lse[kMostParts / 32], most = -INFINITY, total = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kMostParts / 32; ++i) {
+        lse[i] = i * 32 + lane < parts ? p.part_lse[(i * 32 + lane) * all + at] : -INFINITY;
+        most = fmaxf(most, lse[i]);
+    }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
     const float zero = most == -INFINITY ? 0.0f : most;
-    float total = 0.0f, y[4] = {};
-    for (int z = 0; z < splits; ++z) {
-        const float lse = p.part_lse[z * all + at];
-        const float w = exp2_of(__fmul_rn(__fsub_rn(lse, zero), kLog2e));
+    float y[4] = {};
+    const bool mine = lane * 4 < p.dim;
+    const float *from = p.part_y + at * p.dim + lane * 4;
+#pragma unroll
+    for (int i = 0; i < kMostParts / 32; ++i) {
+        if (i * 32 >= parts) break;
+        const float w = exp2_of(__fmul_rn(__fsub_rn(lse[i], zero), kLog2e));
         total = __fadd_rn(total, w);
-        if (lse > -INFINITY && lane * 4 < p.dim) {
-            const float4 v = *reinterpret_cast<const float4 *>(p.part_y + (z * all + at) * p.dim + lane * 4);
-            y[0] = __fmaf_rn(w, v.x, y[0]);
-            y[1] = __fmaf_rn(w, v.y, y[1]);
-            y[2] = __fmaf_rn(w, v.z, y[2]);
-            y[3] = __fmaf_rn(w, v.w, y[3]);
+#pragma unroll 1
+        for (int z = warp; z < min(32, parts - i * 32); z += 16) {
+            float4 v[4];
+            float wz[4];
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                const int part = min(z + 4 * n, 31);
+                wz[n] = __shfl_sync(0xffffffffu, w, part);
+                // (the part of no keys holds nothing: it is not read)
+                const bool some = __shfl_sync(0xffffffffu, lse[i], part) != -INFINITY && z + 4 * n < 32;
+                v[n] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (some && mine) v[n] = *reinterpret_cast<const float4 *>(from + (i * 32 + part) * all * p.dim);
+                if (!some) wz[n] = 0.0f;
+            }
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                y[0] = __fmaf_rn(wz[n], v[n].x, y[0]);
+                y[1] = __fmaf_rn(wz[n], v[n].y, y[1]);
+                y[2] = __fmaf_rn(wz[n], v[n].z, y[2]);
+                y[3] = __fmaf_rn(wz[n], v[n].w, y[3]);
+            }
         }
     }
+    if (mine) *reinterpret_cast<float4 *>(&sums[warp][lane * 4]) = make_float4(y[0], y[1], y[2], y[3]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) total = __fadd_rn(total, __shfl_xor_sync(0xffffffffu, total, o));
+    __syncthreads();
     const float inverse = total == 0.0f ? 0.0f : __fdiv_rn(1.0f, total);
-    if (lane * 4 < p.dim)
-        *reinterpret_cast<uint2 *>(p.y + q * p.ld_y + head * p.head_stride_y + lane * 4) =
-            make_uint2(bf16_pair(__fmul_rn(y[0], inverse), __fmul_rn(y[1], inverse)), bf16_pair(__fmul_rn(y[2], inverse), __fmul_rn(y[3], inverse)));
-    if (lane == 0) p.lse[at] = total == 0.0f ? -INFINITY : __fmaf_rn(log2f(total), kLn2, most);
+    if ((int)threadIdx.x < p.dim)
+        p.y[q * p.ld_y + head * p.head_stride_y + threadIdx.x] = __float2bfloat16_rn(
+            __fmul_rn(__fadd_rn(__fadd_rn(sums[0][threadIdx.x], sums[1][threadIdx.x]), __fadd_rn(sums[2][threadIdx.x], sums[3][threadIdx.x])), inverse));
+    if (threadIdx.x == 0) p.lse[at] = total == 0.0f ? -INFINITY : __fmaf_rn(log2f(total), kLn2, most);
 }
 
 // The table of units.  One CTA per table: units in front of every sequence's, then the units in the order of their work (the
@@ -538,7 +592,7 @@ plan_kernel(const __grid_constant__ PlanArgs a)
 
 // How the keys are cut: only where there are fewer units than would fill two rounds of CTAs, and so few rows that the parts' results,
 // which are written and read once more, are much less than the keys.  A part has at least `chunk` tiles of keys: as many as make
-// the work one round (ragged sequences: three rounds of shorter ones), two at least.  `splits` bounds their number.
+// the work one round (ragged sequences: two rounds of shorter ones), two at least.  `splits` bounds their number.
 struct Splits {
     int chunk, splits;
 };
@@ -546,7 +600,7 @@ Splits splits_of(const AttentionShape &a, int64_t units)
 {
     const int64_t tiles = (a.key_rows + kRows - 1) / kRows, ctas = units * a.kv_heads, sms = 148;
     if (ctas == 0 || ctas >= 2 * sms || tiles < 8 || a.query_rows * (a.heads / a.kv_heads) * 8 > a.key_rows) return Splits{1, 1};
-    const int64_t average = (tiles + a.sequences - 1) / a.sequences, rounds = a.query_start ? 3 : 1;      // tiles of a sequence
+    const int64_t average = (tiles + a.sequences - 1) / a.sequences, rounds = a.query_start ? 2 : 1;      // tiles of a sequence
     int64_t chunk = (average * ctas + rounds * sms - 1) / (rounds * sms);
     if (chunk < 2) chunk = 2;
     int64_t splits = (tiles + chunk - 1) / chunk;
@@ -555,18 +609,18 @@ Splits splits_of(const AttentionShape &a, int64_t units)
 }
 int queries_of_tile(const AttentionShape &a) { return kRows / (a.heads / a.kv_heads); }
 
-template <int DP>
+template <int DP, bool PARTS>
 cudaError_t launch_forward(const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v, const ForwardArgs &p, bool dependent, cudaStream_t s)
 {
     static OncePerDevice configured;
-    cudaError_t e = configured.run([&] { return cudaFuncSetAttribute(attention_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem<DP>); });
+    cudaError_t e = configured.run([&] { return cudaFuncSetAttribute(attention_kernel<DP, PARTS>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem<DP>); });
     if (e != cudaSuccess) return e;
     const int64_t work = p.plan.most * p.kv_heads, sms = sm_count();
     const dim3 grid((unsigned)(work < sms ? work : sms));
     if (dependent) {
-        e = launch_dependent_smem(attention_kernel<DP>, grid, dim3(kThreads), kSmem<DP>, s, q, k, v, p);
+        e = launch_dependent_smem(attention_kernel<DP, PARTS>, grid, dim3(kThreads), kSmem<DP>, s, q, k, v, p);
     } else {
-        attention_kernel<DP><<<grid, kThreads, kSmem<DP>, s>>>(q, k, v, p);
+        attention_kernel<DP, PARTS><<<grid, kThreads, kSmem<DP>, s>>>(q, k, v, p);
         e = cudaGetLastError();
     }
     if (e == cudaSuccess) ++g_kernel_launches;
@@ -605,7 +659,7 @@ size_t attention_scratch(const AttentionShape &a)
     const int per = 2 * queries_of_tile(a);
     const Splits z = splits_of(a, most_units(a.query_start, a.query_rows, per, a.sequences));
     size_t bytes = plan_bytes(a.query_start, a.query_rows, per, a.sequences, z.splits);
-    if (z.splits > 1) bytes += (size_t)a.query_rows * a.heads * ((size_t)z.splits * ((size_t)a.dim + 1) + 1) * 4;
+    if (z.splits > 1) bytes += (size_t)a.query_rows * a.heads * (2 * (size_t)z.splits * ((size_t)a.dim + 1) + 1) * 4;
     return bytes;
 }
 
@@ -626,8 +680,8 @@ cudaError_t launch_attention(const AttentionShape &a, const Heads &q, const Head
     if (z.splits > 1) {
         const size_t all = (size_t)a.query_rows * a.heads;
         p.part_y = reinterpret_cast<float *>(at + plan_bytes(a.query_start, a.query_rows, per, a.sequences, z.splits));
-        p.part_lse = p.part_y + (size_t)z.splits * all * a.dim;
-        p.parts = reinterpret_cast<int *>(p.part_lse + (size_t)z.splits * all);
+        p.part_lse = p.part_y + 2 * (size_t)z.splits * all * a.dim;
+        p.parts = reinterpret_cast<int *>(p.part_lse + 2 * (size_t)z.splits * all);
     }
     CUtensorMap mq, mk, mv;
     cudaError_t e = make_heads_map(&mq, q.p, a.dim, a.heads, a.query_rows, q.head_stride, q.ld, group, queries);
@@ -635,9 +689,11 @@ cudaError_t launch_attention(const AttentionShape &a, const Heads &q, const Head
     if (e == cudaSuccess && a.key_rows > 0) e = make_heads_map(&mv, v.p, a.dim, a.kv_heads, a.key_rows, v.head_stride, v.ld, 1, kRows);
     if (e == cudaSuccess && a.query_start) e = launch_plan(p.runs, p.mask, &p.plan, nullptr, s);
     if (e != cudaSuccess) return e;
-    e = a.dim <= 64 ? launch_forward<64>(mq, mk, mv, p, a.query_start != nullptr, s) : launch_forward<128>(mq, mk, mv, p, a.query_start != nullptr, s);
+    const bool planned = a.query_start != nullptr, parts = z.splits > 1;
+    e = a.dim <= 64 ? (parts ? launch_forward<64, true>(mq, mk, mv, p, planned, s) : launch_forward<64, false>(mq, mk, mv, p, planned, s))
+                    : (parts ? launch_forward<128, true>(mq, mk, mv, p, planned, s) : launch_forward<128, false>(mq, mk, mv, p, planned, s));
     if (e != cudaSuccess || z.splits == 1) return e;
-    e = launch_dependent(join_kernel, dim3((unsigned)((a.query_rows * a.heads + 7) / 8)), dim3(256), s, p);
+    e = launch_dependent(join_kernel, dim3((unsigned)(a.query_rows * a.heads)), dim3(kJoinThreads), s, p);
     if (e == cudaSuccess) ++g_kernel_launches;
     return e;
 }
