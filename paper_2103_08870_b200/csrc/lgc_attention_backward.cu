@@ -12,6 +12,11 @@
 // P^T and dS^T are such operands too.
 //
 // Precision: sums are fp32; P and dS are rounded to bf16 as operands; delta is a sum of bf16 products in fp32.
+//
+// What bounds them (16384 tokens, one causal sequence, 16 heads of 128 on 4: 1165 and 1605 us, 55 % of the measured bf16 rate counting
+// the five products that the gradient needs, 77 % counting the seven that are made): the chain of a tile.  Of the 2500 and
+// 3400 cycles of a pair of tiles the tensor cores work 1540 and 2050; the rest is from the end of P (or dS) to the next S: a barrier, the
+// issuing warp's wake-up (200 cycles), the product's latency (330), reads and writes of tensor memory.
 #include "lgc_attention.cuh"
 
 namespace lgc {
@@ -57,7 +62,9 @@ struct Ring {
 
 // ---- dq: a tile of queries goes over its keys --------------------------------------------------------------------------------
 // Tensor memory: S of two tiles of keys in turn (columns 0 and 128; dS takes its place), dP (256), dQ (384).
-// The tensor cores' order: dP(t + 1) once dP(t) has been read, dQ += dS(t) K(t), S(t + 2): the threads find the next S ready.
+// The tensor cores' order: dP(t + 1) once dP(t) has been read, dQ += dS(t) K(t), S(t + 2): the threads find the next S ready.  (dP only
+// after dS, which saves a barrier: 1410 against 1170 us.)  A quarter of the exponentials by polynomial: 912 against 1007 us with
+// heads of 64, where the products are short; none with heads of 128 (1170 against 1195 us).
 // delta is made by the rows' threads: the loads for a unit are under way while the last unit's results are written.
 constexpr int kKeyStages = 3, kValueStages = 2;
 struct QueryBars {
@@ -337,9 +344,10 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
 // ---- dk and dv: a tile of keys goes over the queries that see it -----------------------------------------------------------------
 // Tensor memory: S^T (columns 0; P^T takes its place), dP^T (128; dS^T takes its place), dV (256), dK (256 + DP).
 // The tensor cores' order: dV += P(t) dY(t), S(t + 1), dK += dS(t) Q(t), dP(t + 1): while the threads are at P
-// they have dK and dP to do, while they are at dS, dV and the next S.  One warp issues them all: two warps' products would share the
-// tensor cores, and the next S, for which the threads wait, would come later (3640 against 3200 us for the whole backward pass of
-// 16384 tokens, 16 heads).
+// they have dK and dP to do, while they are at dS, dV and the next S.  What the issuing warp does between P and the next S is on the
+// path of every tile: 16384 tokens of 16 heads take 1605 us, and took 1800 with one more read of shared memory there.  (A second
+// issuing warp, for dP and dK: 1787 against 1793 us; P in two halves, so that dV begins earlier: 3 % more; a part of the
+// exponentials by polynomial: 4 % more.)
 //
 // Keys that most queries look at (the first of a sequence, often) have gradients hundreds of times the others', and P's rounding to
 // bf16 would be off by as much as the others' gradients.  So the threads keep a sample of a key's probabilities' sum, and

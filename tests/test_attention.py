@@ -119,3 +119,61 @@ def test_scratch_does_not_grow_with_the_square_of_anything(lib):
             for keys in (1, 5000, 1 << 20):
                 assert lib.lgc_attention_scratch(shape(query_rows=rows, key_rows=keys, query_start=4096, key_start=4096, num_sequences=sequences), C.byref(n)) == OK
                 assert n.value < 200 << 20
+
+
+def test_operands_and_streams_of_another_device_are_refused(monkeypatch):
+    from types import SimpleNamespace
+
+    from paper_2103_08870_b200 import layers
+    from test_layers import NothingLaunched, Stub
+    monkeypatch.setattr(lgc, "lib", lambda: NothingLaunched())
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 0, raising=False)
+    bf = torch.bfloat16
+    q = lambda d=0: Stub(6, 4, 64, dtype=bf, device=d)                            # noqa: E731
+    k = lambda d=0: Stub(6, 2, 64, dtype=bf, device=d)                            # noqa: E731
+    lse = lambda d=0: Stub(6, 4, device=d)                                        # noqa: E731
+    at = lambda d=0: Stub(3, dtype=torch.int64, device=d)                         # noqa: E731
+    room = lambda d=0: Stub(1 << 16, dtype=torch.uint8, device=d)                 # noqa: E731
+    positions, frequencies = (lambda d=0: Stub(6, dtype=torch.int64, device=d)), (lambda d=0: Stub(32, dtype=torch.float64, device=d))
+    calls = [
+        (layers.rotary, [q, positions, frequencies, q], {}),
+        (layers.attention, [q, k, k, q, lse], dict(query_start=at, key_start=at, scratch=room)),
+        (layers.attention_backward, [q, q, k, k, q, lse, q, k, k], dict(query_start=at, key_start=at, scratch=room)),
+    ]
+    layers._attention_size.cache_clear()
+    for call, args, named in calls:
+        slots = list(range(len(args))) + list(named)
+        for other in [[s] for s in slots] + [slots]:
+            with pytest.raises(ValueError):
+                call(*[a(1 if i in other else 0) for i, a in enumerate(args)], **{n: a(1 if n in other else 0) for n, a in named.items()})
+        with pytest.raises(AssertionError):                                       # all where they belong: the library is called
+            call(*[a() for a in args], **{n: a() for n, a in named.items()})
+        with pytest.raises(ValueError):
+            call(*[a() for a in args], **{n: a() for n, a in named.items()}, stream=SimpleNamespace(device_index=1, cuda_stream=0))
+    layers._attention_size.cache_clear()
+
+
+def test_the_attention_block_makes_its_device_current(monkeypatch):
+    from paper_2103_08870_b200 import block
+    seen = []
+
+    class Stop(Exception):
+        pass
+
+    def stop(*a, **kw):
+        raise Stop
+
+    monkeypatch.setattr(torch.cuda, "set_device", seen.append)
+    monkeypatch.setattr(torch, "tensor", stop)
+    with pytest.raises(Stop):
+        block.AttentionBlock([4], 8, 1, 1, 8, 1, device=torch.device("cuda", 1))
+    assert seen == [torch.device("cuda", 1)]
+
+
+def test_the_structures_and_their_bytes_agree():
+    from paper_2103_08870_b200 import layers
+    numbers = (1, 2, 3, 4, 5, 6, 4096, 8192, 1, 7, 0.5)
+    a, b = bytes(lgc.lgc_attention_shape(*numbers)), layers._shape_bytes(*numbers)
+    assert len(a) == len(b) and a[:68] == b[:68]                # (padding follows the last number)
+    assert bytes(lgc.lgc_heads(4096, 5, 6)) == layers._heads_bytes(4096, 5, 6)

@@ -363,6 +363,54 @@ def test_rows_beyond_32_bits_of_bytes():
     assert ((x.double() - R.rotary(before, positions, frequencies)).abs() <= (R.UBF + 2.0 ** -18) * 2 * before.double().abs().max()).all()
 
 
+@pytest.mark.parametrize("dim,group", [(64, 4), (128, 1)])
+def test_parts_of_long_keys_with_rows_of_no_sequence(dim, group):
+    """Few queries, cut keys: sequences of one tile, of many, of no keys; rows in front of the first and behind the last."""
+    g = generator("parts", dim, group)
+    query_start, key_start = starts(1, 2, 0, 30, 1, first=3), starts(9000, 60, 700, 3000, 0, first=11)
+    T, S = 3 + 34 + 5, 11 + 12760 + 70
+    q, k, v = randn(g, T, 2 * group, dim).to(BF), randn(g, S, 2, dim).to(BF), randn(g, S, 2, dim).to(BF)
+    for t, at in ((q, query_start), (k, key_start), (v, key_start)):
+        t[:int(at[0])] = math.nan
+        t[int(at[-1]):] = math.inf
+    assert layers.attention_scratch(T, S, 2 * group, 2, dim, 5) > T * 2 * group * dim * 4
+    for causal in (False, True):
+        named = dict(query_start=query_start, key_start=key_start, causal=causal)
+        y, lse = forward(q, k, v, **named)
+        check_forward(q, k, v, y, lse, **named)
+        again = forward(q, k, v, **named)
+        assert torch.equal(y, again[0]) and torch.equal(lse, again[1])
+    layers.check()
+
+
+def test_a_key_that_most_queries_look_at():
+    """Its gradients sum up 12000 probabilities near one: the tiles behind the first ones take them as two bf16 numbers."""
+    g = generator("sink")
+    T, H, D = 3000, 4, 64
+    q, k, v = randn(g, T, H, D), randn(g, T, 1, D), randn(g, T, 1, D).to(BF)
+    common = randn(g, D)
+    q, k[0, 0] = (q + common).to(BF), 3 * common
+    k = k.to(BF)
+    y, lse = forward(q, k, v)
+    check_forward(q, k, v, y, lse)
+    dy = randn(g, T, H, D).to(BF)
+    got = backward(dy, q, k, v, y, lse)
+    check_backward(dy, q, k, v, y, lse, got)
+    want, off = R.attention_backward(dy, q, k, v, y, lse)
+    p0 = torch.exp((q.double() @ k[0, 0].double()) / 8 - lse.double())            # of the first key
+    assert p0.sum() > 2 * 256 * H
+    # Until its sum is 256 times the mean (H a key), in a sample of every eighth of half of the rows (rows of one tile more or less,
+    # and the two tiles that are under way), every product errs by 2^-8 of itself at most; after that by 2^-16.  A sample's sum
+    # of 16 H needs no more than 4 * 256 H of all (the sample would have a quarter of its share: it has thousands of entries).
+    early = (p0.flatten().cumsum(0) <= 4 * 256 * H + 4 * 128).view_as(p0)
+    room = R.UBF * want[2][0, 0].abs() * (1 + 2 * R.UBF) + ((R.UBF * early + 2.0 ** -15) * p0)[..., None].mul(dy.double().abs()).sum((0, 1))
+    room += T * H / 16 * 2.0 ** -23 * p0[..., None].mul(dy.double().abs()).sum((0, 1))
+    assert ((got[2][0, 0].double() - want[2][0, 0]).abs() <= room).all()
+    for a, b in zip(got, backward(dy, q, k, v, y, lse)):
+        assert torch.equal(a, b)
+    layers.check()
+
+
 # ---- streams, graphs, refusals --------------------------------------------------------------------------------------------------
 
 def test_streams_and_graphs_repeat_the_bits():
