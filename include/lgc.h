@@ -443,7 +443,8 @@ lgc_status lgc_attention(const lgc_attention_shape *shape, const lgc_heads *q, c
  *     dv_j = sum_i p_ij dy_i,   dq_i = scale sum_j ds_ij k_j,   dk_j = scale sum_i ds_ij q_i,
  * dk and dv also summed over the heads that share a head of k and v.  dq, dk, dv: bf16, like q, k, v; each sum is fp32 in a
  * fixed order (the same call gives the same bits).  No output may overlap an input or another output.
- * scratch: lgc_attention_backward_scratch bytes, 16-byte aligned. */
+ * scratch: lgc_attention_backward_scratch bytes, 16-byte aligned.  (Both sizes go by the numbers of rows, heads, columns and
+ * sequences and by whether there are starts, not by the mask nor by where the starts are.) */
 lgc_status lgc_attention_backward_scratch(const lgc_attention_shape *shape, size_t *bytes);
 lgc_status lgc_attention_backward(const lgc_attention_shape *shape, const lgc_heads *dy, const lgc_heads *q, const lgc_heads *k,
                                   const lgc_heads *v, const lgc_heads *y, const float *lse, const lgc_heads *dq, const lgc_heads *dk,

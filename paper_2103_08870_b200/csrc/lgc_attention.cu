@@ -485,7 +485,7 @@ __device__ __forceinline__ Unit unit_number(const PlanArgs &a, const Starts &st,
     const int k0 = st.key ? st.key[lo] : start_of(r.key_start, lo, r.key_rows), k1 = st.key ? st.key[lo + 1] : start_of(r.key_start, lo + 1, r.key_rows);
     const int queries = max(0, q1 - q0), keys = max(0, k1 - k0);
     Unit u;
-    u.splits = by_key ? 1 : parts_of(plan, keys);
+    u.splits = parts_of(plan, by_key ? queries : keys);
     const int number = e - st.prefix[lo];
     u.split = number % u.splits;
     u.pos = number / u.splits * plan.per;
@@ -530,8 +530,10 @@ plan_kernel(const __grid_constant__ PlanArgs a)
         const int b = few ? starts[by_key][s] : start_of(start, s, rows), e = few ? starts[by_key][s + 1] : start_of(start, s + 1, rows);
         const int n = (max(0, e - b) + plan.per - 1) / plan.per;
         if (plan.splits == 1) return n;
-        const int k0 = few ? starts[1][s] : start_of(a.runs.key_start, s, a.runs.key_rows), k1 = few ? starts[1][s + 1] : start_of(a.runs.key_start, s + 1, a.runs.key_rows);
-        return n * parts_of(plan, max(0, k1 - k0));
+        const int64_t *other = by_key ? a.runs.query_start : a.runs.key_start;
+        const int64_t all = by_key ? a.runs.query_rows : a.runs.key_rows;
+        const int o0 = few ? starts[!by_key][s] : start_of(other, s, all), o1 = few ? starts[!by_key][s + 1] : start_of(other, s + 1, all);
+        return n * parts_of(plan, max(0, o1 - o0));
     };
     long long mine = 0;
     for (int s = from; s < to; ++s) mine += units(s);
@@ -678,7 +680,7 @@ cudaError_t launch_attention(const AttentionShape &a, const Heads &q, const Head
     ForwardArgs p{};
     p.runs = Runs{a.query_start, a.key_start, a.sequences, a.query_rows, a.key_rows};
     const Splits z = splits_of(a, most_units(a.query_start, a.query_rows, per, a.sequences));
-    p.plan = plan_at(at, a.query_start, a.query_rows, per, a.sequences, z.chunk, z.splits);
+    p.plan = plan_at(at, a.query_start, a.query_rows, per, a.sequences, kRows, z.chunk, z.splits);
     p.mask = Mask{a.causal, a.window};
     p.heads = a.heads, p.kv_heads = a.kv_heads, p.group = group, p.dim = a.dim, p.queries = queries;
     p.scale_log2 = (float)((double)a.scale * 1.4426950408889634);

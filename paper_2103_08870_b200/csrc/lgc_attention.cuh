@@ -30,7 +30,7 @@ struct __align__(16) Unit {
     int pos;                   // of the first row in its sequence
     int other_row, other_len;  // the sequence's keys, or queries
     int shift;                 // number of keys - number of queries: causal: query i sees keys up to i + shift
-    int split, splits;         // the unit takes part `split` of `splits` of the other side (1 but for few queries and many keys)
+    int split, splits;         // the unit takes part `split` of `splits` of the other side (1 but for long ones of few units)
 };
 
 struct Mask {
@@ -45,7 +45,8 @@ struct Plan {
     int *prefix;               // [sequences + 1] units in front of a sequence's
     int per;                   // rows of a unit
     int64_t most;              // units that there is room for
-    int chunk, splits;         // tiles of the other side that a part has at least, parts at most
+    int tile;                  // rows of a tile of the other side
+    int chunk, splits;         // such tiles that a part has at least, parts at most
 };
 
 inline int64_t most_units(const int64_t *start, int64_t rows, int per, int sequences) { return start ? rows / per + sequences : (rows + per - 1) / per; }
@@ -53,16 +54,16 @@ inline size_t plan_bytes(const int64_t *start, int64_t rows, int per, int sequen
 {
     return start ? 16 + (size_t)most_units(start, rows, per, sequences) * splits * sizeof(Unit) + ((size_t)sequences + 1 + 3) / 4 * 16 : 0;
 }
-inline Plan plan_at(char *p, const int64_t *start, int64_t rows, int per, int sequences, int chunk = 1, int splits = 1)
+inline Plan plan_at(char *p, const int64_t *start, int64_t rows, int per, int sequences, int tile, int chunk = 1, int splits = 1)
 {
     const int64_t most = most_units(start, rows, per, sequences) * splits;
     Unit *units = reinterpret_cast<Unit *>(p + 16);
-    return Plan{reinterpret_cast<int *>(p), units, reinterpret_cast<int *>(units + most), per, most, chunk, splits};
+    return Plan{reinterpret_cast<int *>(p), units, reinterpret_cast<int *>(units + most), per, most, tile, chunk, splits};
 }
-// Parts of a sequence's keys.
-__host__ __device__ __forceinline__ int parts_of(const Plan &plan, int keys)
+// Parts of a sequence's rows on the other side.
+__host__ __device__ __forceinline__ int parts_of(const Plan &plan, int rows)
 {
-    const int tiles = (keys + kRows - 1) / kRows, parts = (tiles + plan.chunk - 1) / plan.chunk;
+    const int tiles = (rows + plan.tile - 1) / plan.tile, parts = (tiles + plan.chunk - 1) / plan.chunk;
     return plan.splits == 1 || parts < 1 ? 1 : parts < plan.splits ? parts : plan.splits;
 }
 
@@ -81,7 +82,7 @@ __device__ __forceinline__ Unit unit_at(const Runs &r, const Plan &plan, bool by
     }
     const int rows = (int)(by_key ? r.key_rows : r.query_rows);
     if (!by_key) index = (uint32_t)plan.most - 1 - index;
-    u.splits = by_key ? 1 : parts_of(plan, (int)r.key_rows);      // (one sequence: every unit has plan.splits)
+    u.splits = parts_of(plan, (int)(by_key ? r.query_rows : r.key_rows));      // (one sequence: plan.splits for every unit, or one)
     u.split = plan.splits == 1 ? 0 : (int)(index % (uint32_t)plan.splits);
     u.row = u.pos = (int)(plan.splits == 1 ? index : index / (uint32_t)plan.splits) * plan.per;
     u.rows = min(plan.per, rows - u.row);

@@ -42,6 +42,8 @@ struct BackwardArgs {
     int64_t ld_dq, head_stride_dq, ld_dk, head_stride_dk, ld_dv, head_stride_dv;
     float *minus_lse2, *minus_delta;    // [kv_heads][query rows][group]: -lse * log2(e), -delta
     float heavy;                        // see attention_dkv_kernel
+    float *parts;                       // the queries cut into parts: [parts][key rows][kv_heads][dv, dk][dim]
+    int *number;                        // ... and how many there are, [key rows][kv_heads]
     int32_t *errword;
 };
 
@@ -353,6 +355,10 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
 // bf16 would be off by as much as the others' gradients.  So the threads keep a sample of a key's probabilities' sum, and
 // once it is 256 times what a key has on average, the tiles that follow take P and dS as two bf16 numbers each (the second: what the
 // first has lost) in two more products.  The decision goes by sums of earlier tiles in the unit, the same in every call.
+//
+// Few units of keys with many queries each (shared heads, one sequence) leave SMs idle: their queries are cut into parts, the parts' sums
+// stay fp32 in memory, and join_gradients_kernel adds them up in order.  Whole backward passes, causal, heads of 128: 2048
+// tokens of 16 heads on 4 take 90 us, uncut 166; 8192 of 4 heads on 1 219, uncut 594; 16384 of 8 on 1 1438, uncut 2650.
 constexpr int kQueryStages = 3, kDyStages = 2, kRowStages = 2;
 struct KeyBars {
     uint64_t kv_full, kv_empty, q_full[kQueryStages], q_empty[kQueryStages], dy_full[kDyStages], dy_empty[kDyStages], row_full[kRowStages],
@@ -368,7 +374,8 @@ __device__ __forceinline__ uint32_t bf16_lost(float lo, float hi, uint32_t w)
 {
     return bf16_pair(__fsub_rn(lo, __uint_as_float(w << 16)), __fsub_rn(hi, __uint_as_float(w & 0xffff0000u)));
 }
-template <int DP>
+// PARTS: a unit has a part of its queries, and its sums go to memory as they are.
+template <int DP, bool PARTS>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                      const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ BackwardArgs p)
@@ -409,7 +416,11 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     const auto queries_of = [&](const Unit &u, int &lo) {
         int hi;
         queries_seeing(p.mask, u.pos, u.rows, u.shift, u.other_len, lo, hi);
-        return (hi - lo + p.queries - 1) / p.queries;
+        const int tiles = (hi - lo + p.queries - 1) / p.queries;
+        if (!PARTS || u.splits == 1) return tiles;
+        const int chunk = (tiles + u.splits - 1) / u.splits, from = min(tiles, u.split * chunk);
+        lo += from * p.queries;
+        return min(tiles, from + chunk) - from;
     };
     if (warp >= 8) {
         give_registers<kOtherRegisters>();
@@ -678,8 +689,26 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             }
             // one group of warps writes dv, the other dk
             const int64_t key = (int64_t)u.row + row;
-            __nv_bfloat16 *out = half ? p.dk + key * p.ld_dk + walk.head * p.head_stride_dk : p.dv + key * p.ld_dv + walk.head * p.head_stride_dv;
-            store_rows<DP>(live ? out : nullptr, p.dim, tmem + lanes + 256 + half * DP, half ? p.scale : 1.0f, tiles > 0);
+            if (PARTS) {
+                const int64_t at = key * p.kv_heads + walk.head;
+                if (live && half == 0 && u.split == 0) p.number[at] = u.splits;
+                float *out = p.parts + ((u.split * p.runs.key_rows * p.kv_heads + at) * 2 + half) * p.dim;
+#pragma unroll 1
+                for (int j = 0; j < DP; j += 32) {
+                    uint32_t o[32];
+                    tc_read32(tmem + lanes + 256 + half * DP + j, o);
+                    tc_read_wait(o);
+#pragma unroll
+                    for (int n = 0; n < 32; n += 4)
+                        if (live && j + n < p.dim)
+                            *reinterpret_cast<float4 *>(out + j + n) =
+                                tiles > 0 ? make_float4(__uint_as_float(o[n]), __uint_as_float(o[n + 1]), __uint_as_float(o[n + 2]), __uint_as_float(o[n + 3]))
+                                          : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                }
+            } else {
+                __nv_bfloat16 *out = half ? p.dk + key * p.ld_dk + walk.head * p.head_stride_dk : p.dv + key * p.ld_dv + walk.head * p.head_stride_dv;
+                store_rows<DP>(live ? out : nullptr, p.dim, tmem + lanes + 256 + half * DP, half ? p.scale : 1.0f, tiles > 0);
+            }
             if (tiles > 0) {
                 tc_fence_before();
                 __syncwarp();
@@ -694,16 +723,42 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     if (warp == 8) tc_free(tmem, 512);
 }
 
+// The parts of dk and dv added up, in order.  A thread: four columns.  (A read of what the parts left, 5 us where it counts.)
+__global__ void __launch_bounds__(256)
+join_gradients_kernel(const __grid_constant__ BackwardArgs p)
+{
+    grid_wait();
+    const int64_t all = p.runs.key_rows * p.kv_heads * 2, quarter = p.dim / 4, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= all * quarter) return;
+    const int64_t row = i / quarter, at = row >> 1, key = at / p.kv_heads;
+    const int column = (int)(i - row * quarter) * 4, head = (int)(at - key * p.kv_heads), second = (int)(row & 1);
+    if (p.runs.key_start && (key < max((int64_t)0, p.runs.key_start[0]) || key >= p.runs.key_start[p.runs.sequences])) return;      // in no sequence
+    const int parts = min(p.number[at], p.plan.splits);
+    float s[4] = {};
+#pragma unroll 4
+    for (int z = 0; z < parts; ++z) {
+        const float4 v = *reinterpret_cast<const float4 *>(p.parts + (z * all + row) * p.dim + column);
+        s[0] = __fadd_rn(s[0], v.x);
+        s[1] = __fadd_rn(s[1], v.y);
+        s[2] = __fadd_rn(s[2], v.z);
+        s[3] = __fadd_rn(s[3], v.w);
+    }
+    const float by = second ? p.scale : 1.0f;
+    __nv_bfloat16 *out = second ? p.dk + key * p.ld_dk + head * p.head_stride_dk : p.dv + key * p.ld_dv + head * p.head_stride_dv;
+    *reinterpret_cast<uint2 *>(out + column) =
+        make_uint2(bf16_pair(__fmul_rn(s[0], by), __fmul_rn(s[1], by)), bf16_pair(__fmul_rn(s[2], by), __fmul_rn(s[3], by)));
+}
+
 struct Maps {
     CUtensorMap q, k, v, dy;
 };
-template <int DP>
+template <int DP, bool PARTS>
 cudaError_t launch_both(const Maps &m, const BackwardArgs &by_query, const BackwardArgs &by_key, bool dependent, cudaStream_t s)
 {
     static OncePerDevice configured;
     cudaError_t e = configured.run([&] {
         const cudaError_t f = cudaFuncSetAttribute(attention_dq_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, kQuerySmem<DP>);
-        return f != cudaSuccess ? f : cudaFuncSetAttribute(attention_dkv_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, kKeySmem<DP>);
+        return f != cudaSuccess ? f : cudaFuncSetAttribute(attention_dkv_kernel<DP, PARTS>, cudaFuncAttributeMaxDynamicSharedMemorySize, kKeySmem<DP>);
     });
     if (e != cudaSuccess) return e;
     const int64_t work_q = by_query.plan.most * by_query.kv_heads, work_k = by_key.plan.most * by_key.kv_heads, sms = sm_count();
@@ -719,8 +774,14 @@ cudaError_t launch_both(const Maps &m, const BackwardArgs &by_query, const Backw
         ++g_kernel_launches;
     }
     if (grid_k.x > 0) {
-        e = launch_dependent_smem(attention_dkv_kernel<DP>, grid_k, dim3(kThreads), kKeySmem<DP>, s, m.q, m.k, m.v, m.dy, by_key);
-        if (e == cudaSuccess) ++g_kernel_launches;
+        e = launch_dependent_smem(attention_dkv_kernel<DP, PARTS>, grid_k, dim3(kThreads), kKeySmem<DP>, s, m.q, m.k, m.v, m.dy, by_key);
+        if (e != cudaSuccess) return e;
+        ++g_kernel_launches;
+        if (PARTS) {
+            const int64_t threads = by_key.runs.key_rows * by_key.kv_heads * 2 * (by_key.dim / 4);
+            e = launch_dependent(join_gradients_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), s, by_key);
+            if (e == cudaSuccess) ++g_kernel_launches;
+        }
     }
     return e;
 }
@@ -728,12 +789,48 @@ cudaError_t launch_both(const Maps &m, const BackwardArgs &by_query, const Backw
 int queries_of_tile(const AttentionShape &a) { return kRows / (a.heads / a.kv_heads); }
 size_t row_bytes(const AttentionShape &a) { return ((size_t)a.query_rows * a.heads * 4 + 15) / 16 * 16; }
 
+// How the queries of the units of keys are cut, if at all: by what the grid would take.  A unit's tiles take 1.8 us each, one after the
+// other, its start and end as long as 1.5 tiles; units as long as one another take whole rounds of the SMs, those of a causal mask fill
+// them.  The parts' sums (fp32) are written and read once more, at 4 TB/s, and joining them takes a launch.  Ragged sequences: the
+// longest is taken to be twice the average.  A causal unit sees half of its sequence's queries, on average.
+struct Cut {
+    int chunk, splits;
+};
+Cut cut_queries(const AttentionShape &a, bool causal, int64_t window)
+{
+    const int per = queries_of_tile(a);
+    const double sms = 148.0, tiles = (double)((a.query_rows + per - 1) / per), average = tiles / a.sequences;
+    const double work = (double)(most_units(a.key_start, a.key_rows, kRows, a.sequences) * a.kv_heads);
+    if (work == 0.0 || tiles < 4.0) return Cut{1, 1};
+    const double reach = window > 0 ? (double)(window + kRows) / per + 1.0 : tiles, ragged = a.sequences > 1 && 2.0 * average < tiles ? 2.0 * average : tiles;
+    const double longest = ragged < reach ? ragged : reach, half = causal && a.query_rows * 2 > a.key_rows ? 0.5 : 1.0;
+    const double seen = half * average < reach ? half * average : reach, bytes = (double)a.key_rows * a.kv_heads * 2 * a.dim * 4;
+    const auto time = [&](int n) {
+        const double part = longest / n + 1.5, rounds = (double)(int64_t)((work * n + sms - 1.0) / sms);
+        const double all = seen < longest ? work * (seen + 1.5 * n) / sms : rounds * part;
+        return 1.8 * (part > all ? part : all) + (n > 1 ? 6.0 + n * bytes * 2 / 4e6 : 0.0);
+    };
+    Cut best{1, 1};
+    double least = 0.95 * time(1);
+    for (int n = 2; n <= 16 && longest >= 2.0 * n; ++n)
+        if (time(n) < least) least = time(n), best = Cut{(int)((longest + n - 1) / n), n};
+    return best;
+}
+// The scratch has room for the parts of the mask that cuts the most: its size goes by the shape alone.
+int most_parts(const AttentionShape &a) { return cut_queries(a, true, 0).splits; }
+size_t part_bytes(const AttentionShape &a, int splits)
+{
+    const size_t rows = (size_t)a.key_rows * a.kv_heads;
+    return splits > 1 ? rows * splits * 2 * a.dim * 4 + (rows * 4 + 15) / 16 * 16 : 0;
+}
+
 }  // namespace
 
 size_t attention_backward_scratch(const AttentionShape &a)
 {
+    const int parts = most_parts(a);
     return 2 * row_bytes(a) + plan_bytes(a.query_start, a.query_rows, queries_of_tile(a), a.sequences) +
-           plan_bytes(a.key_start, a.key_rows, kRows, a.sequences) + 16;
+           plan_bytes(a.key_start, a.key_rows, kRows, a.sequences, parts) + part_bytes(a, parts) + 16;
 }
 
 cudaError_t launch_attention_backward(const AttentionShape &a, const Heads &dy, const Heads &q, const Heads &k, const Heads &v, const Heads &y,
@@ -754,13 +851,22 @@ cudaError_t launch_attention_backward(const AttentionShape &a, const Heads &dy, 
     p.dk = static_cast<__nv_bfloat16 *>(dk.p), p.ld_dk = dk.ld, p.head_stride_dk = dk.head_stride;
     p.dv = static_cast<__nv_bfloat16 *>(dv.p), p.ld_dv = dv.ld, p.head_stride_dv = dv.head_stride;
     p.minus_lse2 = reinterpret_cast<float *>(at), p.minus_delta = reinterpret_cast<float *>(at + row_bytes(a));
-    const double mean = a.key_rows > 0 ? (double)a.query_rows * group / a.key_rows : 0.0;     // of a key's sum of probabilities
-    p.heavy = (float)(16.0 * (mean > 1.0 ? mean : 1.0));       // half of the columns, one in eight of them, 256 times the mean
     at += 2 * row_bytes(a);
     BackwardArgs by_key = p;
-    p.plan = plan_at(at, a.query_start, a.query_rows, queries, a.sequences);
+    Cut z = cut_queries(a, a.causal != 0, a.window);
+    if (z.splits > most_parts(a)) z = cut_queries(a, true, 0);
+    // A key is heavy from 256 times the mean sum of probabilities on; a part's share of that (a few samples at least), and a thread has
+    // half of the rows, one in eight of them.
+    const double mean = a.key_rows > 0 ? (double)a.query_rows * group / a.key_rows : 0.0, heavy = 16.0 * (mean > 1.0 ? mean : 1.0) / z.splits;
+    by_key.heavy = (float)(heavy > 2.0 ? heavy : 2.0);
+    p.plan = plan_at(at, a.query_start, a.query_rows, queries, a.sequences, kRows);
     at += plan_bytes(a.query_start, a.query_rows, queries, a.sequences);
-    by_key.plan = plan_at(at, a.key_start, a.key_rows, kRows, a.sequences);
+    by_key.plan = plan_at(at, a.key_start, a.key_rows, kRows, a.sequences, queries, z.chunk, z.splits);
+    if (z.splits > 1) {
+        at += plan_bytes(a.key_start, a.key_rows, kRows, a.sequences, z.splits);
+        by_key.parts = reinterpret_cast<float *>(at);
+        by_key.number = reinterpret_cast<int *>(at + (size_t)a.key_rows * a.kv_heads * z.splits * 2 * a.dim * 4);
+    }
     Maps m;
     cudaError_t e = cudaSuccess;
     if (a.query_rows > 0) {
@@ -773,7 +879,9 @@ cudaError_t launch_attention_backward(const AttentionShape &a, const Heads &dy, 
     }
     if (e == cudaSuccess && a.query_start) e = launch_plan(p.runs, p.mask, &p.plan, &by_key.plan, s);
     if (e != cudaSuccess) return e;
-    return a.dim <= 64 ? launch_both<64>(m, p, by_key, a.query_start != nullptr, s) : launch_both<128>(m, p, by_key, a.query_start != nullptr, s);
+    const bool planned = a.query_start != nullptr;
+    if (z.splits > 1) return a.dim <= 64 ? launch_both<64, true>(m, p, by_key, planned, s) : launch_both<128, true>(m, p, by_key, planned, s);
+    return a.dim <= 64 ? launch_both<64, false>(m, p, by_key, planned, s) : launch_both<128, false>(m, p, by_key, planned, s);
 }
 
 }  // namespace lgc

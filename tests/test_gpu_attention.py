@@ -383,10 +383,11 @@ def test_parts_of_long_keys_with_rows_of_no_sequence(dim, group):
     layers.check()
 
 
-def test_a_key_that_most_queries_look_at():
-    """Its gradients sum up 12000 probabilities near one: the tiles behind the first ones take them as two bf16 numbers."""
-    g = generator("sink")
-    T, H, D = 3000, 4, 64
+@pytest.mark.parametrize("T", [3000, 8000])
+def test_a_key_that_most_queries_look_at(T):
+    """Its gradients sum up thousands of probabilities near one: the tiles behind the first ones take them as two bf16 numbers."""
+    g = generator("sink") if T == 3000 else generator("sink", T)
+    H, D = 4, 64
     q, k, v = randn(g, T, H, D), randn(g, T, 1, D), randn(g, T, 1, D).to(BF)
     common = randn(g, D)
     q, k[0, 0] = (q + common).to(BF), 3 * common
@@ -401,14 +402,54 @@ def test_a_key_that_most_queries_look_at():
     assert p0.sum() > 2 * 256 * H
     # Until its sum is 256 times the mean (H a key), in a sample of every eighth of half of the rows (rows of one tile more or less,
     # and the two tiles that are under way), every product errs by 2^-8 of itself at most; after that by 2^-16.  A sample's sum
-    # of 16 H needs no more than 4 * 256 H of all (the sample would have a quarter of its share: it has thousands of entries).
-    early = (p0.flatten().cumsum(0) <= 4 * 256 * H + 4 * 128).view_as(p0)
+    # of 16 H needs no more than 4 * 256 H of all (the sample would have a quarter of its share).  Where the queries are cut into
+    # parts, each has its share of the sum, and tiles of its own that are under way; the scratch holds dk and dv of every part.
+    most = max(1, layers.attention_backward_scratch(T, T, H, 1, D) // (T * 2 * D * 4))
+    tiles = -(-T // 32)
+    parts = -(-tiles // -(-tiles // most))
+    chunk = -(-tiles // parts) * 32
+    early = torch.cat([p.flatten().cumsum(0) <= 4 * 256 * H / most + 4 * 128 for p in p0.split(chunk)]).view_as(p0)
     room = R.UBF * want[2][0, 0].abs() * (1 + 2 * R.UBF) + ((R.UBF * early + 2.0 ** -15) * p0)[..., None].mul(dy.double().abs()).sum((0, 1))
     room += T * H / 16 * 2.0 ** -23 * p0[..., None].mul(dy.double().abs()).sum((0, 1))
     assert ((got[2][0, 0].double() - want[2][0, 0]).abs() <= room).all()
     for a, b in zip(got, backward(dy, q, k, v, y, lse)):
         assert torch.equal(a, b)
     layers.check()
+
+
+# lengths of queries, of keys, heads, kv_heads, dim, causal, window: few units of keys, and many queries
+CUT = [
+    ([1100], [1100], 16, 2, 72, True, 0),
+    ([2500], [300], 8, 1, 128, False, 0),
+    ([2000], [2000], 16, 1, 64, True, 400),
+    ([1500, 0, 64, 700, 3], [200, 50, 0, 129, 1], 12, 3, 40, False, 0),
+    ([1900, 1, 300], [1900, 1, 300], 8, 1, 128, True, 0),
+    ([4096], [4096], 2, 2, 128, False, 0),
+]
+
+
+@pytest.mark.parametrize("case", CUT, ids=str)
+def test_gradients_of_queries_in_parts(case):
+    lq, lk, heads, kv_heads, dim, causal, window = case
+    g = generator("parts of queries", case)
+    before, behind = (5, 9) if len(lq) > 1 else (0, 0)                            # rows of no sequence
+    T, S = before + sum(lq) + behind, before + sum(lk) + behind
+    assert layers.attention_backward_scratch(T, S, heads, kv_heads, dim, len(lq) if before else 0) > 2 * S * kv_heads * 2 * dim * 4     # two parts
+    q, k, v, dy = (randn(g, n, h, dim).to(BF) for n, h in ((T, heads), (S, kv_heads), (S, kv_heads), (T, heads)))
+    named = dict(causal=causal, window=window)
+    if before:
+        named.update(query_start=starts(*lq, first=before), key_start=starts(*lk, first=before))
+        for t in (q, k, v, dy):
+            t[:before] = math.nan
+            t[-behind:] = math.inf
+    y, lse = forward(q, k, v, **named)
+    dirty = torch.full((layers.attention_backward_scratch(T, S, heads, kv_heads, dim, len(lq) if before else 0) + 64,), 255, dtype=torch.uint8, device="cuda")
+    got = backward(dy, q, k, v, y, lse, scratch=dirty[:-64], **named)             # (as floats: NaN)
+    layers.check()
+    assert (dirty[-64:] == 255).all()
+    check_backward(dy, q, k, v, y, lse, got, **named)
+    for a, b in zip(got, backward(dy, q, k, v, y, lse, **named)):
+        assert torch.equal(a, b)
 
 
 # ---- streams, graphs, refusals --------------------------------------------------------------------------------------------------
