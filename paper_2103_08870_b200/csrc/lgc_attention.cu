@@ -599,24 +599,29 @@ plan_kernel(const __grid_constant__ PlanArgs a)
     }
 }
 
-// How the keys are cut: only where there are fewer units than would fill two rounds of CTAs, and so few rows that the parts' results,
-// which are written and read once more, are much less than the keys.  A part has at least `chunk` tiles of keys: as many as make
-// the work one round (ragged sequences: two rounds of shorter ones), two at least.  `splits` bounds their number.
-struct Splits {
-    int chunk, splits;
-};
-Splits splits_of(const AttentionShape &a, int64_t units)
+int queries_of_tile(const AttentionShape &a) { return kRows / (a.heads / a.kv_heads); }
+
+// How the keys are cut.  So few rows that the parts' results are much less than the keys: into as many parts as make the work one round of
+// the SMs (ragged sequences: two rounds of shorter ones), of two tiles at least.  Else by what it takes: a tile of keys 1.9 us, joining
+// a row's heads 1.4 ns each (512 queries of 8192 keys, 16 heads of 128 on 4: 63 us, uncut 118; 2048 of 32768, 8 heads on 1: 271, uncut 443).
+Cut cut_keys(const AttentionShape &a, bool causal, int64_t window)
 {
-    const int64_t tiles = (a.key_rows + kRows - 1) / kRows, ctas = units * a.kv_heads, sms = 148;
-    if (ctas == 0 || ctas >= 2 * sms || tiles < 8 || a.query_rows * (a.heads / a.kv_heads) * 8 > a.key_rows) return Splits{1, 1};
+    const int per = 2 * queries_of_tile(a), most = 64;
+    const int64_t units = most_units(a.query_start, a.query_rows, per, a.sequences), tiles = (a.key_rows + kRows - 1) / kRows;
+    if (a.query_rows * (a.heads / a.kv_heads) * 8 > a.key_rows)
+        return cut_of(a, causal, tiles, window ? (double)(window + per) / kRows + 1.0 : 0.0, units, 1.9, (double)a.query_rows * a.heads * (a.dim + 1) * 4,
+                      6.0 + 1.4e-3 * a.query_rows * a.heads, 16);
+    const int64_t ctas = units * a.kv_heads, sms = 148;
+    if (ctas == 0 || ctas >= 2 * sms || tiles < 8) return Cut{1, 1};
     const int64_t average = (tiles + a.sequences - 1) / a.sequences, rounds = a.query_start ? 2 : 1;      // tiles of a sequence
     int64_t chunk = (average * ctas + rounds * sms - 1) / (rounds * sms);
     if (chunk < 2) chunk = 2;
     int64_t splits = (tiles + chunk - 1) / chunk;
-    if (splits > 64) splits = 64;
-    return splits > 1 ? Splits{(int)chunk, (int)splits} : Splits{1, 1};
+    if (splits > most) splits = most;
+    return splits > 1 ? Cut{(int)chunk, (int)splits} : Cut{1, 1};
 }
-int queries_of_tile(const AttentionShape &a) { return kRows / (a.heads / a.kv_heads); }
+// The scratch has room for the parts of the mask that cuts the most: its size goes by the shape alone.
+int most_parts(const AttentionShape &a) { return cut_keys(a, true, 0).splits; }
 
 template <int DP, bool PARTS>
 cudaError_t launch_forward(const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v, const ForwardArgs &p, bool dependent, cudaStream_t s)
@@ -666,9 +671,9 @@ bool attention_grid_fits(const AttentionShape &a)
 size_t attention_scratch(const AttentionShape &a)
 {
     const int per = 2 * queries_of_tile(a);
-    const Splits z = splits_of(a, most_units(a.query_start, a.query_rows, per, a.sequences));
-    size_t bytes = plan_bytes(a.query_start, a.query_rows, per, a.sequences, z.splits);
-    if (z.splits > 1) bytes += (size_t)a.query_rows * a.heads * (2 * (size_t)z.splits * ((size_t)a.dim + 1) + 1) * 4;
+    const int parts = most_parts(a);
+    size_t bytes = plan_bytes(a.query_start, a.query_rows, per, a.sequences, parts);
+    if (parts > 1) bytes += (size_t)a.query_rows * a.heads * (2 * (size_t)parts * ((size_t)a.dim + 1) + 1) * 4;
     return bytes;
 }
 
@@ -679,7 +684,8 @@ cudaError_t launch_attention(const AttentionShape &a, const Heads &q, const Head
     char *at = static_cast<char *>(scratch);
     ForwardArgs p{};
     p.runs = Runs{a.query_start, a.key_start, a.sequences, a.query_rows, a.key_rows};
-    const Splits z = splits_of(a, most_units(a.query_start, a.query_rows, per, a.sequences));
+    Cut z = cut_keys(a, a.causal != 0, a.window);
+    if (z.splits > most_parts(a)) z = cut_keys(a, true, 0);
     p.plan = plan_at(at, a.query_start, a.query_rows, per, a.sequences, kRows, z.chunk, z.splits);
     p.mask = Mask{a.causal, a.window};
     p.heads = a.heads, p.kv_heads = a.kv_heads, p.group = group, p.dim = a.dim, p.queries = queries;

@@ -284,6 +284,34 @@ struct AttentionShape {
     int causal, window;
     float scale;
 };
+
+// How the other side of the units is cut into parts, if at all: by what the grid would take.  A unit's tiles take `us` each, one after the
+// other, its start and end as long as 1.5 tiles; units as long as one another take whole rounds of the SMs, those of a causal mask fill
+// them.  The parts' sums (fp32, `bytes` of them) are written and read once more, at 4 TB/s, and joining them takes `join` us.
+// tiles: of the other side; reach: of a window, or 0; units: of each head.  Ragged sequences: the longest is taken to be twice the
+// average.  A causal unit sees half of its sequence's other side, on average.
+struct Cut {
+    int chunk, splits;         // tiles of a part at least, parts at most
+};
+inline Cut cut_of(const AttentionShape &a, bool causal, int64_t tiles, double reach, int64_t units, double us, double bytes, double join, int most)
+{
+    if (units == 0 || tiles < 4) return Cut{1, 1};
+    const double sms = 148.0, work = (double)units * a.kv_heads, average = (double)tiles / a.sequences;
+    const double of_longest = a.sequences > 1 && 2.0 * average < tiles ? 2.0 * average : tiles;
+    const double of_most = causal && a.query_rows * 2 > a.key_rows ? 0.5 * average : average;
+    const double longest = reach > 0.0 && reach < of_longest ? reach : of_longest, seen = reach > 0.0 && reach < of_most ? reach : of_most;
+    const auto time = [&](int n) {
+        const double part = longest / n + 1.5, rounds = (double)(int64_t)((work * n + sms - 1.0) / sms);
+        const double all = seen < longest ? work * (seen + 1.5 * n) / sms : rounds * part;
+        return us * (part > all ? part : all) + (n > 1 ? join + n * bytes * 2 / 4e6 : 0.0);
+    };
+    Cut best{1, 1};
+    double least = 0.95 * time(1);
+    for (int n = 2; n <= most && longest >= 2.0 * n; ++n)
+        if (time(n) < least) least = time(n), best = Cut{(int)((longest + n - 1) / n), n};
+    return best;
+}
+
 size_t attention_scratch(const AttentionShape &a);
 size_t attention_backward_scratch(const AttentionShape &a);
 bool attention_grid_fits(const AttentionShape &a);

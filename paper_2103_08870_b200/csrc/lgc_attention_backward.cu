@@ -789,32 +789,12 @@ cudaError_t launch_both(const Maps &m, const BackwardArgs &by_query, const Backw
 int queries_of_tile(const AttentionShape &a) { return kRows / (a.heads / a.kv_heads); }
 size_t row_bytes(const AttentionShape &a) { return ((size_t)a.query_rows * a.heads * 4 + 15) / 16 * 16; }
 
-// How the queries of the units of keys are cut, if at all: by what the grid would take.  A unit's tiles take 1.8 us each, one after the
-// other, its start and end as long as 1.5 tiles; units as long as one another take whole rounds of the SMs, those of a causal mask fill
-// them.  The parts' sums (fp32) are written and read once more, at 4 TB/s, and joining them takes a launch.  Ragged sequences: the
-// longest is taken to be twice the average.  A causal unit sees half of its sequence's queries, on average.
-struct Cut {
-    int chunk, splits;
-};
+// How the queries of the units of keys are cut: a tile of queries takes 1.8 us.
 Cut cut_queries(const AttentionShape &a, bool causal, int64_t window)
 {
     const int per = queries_of_tile(a);
-    const double sms = 148.0, tiles = (double)((a.query_rows + per - 1) / per), average = tiles / a.sequences;
-    const double work = (double)(most_units(a.key_start, a.key_rows, kRows, a.sequences) * a.kv_heads);
-    if (work == 0.0 || tiles < 4.0) return Cut{1, 1};
-    const double reach = window > 0 ? (double)(window + kRows) / per + 1.0 : tiles, ragged = a.sequences > 1 && 2.0 * average < tiles ? 2.0 * average : tiles;
-    const double longest = ragged < reach ? ragged : reach, half = causal && a.query_rows * 2 > a.key_rows ? 0.5 : 1.0;
-    const double seen = half * average < reach ? half * average : reach, bytes = (double)a.key_rows * a.kv_heads * 2 * a.dim * 4;
-    const auto time = [&](int n) {
-        const double part = longest / n + 1.5, rounds = (double)(int64_t)((work * n + sms - 1.0) / sms);
-        const double all = seen < longest ? work * (seen + 1.5 * n) / sms : rounds * part;
-        return 1.8 * (part > all ? part : all) + (n > 1 ? 6.0 + n * bytes * 2 / 4e6 : 0.0);
-    };
-    Cut best{1, 1};
-    double least = 0.95 * time(1);
-    for (int n = 2; n <= 16 && longest >= 2.0 * n; ++n)
-        if (time(n) < least) least = time(n), best = Cut{(int)((longest + n - 1) / n), n};
-    return best;
+    return cut_of(a, causal, (a.query_rows + per - 1) / per, window ? (double)(window + kRows) / per + 1.0 : 0.0,
+                  most_units(a.key_start, a.key_rows, kRows, a.sequences), 1.8, (double)a.key_rows * a.kv_heads * 2 * a.dim * 4, 6.0, 16);
 }
 // The scratch has room for the parts of the mask that cuts the most: its size goes by the shape alone.
 int most_parts(const AttentionShape &a) { return cut_queries(a, true, 0).splits; }

@@ -383,6 +383,27 @@ def test_parts_of_long_keys_with_rows_of_no_sequence(dim, group):
     layers.check()
 
 
+# as CASES: more queries than one tile of a unit, and keys in parts
+KEYS_CUT = [
+    ([300], [3000], 8, 2, 128, True, 0),
+    ([513], [4001], 4, 1, 64, False, 0),
+    ([600], [9000], 8, 1, 128, True, 3000),                 # the second tile's keys begin and end behind the first's
+    ([200, 130, 1, 0, 64], [3000, 900, 2000, 50, 0], 8, 2, 72, True, 0),
+    ([257, 70], [2500, 40], 16, 2, 128, True, 0),           # more queries than keys: rows that see nothing
+]
+
+
+@pytest.mark.parametrize("case", KEYS_CUT, ids=str)
+def test_keys_in_parts_for_two_tiles_of_queries(case):
+    _, q, k, v, named = operands(case, sharp=2.0)
+    assert layers.attention_scratch(len(q), len(k), case[2], case[3], case[4], len(case[0]) if len(case[0]) > 1 else 0) > 2 * 2 * q.numel() * 4
+    y, lse = forward(q, k, v, **named)
+    layers.check()
+    check_forward(q, k, v, y, lse, **named)
+    again = forward(q, k, v, **named)
+    assert torch.equal(y, again[0]) and torch.equal(lse, again[1])
+
+
 @pytest.mark.parametrize("T", [3000, 8000])
 def test_a_key_that_most_queries_look_at(T):
     """Its gradients sum up thousands of probabilities near one: the tiles behind the first ones take them as two bf16 numbers."""
