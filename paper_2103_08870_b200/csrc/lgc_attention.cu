@@ -397,11 +397,11 @@ join_kernel(const __grid_constant__ ForwardArgs p)
     const int64_t q = at / p.heads;
     const int head = (int)(at - q * p.heads);
     if (p.runs.query_start) {                                 // rows in no sequence stay as they are
-        // (starts ascend: the row lies in a run if it lies between the first and the last)
+        // (a row lies in a run if it lies between the first start and the last)
         if (q < max((int64_t)0, p.runs.query_start[0]) || q >= p.runs.query_start[p.runs.sequences]) return;
     }
     // a lane's weights are those of the parts lane, lane + 32, ...
-    const int parts = min(p.parts[at], kMostParts);
+    const int parts = min(p.parts[at], min(2 * p.plan.splits, kMostParts));       // (starts that do not ascend leave rows without a number)
     float lse[kMostParts / 32], most = -INFINITY, total = 0.0f;
 #pragma unroll
     for (int i = 0; i < kMostParts / 32; ++i) {

@@ -733,7 +733,7 @@ join_gradients_kernel(const __grid_constant__ BackwardArgs p)
     const int64_t row = i / quarter, at = row >> 1, key = at / p.kv_heads;
     const int column = (int)(i - row * quarter) * 4, head = (int)(at - key * p.kv_heads), second = (int)(row & 1);
     if (p.runs.key_start && (key < max((int64_t)0, p.runs.key_start[0]) || key >= p.runs.key_start[p.runs.sequences])) return;      // in no sequence
-    const int parts = min(p.number[at], p.plan.splits);
+    const int parts = min(p.number[at], p.plan.splits);        // (starts that do not ascend leave rows without a number)
     float s[4] = {};
 #pragma unroll 4
     for (int z = 0; z < parts; ++z) {

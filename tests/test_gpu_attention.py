@@ -294,6 +294,23 @@ def test_starts_that_do_not_ascend_stay_inside():
     assert (around[:100] == 7).all() and (around[400:] == 7).all()
 
 
+def test_starts_that_do_not_ascend_stay_inside_where_the_work_is_cut():
+    """Rows that no unit wrote have no number of parts: whatever the scratch holds there, only the call's parts are read."""
+    g = generator("starts of parts")
+    for T, S, heads in ((40, 9000, 4), (2500, 700, 8)):
+        q, k, v = randn(g, T, heads, 64).to(BF), randn(g, S, 1, 64).to(BF), randn(g, S, 1, 64).to(BF)
+        at, keys = torch.tensor([0, T, 5, 9, T - 3, T], device="cuda"), torch.tensor([0, 60, S, 100, 1 << 40, S], device="cuda")
+        y, lse = torch.zeros_like(q), torch.zeros(T, heads, device="cuda")
+        grads = [torch.empty_like(t) for t in (q, k, v)]
+        named = dict(query_start=at.flip(0).contiguous() if T > S else at, key_start=keys, causal=False)
+        for fill in (127, 255):
+            size = layers.attention_scratch(T, S, heads, 1, 64, 5)
+            layers.attention(q, k, v, y, lse, scratch=torch.full((size,), fill, dtype=torch.uint8, device="cuda"), **named)
+            size = layers.attention_backward_scratch(T, S, heads, 1, 64, 5)
+            layers.attention_backward(q, q, k, v, y, lse, *grads, scratch=torch.full((size,), fill, dtype=torch.uint8, device="cuda"), **named)
+        layers.check()
+
+
 def test_no_rows():
     none, some = torch.empty(0, 4, 64, dtype=BF, device="cuda"), torch.ones(5, 4, 64, dtype=BF, device="cuda")
     y, lse = forward(none, some, some)
