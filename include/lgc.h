@@ -423,6 +423,7 @@ lgc_status lgc_rotary(const lgc_heads *x, int32_t type, int64_t num_rows, int32_
  * Logits, the softmax's statistics and the sums are fp32; the probabilities are rounded to bf16 in front of their product
  * with v, and dy's with the logits' gradients likewise.  A NaN or an infinity in a row of a sequence may reach every result of
  * that sequence and kv head (also of queries that do not see the row), never another sequence's.
+ * y and lse may not overlap an input.
  * scratch: lgc_attention_scratch bytes, 16-byte aligned (none are needed without starts and with many queries: it may be NULL then). */
 typedef struct {
     int64_t query_rows, key_rows;        /* 0 to 2^30 */

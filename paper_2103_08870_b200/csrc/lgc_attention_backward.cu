@@ -11,7 +11,8 @@
 // shared memory, read along or across their rows as the product wants.  In the second kernel the keys are the lanes (S^T = K Q^T), so
 // P^T and dS^T are such operands too.
 //
-// Precision: sums are fp32; P and dS are rounded to bf16 as operands; delta is a sum of bf16 products in fp32.
+// Precision: sums are fp32; P and dS are rounded to bf16 as operands (two bf16 numbers each in sequences of at most kBrief rows and for keys
+// that most queries look at); delta is a sum of bf16 products in fp32.
 //
 // What bounds them (16384 tokens, one causal sequence, 16 heads of 128 on 4: 1165 and 1605 us, 55 % of the measured bf16 rate counting
 // the five products that the gradient needs, 77 % counting the seven that are made): the chain of a tile.  Of the 2500 and
@@ -61,6 +62,17 @@ struct Ring {
         if (++at == STAGES) at = 0, phase ^= 1;
     }
 };
+
+// What a pair of numbers loses when it becomes the bf16 pair w.
+__device__ __forceinline__ uint32_t bf16_lost(float lo, float hi, uint32_t w)
+{
+    return bf16_pair(__fsub_rn(lo, __uint_as_float(w << 16)), __fsub_rn(hi, __uint_as_float(w & 0xffff0000u)));
+}
+
+// Sequences with so many rows on the other side have P and dS as two bf16 numbers in every tile: their gradients are sums of few terms,
+// whose roundings do not average out (norm of the error over norm of the gradient up to 2.2 times what the result's own rounding
+// leaves; 1.0 with two; long sequences 1.42 with one).  It adds 3 us to a call of 60 tokens, and nothing to calls of long sequences.
+constexpr int kBrief = 64;
 
 // ---- dq: a tile of queries goes over its keys --------------------------------------------------------------------------------
 // Tensor memory: S of two tiles of keys in turn (columns 0 and 128; dS takes its place), dP (256), dQ (384).
@@ -156,6 +168,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
                 const Unit u = w.unit;
                 int key_lo;
                 const int tiles = keys_of(u, key_lo);
+                const bool brief = u.other_len <= kBrief;
                 if (tiles == 0) continue;
                 // S(t): K's rows behind the sequence become zero, since dQ sums over them
                 const auto make_s = [&](int t) {
@@ -199,6 +212,10 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
 #pragma unroll
                         for (int ks = 0; ks < kRows / 16; ++ks)
                             product_step<DP>(tmem + 384, tmem + ((g + t) & 1) * kRows + ks / 4 * 64 + ks % 4 * 8, k_ring + sd * kTile, ks, t > 0 || ks > 0);
+                        if (brief)
+#pragma unroll
+                            for (int ks = 0; ks < kRows / 16; ++ks)
+                                product_step<DP>(tmem + 384, tmem + ((g + t) & 1) * kRows + 32 + ks / 4 * 64 + ks % 4 * 8, k_ring + sd * kTile, ks, true);
                         tc_commit(smem_addr(&b.k_empty[sd]));
                         if (t == tiles - 1) tc_commit(smem_addr(&b.dq_full));
                     }
@@ -245,7 +262,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
             const int kv_head = walk.head;
             int key_lo;
             const int tiles = keys_of(u, key_lo);
-            const bool live = query < p.queries && query < u.rows;
+            const bool live = query < p.queries && query < u.rows, brief = u.other_len <= kBrief;
             int lo = 0, hi = 0x7fffffff;                         // (rows that nobody reads need no mask)
             if (live) keys_seen(p.mask, u.pos + query, 1, u.shift, u.other_len, lo, hi);
             const int64_t at = ((int64_t)kv_head * p.runs.query_rows + u.row) * p.group;
@@ -303,7 +320,18 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
 #pragma unroll
                 for (int n = 0; n < 64; n += 2) {
                     const f2 x = f2_mul(f2_of(v[n], v[n + 1]), f2_add(f2_of(d[n], d[n + 1]), dd));
-                    w[n >> 1] = bf16_pair(f2_lo(x), f2_hi(x));
+                    v[n] = f2_lo(x);
+                    v[n + 1] = f2_hi(x);
+                    w[n >> 1] = bf16_pair(v[n], v[n + 1]);
+                }
+                if (brief) {
+                    uint32_t second[32];
+#pragma unroll
+                    for (int n = 0; n < 64; n += 2) {
+                        const uint32_t l = bf16_lost(v[n], v[n + 1], w[n >> 1]);
+                        second[n >> 1] = (n >= from && n < to ? l & 0xffffu : 0u) | (n + 1 >= from && n + 1 < to ? l & 0xffff0000u : 0u);
+                    }
+                    tc_write32(s_at + 32, second);
                 }
                 if (masked) {                                    // whatever an unseen entry holds, also a NaN
 #pragma unroll
@@ -369,11 +397,6 @@ struct KeyBars {
 template <int DP>
 constexpr int kKeySmem = (2 + kQueryStages + kDyStages) * kTileBytes<DP> + kRowStages * kRows * 8 + (int)sizeof(KeyBars);
 
-// What a pair of numbers loses when it becomes the bf16 pair w.
-__device__ __forceinline__ uint32_t bf16_lost(float lo, float hi, uint32_t w)
-{
-    return bf16_pair(__fsub_rn(lo, __uint_as_float(w << 16)), __fsub_rn(hi, __uint_as_float(w & 0xffff0000u)));
-}
 // PARTS: a unit has a part of its queries, and its sums go to memory as they are.
 template <int DP, bool PARTS>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -493,6 +516,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 const Unit u = w.unit;
                 int query_lo;
                 const int tiles = queries_of(u, query_lo);
+                const bool brief = u.other_len <= kBrief;
                 ++number;
                 if (tiles == 0) continue;
                 // A tile is there.  Rows that are not the sequence's, or that the group leaves over, become zero: dV and dK sum over them.
@@ -529,12 +553,12 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 };
                 if (!bar_wait_together(smem_addr(&b.kv_full), ph_kv, &failed) || !loaded(b.q_full[made_q.at], made_q.phase, q_ring + made_q.at * kTile, 0)) break;
                 ph_kv ^= 1;
-                make_s(0, 0);
+                make_s(0, brief);
                 if (!loaded(b.dy_full[made_dy.at], made_dy.phase, dy_ring + made_dy.at * kTile, 0)) break;
                 make_dp(0);
                 if (!bar_wait_together(smem_addr(&b.sums_empty), ph_o, &failed)) break;          // the last unit's sums have been read
                 ph_o ^= 1;
-                bool two = false;                                // P and dS of tile t are of two terms
+                bool two = brief;                                // P and dS of tile t are of two terms
                 for (int t = 0; t < tiles; ++t, ++g) {
                     const uint32_t q_tile = q_ring + used_q.at * kTile, dy_tile = dy_ring + used_dy.at * kTile;
                     if (!bar_wait_together(smem_addr(&b.p_full), g & 1, &failed)) { ok = false; break; }
@@ -553,7 +577,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     // (each load is waited for behind the product in front of it, while that runs)
                     if (t + 1 < tiles) {
                         if (!loaded(b.q_full[made_q.at], made_q.phase, q_ring + made_q.at * kTile, t + 1)) { ok = false; break; }
-                        make_s(t + 1, heavy == number);
+                        make_s(t + 1, brief || heavy == number);
                     }
                     if (!bar_wait_together(smem_addr(&b.ds_full), g & 1, &failed)) { ok = false; break; }
                     tc_fence_after();
@@ -569,7 +593,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     }
                     __syncwarp();
                     used_q.next();
-                    two = __any_sync(0xffffffffu, heavy == number);
+                    two = brief || __any_sync(0xffffffffu, heavy == number);
                     if (t + 1 < tiles) {
                         if (!loaded(b.dy_full[made_dy.at], made_dy.phase, dy_ring + made_dy.at * kTile, t + 1)) { ok = false; break; }
                         make_dp(t + 1);

@@ -68,10 +68,11 @@ def attention(q, k, v, query_start=None, key_start=None, causal=True, window=0, 
     return y, lse, off, off_lse
 
 
-def attention_backward(dy, q, k, v, y, lse, query_start=None, key_start=None, causal=True, window=0, scale=None):
+def attention_backward(dy, q, k, v, y, lse, query_start=None, key_start=None, causal=True, window=0, scale=None, operand=UBF):
     """((dq, dk, dv), bounds of their errors) with y and lse as they are given; rows of no sequence: NaN.
 
-    As above; delta and dy v are sums of dim products in fp32; ds is rounded to bf16 once."""
+    As above; delta and dy v are sums of dim products in fp32; p and ds are off by `operand` of themselves at most
+    as operands (rounded to bf16 once)."""
     T, H, D = q.shape
     S, K = k.shape[:2]
     G = H // K
@@ -102,10 +103,10 @@ def attention_backward(dy, q, k, v, y, lse, query_start=None, key_start=None, ca
             out[2][k0:k1, h // G] += p.t() @ g
             e = 3 * (2 * U32 * (D + 4) * scale * (a.abs() @ b.abs().t()).masked_fill(hide, 0) + U32 * (16 + 4 * known.abs()))
             n = 2 * U32 * max(q1 - q0, k1 - k0) * G
-            eds = (UBF + e + n) * (1 + UBF) * ds.abs() + 2 * U32 * (D + 4) * p * (g.abs() @ c.t().abs() + (g * y[q0:q1, h]).abs().sum(1, keepdim=True))
+            eds = (operand + e + n) * (1 + UBF) * ds.abs() + 2 * U32 * (D + 4) * p * (g.abs() @ c.t().abs() + (g * y[q0:q1, h]).abs().sum(1, keepdim=True))
             off[0][q0:q1, h] = scale * eds @ b.abs()
             off[1][k0:k1, h // G] += scale * eds.t() @ a.abs()
-            off[2][k0:k1, h // G] += ((UBF + e + n) * (1 + UBF) * p).t() @ g.abs()
+            off[2][k0:k1, h // G] += ((operand + e + n) * (1 + UBF) * p).t() @ g.abs()
     for o, t in zip(out, off):
         t += UBF * (1 + 2 * UBF) * torch.nan_to_num(o).abs() + 1e-30
     return out, off

@@ -490,6 +490,19 @@ def test_gradients_of_queries_in_parts(case):
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("case", [
+    ([64, 1, 0, 3, 17, 40], None, 8, 2, 128, True, 0), ([16] * 30, None, 6, 6, 40, True, 5), ([2, 30, 64], [50, 1, 64], 12, 3, 64, False, 0), ([3], None, 4, 1, 72, True, 0),
+    ([64], [64], 16, 1, 64, False, 0)], ids=str)
+def test_gradients_of_short_sequences_have_two_terms(case):
+    """p and dS as two bf16 numbers each: they are off by 2^-8 of 2^-8."""
+    g, q, k, v, named = operands(case, sharp=2.0)
+    y, lse = forward(q, k, v, **named)
+    dy = randn(g, *q.shape).to(BF)
+    got = backward(dy, q, k, v, y, lse, **named)
+    layers.check()
+    check_backward(dy, q, k, v, y, lse, got, operand=R.UBF ** 2, **named)
+
+
 # ---- streams, graphs, refusals --------------------------------------------------------------------------------------------------
 
 def test_streams_and_graphs_repeat_the_bits():
