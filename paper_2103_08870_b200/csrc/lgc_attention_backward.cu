@@ -69,9 +69,10 @@ __device__ __forceinline__ uint32_t bf16_lost(float lo, float hi, uint32_t w)
     return bf16_pair(__fsub_rn(lo, __uint_as_float(w << 16)), __fsub_rn(hi, __uint_as_float(w & 0xffff0000u)));
 }
 
-// Sequences with so many rows on the other side have P and dS as two bf16 numbers in every tile: their gradients are sums of few terms,
+// Sequences with at most so many rows on the other side have P and dS as two bf16 numbers in every tile: their gradients are sums of few terms,
 // whose roundings do not average out (norm of the error over norm of the gradient up to 2.2 times what the result's own rounding
-// leaves; 1.0 with two; long sequences 1.42 with one).  It adds 3 us to a call of 60 tokens, and nothing to calls of long sequences.
+// leaves; 1.0 with two; long sequences 1.42 with one).  It adds 3 us to a call of 60 tokens, and 1 to 2 % to the first kernel's time with
+// long sequences (registers).
 constexpr int kBrief = 64;
 
 // ---- dq: a tile of queries goes over its keys --------------------------------------------------------------------------------
@@ -317,21 +318,22 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
                 __syncwarp();
                 if (lane == 0) bar_arrive(smem_addr(&b.dp_taken));
                 uint32_t w[32];
-#pragma unroll
-                for (int n = 0; n < 64; n += 2) {
-                    const f2 x = f2_mul(f2_of(v[n], v[n + 1]), f2_add(f2_of(d[n], d[n + 1]), dd));
-                    v[n] = f2_lo(x);
-                    v[n + 1] = f2_hi(x);
-                    w[n >> 1] = bf16_pair(v[n], v[n + 1]);
-                }
                 if (brief) {
                     uint32_t second[32];
 #pragma unroll
                     for (int n = 0; n < 64; n += 2) {
-                        const uint32_t l = bf16_lost(v[n], v[n + 1], w[n >> 1]);
+                        const f2 x = f2_mul(f2_of(v[n], v[n + 1]), f2_add(f2_of(d[n], d[n + 1]), dd));
+                        w[n >> 1] = bf16_pair(f2_lo(x), f2_hi(x));
+                        const uint32_t l = bf16_lost(f2_lo(x), f2_hi(x), w[n >> 1]);
                         second[n >> 1] = (n >= from && n < to ? l & 0xffffu : 0u) | (n + 1 >= from && n + 1 < to ? l & 0xffff0000u : 0u);
                     }
                     tc_write32(s_at + 32, second);
+                } else {                                         // (apart from the above: 1160 against 1167 us of 16384 tokens)
+#pragma unroll
+                    for (int n = 0; n < 64; n += 2) {
+                        const f2 x = f2_mul(f2_of(v[n], v[n + 1]), f2_add(f2_of(d[n], d[n + 1]), dd));
+                        w[n >> 1] = bf16_pair(f2_lo(x), f2_hi(x));
+                    }
                 }
                 if (masked) {                                    // whatever an unseen entry holds, also a NaN
 #pragma unroll
@@ -562,7 +564,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 for (int t = 0; t < tiles; ++t, ++g) {
                     const uint32_t q_tile = q_ring + used_q.at * kTile, dy_tile = dy_ring + used_dy.at * kTile;
                     if (!bar_wait_together(smem_addr(&b.p_full), g & 1, &failed)) { ok = false; break; }
-                    const int heavy = heavy_unit;                // (on its way while dV is issued)
+                    const int heavy = brief ? number : heavy_unit;                // (on its way while dV is issued)
                     tc_fence_after();
                     if (issuer) add(tmem + 256, tmem, dy_tile, t > 0);
                     __syncwarp();
@@ -577,7 +579,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     // (each load is waited for behind the product in front of it, while that runs)
                     if (t + 1 < tiles) {
                         if (!loaded(b.q_full[made_q.at], made_q.phase, q_ring + made_q.at * kTile, t + 1)) { ok = false; break; }
-                        make_s(t + 1, brief || heavy == number);
+                        make_s(t + 1, heavy == number);
                     }
                     if (!bar_wait_together(smem_addr(&b.ds_full), g & 1, &failed)) { ok = false; break; }
                     tc_fence_after();
@@ -593,7 +595,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     }
                     __syncwarp();
                     used_q.next();
-                    two = brief || __any_sync(0xffffffffu, heavy == number);
+                    two = __any_sync(0xffffffffu, heavy == number);
                     if (t + 1 < tiles) {
                         if (!loaded(b.dy_full[made_dy.at], made_dy.phase, dy_ring + made_dy.at * kTile, t + 1)) { ok = false; break; }
                         make_dp(t + 1);
