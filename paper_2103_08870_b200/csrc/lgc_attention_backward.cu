@@ -749,7 +749,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     if (warp == 8) tc_free(tmem, 512);
 }
 
-// The parts of dk and dv added up, in order.  A thread: four columns.  (A read of what the parts left, 5 us where it counts.)
+// The parts of dk and dv added up, in order.  A thread: four columns.  (A read of what the parts left: 42 MB in 13 us, from DRAM.)
 __global__ void __launch_bounds__(256)
 join_gradients_kernel(const __grid_constant__ BackwardArgs p)
 {
